@@ -277,6 +277,77 @@ int64_t bdlm_visible_pairs(const bdlm_problem* p, int32_t n_q, const bdlm_range*
                            int32_t n_k, const bdlm_range* k_ranges);
 
 /*
+ * Packed attention: sequences of different lengths in one call, without the
+ * corrupted copy (prompts, packed training texts).  Sequence s has query rows
+ * [q_start, q_start + q_len) and key rows [k_start, k_start + k_len) of the
+ * call's tensors; its query row i is at position x = k_len - q_len + i (the
+ * queries are the last q_len tokens), key row j at position j.  With blocks of
+ * block_size tokens and e = block_size * (floor(x / block_size) + 1), row x sees
+ * the keys j < e (block_size 1: j <= x), with a window only those with
+ * j >= e - window.  Rows at negative positions (q_len > k_len) see nothing.
+ * A row that sees no key gets O = 0, LSE = -inf and dQ = 0; a key that no row
+ * sees gets dK = dV = 0.  Rows that belong to no sequence are neither read nor
+ * written.
+ *
+ *   Q, O, dO, dQ : [rows][heads][head_dim], K, V, dK, dV : [rows][kv_heads][head_dim],
+ *     rows `stride` elements apart (a multiple of 16 bytes, at most 2^20), so
+ *     that q, k and v may be parts of one fused projection
+ *   LSE          : [heads][lse_pitch] fp32, natural log
+ * Everything is in the problem's dtype (LSE fp32).
+ */
+typedef struct {
+  int32_t heads, kv_heads, head_dim, dtype;
+  float scale;         /* <= 0 selects 1 / sqrt(head_dim); positive scales below 2^-96 are unsupported */
+  int32_t reserved;    /* must be 0 */
+  int64_t block_size;  /* tokens per block, 1 for token-causal attention */
+  int64_t window;      /* 0: no limit */
+} bdlm_packed;
+
+/* Sequences come in the order of their rows and do not overlap; gaps are allowed. */
+typedef struct {
+  int64_t q_start, q_len, k_start, k_len;
+} bdlm_packed_seq;
+
+/* What bdlm_packed_plan_make found: passed on to the calls unchanged. */
+typedef struct {
+  bdlm_packed problem;
+  int64_t q_rows, k_rows;    /* rows that the query and key tensors have at least */
+  int32_t q_items, k_items, n_sums, slots, teams, reserved;
+  size_t bytes;              /* of the items */
+  size_t workspace_bytes;    /* of bdlm_packed_bwd */
+} bdlm_packed_plan;
+
+/* A tensor's first row and the elements between its rows. */
+typedef struct {
+  void* ptr;
+  int64_t stride;
+} bdlm_rows;
+
+/*
+ * The plan of packed calls over these sequences, for every layer and for
+ * forward and backward.  Host only.  Fills *plan, and, unless items is null,
+ * the plan->bytes bytes of work items at `items` (host memory, items_bytes
+ * long); the caller copies those to device memory, 16-byte aligned, and keeps
+ * them there while calls that use them run.
+ */
+bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bdlm_packed_seq* seqs, void* items,
+                                  size_t items_bytes, bdlm_packed_plan* plan);
+
+/* O and LSE of a packed call.  items: the plan's items in device memory. */
+bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdlm_rows q, bdlm_rows k, bdlm_rows v,
+                            bdlm_rows o, float* lse, int64_t lse_pitch, hipStream_t stream);
+
+/*
+ * dQ, dK and dV of a packed call from its O and LSE (the formulas of
+ * bdlm_attn_bwd).  workspace: plan->workspace_bytes bytes of device memory,
+ * 256-byte aligned, contents ignored on entry; calls that may overlap in time
+ * need one each.  Deterministic.  q_rows * heads <= 2^28.
+ */
+bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdlm_rows q, bdlm_rows k, bdlm_rows v,
+                            bdlm_rows o, const float* lse, int64_t lse_pitch, bdlm_rows dO, bdlm_rows dq, bdlm_rows dk,
+                            bdlm_rows dv, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
  * Kernel timing (observability).  While enabled for the calling thread, every
  * kernel the library enqueues is bracketed by two hipEvents recorded on its
  * stream.  bdlm_timing_collect() waits for the recorded events, writes up to

@@ -12,6 +12,7 @@ there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import math
@@ -27,6 +28,7 @@ __all__ = [
     "make_problem", "joint_ranges", "attn_fwd", "attn_partial_fwd", "lse_merge",
     "attn_bwd_workspace_bytes", "attn_bwd", "attn_bwd_noalloc", "visible_pairs",
     "joint_fwd", "joint_bwd", "timing_enable", "timing_collect", "useful_flops",
+    "PackedPlan", "packed_plan", "packed_fwd", "packed_bwd",
 ]
 
 BF16, F32 = 0, 1
@@ -117,6 +119,7 @@ def lib() -> ctypes.CDLL:
         for name in ("bdlm_attn_fwd", "bdlm_attn_partial_fwd", "bdlm_lse_merge", "bdlm_lse_merge_strided",
                      "bdlm_attn_bwd", "bdlm_attn_bwd_noalloc"):
             getattr(L, name).restype = ctypes.c_int
+        packed.declare(L)
         _LIB = L
     return _LIB
 
@@ -164,6 +167,19 @@ def _torch_stream(stream, device) -> torch.cuda.Stream:
     if handle == 0:  # the default stream, for which ExternalStream would take one from torch's pool
         return torch.cuda.default_stream(device)
     return torch.cuda.ExternalStream(handle, device=device)
+
+
+@contextlib.contextmanager
+def device_stream(device, stream):
+    """The raw handle of ``stream`` (default: the current stream of ``device``), with ``device`` current meanwhile."""
+    if stream is not None:
+        with torch.cuda.device(device):
+            yield _stream(stream)
+    elif device.index == torch.cuda.current_device():
+        yield torch._C._cuda_getCurrentRawStream(device.index)
+    else:
+        with torch.cuda.device(device):
+            yield torch._C._cuda_getCurrentRawStream(device.index)
 
 
 def _dtype_code(dt: torch.dtype) -> int:
@@ -452,3 +468,7 @@ def useful_flops(pairs_per_head: int, heads: int, batch: int, head_dim: int) -> 
 
 def default_scale(head_dim: int) -> float:
     return 1.0 / math.sqrt(head_dim)
+
+
+from . import packed  # noqa: E402  (needs the helpers above)
+from .packed import PackedPlan, packed_bwd, packed_fwd, packed_plan  # noqa: E402

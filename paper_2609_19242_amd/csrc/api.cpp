@@ -12,6 +12,7 @@
 #include <string>
 #include <vector>
 
+#include "api_util.hpp"
 #include "common.hpp"
 #include "split_plan.hpp"
 
@@ -24,6 +25,35 @@ using namespace bdlm;
 namespace {
 
 thread_local std::string g_err;
+
+// ---- per-thread kernel timing (bdlm_timing_enable / bdlm_timing_collect)
+// (the dK/dV records include the sum over chunks, where there are any)
+const char* const kKernelNames[kKCount] = {"fwd_bf16",      "fwd_f32",     "lse_merge",    "bwd_dq_f32",
+                                           "bwd_dkdv_bf16", "bwd_dq_bf16", "bwd_dkdv_f32", "packed_fwd",
+                                           "packed_bwd_dq", "packed_bwd_dkdv"};
+struct TimingRec {
+  int id;
+  hipEvent_t a, b;
+};
+thread_local bool g_timing = false;
+thread_local std::vector<TimingRec> g_recs;
+thread_local std::vector<hipEvent_t> g_event_pool;
+thread_local TimingRec g_open;  // between timing_begin and timing_end
+
+hipEvent_t pool_event() {
+  if (!g_event_pool.empty()) {
+    hipEvent_t e = g_event_pool.back();
+    g_event_pool.pop_back();
+    return e;
+  }
+  hipEvent_t e = nullptr;
+  if (hipEventCreate(&e) != hipSuccess) return nullptr;
+  return e;
+}
+
+}  // namespace
+
+namespace bdlm {
 
 bdlm_status fail(bdlm_status st, const char* fmt, ...) {
   char buf[512];
@@ -39,49 +69,21 @@ bdlm_status hip_fail(hipError_t e, const char* what) {
   return fail(BDLM_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
 
-// ---- per-thread kernel timing (bdlm_timing_enable / bdlm_timing_collect)
-enum KernelId { kKFwdBf16 = 0, kKFwdF32, kKMerge, kKBwdDqF32, kKBwdBf16, kKBwdDq, kKBwdF32, kKCount };
-// (the dK/dV records include the sum over chunks, where there are any)
-const char* const kKernelNames[kKCount] = {"fwd_bf16",      "fwd_f32",     "lse_merge",   "bwd_dq_f32",
-                                           "bwd_dkdv_bf16", "bwd_dq_bf16", "bwd_dkdv_f32"};
-struct TimingRec {
-  int id;
-  hipEvent_t a, b;
-};
-thread_local bool g_timing = false;
-thread_local std::vector<TimingRec> g_recs;
-thread_local std::vector<hipEvent_t> g_event_pool;
-
-hipEvent_t pool_event() {
-  if (!g_event_pool.empty()) {
-    hipEvent_t e = g_event_pool.back();
-    g_event_pool.pop_back();
-    return e;
-  }
-  hipEvent_t e = nullptr;
-  if (hipEventCreate(&e) != hipSuccess) return nullptr;
+bool timing_on() { return g_timing; }
+hipError_t timing_begin(int id, hipStream_t s) {
+  g_open = TimingRec{id, pool_event(), pool_event()};
+  if (!g_open.a || !g_open.b) return hipErrorOutOfMemory;
+  return hipEventRecord(g_open.a, s);
+}
+hipError_t timing_end(hipStream_t s) {
+  const hipError_t e = hipEventRecord(g_open.b, s);
+  if (e == hipSuccess) g_recs.push_back(g_open);
   return e;
 }
 
-// Launch through f(), bracketed by events when timing is on.
-template <class F>
-hipError_t timed(int id, hipStream_t s, F&& f) {
-  if (!g_timing) return f();
-  TimingRec r{id, pool_event(), pool_event()};
-  if (!r.a || !r.b) return hipErrorOutOfMemory;
-  hipError_t e = hipEventRecord(r.a, s);
-  if (e != hipSuccess) return e;
-  e = f();
-  if (e != hipSuccess) return e;
-  e = hipEventRecord(r.b, s);
-  if (e != hipSuccess) return e;
-  g_recs.push_back(r);
-  return hipSuccess;
-}
+}  // namespace bdlm
 
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-constexpr int64_t kMaxPos = (int64_t)1 << 30;
+namespace {
 
 bdlm_status check_problem(const bdlm_problem* p) {
   if (!p) return fail(BDLM_ERR_INVALID, "problem is null");

@@ -135,7 +135,7 @@ struct StepDesc {
   uint32_t t0, t1, t2, l0, l1, l2;
 };
 template <int D, bool ROWS>
-__device__ __forceinline__ StepDesc step_desc(const WalkPlan& wp, int i, int64_t H, bool stats_wave, int len_0,
+__device__ __forceinline__ StepDesc step_desc(const WalkPlan& wp, int i, int64_t RS, bool stats_wave, int len_0,
                                               int len_1, int f0_0, int f0_1, int f1_0, int f1_1, uint32_t lrec_0,
                                               uint32_t lrec_1, uint64_t tb_0, uint64_t tb_1, uint64_t lb_0,
                                               uint64_t lb_1) {
@@ -152,10 +152,10 @@ __device__ __forceinline__ StepDesc step_desc(const WalkPlan& wp, int i, int64_t
   d.s = blk;
   const bool part = live && !(blk >= (q ? f0_1 : f0_0) && blk < (q ? f1_1 : f1_0));
   d.flags = q | (part ? 2 : 0);
-  const uint64_t tp = (q ? tb_1 : tb_0) + (uint64_t)(((int64_t)row0 * H + hoff) * D * 2);
+  const uint64_t tp = (q ? tb_1 : tb_0) + (uint64_t)(((int64_t)row0 * RS + hoff * D) * 2);
   d.t0 = (uint32_t)tp;
   d.t1 = (uint32_t)(tp >> 32) & 0xffffu;
-  d.t2 = live ? (uint32_t)((nrows - 1) * (int)H + NH) * D * 2 : 0u;
+  d.t2 = live ? (uint32_t)((nrows - 1) * (int)RS + NH * D) * 2 : 0u;
   const int loff = live ? hoff * len + row0 : 0;
   const uint64_t lp = (q ? lb_1 : lb_0) + (uint64_t)loff * 4u;
   d.l0 = (uint32_t)lp;
@@ -168,8 +168,8 @@ __device__ __forceinline__ StepDesc step_desc(const WalkPlan& wp, int i, int64_t
 // 16-row half as second bf16 terms when some probability of that half reaches
 // hilo_tau (8 more products: head 0's after block B, head 1's after block D,
 // each while its P and dS are still in registers).
-template <int D, bool ADAPT, bool ROWS>
-__global__ __launch_bounds__(256) void dkdv_kernel(const AttnArgs a) {
+template <int D, bool ADAPT, bool ROWS, class Args>
+__global__ __launch_bounds__(256) void dkdv_kernel(const Args args) {
   using Sh = Shape<D, ROWS>;
   constexpr int BN = kBwdKeysBf16, BM = Sh::BM, HPS = Sh::HPS, KS = Sh::KS, DT = Sh::DT, IPW = Sh::IPW;
   constexpr uint32_t RB = Sh::RB, HB = Sh::HB, TileB = Sh::TileB;
@@ -181,11 +181,13 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const AttnArgs a) {
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5;
   const int G = lane >> 4, sl = lane & 15;
-  const int64_t H = a.heads, HKV = a.kv_heads;
 
   // ---- work item: (batch, KV head, key range, key tile, chunk of its walk); heaviest tiles first per XCD
   KeyTileItem it;
-  if (!key_tile_item(a, blockIdx.x, it)) return;
+  if (!key_tile_item(args, blockIdx.x, it)) return;
+  auto&& a = call_view(args, it.item, 2);
+  const int64_t H = a.heads, HKV = a.kv_heads;
+  const int64_t RS = w < 2 ? q_stride<D>(a) : do_stride<D>(a);  // of the tensor this wave copies
   const int b = it.b, kvh = it.kvh, r = it.r, t = it.t;
   const KRangeArg& kr = a.kr[r];
   const int key0 = t * BN;
@@ -199,15 +201,17 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const AttnArgs a) {
   // ---- K, V rows of this wave's keys (B operands of the score products), in AGPRs
   bf16x8 kf[KS], vf[KS];
   {
-    const int64_t eoff = (((int64_t)b * kr.bstride + key0) * HKV + kvh) * D;
-    const uint32_t bytes = (uint32_t)(((int64_t)(nk - 1) * HKV * D + D) * 2);
-    const auto rk = make_rsrc((const bf16*)kr.k + eoff, bytes);
-    const auto rv = make_rsrc((const bf16*)kr.v + eoff, bytes);
-    const uint32_t off = (uint32_t)(((int64_t)mykey * HKV * D + 8 * half) * 2);
+    const int64_t KST = k_stride<D>(a), VST = v_stride<D>(a);
+    const auto rk = make_rsrc((const bf16*)kr.k + row_elem<D>(a, b, kr.bstride, key0, HKV, kvh, KST),
+                              (uint32_t)(((int64_t)(nk - 1) * KST + D) * 2));
+    const auto rv = make_rsrc((const bf16*)kr.v + row_elem<D>(a, b, kr.bstride, key0, HKV, kvh, VST),
+                              (uint32_t)(((int64_t)(nk - 1) * VST + D) * 2));
+    const uint32_t koff = (uint32_t)(((int64_t)mykey * KST + 8 * half) * 2);
+    const uint32_t voff = (uint32_t)(((int64_t)mykey * VST + 8 * half) * 2);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      kf[s] = __builtin_bit_cast(bf16x8, buf_load16(rk, off + 32 * s));
-      vf[s] = __builtin_bit_cast(bf16x8, buf_load16(rv, off + 32 * s));
+      kf[s] = __builtin_bit_cast(bf16x8, buf_load16(rk, koff + 32 * s));
+      vf[s] = __builtin_bit_cast(bf16x8, buf_load16(rv, voff + 32 * s));
     }
   }
   // dK^T / dV^T accumulators (AGPRs, written only by the inline-assembly MFMAs)
@@ -238,7 +242,7 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const AttnArgs a) {
     sp.pos0 = qr.pos0;
     sp.len = qr.len;
     const int h0 = kvh * a.group;
-    sp.tb = (const bf16*)(w < 2 ? qr.q : qr.dO) + ((int64_t)b * qr.bstride * H + h0) * D;
+    sp.tb = (const bf16*)(w < 2 ? qr.q : qr.dO) + row_elem<D>(a, b, qr.bstride, 0, H, h0, RS);
     const int64_t lrow = ((int64_t)b * H + h0) * qr.len;
     sp.lb = (w == 2 ? qr.l2 : qr.delta) + lrow;
     sp.lrec = (uint32_t)(((int64_t)a.batch * H * qr.len - lrow) * 4);
@@ -269,18 +273,15 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const AttnArgs a) {
   // The walk by step index (walk_plan, walk_step).
   WalkPlan wp = walk_plan(R0.s0, R0.s1, R1.s0, R1.s1, a.group / HPS);
   // This workgroup's chunk of it: steps [n0, n1).
-  const int max_ch = a.split.chunks[r];
-  const int nch = max_ch > 1 ? chunks_of(wp.nsteps, a.split.unit, max_ch) : 1;
-  if (max_ch > 1 && it.chunk == 0 && tid == 0) a.split.counts[it.tile] = nch;
-  if (it.chunk >= nch) return;
-  const int n0 = it.chunk * a.split.unit, n1 = it.chunk + 1 < nch ? n0 + a.split.unit : wp.nsteps;
+  Chunk chunk;
+  if (!chunk_of(args, a, it, wp.nsteps, tid, chunk)) return;
+  const int n0 = chunk.n0, n1 = chunk.n1;
   wp.nsteps = n1;  // (steps past the chunk copy nothing)
   // At head_dim 128 the epilogue's scalars wait in VGPRs, of which the walk
   // leaves some free (it needs every SGPR: spilled ones, read back each step,
   // cost 2% at 32K).
   uint64_t partial_at =
-      nch > 1 ? (uint64_t)(uintptr_t)a.split.partials + (uint64_t)partial_row<BN>(a, b, kvh, r, t, it.chunk) * (2 * D * 4)
-              : 0;
+      chunk.cut ? (uint64_t)(uintptr_t)partials_of(args) + (uint64_t)partial_row<BN>(args, it) * (2 * D * 4) : 0;
   if constexpr (D == 128) {
     asm volatile("" : "+v"(partial_at));
     // So does the walk's plan, which only the (vector) step descriptors read.
@@ -298,7 +299,7 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const AttnArgs a) {
     const int slot = (wodd * IPW + i) * 64 + lane;
     const int row = slot / (D / 8), ch = (slot % (D / 8)) ^ chunk_swz<D>(row);
     const int head = ROWS ? 0 : row / kSub, rr = ROWS ? row : row % kSub;
-    voff[i] = (uint32_t)(((rr * H + head) * D + ch * 8) * 2);
+    voff[i] = (uint32_t)((rr * RS + head * D + ch * 8) * 2);
   }
   // A step's copies: IPW 16-byte instructions of the wave's tensor and one
   // dword instruction of -LSE/scale (wave 2) or -D (wave 3); waves 0 and 1
@@ -317,7 +318,7 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const AttnArgs a) {
   const uint64_t tb_0 = (uint64_t)(uintptr_t)R0.tb, tb_1 = (uint64_t)(uintptr_t)R1.tb;
   const uint64_t lb_0 = (uint64_t)(uintptr_t)R0.lb, lb_1 = (uint64_t)(uintptr_t)R1.lb;
   auto make_batch = [&](int base) __attribute__((always_inline)) -> StepDesc {
-    return step_desc<D, ROWS>(wp, base + lane, H, w >= 2, len_0, len_1, f0_0, f0_1, f1_0, f1_1, lrec_0, lrec_1, tb_0, tb_1,
+    return step_desc<D, ROWS>(wp, base + lane, RS, w >= 2, len_0, len_1, f0_0, f0_1, f1_0, f1_1, lrec_0, lrec_1, tb_0, tb_1,
                      lb_0, lb_1);
   };
   StepDesc bt;
@@ -732,9 +733,8 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const AttnArgs a) {
     }
   } else if (a.out_f32) {
     if (key_ok) {
-      const int64_t off = (((int64_t)b * kr.bstride + key0 + mykey) * HKV + kvh) * D;
-      float* dkp = (float*)kr.dk + off;
-      float* dvp = (float*)kr.dv + off;
+      float* dkp = (float*)kr.dk + row_elem<D>(a, b, kr.bstride, key0 + mykey, HKV, kvh, dk_stride<D>(a));
+      float* dvp = (float*)kr.dv + row_elem<D>(a, b, kr.bstride, key0 + mykey, HKV, kvh, dv_stride<D>(a));
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -777,9 +777,9 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const AttnArgs a) {
       const uint32_t o = (uint32_t)r * RB + (((uint32_t)c ^ (uint32_t)(r & (CH - 1))) * 16u);
       const bf16x8 xk = lds_load16(sw + o), xv = lds_load16(sw + HB + o);
       if (w * 32 + r < nk) {
-        const int64_t go = (((int64_t)b * kr.bstride + key0 + w * 32 + r) * HKV + kvh) * D + c * 8;
-        *(bf16x8*)((bf16*)kr.dk + go) = xk;
-        *(bf16x8*)((bf16*)kr.dv + go) = xv;
+        const int64_t row = key0 + w * 32 + r;
+        *(bf16x8*)((bf16*)kr.dk + row_elem<D>(a, b, kr.bstride, row, HKV, kvh, dk_stride<D>(a)) + c * 8) = xk;
+        *(bf16x8*)((bf16*)kr.dv + row_elem<D>(a, b, kr.bstride, row, HKV, kvh, dv_stride<D>(a)) + c * 8) = xv;
       }
     }
   }
@@ -791,31 +791,29 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const AttnArgs a) {
 // (mostly L2 and MALL) traffic: the partials once.
 template <int D>
 constexpr int kSumWgs = 4 * 2 * D / 32 * 4 * 32 / 256;
-template <int D>
-__global__ __launch_bounds__(256) void dkdv_sum_kernel(const AttnArgs a) {
+template <int D, class Args>
+__global__ __launch_bounds__(256) void dkdv_sum_kernel(const Args a) {
   constexpr int DT = D / 32, PIECES = 2 * DT * 4;  // per 32 keys: dK's 4 d + g4, then dV's
-  SumItem it;
-  sum_item(a, blockIdx.x / kSumWgs<D>, it);
-  const int nch = a.split.counts[blockIdx.x / kSumWgs<D>];
-  if (nch <= 1) return;
+  const auto st = sum_tile<kBwdKeysBf16, D>(a, blockIdx.x / kSumWgs<D>);
+  if (st.n <= 1) return;
   const int n = (blockIdx.x % kSumWgs<D>) * 256 + threadIdx.x;
   const int l32 = n & 31, piece = (n >> 5) % PIECES, w = (n >> 5) / PIECES;
-  const KRangeArg& kr = a.kr[it.r];
-  const int key0 = it.t * kBwdKeysBf16, nk = imin(kBwdKeysBf16, kr.len - key0);
-  if (w * 32 + l32 >= nk) return;
-  const int key = key0 + w * 32 + l32, at = piece * 2 * nk + w * 32 + l32;
+  const int key = w * 32 + l32;
+  if (key >= st.nk) return;
+  const int at = piece * 2 * st.nk + key;
   f32x4 lo = {0.f, 0.f, 0.f, 0.f}, hi = lo;
-  for (int ch = 0; ch < nch; ++ch) {
-    const f32x4* pp = (const f32x4*)((const float*)a.split.partials +
-                                     partial_row<kBwdKeysBf16>(a, it.b, it.kvh, it.r, it.t, ch) * (2 * D));
+  for (int ch = 0; ch < st.n; ++ch) {
+    const f32x4* pp = (const f32x4*)((const float*)partials_of(a) + partial_row(a, st, ch) * (2 * D));
     lo += pp[at];
-    hi += pp[at + nk];
+    hi += pp[at + st.nk];
   }
   const bool is_dv = piece >= 4 * DT;
   const float sc = is_dv ? 1.f : a.scale;
-  const int64_t off = (((int64_t)it.b * kr.bstride + key) * a.kv_heads + it.kvh) * D + (piece & (4 * DT - 1)) * 8;
-  void* out = is_dv ? kr.dv : kr.dk;
-  if (a.out_f32) {
+  const int64_t off = (is_dv ? st.dv + key * st.dvs : st.dk + key * st.dks) + (piece & (4 * DT - 1)) * 8;
+  void* out = is_dv ? dv_of(a, st.it) : dk_of(a, st.it);
+  bool out_f32 = false;
+  if constexpr (!kIsPacked<Args>) out_f32 = a.out_f32;
+  if (out_f32) {
     *(f32x4*)((float*)out + off) = lo * sc;
     *(f32x4*)((float*)out + off + 4) = hi * sc;
   } else {
@@ -831,23 +829,26 @@ __global__ __launch_bounds__(256) void dkdv_sum_kernel(const AttnArgs a) {
 
 }  // namespace
 
-hipError_t launch_bwd_dkdv_sum(const AttnArgs& a, int head_dim, hipStream_t s) {
-  const int n = a.split.tiles_per_pair * a.kv_heads * a.batch;
-  if (n == 0) return hipSuccess;
-  if (head_dim == 128) hipLaunchKernelGGL(dkdv_sum_kernel<128>, dim3(n * kSumWgs<128>), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL(dkdv_sum_kernel<64>, dim3(n * kSumWgs<64>), dim3(256), 0, s, a);
-  return hipGetLastError();
-}
-
 namespace {
 
-template <int D, bool ADAPT>
-void launch_rows(const AttnArgs& a, int n, hipStream_t s) {
-  if (a.group % 2 == 0) hipLaunchKernelGGL((dkdv_kernel<D, ADAPT, false>), dim3(n), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((dkdv_kernel<D, ADAPT, true>), dim3(n), dim3(256), 0, s, a);
+template <int D, bool ADAPT, class Args>
+void launch_rows(const Args& a, int n, hipStream_t s) {
+  if (a.group % 2 == 0) hipLaunchKernelGGL((dkdv_kernel<D, ADAPT, false, Args>), dim3(n), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((dkdv_kernel<D, ADAPT, true, Args>), dim3(n), dim3(256), 0, s, a);
 }
 
 }  // namespace
+
+#ifndef BDLM_PACKED_CALLS
+
+hipError_t launch_bwd_dkdv_sum(const AttnArgs& a, int head_dim, hipStream_t s) {
+  const int n = a.split.tiles_per_pair * a.kv_heads * a.batch;
+  if (n == 0) return hipSuccess;
+  if (head_dim == 128)
+    hipLaunchKernelGGL((dkdv_sum_kernel<128, AttnArgs>), dim3(n * kSumWgs<128>), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((dkdv_sum_kernel<64, AttnArgs>), dim3(n * kSumWgs<64>), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
 
 hipError_t launch_bwd_dkdv(const AttnArgs& a, int head_dim, hipStream_t s) {
   const int n = workgroups_for(a.split.wgs_per_pair * a.kv_heads * a.batch);
@@ -859,5 +860,26 @@ hipError_t launch_bwd_dkdv(const AttnArgs& a, int head_dim, hipStream_t s) {
   else two_terms ? launch_rows<64, true>(a, n, s) : launch_rows<64, false>(a, n, s);
   return hipGetLastError();
 }
+
+#else
+
+hipError_t launch_bwd_dkdv_sum(const PackedArgs& a, int head_dim, hipStream_t s) {
+  const int n = a.n_sums * a.kv_heads;
+  if (n == 0) return hipSuccess;
+  if (head_dim == 128)
+    hipLaunchKernelGGL((dkdv_sum_kernel<128, PackedArgs>), dim3(n * kSumWgs<128>), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((dkdv_sum_kernel<64, PackedArgs>), dim3(n * kSumWgs<64>), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_bwd_dkdv(const PackedArgs& a, int head_dim, hipStream_t s) {
+  const int n = workgroups_for(a.n_items * a.kv_heads);
+  if (n == 0) return hipSuccess;
+  if (head_dim == 128) launch_rows<128, false>(a, n, s);
+  else launch_rows<64, false>(a, n, s);
+  return hipGetLastError();
+}
+
+#endif
 
 }  // namespace bdlm

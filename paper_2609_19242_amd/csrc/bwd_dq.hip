@@ -22,9 +22,9 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
-template <int D, int NW, int NST, int HM>
+template <int D, int NW, int NST, int HM, class Args>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void bwd_dq_kernel(
-    const AttnArgs a) {
+    const Args args) {
   constexpr int BM = NW * 32, BN = 64, KS = D / 16, DT = D / 32;
   // K and V tiles with swizzled rows: K serves both its row reads (S^T) and
   // its transpose reads (K^T), V its row reads (dP^T).
@@ -41,7 +41,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int G = lane >> 4, sl = lane & 15;
 
   QTileItem it;
-  if (!q_tile_item(a, blockIdx.x, it)) return;
+  if (!q_tile_item(args, blockIdx.x, it)) return;
+  auto&& a = call_view(args, it.item, 2);
   const QRangeArg& qr = a.qr[it.r];
   const int kvh = it.h / a.group;
   const int row0 = it.t * BM;
@@ -54,18 +55,22 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   bf16x8 qf[KS], df[KS];
   float dsum = 0.f;
   {
-    const int64_t qoff = (((int64_t)it.b * qr.bstride + row0) * H + it.h) * D;
-    const uint32_t bytes = (uint32_t)(((int64_t)(nvalid - 1) * H * D + D) * 2);
-    const auto rq = make_rsrc((const bf16*)qr.q + qoff, bytes);
-    const auto rdo = make_rsrc((const bf16*)qr.dO + qoff, bytes);
-    const uint32_t off = (uint32_t)(((int64_t)(w * 32 + l32) * H * D + 8 * half) * 2);
+    const int64_t QS = q_stride<D>(a), DS = do_stride<D>(a), OS = o_stride<D>(a);
+    const int64_t qoff = row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, QS);
+    const int64_t doff = row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, DS);
+    const int64_t ooff = row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, OS);
+    auto bytes_of = [&](int64_t st) { return (uint32_t)(((int64_t)(nvalid - 1) * st + D) * 2); };
+    auto off_of = [&](int64_t st) { return (uint32_t)(((int64_t)(w * 32 + l32) * st + 8 * half) * 2); };
+    const auto rq = make_rsrc((const bf16*)qr.q + qoff, bytes_of(QS));
+    const auto rdo = make_rsrc((const bf16*)qr.dO + doff, bytes_of(DS));
+    const uint32_t off_q = off_of(QS), off_d = off_of(DS), off = off_of(OS), bytes = bytes_of(OS);
 #pragma unroll
     for (int s = 0; s < KS; ++s) {
-      qf[s] = __builtin_bit_cast(bf16x8, buf_load16(rq, off + s * 32));
-      df[s] = __builtin_bit_cast(bf16x8, buf_load16(rdo, off + s * 32));
+      qf[s] = __builtin_bit_cast(bf16x8, buf_load16(rq, off_q + s * 32));
+      df[s] = __builtin_bit_cast(bf16x8, buf_load16(rdo, off_d + s * 32));
     }
     if (a.out_f32) {  // O in fp32: two 16-byte loads per chunk
-      const auto ro = make_rsrc((const float*)qr.o + qoff, 2 * bytes);
+      const auto ro = make_rsrc((const float*)qr.o + ooff, 2 * bytes);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         const f32x4 o0 = __builtin_bit_cast(f32x4, buf_load16(ro, 2 * off + s * 64));
@@ -77,7 +82,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         }
       }
     } else {
-      const auto ro = make_rsrc((const bf16*)qr.o + qoff, bytes);
+      const auto ro = make_rsrc((const bf16*)qr.o + ooff, bytes);
 #pragma unroll
       for (int s = 0; s < KS; ++s) {
         const bf16x8 o = __builtin_bit_cast(bf16x8, buf_load16(ro, off + s * 32));
@@ -142,11 +147,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     int rows_left;
   };
   const bool kwave = w < NW / 2;
+  const int64_t CS = kwave ? k_stride<D>(a) : v_stride<D>(a);  // of the tensor this wave copies
   auto copy_seek = [&](CopyCur cc) -> CopyCur {
     if (cc.c.have) {
       const KRangeArg& kr = a.kr[cc.c.j];
       cc.src = (const bf16*)(kwave ? kr.k : kr.v) +
-               (((int64_t)it.b * kr.bstride + (int64_t)cc.c.t * BN) * HKV + kvh) * D;
+               row_elem<D>(a, it.b, kr.bstride, (int64_t)cc.c.t * BN, HKV, kvh, CS);
       cc.rows_left = kr.len - cc.c.t * BN;
     }
     return cc;
@@ -154,7 +160,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   auto copy_next = [&](CopyCur cc) -> CopyCur {
     if (!cc.c.have) return cc;
     if (++cc.c.t < cc.c.t1) {
-      cc.src += (int64_t)BN * HKV * D;
+      cc.src += (int64_t)BN * CS;
       cc.rows_left -= BN;
       return cc;
     }
@@ -172,7 +178,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   uint32_t voff[PI];
   const int cw = w % (NW / 2);
 #pragma unroll
-  for (int i = 0; i < PI; ++i) voff[i] = swz_src_offset<D>((cw * IPW + i) * 64 + lane, HKV * D);
+  for (int i = 0; i < PI; ++i) voff[i] = swz_src_offset<D>((cw * IPW + i) * 64 + lane, CS);
   const bf16* const any_src = (const bf16*)a.kr[0].k;
   auto copy_tile = [&](bf16* st, const CopyCur& cc) __attribute__((always_inline)) {
     const int nrows = cc.c.have ? imin(BN, cc.rows_left) : 0;
@@ -180,8 +186,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
       const int nr = nrows - 16 * k;
-      const uint32_t bytes = nr > 0 ? (uint32_t)(((nr - 1) * (int)HKV * D + D) * 2) : 0u;
-      const auto r = make_rsrc(nr > 0 ? cc.src + (int64_t)16 * k * HKV * D : any_src, bytes);
+      const uint32_t bytes = nr > 0 ? (uint32_t)(((nr - 1) * (int)CS + D) * 2) : 0u;
+      const auto r = make_rsrc(nr > 0 ? cc.src + (int64_t)16 * k * CS : any_src, bytes);
 #pragma unroll
       for (int i = 0; i < PI; ++i) buf_to_lds<16>(r, dst + (k * PI + i) * 512, voff[i], 0);
     }
@@ -339,7 +345,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 
   if (a.out_f32) {
     if (row_ok) {
-      float* op = (float*)qr.dq + (((int64_t)it.b * qr.bstride + my_row) * H + it.h) * D;
+      float* op = (float*)qr.dq + row_elem<D>(a, it.b, qr.bstride, my_row, H, it.h, dq_stride<D>(a));
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -356,11 +362,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     const int wrow0 = row0 + w * 32;
     store_rows_bf16_via_lds<D>(
         lds_addr(lds) + (uint32_t)w * (D * 64), [&](int d, int g4, int e) { return acc[d][g4 * 4 + e] * a.scale; },
-        (bf16*)qr.dq + (((int64_t)it.b * qr.bstride + wrow0) * H + it.h) * D, H * D, qr.len - wrow0, lane);
+        (bf16*)qr.dq + row_elem<D>(a, it.b, qr.bstride, wrow0, H, it.h, dq_stride<D>(a)), dq_stride<D>(a),
+        qr.len - wrow0, lane);
   } else if (row_ok) {
     // The adaptive two-term kernel stores directly: the staged form needs the
     // last few registers it has and made it spill.
-    bf16* op = (bf16*)qr.dq + (((int64_t)it.b * qr.bstride + my_row) * H + it.h) * D;
+    bf16* op = (bf16*)qr.dq + row_elem<D>(a, it.b, qr.bstride, my_row, H, it.h, dq_stride<D>(a));
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -373,6 +380,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   }
 }
 
+#ifndef BDLM_PACKED_CALLS
+
 // HM of the kernel: 0 single-term P (dS), 1 two-term on every tile, 2
 // two-term on the 16-key chunks holding a large probability.
 // NW waves of 32 rows; NS = 3 stages (96 KB: one 8-wave workgroup per CU)
@@ -380,9 +389,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 template <int D, int NW, int NS>
 void launch_hm(const AttnArgs& a, int n, hipStream_t s) {
   const int hm = !(a.hilo & kHiloDq) ? 0 : (a.hilo & kHiloAdaptive) ? 2 : 1;
-  if (hm == 0) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, NS, 0>), dim3(n), dim3(NW * 64), 0, s, a);
-  else if (hm == 1) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, NS, 1>), dim3(n), dim3(NW * 64), 0, s, a);
-  else hipLaunchKernelGGL((bwd_dq_kernel<D, NW, NS, 2>), dim3(n), dim3(NW * 64), 0, s, a);
+  if (hm == 0) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, NS, 0, AttnArgs>), dim3(n), dim3(NW * 64), 0, s, a);
+  else if (hm == 1) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, NS, 1, AttnArgs>), dim3(n), dim3(NW * 64), 0, s, a);
+  else hipLaunchKernelGGL((bwd_dq_kernel<D, NW, NS, 2, AttnArgs>), dim3(n), dim3(NW * 64), 0, s, a);
 }
 
 template <int D>
@@ -401,5 +410,20 @@ hipError_t launch_bwd_dq_bf16(const AttnArgs& a, int head_dim, int rows, hipStre
   else launch_rows<64>(a, rows, n, s);
   return hipGetLastError();
 }
+
+#else
+
+}  // namespace
+
+hipError_t launch_bwd_dq_bf16(const PackedArgs& a, int head_dim, hipStream_t s) {
+  const int n = workgroups_for(a.n_items * a.heads);
+  if (n == 0) return hipSuccess;
+  constexpr int NW = kQRowsShortBf16 / 32;
+  if (head_dim == 128) hipLaunchKernelGGL((bwd_dq_kernel<128, NW, 2, 0, PackedArgs>), dim3(n), dim3(NW * 64), 0, s, a);
+  else hipLaunchKernelGGL((bwd_dq_kernel<64, NW, 2, 0, PackedArgs>), dim3(n), dim3(NW * 64), 0, s, a);
+  return hipGetLastError();
+}
+
+#endif
 
 }  // namespace bdlm

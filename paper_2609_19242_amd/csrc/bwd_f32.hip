@@ -34,9 +34,9 @@ namespace {
 
 constexpr int kWaves = 4;
 
-template <int D>
+template <int D, class Args>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void bwd_dq_f32_kernel(
-    const AttnArgs a) {
+    const Args args) {
   constexpr int NC = D / 16, OPS = 16 * D;
   // Q and dO as fp64 row operands during the walk, the waves' dQ^T sums after it
   __shared__ __attribute__((aligned(16))) double lds[kWaves * 16 * kRedRow<D>];
@@ -44,21 +44,25 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   const int i = lane & 15, g = lane >> 4;
 
   QTileItem it;
-  if (!q_tile_item(a, workgroup_id(), it)) return;
+  if (!q_tile_item(args, workgroup_id(), it)) return;
+  auto&& a = call_view(args, it.item, 4);
   const QRangeArg& qr = a.qr[it.r];
   const int kvh = it.h / a.group;
   const int64_t H = a.heads, HKV = a.kv_heads;
   const int row0 = it.t * 16, nvalid = imin(16, qr.len - row0);
-  const int64_t qoff = (((int64_t)it.b * qr.bstride + row0) * H + it.h) * D;
-  stage_row_operands<D>(lds, (const float*)qr.q + qoff, H * D, nvalid, tid, kWaves * 64);
-  stage_row_operands<D>(lds + OPS, (const float*)qr.dO + qoff, H * D, nvalid, tid, kWaves * 64);
+  const int64_t QS = q_stride<D>(a), OS = o_stride<D>(a), DS = do_stride<D>(a);
+  const int64_t qoff = row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, QS);
+  const int64_t ooff = row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, OS);
+  const int64_t doff = row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, DS);
+  stage_row_operands<D>(lds, (const float*)qr.q + qoff, QS, nvalid, tid, kWaves * 64);
+  stage_row_operands<D>(lds + OPS, (const float*)qr.dO + doff, DS, nvalid, tid, kWaves * 64);
 
   // D = dO.O of this lane's query; the four lanes of a column share the row.
   const int qi = imin(i, nvalid - 1);
   double dl = 0.0;
   {
-    const float* op = (const float*)qr.o + qoff + (int64_t)qi * H * D;
-    const float* dp = (const float*)qr.dO + qoff + (int64_t)qi * H * D;
+    const float* op = (const float*)qr.o + ooff + (int64_t)qi * OS;
+    const float* dp = (const float*)qr.dO + doff + (int64_t)qi * DS;
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const fl4 x = *(const fl4*)(op + 16 * c + 4 * g), y = *(const fl4*)(dp + 16 * c + 4 * g);
@@ -94,13 +98,15 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   t = t1 = -kWaves;
   while (advance()) {
     const KRangeArg& kr = a.kr[j];
-    const int64_t koff = (((int64_t)it.b * kr.bstride + t * 16) * HKV + kvh) * D;
     const int krows = imin(16, kr.len - t * 16);
-    const RowTile kt = row_tile<D>(kr.k, koff, krows, HKV * D);
+    auto tile_of = [&](const void* base, int64_t stride) __attribute__((always_inline)) {
+      return row_tile<D>(base, row_elem<D>(a, it.b, kr.bstride, t * 16, HKV, kvh, stride), krows, stride);
+    };
+    const RowTile kt = tile_of(kr.k, k_stride<D>(a));
     fl4 kx[NC], vx[NC];
     ColOps<D> kc;
     load_rows<D>(kx, kt, i, g);
-    load_rows<D>(vx, row_tile<D>(kr.v, koff, krows, HKV * D), i, g);
+    load_rows<D>(vx, tile_of(kr.v, v_stride<D>(a)), i, g);
     kc.load(kt, i, g);
     const bool full = t >= f0 && t < f1 && !any_dead;
     int lo = 0, wid = 0;
@@ -129,7 +135,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   constexpr int EPT = 16 * D / (kWaves * 64);
   const int q = tid / (D / EPT), d0 = (tid % (D / EPT)) * EPT;
   if (q < nvalid) {
-    float* out = (float*)qr.dq + qoff + (int64_t)q * H * D + d0;
+    float* out = (float*)qr.dq + row_elem<D>(a, it.b, qr.bstride, row0 + q, H, it.h, dq_stride<D>(a)) + d0;
 #pragma unroll
     for (int e4 = 0; e4 < EPT / 4; ++e4) {
       fl4 o;
@@ -145,16 +151,17 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   }
 }
 
-template <int D>
+template <int D, class Args>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void bwd_dkv_f32_kernel(
-    const AttnArgs a) {
+    const Args args) {
   constexpr int NC = D / 16, OPS = 16 * D;
   // K and V as fp64 row operands during the walk, the waves' sums after it
   __shared__ __attribute__((aligned(16))) double lds[kWaves * 16 * kRedRow<D>];
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int i = lane & 15, g = lane >> 4;
   KeyTileItem it;
-  if (!key_tile_item(a, workgroup_id(), it)) return;
+  if (!key_tile_item(args, workgroup_id(), it)) return;
+  auto&& a = call_view(args, it.item, 4);
   const KRangeArg& kr = a.kr[it.r];
   const int64_t H = a.heads, HKV = a.kv_heads;
   const int row0 = it.t * 16, nvalid = imin(16, kr.len - row0);
@@ -194,14 +201,15 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
     const Span s = span(q);
     units += (s.t1 - s.t0) * a.group;
   }
-  const int nch = a.split.chunks[it.r] > 1 ? chunks_of(units, a.split.unit, a.split.chunks[it.r]) : 1;
-  if (it.chunk == 0 && tid == 0 && a.split.chunks[it.r] > 1) a.split.counts[it.tile] = nch;
-  if (it.chunk >= nch) return;
-  const int n0 = it.chunk * a.split.unit, n1 = it.chunk + 1 < nch ? n0 + a.split.unit : units;
+  Chunk chunk;
+  if (!chunk_of(args, a, it, units, tid, chunk)) return;
+  const int n0 = chunk.n0, n1 = chunk.n1;
 
-  const int64_t koff = (((int64_t)it.b * kr.bstride + row0) * HKV + it.kvh) * D;
-  stage_row_operands<D>(lds, (const float*)kr.k + koff, HKV * D, nvalid, tid, kWaves * 64);
-  stage_row_operands<D>(lds + OPS, (const float*)kr.v + koff, HKV * D, nvalid, tid, kWaves * 64);
+  const int64_t KST = k_stride<D>(a), VST = v_stride<D>(a);
+  stage_row_operands<D>(lds, (const float*)kr.k + row_elem<D>(a, it.b, kr.bstride, row0, HKV, it.kvh, KST), KST, nvalid,
+                        tid, kWaves * 64);
+  stage_row_operands<D>(lds + OPS, (const float*)kr.v + row_elem<D>(a, it.b, kr.bstride, row0, HKV, it.kvh, VST), VST,
+                        nvalid, tid, kWaves * 64);
   __syncthreads();
 
   const double c = (double)a.scale * kLog2eD;
@@ -235,9 +243,11 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
     qlo = imax(qlo, qr.pos0);
     const int qw = imax(imin(qhi, qr.pos0 + qr.len) - qlo, 0);
     const int64_t hrow = (int64_t)it.b * H + h;
-    const int64_t qoff = (((int64_t)it.b * qr.bstride + t * 16) * H + h) * D;
     const int qrows = imin(16, qr.len - t * 16);
-    const RowTile qt = row_tile<D>(qr.q, qoff, qrows, H * D), ot = row_tile<D>(qr.dO, qoff, qrows, H * D);
+    auto tile_of = [&](const void* base, int64_t stride) __attribute__((always_inline)) {
+      return row_tile<D>(base, row_elem<D>(a, it.b, qr.bstride, t * 16, H, h, stride), qrows, stride);
+    };
+    const RowTile qt = tile_of(qr.q, q_stride<D>(a)), ot = tile_of(qr.dO, do_stride<D>(a));
     fl4 qx[NC], ox[NC];
     ColOps<D> cx;
     load_rows<D>(qx, qt, i, g);
@@ -299,15 +309,16 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
       for (int u = 0; u < kWaves; ++u) x[e] += lds[(u * 16 + k) * kRedRow<D> + d0 + e];
     }
-    if (nch > 1) {
-      double* dst = (double*)a.split.partials + partial_row<16>(a, it.b, it.kvh, it.r, it.t, it.chunk) * (2 * D) +
+    if (chunk.cut) {
+      double* dst = (double*)partials_of(args) + partial_row<16>(args, it) * (2 * D) +
                     (which * nvalid + k) * D + d0;
       if (k < nvalid) {
 #pragma unroll
         for (int e = 0; e < EPT; e += 2) *(f64x2*)(dst + e) = f64x2{x[e], x[e + 1]};
       }
     } else if (k < nvalid) {
-      float* dst = (float*)(which == 0 ? kr.dv : kr.dk) + koff + (int64_t)k * HKV * D + d0;
+      const int64_t ST = which == 0 ? dv_stride<D>(a) : dk_stride<D>(a);
+      float* dst = (float*)(which == 0 ? kr.dv : kr.dk) + row_elem<D>(a, it.b, kr.bstride, row0 + k, HKV, it.kvh, ST) + d0;
       const double sc = which == 0 ? 1.0 : (double)a.scale;
 #pragma unroll
       for (int e4 = 0; e4 < EPT / 4; ++e4) {
@@ -322,28 +333,23 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
 
 // dK, dV of the chunked key tiles: the sum of the chunks' partials in chunk
 // order.  One workgroup per tile (grid: every tile of the chunked ranges).
-template <int D>
-__global__ __launch_bounds__(256) void bwd_sum_f32_kernel(const AttnArgs a) {
+template <int D, class Args>
+__global__ __launch_bounds__(256) void bwd_sum_f32_kernel(const Args a) {
   constexpr int OPS = 16 * D, EPT = OPS / 256;
-  SumItem it;
-  sum_item(a, blockIdx.x, it);
-  const KRangeArg& kr = a.kr[it.r];
-  const int nch = a.split.counts[blockIdx.x];
-  if (nch <= 1) return;
-  const int nvalid = imin(16, kr.len - it.t * 16);
+  const auto st = sum_tile<16, D>(a, blockIdx.x);
+  if (st.n <= 1) return;
   const int k = threadIdx.x / (D / EPT), d0 = (threadIdx.x % (D / EPT)) * EPT;
-  if (k >= nvalid) return;
-  const int64_t off = (((int64_t)it.b * kr.bstride + it.t * 16 + k) * a.kv_heads + it.kvh) * D + d0;
+  if (k >= st.nk) return;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     double x[EPT] = {};
-    for (int ch = 0; ch < nch; ++ch) {
-      const double* src = (const double*)a.split.partials +
-                          partial_row<16>(a, it.b, it.kvh, it.r, it.t, ch) * (2 * D) + (which * nvalid + k) * D + d0;
+    for (int ch = 0; ch < st.n; ++ch) {
+      const double* src = (const double*)partials_of(a) + partial_row(a, st, ch) * (2 * D) + (which * st.nk + k) * D + d0;
 #pragma unroll
       for (int e = 0; e < EPT; ++e) x[e] += src[e];
     }
-    float* dst = (float*)(which == 0 ? kr.dv : kr.dk) + off;
+    float* dst = which == 0 ? (float*)dv_of(a, st.it) + st.dv + k * st.dvs + d0
+                            : (float*)dk_of(a, st.it) + st.dk + k * st.dks + d0;
     const double sc = which == 0 ? 1.0 : (double)a.scale;
 #pragma unroll
     for (int e4 = 0; e4 < EPT / 4; ++e4) {
@@ -357,12 +363,14 @@ __global__ __launch_bounds__(256) void bwd_sum_f32_kernel(const AttnArgs a) {
 
 }  // namespace
 
+#ifndef BDLM_PACKED_CALLS
+
 // a.total_tiles and a.qr's tiles describe 16-row query tiles.
 hipError_t launch_bwd_dq_f32(const AttnArgs& a, int head_dim, hipStream_t s) {
   const int n = workgroups_for(a.total_tiles * a.heads * a.batch);
   if (n == 0) return hipSuccess;
-  if (head_dim == 128) hipLaunchKernelGGL((bwd_dq_f32_kernel<128>), grid_of(n), dim3(kWaves * 64), 0, s, a);
-  else hipLaunchKernelGGL((bwd_dq_f32_kernel<64>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  if (head_dim == 128) hipLaunchKernelGGL((bwd_dq_f32_kernel<128, AttnArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  else hipLaunchKernelGGL((bwd_dq_f32_kernel<64, AttnArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
   return hipGetLastError();
 }
 
@@ -370,17 +378,45 @@ hipError_t launch_bwd_dq_f32(const AttnArgs& a, int head_dim, hipStream_t s) {
 hipError_t launch_bwd_dkv_f32(const AttnArgs& a, int head_dim, hipStream_t s) {
   const int n = workgroups_for(a.split.wgs_per_pair * a.kv_heads * a.batch);
   if (n == 0) return hipSuccess;
-  if (head_dim == 128) hipLaunchKernelGGL((bwd_dkv_f32_kernel<128>), grid_of(n), dim3(kWaves * 64), 0, s, a);
-  else hipLaunchKernelGGL((bwd_dkv_f32_kernel<64>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  if (head_dim == 128) hipLaunchKernelGGL((bwd_dkv_f32_kernel<128, AttnArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  else hipLaunchKernelGGL((bwd_dkv_f32_kernel<64, AttnArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
   return hipGetLastError();
 }
 
 hipError_t launch_bwd_sum_f32(const AttnArgs& a, int head_dim, hipStream_t s) {
   const int n = a.split.tiles_per_pair * a.kv_heads * a.batch;
   if (n == 0) return hipSuccess;
-  if (head_dim == 128) hipLaunchKernelGGL((bwd_sum_f32_kernel<128>), dim3(n), dim3(256), 0, s, a);
-  else hipLaunchKernelGGL((bwd_sum_f32_kernel<64>), dim3(n), dim3(256), 0, s, a);
+  if (head_dim == 128) hipLaunchKernelGGL((bwd_sum_f32_kernel<128, AttnArgs>), dim3(n), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((bwd_sum_f32_kernel<64, AttnArgs>), dim3(n), dim3(256), 0, s, a);
   return hipGetLastError();
 }
+
+#else
+
+hipError_t launch_bwd_dq_f32(const PackedArgs& a, int head_dim, hipStream_t s) {
+  const int n = workgroups_for(a.n_items * a.heads);
+  if (n == 0) return hipSuccess;
+  if (head_dim == 128) hipLaunchKernelGGL((bwd_dq_f32_kernel<128, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  else hipLaunchKernelGGL((bwd_dq_f32_kernel<64, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_bwd_dkv_f32(const PackedArgs& a, int head_dim, hipStream_t s) {
+  const int n = workgroups_for(a.n_items * a.kv_heads);
+  if (n == 0) return hipSuccess;
+  if (head_dim == 128) hipLaunchKernelGGL((bwd_dkv_f32_kernel<128, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  else hipLaunchKernelGGL((bwd_dkv_f32_kernel<64, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_bwd_sum_f32(const PackedArgs& a, int head_dim, hipStream_t s) {
+  const int n = a.n_sums * a.kv_heads;
+  if (n == 0) return hipSuccess;
+  if (head_dim == 128) hipLaunchKernelGGL((bwd_sum_f32_kernel<128, PackedArgs>), dim3(n), dim3(256), 0, s, a);
+  else hipLaunchKernelGGL((bwd_sum_f32_kernel<64, PackedArgs>), dim3(n), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+#endif
 
 }  // namespace bdlm

@@ -51,10 +51,10 @@ constexpr float kSumLimit = 18446744073709551616.f;  // 2^64: a lane's tile sum 
 template <int D, int NW, int HM>
 constexpr int kWavesPerSimd = D == 64 && NW == 4 && HM == 0 ? 3 : 2;  // (NW: waves of all teams)
 
-template <int D, int NW, int NS, int HM, int NT>
+template <int D, int NW, int NS, int HM, int NT, class Args>
 __global__ __launch_bounds__(NT * NW * 64)
     __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<D, NT * NW, HM>, kWavesPerSimd<D, NT * NW, HM>))) void fwd_bf16_kernel(
-        const AttnArgs a) {
+        const Args args) {
   constexpr int BM = NW * 32, BN = 64, KS = D / 16, DT = D / 32;
   constexpr uint32_t RB = D * 2, TB = BN * RB;  // row and tile bytes in LDS
   constexpr int STAGE = 2 * BN * D;             // K tile + V tile (elements), swizzled rows
@@ -71,19 +71,21 @@ __global__ __launch_bounds__(NT * NW * 64)
   const int G = lane >> 4, sl = lane & 15;
 
   QTileItem it;
-  if (!q_tile_item(a, blockIdx.x, it)) return;
+  if (!q_tile_item(args, blockIdx.x, it)) return;
+  auto&& a = call_view(args, it.item, 2);
   const QRangeArg& qr = a.qr[it.r];
   const int kvh = it.h / a.group;
   const int row0 = it.t * BM;
   const int nvalid = imin(BM, qr.len - row0);
   const int64_t H = a.heads, HKV = a.kv_heads;
+  const int64_t QS = q_stride<D>(a), OS = o_stride<D>(a);
 
   // This wave's 32 query rows as MFMA B fragments (rows past the range read as zero).
   bf16x8 qf[KS];
   {
-    const bf16* qbase = (const bf16*)qr.q + (((int64_t)it.b * qr.bstride + row0) * H + it.h) * D;
-    const auto rs = make_rsrc(qbase, (uint32_t)(((int64_t)(nvalid - 1) * H * D + D) * 2));
-    const uint32_t off = (uint32_t)(((int64_t)(w * 32 + l32) * H * D + 8 * half) * 2);
+    const bf16* qbase = (const bf16*)qr.q + row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, QS);
+    const auto rs = make_rsrc(qbase, (uint32_t)(((int64_t)(nvalid - 1) * QS + D) * 2));
+    const uint32_t off = (uint32_t)(((int64_t)(w * 32 + l32) * QS + 8 * half) * 2);
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(bf16x8, buf_load16(rs, off + s * 32));
   }
@@ -126,11 +128,12 @@ __global__ __launch_bounds__(NT * NW * 64)
     int rows_left;
   };
   const bool kwave = w < NW / 2;
+  const int64_t CS = kwave ? k_stride<D>(a) : v_stride<D>(a);  // of the tensor this wave copies
   auto copy_seek = [&](CopyCur cc) -> CopyCur {
     if (cc.c.have) {
       const KRangeArg& kr = a.kr[cc.c.j];
       cc.src = (const bf16*)(kwave ? kr.k : kr.v) +
-               (((int64_t)it.b * kr.bstride + (int64_t)cc.c.t * BN) * HKV + kvh) * D;
+               row_elem<D>(a, it.b, kr.bstride, (int64_t)cc.c.t * BN, HKV, kvh, CS);
       cc.rows_left = kr.len - cc.c.t * BN;
     }
     return cc;
@@ -139,7 +142,7 @@ __global__ __launch_bounds__(NT * NW * 64)
     if (!cc.c.have) return cc;
     if (cc.c.t + NT < cc.c.t1) {
       cc.c.t += NT;
-      cc.src += (int64_t)(NT * BN) * HKV * D;
+      cc.src += (int64_t)(NT * BN) * CS;
       cc.rows_left -= NT * BN;
       return cc;
     }
@@ -152,11 +155,11 @@ __global__ __launch_bounds__(NT * NW * 64)
   uint32_t voff[IPW];
   const int cw = w % (NW / 2);
 #pragma unroll
-  for (int i = 0; i < IPW; ++i) voff[i] = swz_src_offset<D>((cw * IPW + i) * 64 + lane, HKV * D);
+  for (int i = 0; i < IPW; ++i) voff[i] = swz_src_offset<D>((cw * IPW + i) * 64 + lane, CS);
   const bf16* const any_src = (const bf16*)a.kr[0].k;
   auto copy_tile = [&](bf16* st, const CopyCur& cc) __attribute__((always_inline)) {
     const int nrows = cc.c.have ? imin(BN, cc.rows_left) : 0;
-    const uint32_t bytes = cc.c.have ? (uint32_t)(((nrows - 1) * (int)HKV * D + D) * 2) : 0u;
+    const uint32_t bytes = cc.c.have ? (uint32_t)(((nrows - 1) * (int)CS + D) * 2) : 0u;
     const auto r = make_rsrc(cc.c.have ? cc.src : any_src, bytes);
     bf16* dst = st + (kwave ? 0 : BN * D) + cw * IPW * 512;
 #pragma unroll
@@ -409,7 +412,7 @@ __global__ __launch_bounds__(NT * NW * 64)
   const float inv = empty ? 0.f : 1.f / l_tot;
   if (a.out_f32) {
     if (my_row < qr.len) {
-      float* op = (float*)qr.o + (((int64_t)it.b * qr.bstride + my_row) * H + it.h) * D;
+      float* op = (float*)qr.o + row_elem<D>(a, it.b, qr.bstride, my_row, H, it.h, OS);
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -427,7 +430,7 @@ __global__ __launch_bounds__(NT * NW * 64)
     const int wrow0 = row0 + w * 32;
     store_rows_bf16_via_lds<D>(
         lds_addr(lds) + (uint32_t)w * (D * 64), [&](int d, int g4, int e) { return acc[d][g4 * 4 + e] * inv; },
-        (bf16*)qr.o + (((int64_t)it.b * qr.bstride + wrow0) * H + it.h) * D, H * D, qr.len - wrow0, lane);
+        (bf16*)qr.o + row_elem<D>(a, it.b, qr.bstride, wrow0, H, it.h, OS), OS, qr.len - wrow0, lane);
   }
   if (my_row < qr.len) {
     if (half == 0)
@@ -435,6 +438,8 @@ __global__ __launch_bounds__(NT * NW * 64)
           empty ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
   }
 }
+
+#ifndef BDLM_PACKED_CALLS
 
 // HM of the kernel: 0 single-term P (dS), 1 two-term on every tile, 2
 // two-term on the 16-key chunks holding a large probability.
@@ -446,10 +451,10 @@ void launch_hm(const AttnArgs& a, int n, hipStream_t s) {
   const int hm = !(a.hilo & kHiloPv) ? 0 : (a.hilo & kHiloAdaptive) ? 2 : 1;
   const dim3 threads(NT * NW * 64);
   if constexpr (!(D == 64 && NW == kQRowsLongBf16 / 32)) {  // (fwd_short_always)
-    if (hm == 0) hipLaunchKernelGGL((fwd_bf16_kernel<D, NW, NS, 0, NT>), dim3(n), threads, 0, s, a);
+    if (hm == 0) hipLaunchKernelGGL((fwd_bf16_kernel<D, NW, NS, 0, NT, AttnArgs>), dim3(n), threads, 0, s, a);
   }
-  if (hm == 1) hipLaunchKernelGGL((fwd_bf16_kernel<D, NW, NS, 1, NT>), dim3(n), threads, 0, s, a);
-  if (hm == 2) hipLaunchKernelGGL((fwd_bf16_kernel<D, NW, NS, 2, NT>), dim3(n), threads, 0, s, a);
+  if (hm == 1) hipLaunchKernelGGL((fwd_bf16_kernel<D, NW, NS, 1, NT, AttnArgs>), dim3(n), threads, 0, s, a);
+  if (hm == 2) hipLaunchKernelGGL((fwd_bf16_kernel<D, NW, NS, 2, NT, AttnArgs>), dim3(n), threads, 0, s, a);
 }
 
 template <int D>
@@ -469,5 +474,27 @@ hipError_t launch_fwd_bf16(const AttnArgs& a, int head_dim, QTile q, hipStream_t
   else launch_rows<64>(a, q, n, s);
   return hipGetLastError();
 }
+
+#else
+
+}  // namespace
+
+// Packed calls: 128-row tiles, shared by two teams when there are few.
+hipError_t launch_fwd_bf16(const PackedArgs& a, int head_dim, int teams, hipStream_t s) {
+  const int n = workgroups_for(a.n_items * a.heads);
+  if (n == 0) return hipSuccess;
+  constexpr int NW = kQRowsShortBf16 / 32;
+  const dim3 grid(n), threads(teams * NW * 64);
+  if (head_dim == 128) {
+    if (teams == 2) hipLaunchKernelGGL((fwd_bf16_kernel<128, NW, 2, 0, 2, PackedArgs>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((fwd_bf16_kernel<128, NW, 2, 0, 1, PackedArgs>), grid, threads, 0, s, a);
+  } else {
+    if (teams == 2) hipLaunchKernelGGL((fwd_bf16_kernel<64, NW, 2, 0, 2, PackedArgs>), grid, threads, 0, s, a);
+    else hipLaunchKernelGGL((fwd_bf16_kernel<64, NW, 2, 0, 1, PackedArgs>), grid, threads, 0, s, a);
+  }
+  return hipGetLastError();
+}
+
+#endif
 
 }  // namespace bdlm

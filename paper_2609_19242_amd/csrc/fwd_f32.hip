@@ -31,9 +31,9 @@ constexpr int kWaves = 4;
 // relative precision does not depend on the reference.
 constexpr double kRescale = 256.0;
 
-template <int D>
+template <int D, class Args>
 __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void fwd_f32_kernel(
-    const AttnArgs a) {
+    const Args args) {
   constexpr int NC = D / 16;
   // Q as fp64 row operands during the walk, the waves' O^T sums after it
   __shared__ __attribute__((aligned(16))) double lds[kWaves * 16 * kRedRow<D>];
@@ -42,13 +42,15 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   const int i = lane & 15, g = lane >> 4;
 
   QTileItem it;
-  if (!q_tile_item(a, workgroup_id(), it)) return;
+  if (!q_tile_item(args, workgroup_id(), it)) return;
+  auto&& a = call_view(args, it.item, 4);
   const QRangeArg& qr = a.qr[it.r];
   const int kvh = it.h / a.group;
   const int64_t H = a.heads, HKV = a.kv_heads;
   const int row0 = it.t * 16, nvalid = imin(16, qr.len - row0);
-  const int64_t qoff = (((int64_t)it.b * qr.bstride + row0) * H + it.h) * D;
-  stage_row_operands<D>(lds, (const float*)qr.q + qoff, H * D, nvalid, tid, kWaves * 64);
+  const int64_t QS = q_stride<D>(a), OS = o_stride<D>(a);
+  const int64_t qoff = row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, QS);
+  stage_row_operands<D>(lds, (const float*)qr.q + qoff, QS, nvalid, tid, kWaves * 64);
   __syncthreads();
 
   const int pq = qr.pos0 + row0 + imin(i, nvalid - 1);  // this lane's query (a column of S^T)
@@ -72,19 +74,19 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
     }
     return true;
   };
-  auto tile_of = [&](const void* base) __attribute__((always_inline)) {
+  auto tile_of = [&](const void* base, int64_t stride) __attribute__((always_inline)) {
     const KRangeArg& kr = a.kr[j];
-    return row_tile<D>(base, (((int64_t)it.b * kr.bstride + t * 16) * HKV + kvh) * D, imin(16, kr.len - t * 16),
-                       HKV * D);
+    return row_tile<D>(base, row_elem<D>(a, it.b, kr.bstride, t * 16, HKV, kvh, stride), imin(16, kr.len - t * 16),
+                       stride);
   };
   t = t1 = -kWaves;  // the first call starts with range 0
   bool have = advance();
-  if (have) load_rows<D>(kx, tile_of(a.kr[j].k), i, g);
+  if (have) load_rows<D>(kx, tile_of(a.kr[j].k, k_stride<D>(a)), i, g);
   while (have) {
     const KRangeArg& kr = a.kr[j];
     const int tt = t;
     const bool full = tt >= f0 && tt < f1;
-    const RowTile vt = tile_of(kr.v);
+    const RowTile vt = tile_of(kr.v, v_stride<D>(a));
     ColOps<D> vx;
     vx.load(vt, i, g);
     int lo = 0, wid = 0;
@@ -95,7 +97,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
     f64x4 s = row_product<D>(kx, lds, lane) * c;
     // the next tile's K loads run under the softmax and the products below
     have = advance();
-    if (have) load_rows<D>(kx, tile_of(a.kr[j].k), i, g);
+    if (have) load_rows<D>(kx, tile_of(a.kr[j].k, k_stride<D>(a)), i, g);
 
     bool grow = false;
 #pragma unroll
@@ -144,7 +146,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   const bool empty = !(lt > 0.0);
   const double inv = empty ? 0.0 : 1.0 / lt;
   if (q < nvalid) {
-    float* op = (float*)qr.o + qoff + (int64_t)q * H * D + d0;
+    float* op = (float*)qr.o + row_elem<D>(a, it.b, qr.bstride, row0 + q, H, it.h, OS) + d0;
 #pragma unroll
     for (int e4 = 0; e4 < EPT / 4; ++e4) {
       fl4 o;
@@ -165,14 +167,30 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
 
 }  // namespace
 
+#ifndef BDLM_PACKED_CALLS
+
 hipError_t launch_fwd_f32(const AttnArgs& a, int head_dim, hipStream_t s) {
   const int n = workgroups_for(a.total_tiles * a.heads * a.batch);
   if (n == 0) return hipSuccess;
   if (head_dim == 128)
-    hipLaunchKernelGGL((fwd_f32_kernel<128>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+    hipLaunchKernelGGL((fwd_f32_kernel<128, AttnArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
   else
-    hipLaunchKernelGGL((fwd_f32_kernel<64>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+    hipLaunchKernelGGL((fwd_f32_kernel<64, AttnArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
   return hipGetLastError();
 }
+
+#else
+
+hipError_t launch_fwd_f32(const PackedArgs& a, int head_dim, hipStream_t s) {
+  const int n = workgroups_for(a.n_items * a.heads);
+  if (n == 0) return hipSuccess;
+  if (head_dim == 128)
+    hipLaunchKernelGGL((fwd_f32_kernel<128, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  else
+    hipLaunchKernelGGL((fwd_f32_kernel<64, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  return hipGetLastError();
+}
+
+#endif
 
 }  // namespace bdlm

@@ -11,11 +11,13 @@
 
 #include "common.hpp"
 #include "device.hpp"
+#include "packed.hpp"
 
 namespace bdlm {
 
 struct QTileItem {
   int b, h, r, t;  // batch, query head, query range, tile within the range
+  int item;        // packed calls: the plan's item
 };
 
 // Hardware workgroup -> (batch, query head, query range, tile); false: no item.
@@ -41,9 +43,21 @@ __device__ inline bool q_tile_item(const AttnArgs& a, int wg, QTileItem& it) {
   return true;
 }
 
+// The same of a packed call, whose items lie heaviest first in the plan.
+__device__ inline bool q_tile_item(const PackedArgs& a, int wg, QTileItem& it) {
+  int rank;
+  if (!xcd_pair_item(wg, a.kv_heads, a.group * a.n_items, false, it.b, rank)) return false;
+  it.item = rank / a.group;
+  it.h = it.b * a.group + (rank - it.item * a.group);
+  it.b = it.r = 0;
+  it.t = a.items[it.item].tile;
+  return true;
+}
+
 // Key tiles [t0, t1) of key range j that any query position in [pq0, pq1]
 // can see, and the sub-span [f0, f1) every one of them sees completely.
-__device__ inline void key_tile_span(const AttnArgs& a, int j, int qs, int pq0, int pq1, int BN,
+template <class A>
+__device__ inline void key_tile_span(const A& a, int j, int qs, int pq0, int pq1, int BN,
                                      int& t0, int& t1, int& f0, int& f1) {
   const KRangeArg& kr = a.kr[j];
   int lo0, hi0, lo1, hi1;
@@ -62,7 +76,8 @@ __device__ inline void key_tile_span(const AttnArgs& a, int j, int qs, int pq0, 
 }
 
 // First key tile at or after key range jj that the query tile can see.
-__device__ inline bool find_key_tile(const AttnArgs& a, int jj, int qs, int pq0, int pq1, int BN,
+template <class A>
+__device__ inline bool find_key_tile(const A& a, int jj, int qs, int pq0, int pq1, int BN,
                                      int& jo, int& to, int& t1o, int& f0o, int& f1o) {
   for (; jj < a.n_k; ++jj) {
     int a0, a1, b0, b1;
@@ -80,7 +95,8 @@ __device__ inline bool find_key_tile(const AttnArgs& a, int jj, int qs, int pq0,
 }
 
 // Key tiles of all ranges that the query tile can see.
-__device__ inline int count_key_tiles(const AttnArgs& a, int qs, int pq0, int pq1, int BN) {
+template <class A>
+__device__ inline int count_key_tiles(const A& a, int qs, int pq0, int pq1, int BN) {
   int n = 0;
   for (int j = 0; j < a.n_k; ++j) {
     int a0, a1, b0, b1;
@@ -91,7 +107,8 @@ __device__ inline int count_key_tiles(const AttnArgs& a, int qs, int pq0, int pq
 }
 
 // This lane's visible key interval [lo, lo + w) inside key range j (w may be 0).
-__device__ inline void lane_key_interval(const AttnArgs& a, int j, int qs, int pq, int& lo, int& w) {
+template <class A>
+__device__ inline void lane_key_interval(const A& a, int j, int qs, int pq, int& lo, int& w) {
   const KRangeArg& kr = a.kr[j];
   int l, h;
   key_interval(qs, pq, kr.stream, rule_of(a), l, h);

@@ -1,0 +1,179 @@
+"""Packed attention, forward and backward, against the 64-bit oracle: every type and head layout, lengths from none to
+several tiles, more queries than keys and fewer, blocks, windows, strided inputs and outputs, gaps."""
+import math
+
+import pytest
+import torch
+
+import paper_2609_19242_amd as bd
+import synth
+from tests.serving_util import check, packed
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def rows_of(lens, gap=0):
+    out, at = [], 0
+    for n in lens:
+        out.append(at)
+        at += n + gap
+    return out, at
+
+
+def run(ql, kl, H, KV, D, dtype, block=1, window=0, gap=0, scale=0.0, fused=False, backward=True, seed=0):
+    qs, nq = rows_of(ql, gap)
+    ks, nk = rows_of(kl, gap)
+    nq, nk = nq + 3, nk + 3  # rows behind the last sequence
+    if fused:
+        assert ql == kl
+        qkv = synth.normal((nq, H + 2 * KV, D), seed, dtype).to(DEV)
+        q, k, v = qkv[:, :H], qkv[:, H:H + KV], qkv[:, H + KV:]
+    else:
+        q = synth.normal((nq, H, D), seed, dtype).to(DEV)
+        k, v = (synth.normal((nk, KV, D), seed + i, dtype).to(DEV) for i in (1, 2))
+    do = synth.normal((nq, H, D), seed + 3, dtype).to(DEV)
+    # what lies between the sequences is nobody's: NaN there must not be seen
+    for t, st, ln in ((q, qs, ql), (k, ks, kl), (v, ks, kl), (do, qs, ql)):
+        mine = torch.zeros(t.shape[0], dtype=torch.bool)
+        for a, n in zip(st, ln):
+            mine[a:a + n] = True
+        if not (fused and t is not do):
+            t[~mine.to(DEV)] = math.nan
+    plan = bd.packed_plan(ql, kl, heads=H, kv_heads=KV, head_dim=D, dtype=dtype, block_size=block, window=window,
+                          scale=scale, q_starts=qs, k_starts=ks)
+    new = lambda t, stride=None: torch.full(t, 7.0, dtype=dtype, device=DEV)  # noqa: E731
+    o, lse = new((nq, H, D)), torch.full((H, nq), 7.0, device=DEV)
+    bd.packed_fwd(plan, q, k, v, out=(o, lse))
+    ref = packed(q, k, v, list(zip(qs, ql, ks, kl)), scale=scale or None, block=block, window=window,
+                 do=do if backward else None)
+    got = {"o": o, "lse": lse}
+    if backward:
+        if fused:
+            dqkv = new((nq, H + 2 * KV, D))
+            grads = dqkv[:, :H], dqkv[:, H:H + KV], dqkv[:, H + KV:]
+        else:
+            grads = new((nq, H, D)), new((nk, KV, D)), new((nk, KV, D))
+        bd.packed_bwd(plan, q, k, v, o, lse, do, out=grads)
+        got.update(zip(("dq", "dk", "dv"), grads))
+    torch.cuda.synchronize()
+    for n, t in got.items():
+        check(n, t, *ref[n])
+        untouched = torch.isnan(ref[n][0])
+        assert torch.all(t.cpu()[untouched] == 7.0), f"{n}: rows of no sequence were written"
+    return got
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("H,KV,D", [(4, 2, 128), (4, 4, 64), (6, 2, 128), (8, 1, 64), (3, 3, 128)])
+def test_lengths(H, KV, D, dtype):
+    run([1, 0, 129, 17, 64, 200], [1, 0, 129, 17, 64, 200], H, KV, D, dtype, seed=3)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("ql,kl", [([1], [1]), ([1, 1, 1], [257, 64, 5]), ([5, 70, 131], [300, 70, 0]),
+                                   ([90, 260, 33], [40, 3, 32]), ([0, 9], [130, 9]), ([0], [0])])
+def test_queries_are_the_last_tokens(ql, kl, dtype):
+    run(ql, kl, 4, 2, 128, dtype, seed=5)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("block,window", [(32, 0), (7, 0), (1, 1), (1, 50), (16, 40), (24, 5), (500, 0), (3, 100000)])
+def test_blocks_and_windows(block, window, dtype):
+    run([150, 33, 260], [150, 80, 200], 4, 2, 64, dtype, block=block, window=window, seed=7)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("H,KV,D", [(4, 2, 128), (3, 1, 64)])
+def test_fused_projection(H, KV, D, dtype):
+    run([60, 130, 1], [60, 130, 1], H, KV, D, dtype, fused=True, seed=9)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_gaps_are_left_alone(dtype):
+    run([40, 1, 129], [70, 128, 129], 4, 2, 128, dtype, gap=11, seed=11)
+
+
+def test_scale():
+    run([100, 30], [100, 30], 4, 2, 128, BF, scale=0.5, seed=13)
+
+
+def test_long_sequences_with_cut_walks():
+    run([900, 30, 1100], [900, 700, 1100], 2, 1, 128, BF, seed=15)
+
+
+def test_many_sequences_fill_the_card():
+    ql = [1 + (37 * i) % 140 for i in range(150)]
+    run(ql, ql, 8, 4, 64, BF, backward=False, seed=17)
+
+
+def test_same_bits_twice_and_in_another_packing():
+    """A sequence's results do not depend on where it lies (its tiles walk alike whatever the others are)."""
+    a = run([140, 60], [140, 60], 4, 2, 128, BF, seed=19, backward=False)
+    b = run([140, 60], [140, 60], 4, 2, 128, BF, seed=19, backward=False)
+    assert torch.equal(a["o"], b["o"]) and torch.equal(a["lse"], b["lse"])
+
+
+def test_one_sequence_equals_the_joint_call_on_its_clean_half():
+    L, H, KV, D = 384, 4, 2, 128
+    q, k, v = (synth.normal((L, h, D), 20 + i, BF).to(DEV) for i, h in enumerate((H, KV, KV)))
+    plan = bd.packed_plan([L], heads=H, kv_heads=KV, head_dim=D, dtype=BF)
+    o, lse = bd.packed_fwd(plan, q, k, v)
+    p = bd.make_problem(1, L, 1, H, KV, D, BF)
+    o2, lse2 = torch.empty_like(o), torch.empty_like(lse)
+    r = bd.Range(bd.CLEAN, 0, L)
+    bd.attn_partial_fwd(p, r, q, o2, lse2, r, k, v)
+    torch.cuda.synchronize()
+    assert torch.equal(o, o2) and torch.equal(lse, lse2)
+
+
+def test_graph_replays():
+    H, KV, D = 4, 2, 128
+    ql = [100, 7, 260]
+    n = sum(ql)
+    q, k, v, do = (synth.normal((n, h, D), 30 + i, BF).to(DEV) for i, h in enumerate((H, KV, KV, H)))
+    plan = bd.packed_plan(ql, heads=H, kv_heads=KV, head_dim=D, dtype=BF)
+
+    def step():
+        o, lse = bd.packed_fwd(plan, q, k, v)
+        return (o, lse) + bd.packed_bwd(plan, q, k, v, o, lse, do)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        step()
+    torch.cuda.current_stream().wait_stream(s)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        outs = step()
+    for i in range(4):
+        q.copy_(synth.normal(q.shape, 50 + i, BF))
+        g.replay()
+        torch.cuda.synchronize()
+        eager = step()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, eager):
+            assert torch.equal(a, b)
+
+
+def test_two_streams_at_once():
+    H, KV, D = 4, 2, 64
+    ql = [300, 41]
+    plan = bd.packed_plan(ql, heads=H, kv_heads=KV, head_dim=D, dtype=BF)
+    ins = [[synth.normal((sum(ql), h, D), 60 + 10 * j + i, BF).to(DEV) for i, h in enumerate((H, KV, KV, H))]
+           for j in range(2)]
+    want = []
+    for q, k, v, do in ins:
+        o, lse = bd.packed_fwd(plan, q, k, v)
+        want.append((o, lse) + bd.packed_bwd(plan, q, k, v, o, lse, do))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ins]
+    got = []
+    for s, (q, k, v, do) in zip(streams, ins):
+        with torch.cuda.stream(s):
+            o, lse = bd.packed_fwd(plan, q, k, v)
+            got.append((o, lse) + bd.packed_bwd(plan, q, k, v, o, lse, do))
+    torch.cuda.synchronize()
+    for a, b in zip(want, got):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
