@@ -348,6 +348,91 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
                             bdlm_rows dv, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
+ * A paged cache of keys and values, and its pages' bookkeeping, all in device
+ * memory owned by the caller.  Sequence s holds lens[s] tokens; token t is row
+ * t % page_size of page table[s][t / page_size].  refs[p] counts the tables
+ * that hold page p (0: free).  A page that is not full belongs to one sequence.
+ *
+ * The page operations run in stream order and must not overlap in time with
+ * each other or with attention over the same cache; they need no host round
+ * trip and may be captured in a graph.  They check the lists that they are
+ * given, which lie in device memory, on the device: status[0] becomes a
+ * bdlm_cache_status, and, except for BDLM_CACHE_OK, grow and fork change nothing else.
+ * status holds the outcome of the last grow, fork, free or compact.
+ */
+typedef enum {
+  BDLM_CACHE_OK = 0,
+  BDLM_CACHE_BAD_LIST = 1, /* a number out of range or listed twice, or against the call's rules */
+  BDLM_CACHE_NO_PAGES = 2  /* too few free pages: status[1] more are needed */
+} bdlm_cache_status;
+
+typedef struct {
+  void *k, *v;      /* [layers][pages][page_size][kv_heads][head_dim], 16-byte aligned */
+  int32_t* table;   /* [seqs][max_pages] */
+  int32_t* lens;    /* [seqs] */
+  int32_t* refs;    /* [pages] */
+  int32_t* status;  /* [2] */
+  int32_t* work;    /* bdlm_cache_work_bytes() bytes, contents ignored on entry */
+  int64_t layers, pages, page_size, seqs, max_pages; /* seqs <= 2^19; max_pages * page_size < 2^30 */
+  int32_t kv_heads, head_dim, dtype, reserved;       /* reserved must be 0 */
+} bdlm_cache;
+
+size_t bdlm_cache_work_bytes(int64_t pages, int64_t seqs);
+
+/* Makes room for counts[i] >= 0 more tokens of sequence seqs[i] (n different
+ * sequences): lens grows, and new pages come from the free ones, lowest
+ * numbers first, to the sequences in the order of the list. */
+bdlm_status bdlm_cache_grow(const bdlm_cache* c, int64_t n, const int32_t* seqs, const int32_t* counts,
+                            hipStream_t stream);
+
+/* Makes sequence children[i] a copy of parents[i]: full pages are shared, the
+ * rows of a last partial page are copied, in all layers, to a page of its own
+ * (free ones, lowest numbers first).  Children are different, empty and no
+ * parents; a parent may have several. */
+bdlm_status bdlm_cache_fork(const bdlm_cache* c, int64_t n, const int32_t* parents, const int32_t* children,
+                            hipStream_t stream);
+
+/* Empties sequences: their pages lose a reference each, their table entries
+ * become -1.  One listed twice is freed once; a number out of range is passed
+ * over (BDLM_CACHE_BAD_LIST, the others are freed). */
+bdlm_status bdlm_cache_free(const bdlm_cache* c, int64_t n, const int32_t* seqs, hipStream_t stream);
+
+/* Moves live pages to the lowest numbers: with L of them, the i-th free page
+ * below L takes the data, in all layers, and the references of the i-th live page from L on; all
+ * tables follow.  Afterwards pages L and up are free. */
+bdlm_status bdlm_cache_compact(const bdlm_cache* c, hipStream_t stream);
+
+/* Writes K and V rows of a layer: counts[i] rows from row starts[i] of k and v
+ * on (starts NULL: from row i * rows / n on, at most rows / n) become the last
+ * counts[i] tokens of sequence seqs[i] (after grow).  Rows out of `rows`, out
+ * of the sequence or in pages out of the cache are passed over.  Sequences are
+ * different. */
+bdlm_status bdlm_cache_write(const bdlm_cache* c, int64_t layer, int64_t n, const int32_t* seqs, const int32_t* counts,
+                             const int32_t* starts, int64_t rows, bdlm_rows k, bdlm_rows v, hipStream_t stream);
+
+/*
+ * Attention of decoding requests over the cache: request r is sequence
+ * seqs[r], whose keys and values are in the cache, and its `rows` query rows
+ * are its last tokens.  Row i sees the keys up to its own position, lens - rows
+ * + i, or, with block = 1 (a block that is being denoised), all lens keys.  The
+ * first `prefix` tokens are the same pages' in all requests and are read
+ * through the first request's table, once for all; the result is that of
+ * attention over each request's own tokens.
+ *   q, o : [requests][rows][heads][head_dim] in the cache's dtype
+ *   lse  : [requests][heads][rows] fp32, natural log
+ * Rows that see nothing (also: of a sequence number out of range) get O = 0
+ * and LSE = -inf.  A page number outside the cache reads as rows of zeros, and
+ * lens are taken between 0 and what a table holds.
+ * workspace: bdlm_prefix_attn_workspace_bytes() bytes, 256-byte aligned, contents ignored on
+ * entry; calls that may overlap in time need one each.
+ */
+size_t bdlm_prefix_attn_workspace_bytes(const bdlm_cache* c, int64_t requests, int64_t rows, int32_t heads,
+                                        int64_t prefix);
+bdlm_status bdlm_prefix_attn(const bdlm_cache* c, int64_t layer, int64_t requests, const int32_t* seqs, int64_t rows,
+                             int32_t heads, int64_t prefix, int32_t block, float scale, const void* q, void* o,
+                             float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
  * Kernel timing (observability).  While enabled for the calling thread, every
  * kernel the library enqueues is bracketed by two hipEvents recorded on its
  * stream.  bdlm_timing_collect() waits for the recorded events, writes up to

@@ -29,6 +29,8 @@ __all__ = [
     "attn_bwd_workspace_bytes", "attn_bwd", "attn_bwd_noalloc", "visible_pairs",
     "joint_fwd", "joint_bwd", "timing_enable", "timing_collect", "useful_flops",
     "PackedPlan", "packed_plan", "packed_fwd", "packed_bwd",
+    "Cache", "cache_new", "cache_grow", "cache_write", "cache_fork", "cache_free", "cache_compact",
+    "prefix_attn", "prefix_attn_workspace_bytes", "CACHE_OK", "CACHE_BAD_LIST", "CACHE_NO_PAGES",
 ]
 
 BF16, F32 = 0, 1
@@ -120,6 +122,7 @@ def lib() -> ctypes.CDLL:
                      "bdlm_attn_bwd", "bdlm_attn_bwd_noalloc"):
             getattr(L, name).restype = ctypes.c_int
         packed.declare(L)
+        cache.declare(L)
         _LIB = L
     return _LIB
 
@@ -472,3 +475,6 @@ def default_scale(head_dim: int) -> float:
 
 from . import packed  # noqa: E402  (needs the helpers above)
 from .packed import PackedPlan, packed_bwd, packed_fwd, packed_plan  # noqa: E402
+from . import cache  # noqa: E402
+from .cache import (CACHE_BAD_LIST, CACHE_NO_PAGES, CACHE_OK, Cache, cache_compact, cache_fork, cache_free,  # noqa: E402
+                    cache_grow, cache_new, cache_write, prefix_attn, prefix_attn_workspace_bytes)

@@ -17,9 +17,9 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libbdlm_attn.so")
 BUILD_DIR = os.path.join(HERE, "_build")
-SOURCES = ["api.cpp", "packed_api.cpp", "fwd_bf16.hip", "fwd_f32.hip", "merge.hip", "bwd_bf16.hip", "bwd_dkdv.hip", "bwd_dq.hip",
+SOURCES = ["api.cpp", "packed_api.cpp", "cache_api.cpp", "fwd_bf16.hip", "fwd_f32.hip", "merge.hip", "bwd_bf16.hip", "bwd_dkdv.hip", "bwd_dq.hip",
            "bwd_f32.hip", "packed_fwd_bf16.hip", "packed_fwd_f32.hip", "packed_bwd_dq.hip", "packed_bwd_dkdv.hip",
-           "packed_bwd_f32.hip"]
+           "packed_bwd_f32.hip", "prefix_bf16.hip", "prefix_f32.hip", "prefix_merge.hip", "cache_pages.hip"]
 ARCH = os.environ.get("BDLM_OFFLOAD_ARCH", "gfx950")
 # Per-source code-generation options.  The dK/dV kernel runs one wave per SIMD,
 # so its speed is its own instruction stream: the iterative ILP scheduler keeps
@@ -35,7 +35,8 @@ EXTRA_FLAGS = {"bwd_bf16.hip": ["-mllvm", "-amdgpu-sched-strategy=iterative-ilp"
                # back around every loop iteration (36 instead of 71 TFLOP/s in a
                # stand-alone stream of v_mfma_f64_16x16x4_f64)
                "fwd_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-               "bwd_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+               "bwd_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+               "prefix_f32.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 
 # the same kernels for packed calls
 EXTRA_FLAGS.update({"packed_" + src: EXTRA_FLAGS[src] for src in ("bwd_dkdv.hip", "fwd_f32.hip", "bwd_f32.hip")})

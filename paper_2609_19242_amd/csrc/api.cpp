@@ -30,7 +30,8 @@ thread_local std::string g_err;
 // (the dK/dV records include the sum over chunks, where there are any)
 const char* const kKernelNames[kKCount] = {"fwd_bf16",      "fwd_f32",     "lse_merge",    "bwd_dq_f32",
                                            "bwd_dkdv_bf16", "bwd_dq_bf16", "bwd_dkdv_f32", "packed_fwd",
-                                           "packed_bwd_dq", "packed_bwd_dkdv"};
+                                           "packed_bwd_dq", "packed_bwd_dkdv",
+                                           "prefix_attn", "prefix_merge", "cache_pages", "cache_write"};
 struct TimingRec {
   int id;
   hipEvent_t a, b;

@@ -1,0 +1,392 @@
+// Operations on the pages of a cache, gfx950: grow, fork, free, compact, and
+// writing new rows.  All bookkeeping is on the device (tables, lengths and
+// reference counts), so a decoding loop needs no host round trip and can be
+// captured; the results do not depend on timing: free pages are given out in
+// ascending order to the listed sequences in their order, and counts change by
+// integer atomics.
+//
+// Bookkeeping runs in one workgroup (a few microseconds: the work is a scan of
+// the reference counts up to the pages needed and of the list); it checks the
+// list first and changes nothing but the status if it does not hold.  Page data
+// is moved by a second kernel, 16 bytes per lane, at the speed of a copy.
+#include "cache.hpp"
+#include "device.hpp"
+
+namespace bdlm {
+
+namespace {
+
+constexpr int kT = 1024;         // threads of the bookkeeping workgroup
+constexpr int kWordsLds = 16384; // a bit per sequence: 2^19 sequences
+
+// Outcomes (bdlm_cache_status).
+enum : int { kOk = 0, kBadList = 1, kNoPages = 2 };
+
+// Exclusive prefix sum over the workgroup's threads; total of all.
+__device__ __forceinline__ int block_scan(int x, int& total, int* wsum) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+  int v = x;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const int y = __shfl_up(v, s);
+    if (lane >= s) v += y;
+  }
+  __syncthreads();  // (the sums of a scan before are read)
+  if (lane == 63) wsum[w] = v;
+  __syncthreads();
+  int base = 0, t = 0;
+  for (int k = 0; k < kT / 64; ++k) {
+    const int y = wsum[k];
+    if (k < w) base += y;
+    t += y;
+  }
+  total = t;
+  return base + v - x;
+}
+
+__device__ __forceinline__ int clamped_len(const CacheArg& c, int seq) {
+  const int64_t top = (int64_t)c.max_pages * c.page_size;
+  const int n = c.lens[seq];
+  return n < 0 ? 0 : (int64_t)n > top ? (int)top : n;
+}
+__device__ __forceinline__ int pages_of(const CacheArg& c, int64_t tokens) {
+  return (int)((tokens + c.page_size - 1) / c.page_size);
+}
+
+// The first `need` free pages in ascending order into list[0 .. need); false:
+// fewer are free (found: how many).
+__device__ bool take_free(const CacheArg& c, int64_t need, int32_t* list, int* wsum, int& found) {
+  found = 0;
+  for (int64_t p0 = 0; p0 < c.pages && found < need; p0 += kT) {
+    const int64_t p = p0 + threadIdx.x;
+    const bool is_free = p < c.pages && c.refs[p] == 0;
+    int total;
+    const int at = found + block_scan(is_free ? 1 : 0, total, wsum);
+    if (is_free && at < need) list[at] = (int32_t)p;
+    found += total;
+  }
+  __syncthreads();  // the list is read by other threads
+  return found >= need;
+}
+
+// One bit per sequence: false if a listed number is out of range or listed twice.
+__device__ bool mark(const CacheArg& c, const int32_t* list, int n, unsigned* bits, int* bad) {
+  for (int i = threadIdx.x; i < (c.seqs + 31) / 32; i += kT) bits[i] = 0;
+  if (threadIdx.x == 0) *bad = 0;
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += kT) {
+    const int s = list[i];
+    if ((unsigned)s >= (unsigned)c.seqs) *bad = 1;
+    else if (atomicOr(&bits[s >> 5], 1u << (s & 31)) >> (s & 31) & 1) *bad = 1;
+  }
+  __syncthreads();
+  return *bad == 0;
+}
+
+// work: [0] 1 if the operation goes ahead, [1] moves; then a list of pages.
+__global__ __launch_bounds__(kT) void cache_grow_kernel(const CacheArg c, const CacheList l, int32_t* work) {
+  __shared__ unsigned bits[kWordsLds];
+  __shared__ int wsum[kT / 64], bad;
+  int32_t* const list = work + kCacheHead;
+  bool ok = mark(c, l.a, l.n, bits, &bad);
+  if (ok) {
+    for (int i = threadIdx.x; i < l.n; i += kT) {
+      const int s = l.a[i], add = l.b[i];
+      if (add < 0 || (int64_t)clamped_len(c, s) + add > (int64_t)c.max_pages * c.page_size) bad = 1;
+    }
+    __syncthreads();
+    ok = bad == 0;
+  }
+  int64_t need = 0;
+  int found = 0;
+  bool enough = true;
+  if (ok) {
+    for (int i0 = 0; i0 < l.n; i0 += kT) {
+      const int i = i0 + threadIdx.x;
+      int pages = 0;
+      if (i < l.n) {
+        const int n = clamped_len(c, l.a[i]);
+        pages = pages_of(c, (int64_t)n + l.b[i]) - pages_of(c, n);
+      }
+      int total;
+      block_scan(pages, total, wsum);
+      need += total;
+    }
+    enough = take_free(c, need, list, wsum, found);
+  }
+  if (threadIdx.x == 0) {
+    c.status[0] = !ok ? kBadList : enough ? kOk : kNoPages;
+    c.status[1] = ok && !enough ? (int32_t)(need - found) : 0;
+  }
+  if (!ok || !enough) return;
+  int64_t given = 0;
+  for (int i0 = 0; i0 < l.n; i0 += kT) {
+    const int i = i0 + threadIdx.x;
+    int n = 0, add = 0, first = 0, pages = 0;
+    if (i < l.n) {
+      n = clamped_len(c, l.a[i]);
+      add = l.b[i];
+      first = pages_of(c, n);
+      pages = pages_of(c, (int64_t)n + add) - first;
+    }
+    int total;
+    const int64_t at = given + block_scan(pages, total, wsum);
+    given += total;
+    if (i < l.n) {
+      const int s = l.a[i];
+      for (int k = 0; k < pages; ++k) {
+        const int32_t p = list[at + k];
+        c.table[(int64_t)s * c.max_pages + first + k] = p;
+        c.refs[p] = 1;
+      }
+      c.lens[s] = n + add;
+    }
+  }
+}
+
+// Pages for the children's partial last pages: list[i] = child i's page or -1.
+__global__ __launch_bounds__(kT) void cache_fork_plan_kernel(const CacheArg c, const CacheList l, int32_t* work) {
+  __shared__ unsigned bits[kWordsLds];
+  __shared__ int wsum[kT / 64], bad;
+  int32_t* const of_child = work + kCacheHead;
+  int32_t* const list = of_child + l.n;
+  bool ok = mark(c, l.b, l.n, bits, &bad);
+  if (ok) {
+    for (int i = threadIdx.x; i < l.n; i += kT) {
+      const int p = l.a[i];
+      // parents in range and no children themselves; children empty
+      if ((unsigned)p >= (unsigned)c.seqs || (bits[p >> 5] >> (p & 31) & 1) || c.lens[l.b[i]] != 0) bad = 1;
+    }
+    __syncthreads();
+    ok = bad == 0;
+  }
+  int64_t need = 0;
+  int found = 0;
+  bool enough = true;
+  if (ok) {
+    for (int i0 = 0; i0 < l.n; i0 += kT) {
+      const int i = i0 + threadIdx.x;
+      const int part = i < l.n && clamped_len(c, l.a[i]) % c.page_size != 0;
+      int total;
+      const int at = block_scan(part, total, wsum);
+      if (i < l.n) of_child[i] = part ? (int32_t)(need + at) : -1;
+      need += total;
+    }
+    enough = take_free(c, need, list, wsum, found);
+  }
+  if (threadIdx.x == 0) {
+    c.status[0] = !ok ? kBadList : enough ? kOk : kNoPages;
+    c.status[1] = ok && !enough ? (int32_t)(need - found) : 0;
+    work[0] = ok && enough;
+  }
+  if (!ok || !enough) return;
+  for (int i = threadIdx.x; i < l.n; i += kT) {
+    const int at = of_child[i];
+    if (at >= 0) of_child[i] = list[at];
+  }
+}
+
+// 16-byte copies of n bytes by the workgroup's threads.
+__device__ __forceinline__ void copy_bytes(char* dst, const char* src, int64_t n) {
+  const int64_t step = (int64_t)blockDim.x * 16;
+  int64_t b = (int64_t)threadIdx.x * 16;
+  for (; b + 3 * step < n; b += 4 * step) {
+    u32x4 x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = *(const u32x4*)(src + b + k * step);
+#pragma unroll
+    for (int k = 0; k < 4; ++k) *(u32x4*)(dst + b + k * step) = x[k];
+  }
+  for (; b < n; b += step) *(u32x4*)(dst + b) = *(const u32x4*)(src + b);
+}
+
+// Workgroup (i, y): the rows of child i's partial page in K (V) of layer y / 2; y = 0 also writes its table row.
+__global__ __launch_bounds__(256) void cache_fork_kernel(const CacheArg c, const CacheList l, const int32_t* work) {
+  if (work[0] == 0) return;
+  const int i = blockIdx.x, parent = l.a[i], child = l.b[i];
+  const int n = clamped_len(c, parent), full = n / c.page_size, part = n - full * c.page_size;
+  const int page = work[kCacheHead + i];
+  const int32_t* const from = c.table + (int64_t)parent * c.max_pages;
+  for (int y = blockIdx.y; y < 2 * c.layers; y += gridDim.y) {
+    if (part > 0) {
+      const int old = from[full];
+      if ((unsigned)old < (unsigned)c.pages) {
+        char* const base = ((y & 1) ? c.v : c.k) + (y >> 1) * c.layer_bytes;
+        copy_bytes(base + page * c.page_bytes, base + old * c.page_bytes, (int64_t)part * c.row_bytes);
+      }
+    }
+  }
+  if (blockIdx.y != 0) return;
+  int32_t* const to = c.table + (int64_t)child * c.max_pages;
+  for (int k = threadIdx.x; k < c.max_pages; k += 256) {
+    int p = -1;
+    if (k < full) {
+      p = from[k];
+      if ((unsigned)p < (unsigned)c.pages) atomicAdd(&c.refs[p], 1);
+    } else if (k == full && part > 0) {
+      p = page;
+      c.refs[p] = 1;
+    }
+    to[k] = p;
+  }
+  if (threadIdx.x == 0) c.lens[child] = n;
+}
+
+// A sequence listed twice is freed once: whoever takes its length frees it.
+__global__ __launch_bounds__(256) void cache_free_kernel(const CacheArg c, const CacheList l) {
+  __shared__ int len;
+  const int s = l.a[blockIdx.x];
+  if ((unsigned)s >= (unsigned)c.seqs) {
+    if (threadIdx.x == 0) c.status[0] = kBadList;
+    return;
+  }
+  if (threadIdx.x == 0) len = atomicExch(&c.lens[s], 0);
+  __syncthreads();
+  if (len <= 0) return;
+  const int64_t top = (int64_t)c.max_pages * c.page_size;
+  const int held = pages_of(c, len < top ? len : top);
+  int32_t* const row = c.table + (int64_t)s * c.max_pages;
+  for (int k = threadIdx.x; k < held; k += 256) {
+    const int p = row[k];
+    row[k] = -1;
+    if ((unsigned)p >= (unsigned)c.pages) continue;
+    int old = c.refs[p];
+    while (old > 0) {  // (a count never falls below none)
+      const int seen = atomicCAS(&c.refs[p], old, old - 1);
+      if (seen == old) break;
+      old = seen;
+    }
+  }
+}
+
+__global__ void cache_status_kernel(int32_t* status) { status[threadIdx.x] = 0; }
+
+// Moves: the i-th free page below the live count takes the i-th live page at
+// or above it.  list[0 .. n): free pages, list[pages .. pages + n): live ones;
+// list[2 pages + p]: where page p goes.
+__global__ __launch_bounds__(kT) void cache_compact_plan_kernel(const CacheArg c, int32_t* work) {
+  __shared__ int wsum[kT / 64];
+  int32_t* const dst = work + kCacheHead;
+  int32_t* const src = dst + c.pages;
+  int64_t live = 0;
+  for (int64_t p0 = 0; p0 < c.pages; p0 += kT) {
+    const int64_t p = p0 + threadIdx.x;
+    int total;
+    block_scan(p < c.pages && c.refs[p] > 0 ? 1 : 0, total, wsum);
+    live += total;
+  }
+  int64_t holes = 0, moves = 0;
+  for (int64_t p0 = 0; p0 < c.pages; p0 += kT) {
+    const int64_t p = p0 + threadIdx.x;
+    const bool in = p < c.pages, used = in && c.refs[p] > 0;
+    const bool hole = in && !used && p < live, move = used && p >= live;
+    int th, tm;
+    const int64_t ah = holes + block_scan(hole ? 1 : 0, th, wsum), am = moves + block_scan(move ? 1 : 0, tm, wsum);
+    if (hole) dst[ah] = (int32_t)p;
+    if (move) {
+      src[am] = (int32_t)p;
+      src[c.pages + p] = (int32_t)am;
+    }
+    holes += th;
+    moves += tm;
+  }
+  if (threadIdx.x == 0) {
+    work[0] = (int32_t)live;
+    work[1] = (int32_t)moves;
+    c.status[0] = kOk;
+    c.status[1] = 0;
+  }
+}
+
+__global__ __launch_bounds__(256) void cache_compact_kernel(const CacheArg c, const int32_t* work) {
+  const int32_t* const dst = work + kCacheHead;
+  const int32_t* const src = dst + c.pages;
+  const int live = work[0], moves = work[1];
+  const int64_t units = (int64_t)moves * 2 * c.layers;
+  for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
+    const int y = (int)(u / moves), m = (int)(u - (int64_t)y * moves);
+    char* const base = ((y & 1) ? c.v : c.k) + (y >> 1) * c.layer_bytes;
+    copy_bytes(base + dst[m] * c.page_bytes, base + src[m] * c.page_bytes, c.page_bytes);
+  }
+  const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
+  for (int64_t e = at; e < (int64_t)c.seqs * c.max_pages; e += step) {
+    const int p = c.table[e];
+    // (a number that no table should hold, a free page's, stays)
+    if (p >= live && p < c.pages && c.refs[p] > 0) c.table[e] = dst[src[c.pages + p]];
+  }
+}
+// The counts move last: the kernel before reads them.
+__global__ __launch_bounds__(256) void cache_compact_refs_kernel(const CacheArg c, const int32_t* work) {
+  const int32_t* const dst = work + kCacheHead;
+  const int32_t* const src = dst + c.pages;
+  const int moves = work[1];
+  for (int m = blockIdx.x * 256 + threadIdx.x; m < moves; m += gridDim.x * 256) {
+    c.refs[dst[m]] = c.refs[src[m]];
+    c.refs[src[m]] = 0;
+  }
+}
+
+// Rows of new tokens: sequence i's counts[i] rows go to its last positions.  Workgroup (i, y): every gridDim.y-th row.
+__global__ __launch_bounds__(256) void cache_write_kernel(const CacheArg c, const CacheRows r) {
+  const int i = blockIdx.x, s = r.seqs[i];
+  if ((unsigned)s >= (unsigned)c.seqs) return;
+  const int per = r.rows / r.n;
+  const int64_t first = r.starts ? r.starts[i] : (int64_t)i * per;
+  const int count = r.counts[i], n = clamped_len(c, s);
+  const int64_t limit = r.starts ? r.rows : first + per;  // rows of this sequence in the new tensors end here
+  // 16-byte pieces of several rows at a time
+  const int pieces = c.row_bytes / 16;
+  const int64_t total = (int64_t)count * pieces;
+  for (int64_t x = (int64_t)blockIdx.y * 256 + threadIdx.x; x < total; x += (int64_t)gridDim.y * 256) {
+    const int j = (int)(x / pieces), b = (int)(x - (int64_t)j * pieces) * 16;
+    const int64_t row = first + j;
+    const int pos = n - count + j;
+    if (row < 0 || row >= limit || pos < 0) continue;
+    const int e = pos / c.page_size;
+    const int page = c.table[(int64_t)s * c.max_pages + e];
+    if ((unsigned)page >= (unsigned)c.pages) continue;
+    const int64_t at = r.layer * c.layer_bytes + page * c.page_bytes + (int64_t)(pos - e * c.page_size) * c.row_bytes + b;
+    const u32x4 xk = *(const u32x4*)(r.k + row * r.k_stride + b), xv = *(const u32x4*)(r.v + row * r.v_stride + b);
+    *(u32x4*)(c.k + at) = xk;
+    *(u32x4*)(c.v + at) = xv;
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_grow(const CacheArg& c, const CacheList& l, int32_t* work, hipStream_t s) {
+  hipLaunchKernelGGL(cache_grow_kernel, dim3(1), dim3(kT), 0, s, c, l, work);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_fork(const CacheArg& c, const CacheList& l, int32_t* work, hipStream_t s) {
+  hipLaunchKernelGGL(cache_fork_plan_kernel, dim3(1), dim3(kT), 0, s, c, l, work);
+  if (l.n > 0) {
+    const int y = 2 * c.layers;
+    hipLaunchKernelGGL(cache_fork_kernel, dim3(l.n, y < 4096 ? y : 4096), dim3(256), 0, s, c, l, work);
+  }
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_free(const CacheArg& c, const CacheList& l, hipStream_t s) {
+  hipLaunchKernelGGL(cache_status_kernel, dim3(1), dim3(2), 0, s, c.status);
+  if (l.n > 0) hipLaunchKernelGGL(cache_free_kernel, dim3(l.n), dim3(256), 0, s, c, l);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_compact(const CacheArg& c, int32_t* work, hipStream_t s) {
+  hipLaunchKernelGGL(cache_compact_plan_kernel, dim3(1), dim3(kT), 0, s, c, work);
+  hipLaunchKernelGGL(cache_compact_kernel, dim3(2048), dim3(256), 0, s, c, work);
+  hipLaunchKernelGGL(cache_compact_refs_kernel, dim3(64), dim3(256), 0, s, c, work);
+  return hipGetLastError();
+}
+
+hipError_t launch_cache_write(const CacheArg& c, const CacheRows& r, hipStream_t s) {
+  if (r.n == 0 || r.rows == 0) return hipSuccess;
+  const int64_t per = ((r.starts ? r.rows : r.rows / r.n) * (int64_t)(c.row_bytes / 16) + 255) / 256;
+  const int y = (int)(per < 1 ? 1 : per > 64 ? 64 : per);
+  hipLaunchKernelGGL(cache_write_kernel, dim3(r.n, y), dim3(256), 0, s, c, r);
+  return hipGetLastError();
+}
+
+}  // namespace bdlm

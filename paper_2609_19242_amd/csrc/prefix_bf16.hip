@@ -1,0 +1,378 @@
+// Attention of decoding requests over a paged cache, bf16, gfx950: a long
+// prefix that all requests share is read once for all of them, each request's
+// own keys once (PrefixArgs in cache.hpp says how rows and keys are cut up).
+//
+// Per chunk of keys and tile of rows: S^T = K Q^T, an online softmax, and
+// O^T += V^T P^T with v_mfma_f32_32x32x16_bf16, the products, layouts and LDS
+// swizzle of the forward (fwd_bf16.hip).  A workgroup of eight waves runs an
+// item in one of two forms:
+//  * shared: 256 rows, 32 per wave; the waves share 64-key tiles in three LDS
+//    stages, copied two tiles ahead.  For the prefix of a batch and for blocks
+//    of query rows: bound by the matrix cores from some 300 rows on.
+//  * by waves: 32 rows; every wave takes every eighth 32-key tile through its
+//    own 16 KB of LDS, without barriers, and the waves' sums are merged at the
+//    end.  For single tokens (few rows): bound by reading K and V.  A wave asks
+//    for the next tile's keys as soon as its scores are there, and for its
+//    values after P V, so that it always has copies in flight.
+// Keys come by LDS-DMA copies with a 64-bit address per lane (a cache may be
+// larger than 4 GB), rows past the chunk from a row of zeros; the page numbers
+// of a chunk wait in LDS.
+#include "cache.hpp"
+#include "device.hpp"
+
+namespace bdlm {
+
+namespace {
+
+constexpr int kNW = 8;
+constexpr float kLn2 = 0.69314718055994530942f;
+constexpr float kLimit = 64.f;  // the running max moves when a score passes it by this much (powers of two)
+
+__device__ __attribute__((aligned(256))) const uint32_t zero_row[64] = {};
+
+// Global -> LDS copy of 16 bytes per lane: lane i's land at m0 + 16 i.  Inline
+// assembly, as in bwd_dkdv.hip: for the builtin the compiler waits for all
+// copies in flight before any LDS read.
+__device__ __forceinline__ void dma16(const char* src, uint32_t lds_byte) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(lds_byte) : "memory");
+}
+__device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void vm_wait() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+// Softmax state and O^T of a wave's 32 rows (a lane owns row lane % 32; its
+// sum covers the keys of its half until the end).
+template <int D>
+struct RowState {
+  f32x16 acc[D / 32];
+  float m, l;
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) acc[d][i] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+  }
+};
+
+// P of U 32-key steps from the scores (in place in s), as bf16 operands;
+// rounding P to bf16 is off by at most 2^-9 relative, as in the forward.
+template <int D, int U>
+__device__ __forceinline__ void softmax_step(RowState<D>& st, f32x16 (&s)[U], bf16x8 (&pb)[2 * U], float c) {
+  float mx = s[0][0];
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);
+  mx = fmaxf(mx, partner(mx)) * c;
+  if (__builtin_amdgcn_ballot_w64(mx > st.m + kLimit || (st.m == -INFINITY && mx > -INFINITY)) != 0) {
+    const float mn = fmaxf(st.m, mx);
+    const float al = st.m == -INFINITY ? 0.f : exp2f_fast(st.m - mn);
+    st.l *= al;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) st.acc[d][i] *= al;
+    st.m = mn;
+  }
+  const float m = st.m == -INFINITY ? 0.f : st.m;
+#pragma unroll
+  for (int u = 0; u < U; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float p = exp2f_fast(fmaf(s[u][i], c, -m));
+      st.l += p;
+      pb[2 * u + (i >> 3)][i & 7] = to_bf16(p);
+    }
+}
+
+template <int D>
+struct Lds {
+  static constexpr uint32_t RB = D * 2;
+  static constexpr uint32_t Stage = 2 * 64 * RB;     // K and V of 64 keys
+  static constexpr uint32_t Wave = 2 * 32 * RB;      // K and V of 32 keys; later 32 rows of sums
+  static constexpr uint32_t Tiles = kNW * Wave > 3 * Stage ? kNW * Wave : 3 * Stage;
+  static constexpr uint32_t Pages = Tiles;
+  static constexpr uint32_t Ml = Pages + kPrefixTableEntries * 4;
+  static constexpr uint32_t Bytes = Ml + kNW * 32 * 8;
+  static_assert(Wave == 32 * D * 4, "a wave's sums fit its tiles");
+};
+
+template <int D>
+__global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void prefix_bf16_kernel(
+    const PrefixArgs a) {
+  using L = Lds<D>;
+  constexpr int KS = D / 16, DT = D / 32, CH = D / 8;
+  constexpr uint32_t RB = L::RB;
+  __shared__ __attribute__((aligned(1024))) unsigned char lds[L::Bytes];
+  const uint32_t L0 = lds_addr(lds);
+  int* const pages = (int*)(lds + L::Pages);
+  float* const red_m = (float*)(lds + L::Ml);  // [wave][32], the sums behind it
+  float* const red_l = red_m + kNW * 32;
+
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int l32 = lane & 31, half = lane >> 5, G = lane >> 4, sl = lane & 15;
+
+  PrefixItem it;
+  if (!prefix_item(a, blockIdx.x, a.prefix_shared ? kPrefixSharedRows : kPrefixWaveRows,
+                   a.own_shared ? kPrefixSharedRows : kPrefixWaveRows, it))
+    return;
+  const bool single = a.prefix_chunks + a.own_chunks == 1;
+  const float c = a.scale_log2;
+  const int nkeys = it.k1 - it.k0;
+
+  // The chunk's page numbers; those outside the cache become -1, whose rows read as zeros.
+  const int page0 = it.k0 / a.page_size;
+  if (nkeys > 0) {
+    const int n = (it.k1 - 1) / a.page_size - page0 + 1;
+    for (int e = tid; e < n; e += kNW * 64) {
+      const int p = a.table[(int64_t)it.seq * a.max_pages + page0 + e];
+      pages[e] = (unsigned)p < (unsigned)a.pages ? p : -1;
+    }
+  }
+
+  // This wave's rows as MFMA B fragments.
+  const int lrow = (it.shared ? w * 32 : 0) + l32;  // within the item's rows
+  const bool row_ok = lrow < it.nrows;
+  const PrefixRow row = prefix_row(a, it.kvh, it.row0 + imin(lrow, it.nrows - 1));
+  const int64_t out_row = (int64_t)row.token * a.heads + row.head;
+  bf16x8 qf[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s)
+    qf[s] = *(const bf16x8*)((const bf16*)a.q + out_row * D + 16 * s + 8 * half);
+  const int end = imin(row.end, it.k1);
+  __syncthreads();
+  // (waited for here: the loops' own waits count copies that the compiler does not know of)
+#pragma unroll
+  for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
+
+  const int64_t row_bytes = (int64_t)a.kv_heads * RB;
+  const char* const kb = a.k + (int64_t)it.kvh * RB;
+  const char* const vb = a.v + (int64_t)it.kvh * RB;
+  const char* const zero = (const char*)zero_row;
+  // Byte offset of a key's row in K (and V), -1: a row of zeros.
+  auto key_offset = [&](int key) __attribute__((always_inline)) -> int64_t {
+    if (key >= it.k1) return -1;
+    const int e = key / a.page_size;
+    const int p = pages[e - page0];
+    return p < 0 ? -1 : ((int64_t)p * a.page_size + (key - e * a.page_size)) * row_bytes;
+  };
+  const uint32_t yrow = swz_row_part<D>(l32, half);
+  const uint32_t ytr0 = swz_tr_part<D>(G, sl, 0), ytr1 = swz_tr_part<D>(G, sl, 8);
+  // The 16-byte chunk of its row that lane `lane` fetches when the copy's first row is row0 of a tile.
+  constexpr int RPI = 64 / CH;  // rows per copy
+  auto copy_chunk = [&](int row0) { return (uint32_t)((lane % CH) ^ chunk_swz<D>(row0 + lane / CH)) * 16u; };
+
+  RowState<D> st;
+  st.init();
+
+  if (it.shared) {
+    // ---- eight waves share 64-key tiles; waves 0-3 copy K, 4-7 V, 16 rows each
+    constexpr int NS = 3, IPW = 16 / RPI;
+    const int ntiles = (nkeys + 63) / 64;
+    const char* const base = w < 4 ? kb : vb;
+    const int crow = (w & 3) * 16;
+    auto copy_tile = [&](int t, int stage) __attribute__((always_inline)) {
+      const int64_t mine = key_offset(t < ntiles ? it.k0 + t * 64 + crow + (lane & 15) : it.k1);
+      const uint32_t dst = L0 + stage * L::Stage + (w < 4 ? 0u : 64 * RB) + crow * RB;
+#pragma unroll
+      for (int i = 0; i < IPW; ++i) {
+        const int r = i * RPI + lane / CH;
+        const int lo = __shfl((int)(uint32_t)mine, r), hi = __shfl((int)(mine >> 32), r);
+        const int64_t off = ((int64_t)hi << 32) | (uint32_t)lo;
+        dma16((off < 0 ? zero : base + off) + copy_chunk(crow + i * RPI), dst + i * 1024);
+      }
+    };
+    const bool any = __builtin_amdgcn_ballot_w64(row_ok && end > it.k0) != 0;
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s) copy_tile(s, s);
+    vm_wait_barrier<IPW*(NS - 2)>();
+    int cur = 0;
+    for (int t = 0; t < ntiles; ++t) {
+      copy_tile(t + NS - 1, cur == 0 ? NS - 1 : cur - 1);
+      const int key0 = it.k0 + t * 64;
+      if (any && __builtin_amdgcn_ballot_w64(end > key0) != 0) {
+        const uint32_t sb = L0 + cur * L::Stage;
+        const uint32_t zr = sb + yrow;
+        f32x16 s[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) s[u] = mfma32(lds_load16((zr ^ (32u * k)) + u * 32 * RB), qf[k], s[u]);
+        if (__builtin_amdgcn_ballot_w64(end < key0 + 64) != 0) {
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+              if (key0 + u * 32 + (i >> 2) * 8 + 4 * half + (i & 3) >= end) s[u][i] = -INFINITY;
+        }
+        bf16x8 pb[4];
+        softmax_step<D, 2>(st, s, pb, c);
+        const uint32_t zt0 = sb + 64 * RB + ytr0, zt1 = sb + 64 * RB + ytr1;
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+            st.acc[d] = mfma32(cat(lds_read_tr_at((zt0 ^ (64u * d)) + u * 16 * RB),
+                                   lds_read_tr_at((zt1 ^ (64u * d)) + u * 16 * RB)),
+                               pb[u], st.acc[d]);
+      }
+      vm_wait_barrier<IPW*(NS - 2)>();
+      cur = cur == NS - 1 ? 0 : cur + 1;
+    }
+    vm_wait<0>();  // copies in flight land before the LDS is released
+    const float l = st.l + partner(st.l);
+    const bool empty = !(l > 0.f);
+    const float inv = empty ? 0.f : 1.f / l;
+    if (row_ok) {
+      if (single) {
+        bf16* op = (bf16*)a.o + out_row * D;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int g4 = 0; g4 < 4; ++g4) {
+            bf16x4 x;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) x[e] = to_bf16(st.acc[d][4 * g4 + e] * inv);
+            *(bf16x4*)(op + 32 * d + 8 * g4 + 4 * half) = x;
+          }
+        if (half == 0) a.lse[prefix_lse_at(a, row)] = empty ? -INFINITY : (st.m + log2f(l)) * kLn2;
+      } else {
+        const int64_t at = (int64_t)it.part * a.requests * a.rows * a.heads + out_row;
+        if (!empty) {
+          float* op = a.part_o + at * D;
+#pragma unroll
+          for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int g4 = 0; g4 < 4; ++g4) {
+              f32x4 x;
+#pragma unroll
+              for (int e = 0; e < 4; ++e) x[e] = st.acc[d][4 * g4 + e] * inv;
+              *(f32x4*)(op + 32 * d + 8 * g4 + 4 * half) = x;
+            }
+        }
+        if (half == 0) a.part_lse[at] = empty ? -INFINITY : st.m + log2f(l);
+      }
+    }
+    return;
+  }
+
+  // ---- by waves: tile t of 32 keys to wave t % 8
+  constexpr int NI = 32 / RPI;  // copies per tensor and tile
+  const int ntiles = (nkeys + 31) / 32;
+  const uint32_t wb = L0 + w * L::Wave, wv = wb + 32 * RB;
+  auto row_offset = [&](int t) { return key_offset(it.k0 + t * 32 + l32); };
+  auto copy = [&](const char* base, int64_t mine, uint32_t dst) __attribute__((always_inline)) {
+    lds_done();  // the tile there has been read
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = i * RPI + lane / CH;
+      const int lo = __shfl((int)(uint32_t)mine, r), hi = __shfl((int)(mine >> 32), r);
+      const int64_t off = ((int64_t)hi << 32) | (uint32_t)lo;
+      dma16((off < 0 ? zero : base + off) + copy_chunk(i * RPI), dst + i * 1024);
+    }
+  };
+  if (w < ntiles) {
+    int64_t mine = row_offset(w);
+    copy(kb, mine, wb);
+    copy(vb, mine, wv);
+    for (int t = w; t < ntiles; t += kNW) {
+      const int key0 = it.k0 + t * 32;
+      const int64_t next = row_offset(t + kNW);  // (past the chunk: zeros)
+      vm_wait<NI>();                             // the keys are there, the values in flight
+      f32x16 s[1];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
+#pragma unroll
+      for (int k = 0; k < KS; ++k) s[0] = mfma32(lds_load16((wb + yrow) ^ (32u * k)), qf[k], s[0]);
+      copy(kb, next, wb);
+      if (__builtin_amdgcn_ballot_w64(end < key0 + 32) != 0) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          if (key0 + (i >> 2) * 8 + 4 * half + (i & 3) >= end) s[0][i] = -INFINITY;
+      }
+      bf16x8 pb[2];
+      softmax_step<D, 1>(st, s, pb, c);
+      vm_wait<NI>();  // the values are there, the next keys in flight
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+          st.acc[d] = mfma32(cat(lds_read_tr_at(((wv + ytr0) ^ (64u * d)) + u * 16 * RB),
+                                 lds_read_tr_at(((wv + ytr1) ^ (64u * d)) + u * 16 * RB)),
+                             pb[u], st.acc[d]);
+      copy(vb, next, wv);
+    }
+    vm_wait<0>();
+  }
+  // Merge the waves: sums of 32 rows per wave through LDS, [row][D], with the
+  // 16-byte pieces of row r rotated by r so that the lanes' stores spread over the banks.
+  const float l = st.l + partner(st.l);
+  if (half == 0) {
+    red_m[w * 32 + l32] = st.m;
+    red_l[w * 32 + l32] = l;
+  }
+  constexpr int PC = D / 4;  // 16-byte pieces of a row of sums
+  if (w < ntiles) {
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) {
+        f32x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = st.acc[d][4 * g4 + e];
+        const int piece = (8 * d + 2 * g4 + half + l32) % PC;
+        *(f32x4*)(lds + w * L::Wave + l32 * (D * 4) + piece * 16) = x;
+      }
+  }
+  __syncthreads();
+  const int used = imin(ntiles, kNW);
+  for (int n = tid; n < it.nrows * PC; n += kNW * 64) {
+    const int r = n / PC, piece = n % PC;
+    float m = -INFINITY;
+    for (int k = 0; k < used; ++k) m = fmaxf(m, red_m[k * 32 + r]);
+    float lt = 0.f;
+    f32x4 x = {0.f, 0.f, 0.f, 0.f};
+    for (int k = 0; k < used; ++k) {
+      const float mk = red_m[k * 32 + r];
+      if (mk == -INFINITY) continue;
+      const float f = exp2f_fast(mk - m);
+      lt += red_l[k * 32 + r] * f;
+      x += *(const f32x4*)(lds + k * L::Wave + r * (D * 4) + ((piece + r) % PC) * 16) * f;
+    }
+    const bool empty = !(lt > 0.f);
+    x *= empty ? 0.f : 1.f / lt;
+    const PrefixRow pr = prefix_row(a, it.kvh, it.row0 + r);
+    const int64_t orow = (int64_t)pr.token * a.heads + pr.head;
+    if (single) {
+      bf16x4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = to_bf16(x[e]);
+      *(bf16x4*)((bf16*)a.o + orow * D + piece * 4) = y;
+      if (piece == 0) a.lse[prefix_lse_at(a, pr)] = empty ? -INFINITY : (m + log2f(lt)) * kLn2;
+    } else {
+      const int64_t at = (int64_t)it.part * a.requests * a.rows * a.heads + orow;
+      if (!empty) *(f32x4*)(a.part_o + at * D + piece * 4) = x;
+      if (piece == 0) a.part_lse[at] = empty ? -INFINITY : m + log2f(lt);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_prefix_bf16(const PrefixArgs& a, int head_dim, hipStream_t s) {
+  const int n = a.prefix_items + a.own_items;
+  if (n == 0) return hipSuccess;
+  if (head_dim == 128) hipLaunchKernelGGL((prefix_bf16_kernel<128>), dim3(n), dim3(kNW * 64), 0, s, a);
+  else hipLaunchKernelGGL((prefix_bf16_kernel<64>), dim3(n), dim3(kNW * 64), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace bdlm
