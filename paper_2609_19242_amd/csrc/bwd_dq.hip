@@ -30,6 +30,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // its transpose reads (K^T), V its row reads (dP^T).
   constexpr uint32_t RB = D * 2, TB = BN * RB;
   constexpr int STAGE = 2 * BN * D;
+  constexpr bool kPacked = kIsPacked<Args>;
   // Copies: each tile is BN * D / 8 16-byte slots, TI instructions of 64 lanes;
   // waves 0 .. NW/2 - 1 copy K and the others V, IPW instructions each.
   constexpr int TI = BN * D / 8 / 64, IPW = TI / (NW / 2);
@@ -101,14 +102,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // workspace: (LSE log2(e), D), or (-LSE / scale, -D) for the scheduled
   // kernel (stats form 1).
   float lse2 = INFINITY;
-  const float dl = dsum;
+  float dl = dsum;
   if (row_ok) {
     const float z = qr.lse[((int64_t)it.b * H + it.h) * qr.bstride + my_row];
     lse2 = (z == -INFINITY) ? INFINITY : z * kLog2e;
     if (half == 0) {
       const int64_t si = ((int64_t)it.b * H + it.h) * qr.len + my_row;
       if (a.stats_form) {
-        qr.delta[si] = -dsum;
+        if constexpr (!kPacked) qr.delta[si] = -dsum;  // (packed calls: behind the walk)
         qr.l2[si] = (z == -INFINITY) ? -INFINITY : -z / a.scale;
       } else {
         qr.delta[si] = dsum;
@@ -271,6 +272,29 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
             const int kk = base + u * 32 + (i >> 2) * 8 + (i & 3);
             if ((unsigned)kk >= (unsigned)lane_w) sacc[u][i] = -INFINITY;
           }
+        // Packed calls: a row all of whose keys lie in this tile gets its D from
+        // here.  D = sum_j P_ij dP_ij, so that sum_j dS_ij = 0; the D formed from
+        // the rounded O misses it by up to 2^-9 |dO||O|, which is much of dS where
+        // a row has few keys (one key: all of it).  (D lies in dpacc already.)
+        if constexpr (kPacked) {
+          const int kstart = a.kr[j].pos0 + t * BN - lane_lo;
+          float rest = 0.f, z = lse2;
+          asm volatile("" : "+v"(z));  // (or the compiler keeps these exponentials for the ones below, and spills)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              rest = fmaf(exp2f_fast(fmaf(sacc[u][i], c, -z)), dpacc[u][i], rest);
+              if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
+            }
+          rest += partner(rest);
+          if (kstart > 0 || kstart + BN < lane_w) rest = 0.f;
+          dl += rest;  // (no other tile has keys of the row)
+#pragma unroll
+          for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dpacc[u][i] -= rest;
+        }
       }
 
       // dS^T = P^T (dP^T - D) in the S^T register layout, rounded to bf16; HM 1
@@ -343,6 +367,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // the workgroup's LDS is released.
   __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
 
+  if constexpr (kPacked) {
+    if (row_ok && half == 0) qr.delta[((int64_t)it.b * H + it.h) * qr.len + my_row] = -dl;
+  }
   if (a.out_f32) {
     if (row_ok) {
       float* op = (float*)qr.dq + row_elem<D>(a, it.b, qr.bstride, my_row, H, it.h, dq_stride<D>(a));
