@@ -12,7 +12,6 @@ there is no fallback path.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import functools
 import math
@@ -172,17 +171,16 @@ def _torch_stream(stream, device) -> torch.cuda.Stream:
     return torch.cuda.ExternalStream(handle, device=device)
 
 
-@contextlib.contextmanager
-def device_stream(device, stream):
-    """The raw handle of ``stream`` (default: the current stream of ``device``), with ``device`` current meanwhile."""
-    if stream is not None:
+def _launch(device, stream, call, *args):
+    """``call(*args, handle)``, with the handle of ``stream`` (default: the current stream of ``device``) and with
+    ``device`` current meanwhile; raises if it fails."""
+    if device.index != torch._C._cuda_getDevice():
         with torch.cuda.device(device):
-            yield _stream(stream)
-    elif device.index == torch.cuda.current_device():
-        yield torch._C._cuda_getCurrentRawStream(device.index)
-    else:
-        with torch.cuda.device(device):
-            yield torch._C._cuda_getCurrentRawStream(device.index)
+            return _launch(device, stream, call, *args)
+    handle = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else _stream(stream)
+    status = call(*args, handle)
+    if status != 0:
+        _check(status)
 
 
 def _dtype_code(dt: torch.dtype) -> int:

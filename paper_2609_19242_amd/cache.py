@@ -10,8 +10,8 @@ from typing import Optional
 
 import torch
 
-from . import _check, _dtype_code, _expect, _on_device, device_stream, lib
-from .packed import _Rows, _workspace
+from . import _dtype_code, _expect, _launch, _on_device, lib
+from .packed import _Rows, _rows, _workspace
 
 __all__ = ["Cache", "cache_new", "cache_grow", "cache_write", "cache_fork", "cache_free", "cache_compact",
            "prefix_attn", "prefix_attn_workspace_bytes", "CACHE_OK", "CACHE_BAD_LIST", "CACHE_NO_PAGES"]
@@ -76,6 +76,7 @@ class Cache:
         self._record = _Cache(k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(), refs.data_ptr(),
                               status.data_ptr(), self._work.data_ptr(), layers, pages, page_size, seqs, max_pages,
                               kv_heads, head_dim, code, 0)
+        self._ref = ctypes.byref(self._record)
 
     def __repr__(self):
         return (f"Cache(layers={self.layers}, pages={self.pages} x {self.page_size}, seqs={self.seqs} x {self.max_pages} "
@@ -99,10 +100,17 @@ def _cache(c):
 
 
 def _list(c, name, t, n=None):
+    """An int32 list on the cache's device: its address."""
     if not isinstance(t, torch.Tensor) or t.dim() != 1:
         raise ValueError(f"{name} must be a one-dimensional int32 tensor")
-    _expect(name, t, torch.int32, t.shape if n is None else (n,))
-    _on_device(c.device, **{name: t})
+    if t.dtype is not torch.int32:
+        raise TypeError(f"{name} must be torch.int32, got {t.dtype}")
+    if n is not None and t.shape[0] != n:
+        raise ValueError(f"{name} has {t.shape[0]} entries, not {n}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.device != c.device:
+        raise ValueError(f"{name} must be on {c.device}, got {t.device}")
     return t.data_ptr()
 
 
@@ -111,8 +119,7 @@ def cache_grow(cache: Cache, seqs, counts, stream=None):
     c = _cache(cache)
     a = _list(c, "seqs", seqs)
     b = _list(c, "counts", counts, seqs.shape[0])
-    with device_stream(c.device, stream) as s:
-        _check(lib().bdlm_cache_grow(ctypes.byref(c._record), seqs.shape[0], a, b, s))
+    _launch(c.device, stream, lib().bdlm_cache_grow, c._ref, seqs.shape[0], a, b)
 
 
 def cache_fork(cache: Cache, parents, children, stream=None):
@@ -120,37 +127,20 @@ def cache_fork(cache: Cache, parents, children, stream=None):
     c = _cache(cache)
     a = _list(c, "parents", parents)
     b = _list(c, "children", children, parents.shape[0])
-    with device_stream(c.device, stream) as s:
-        _check(lib().bdlm_cache_fork(ctypes.byref(c._record), parents.shape[0], a, b, s))
+    _launch(c.device, stream, lib().bdlm_cache_fork, c._ref, parents.shape[0], a, b)
 
 
 def cache_free(cache: Cache, seqs, stream=None):
     """Empties sequences and gives back the pages that no other sequence holds."""
     c = _cache(cache)
     a = _list(c, "seqs", seqs)
-    with device_stream(c.device, stream) as s:
-        _check(lib().bdlm_cache_free(ctypes.byref(c._record), seqs.shape[0], a, s))
+    _launch(c.device, stream, lib().bdlm_cache_free, c._ref, seqs.shape[0], a)
 
 
 def cache_compact(cache: Cache, stream=None):
     """Moves live pages into the holes below them, so that the free pages are the last ones."""
     c = _cache(cache)
-    with device_stream(c.device, stream) as s:
-        _check(lib().bdlm_cache_compact(ctypes.byref(c._record), s))
-
-
-def _new_rows(c, name, t):
-    if not isinstance(t, torch.Tensor):
-        raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
-    if t.dtype != c.dtype:
-        raise TypeError(f"{name} must be {c.dtype}, got {t.dtype}")
-    KV, D = c.kv_heads, c.head_dim
-    if t.dim() != 3 or t.shape[1:] != (KV, D):
-        raise ValueError(f"{name} must have shape (rows, {KV}, {D}), got {tuple(t.shape)}")
-    n, st = t.shape[0], t.stride()
-    if n and (st[2] != 1 or (KV > 1 and st[1] != D) or (n > 1 and st[0] < KV * D)):
-        raise ValueError(f"{name} must hold each row's heads contiguously (only rows may lie apart)")
-    return _Rows(t.data_ptr(), st[0] if n > 1 else KV * D)
+    _launch(c.device, stream, lib().bdlm_cache_compact, c._ref)
 
 
 def cache_write(cache: Cache, layer: int, seqs, counts, k, v, starts: Optional[torch.Tensor] = None, stream=None):
@@ -161,26 +151,28 @@ def cache_write(cache: Cache, layer: int, seqs, counts, k, v, starts: Optional[t
     n = seqs.shape[0]
     b = _list(c, "counts", counts, n)
     at = _list(c, "starts", starts, n) if starts is not None else None
-    rk, rv = _new_rows(c, "k", k), _new_rows(c, "v", v)
-    if k.shape[0] != v.shape[0]:
-        raise ValueError(f"k has {k.shape[0]} rows, v has {v.shape[0]}")
-    _on_device(c.device, k=k, v=v)
-    with device_stream(c.device, stream) as s:
-        _check(lib().bdlm_cache_write(ctypes.byref(c._record), layer, n, a, b, at, k.shape[0], rk, rv, s))
+    rk, rv = _rows(c, "k", k, c.kv_heads, 0), _rows(c, "v", v, c.kv_heads, 0)
+    rows = k.shape[0]
+    if rows != v.shape[0]:
+        raise ValueError(f"k has {rows} rows, v has {v.shape[0]}")
+    _launch(c.device, stream, lib().bdlm_cache_write, c._ref, layer, n, a, b, at, rows, rk, rv)
 
 
 def _check_q(c, q):
     if not isinstance(q, torch.Tensor) or q.dim() != 4:
         raise ValueError("q must be a [requests][rows][heads][head_dim] tensor")
-    _expect("q", q, c.dtype, (q.shape[0], q.shape[1], q.shape[2], c.head_dim))
+    R, n, H, D = q.shape
+    _expect("q", q, c.dtype, (R, n, H, c.head_dim))
+    if q.device != c.device:
+        raise ValueError(f"q must be on {c.device}, got {q.device}")
+    return R, n, H
 
 
-def prefix_attn_workspace_bytes(q, cache: Cache, prefix: int) -> int:
+def prefix_attn_workspace_bytes(q, cache: Cache, prefix: int = 0) -> int:
     """Workspace of :func:`prefix_attn` for queries like ``q``."""
     c = _cache(cache)
-    _check_q(c, q)
-    R, n, H, _ = q.shape
-    return int(lib().bdlm_prefix_attn_workspace_bytes(ctypes.byref(c._record), R, n, H, prefix))
+    R, n, H = _check_q(c, q)
+    return int(lib().bdlm_prefix_attn_workspace_bytes(c._ref, R, n, H, prefix))
 
 
 def prefix_attn(q, cache: Cache, layer: int, seqs, prefix: int = 0, block: bool = False, scale: float = 0.0,
@@ -188,29 +180,28 @@ def prefix_attn(q, cache: Cache, layer: int, seqs, prefix: int = 0, block: bool 
     """Attention of the last ``rows`` tokens of the sequences ``seqs`` (int32 ``[requests]``) over their keys in the
     cache: q ``[requests][rows][heads][head_dim]``, causal, or, with ``block``, every row sees all of its sequence.
     The first ``prefix`` tokens, which all requests share, are read once for all of them, through the first one's table.
-    Returns ``(o, lse)`` with ``lse [requests][heads][rows]`` fp32, or writes into ``out``."""
+    Returns ``(o, lse)`` with ``lse [requests][heads][rows]`` fp32, or writes into ``out``.  ``workspace``: a device
+    tensor of :func:`prefix_attn_workspace_bytes` (calls that may overlap in time need one each); allocated if not
+    given."""
     c = _cache(cache)
-    _check_q(c, q)
-    R, n, H, D = q.shape
+    R, n, H = _check_q(c, q)
     a = _list(c, "seqs", seqs, R)
-    if out is not None:
+    if out is None:
+        o = torch.empty_like(q)
+        lse = torch.empty((R, H, n), dtype=torch.float32, device=q.device)
+    else:
         if len(out) != 2:
             raise ValueError("out must be (o, lse)")
         o, lse = out
         _expect("o", o, c.dtype, q.shape)
         _expect("lse", lse, torch.float32, (R, H, n))
-    _on_device(c.device, q=q)
-    if out is None:
-        o = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        lse = torch.empty((R, H, n), dtype=torch.float32, device=q.device)
-    else:
         _on_device(c.device, o=o, lse=lse)
-    nbytes = 0
     if workspace is None:
-        nbytes = lib().bdlm_prefix_attn_workspace_bytes(ctypes.byref(c._record), R, n, H, prefix)
-    workspace = _workspace(workspace, nbytes, c.device, stream)
-    with device_stream(c.device, stream) as s:
-        _check(lib().bdlm_prefix_attn(ctypes.byref(c._record), layer, R, a, n, H, prefix, int(bool(block)), scale,
-                                      q.data_ptr(), o.data_ptr(), lse.data_ptr(), workspace.data_ptr(),
-                                      workspace.numel() * workspace.element_size(), s))
+        nbytes = lib().bdlm_prefix_attn_workspace_bytes(c._ref, R, n, H, prefix)
+        workspace = _workspace(None, nbytes, c.device, stream)
+    else:
+        _workspace(workspace, 0, c.device, stream)
+        nbytes = workspace.numel() * workspace.element_size()
+    _launch(c.device, stream, lib().bdlm_prefix_attn, c._ref, layer, R, a, n, H, prefix, 1 if block else 0, scale,
+            q.data_ptr(), o.data_ptr(), lse.data_ptr(), workspace.data_ptr(), nbytes)
     return o, lse

@@ -22,10 +22,10 @@ namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
 
-template <int D, int NW, int NST, int HM, class Args>
+template <int D, int NW, int NST, int HM, class Args, int HP = 1>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void bwd_dq_kernel(
     const Args args) {
-  constexpr int BM = NW * 32, BN = 64, KS = D / 16, DT = D / 32;
+  constexpr int BM = NW * 32 / HP, BN = 64, KS = D / 16, DT = D / 32;
   // K and V tiles with swizzled rows: K serves both its row reads (S^T) and
   // its transpose reads (K^T), V its row reads (dP^T).
   constexpr uint32_t RB = D * 2, TB = BN * RB;
@@ -42,10 +42,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int G = lane >> 4, sl = lane & 15;
 
   QTileItem it;
-  if (!q_tile_item(args, blockIdx.x, it)) return;
+  if (!q_tile_item<HP>(args, blockIdx.x, it)) return;
   auto&& a = call_view(args, it.item, 2);
   const QRangeArg& qr = a.qr[it.r];
   const int kvh = it.h / a.group;
+  const int h = HP == 1 ? it.h : it.h + w % HP, wrow = w / HP * 32;  // this wave's head and rows of the tile
   const int row0 = it.t * BM;
   const int nvalid = imin(BM, qr.len - row0);
   const int64_t H = a.heads;
@@ -57,11 +58,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   float dsum = 0.f;
   {
     const int64_t QS = q_stride<D>(a), DS = do_stride<D>(a), OS = o_stride<D>(a);
-    const int64_t qoff = row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, QS);
-    const int64_t doff = row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, DS);
-    const int64_t ooff = row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, OS);
+    const int64_t qoff = row_elem<D>(a, it.b, qr.bstride, row0, H, h, QS);
+    const int64_t doff = row_elem<D>(a, it.b, qr.bstride, row0, H, h, DS);
+    const int64_t ooff = row_elem<D>(a, it.b, qr.bstride, row0, H, h, OS);
     auto bytes_of = [&](int64_t st) { return (uint32_t)(((int64_t)(nvalid - 1) * st + D) * 2); };
-    auto off_of = [&](int64_t st) { return (uint32_t)(((int64_t)(w * 32 + l32) * st + 8 * half) * 2); };
+    auto off_of = [&](int64_t st) { return (uint32_t)(((int64_t)(wrow + l32) * st + 8 * half) * 2); };
     const auto rq = make_rsrc((const bf16*)qr.q + qoff, bytes_of(QS));
     const auto rdo = make_rsrc((const bf16*)qr.dO + doff, bytes_of(DS));
     const uint32_t off_q = off_of(QS), off_d = off_of(DS), off = off_of(OS), bytes = bytes_of(OS);
@@ -93,7 +94,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     }
   }
   dsum += partner(dsum);
-  const int my_row = row0 + w * 32 + l32;
+  const int my_row = row0 + wrow + l32;
   const bool row_ok = my_row < qr.len;
   const int pq = qr.pos0 + imin(my_row, qr.len - 1);
   const int pq0 = qr.pos0 + row0, pq1 = qr.pos0 + row0 + nvalid - 1;
@@ -104,10 +105,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   float lse2 = INFINITY;
   float dl = dsum;
   if (row_ok) {
-    const float z = qr.lse[((int64_t)it.b * H + it.h) * qr.bstride + my_row];
+    const float z = qr.lse[((int64_t)it.b * H + h) * qr.bstride + my_row];
     lse2 = (z == -INFINITY) ? INFINITY : z * kLog2e;
     if (half == 0) {
-      const int64_t si = ((int64_t)it.b * H + it.h) * qr.len + my_row;
+      const int64_t si = ((int64_t)it.b * H + h) * qr.len + my_row;
       if (a.stats_form) {
         if constexpr (!kPacked) qr.delta[si] = -dsum;  // (packed calls: behind the walk)
         qr.l2[si] = (z == -INFINITY) ? -INFINITY : -z / a.scale;
@@ -368,11 +369,11 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
 
   if constexpr (kPacked) {
-    if (row_ok && half == 0) qr.delta[((int64_t)it.b * H + it.h) * qr.len + my_row] = -dl;
+    if (row_ok && half == 0) qr.delta[((int64_t)it.b * H + h) * qr.len + my_row] = -dl;
   }
   if (a.out_f32) {
     if (row_ok) {
-      float* op = (float*)qr.dq + row_elem<D>(a, it.b, qr.bstride, my_row, H, it.h, dq_stride<D>(a));
+      float* op = (float*)qr.dq + row_elem<D>(a, it.b, qr.bstride, my_row, H, h, dq_stride<D>(a));
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -386,15 +387,15 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   } else if constexpr (HM != 2) {
     // bf16 dQ through LDS, as the forward's O.
     asm volatile("s_barrier" ::: "memory");
-    const int wrow0 = row0 + w * 32;
+    const int wrow0 = row0 + wrow;
     store_rows_bf16_via_lds<D>(
         lds_addr(lds) + (uint32_t)w * (D * 64), [&](int d, int g4, int e) { return acc[d][g4 * 4 + e] * a.scale; },
-        (bf16*)qr.dq + row_elem<D>(a, it.b, qr.bstride, wrow0, H, it.h, dq_stride<D>(a)), dq_stride<D>(a),
+        (bf16*)qr.dq + row_elem<D>(a, it.b, qr.bstride, wrow0, H, h, dq_stride<D>(a)), dq_stride<D>(a),
         qr.len - wrow0, lane);
   } else if (row_ok) {
     // The adaptive two-term kernel stores directly: the staged form needs the
     // last few registers it has and made it spill.
-    bf16* op = (bf16*)qr.dq + row_elem<D>(a, it.b, qr.bstride, my_row, H, it.h, dq_stride<D>(a));
+    bf16* op = (bf16*)qr.dq + row_elem<D>(a, it.b, qr.bstride, my_row, H, h, dq_stride<D>(a));
 #pragma unroll
     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -442,12 +443,20 @@ hipError_t launch_bwd_dq_bf16(const AttnArgs& a, int head_dim, int rows, hipStre
 
 }  // namespace
 
-hipError_t launch_bwd_dq_bf16(const PackedArgs& a, int head_dim, hipStream_t s) {
-  const int n = workgroups_for(a.n_items * a.heads);
-  if (n == 0) return hipSuccess;
+template <int D>
+void launch_packed(const PackedArgs& a, int n, hipStream_t s) {
   constexpr int NW = kQRowsShortBf16 / 32;
-  if (head_dim == 128) hipLaunchKernelGGL((bwd_dq_kernel<128, NW, 2, 0, PackedArgs>), dim3(n), dim3(NW * 64), 0, s, a);
-  else hipLaunchKernelGGL((bwd_dq_kernel<64, NW, 2, 0, PackedArgs>), dim3(n), dim3(NW * 64), 0, s, a);
+  const int hp = packed_tile_heads(a.group);
+  const dim3 grid(n), threads(NW * 64);
+  if (hp == 4) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedArgs, 4>), grid, threads, 0, s, a);
+  else if (hp == 2) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedArgs, 2>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedArgs, 1>), grid, threads, 0, s, a);
+}
+
+hipError_t launch_bwd_dq_bf16(const PackedArgs& a, int head_dim, hipStream_t s) {
+  const int n = workgroups_for(a.n_items * (a.heads / packed_tile_heads(a.group)));
+  if (n == 0) return hipSuccess;
+  head_dim == 128 ? launch_packed<128>(a, n, s) : launch_packed<64>(a, n, s);
   return hipGetLastError();
 }
 

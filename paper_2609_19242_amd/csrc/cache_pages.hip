@@ -233,13 +233,23 @@ __global__ __launch_bounds__(256) void cache_fork_kernel(const CacheArg c, const
 }
 
 // A sequence listed twice is freed once: whoever takes its length frees it.
+// The first workgroup also writes the status.
 __global__ __launch_bounds__(256) void cache_free_kernel(const CacheArg c, const CacheList l) {
-  __shared__ int len;
-  const int s = l.a[blockIdx.x];
-  if ((unsigned)s >= (unsigned)c.seqs) {
-    if (threadIdx.x == 0) c.status[0] = kBadList;
-    return;
+  __shared__ int len, bad;
+  if (blockIdx.x == 0) {
+    if (threadIdx.x == 0) bad = 0;
+    __syncthreads();
+    for (int i = threadIdx.x; i < l.n; i += 256)
+      if ((unsigned)l.a[i] >= (unsigned)c.seqs) bad = 1;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      c.status[0] = bad ? kBadList : kOk;
+      c.status[1] = 0;
+    }
+    if (l.n == 0) return;
   }
+  const int s = l.a[blockIdx.x];
+  if ((unsigned)s >= (unsigned)c.seqs) return;
   if (threadIdx.x == 0) len = atomicExch(&c.lens[s], 0);
   __syncthreads();
   if (len <= 0) return;
@@ -259,11 +269,10 @@ __global__ __launch_bounds__(256) void cache_free_kernel(const CacheArg c, const
   }
 }
 
-__global__ void cache_status_kernel(int32_t* status) { status[threadIdx.x] = 0; }
-
 // Moves: the i-th free page below the live count takes the i-th live page at
 // or above it.  list[0 .. n): free pages, list[pages .. pages + n): live ones;
-// list[2 pages + p]: where page p goes.
+// list[2 pages + p]: where page p >= live goes, -1 for a page that no table
+// should hold.  The references move here, before the data.
 __global__ __launch_bounds__(kT) void cache_compact_plan_kernel(const CacheArg c, int32_t* work) {
   __shared__ int wsum[kT / 64];
   int32_t* const dst = work + kCacheHead;
@@ -283,10 +292,8 @@ __global__ __launch_bounds__(kT) void cache_compact_plan_kernel(const CacheArg c
     int th, tm;
     const int64_t ah = holes + block_scan(hole ? 1 : 0, th, wsum), am = moves + block_scan(move ? 1 : 0, tm, wsum);
     if (hole) dst[ah] = (int32_t)p;
-    if (move) {
-      src[am] = (int32_t)p;
-      src[c.pages + p] = (int32_t)am;
-    }
+    if (move) src[am] = (int32_t)p;
+    if (in && p >= live) src[c.pages + p] = move ? (int32_t)am : -1;
     holes += th;
     moves += tm;
   }
@@ -295,6 +302,13 @@ __global__ __launch_bounds__(kT) void cache_compact_plan_kernel(const CacheArg c
     work[1] = (int32_t)moves;
     c.status[0] = kOk;
     c.status[1] = 0;
+  }
+  __syncthreads();  // the lists are read by other threads
+  for (int64_t m = threadIdx.x; m < moves; m += kT) {
+    const int from = src[m], to = dst[m];
+    src[c.pages + from] = to;
+    c.refs[to] = c.refs[from];
+    c.refs[from] = 0;
   }
 }
 
@@ -311,18 +325,9 @@ __global__ __launch_bounds__(256) void cache_compact_kernel(const CacheArg c, co
   const int64_t at = (int64_t)blockIdx.x * 256 + threadIdx.x, step = (int64_t)gridDim.x * 256;
   for (int64_t e = at; e < (int64_t)c.seqs * c.max_pages; e += step) {
     const int p = c.table[e];
-    // (a number that no table should hold, a free page's, stays)
-    if (p >= live && p < c.pages && c.refs[p] > 0) c.table[e] = dst[src[c.pages + p]];
-  }
-}
-// The counts move last: the kernel before reads them.
-__global__ __launch_bounds__(256) void cache_compact_refs_kernel(const CacheArg c, const int32_t* work) {
-  const int32_t* const dst = work + kCacheHead;
-  const int32_t* const src = dst + c.pages;
-  const int moves = work[1];
-  for (int m = blockIdx.x * 256 + threadIdx.x; m < moves; m += gridDim.x * 256) {
-    c.refs[dst[m]] = c.refs[src[m]];
-    c.refs[src[m]] = 0;
+    if (p < live || p >= c.pages) continue;
+    const int to = src[c.pages + p];
+    if (to >= 0) c.table[e] = to;
   }
 }
 
@@ -369,15 +374,13 @@ hipError_t launch_cache_fork(const CacheArg& c, const CacheList& l, int32_t* wor
 }
 
 hipError_t launch_cache_free(const CacheArg& c, const CacheList& l, hipStream_t s) {
-  hipLaunchKernelGGL(cache_status_kernel, dim3(1), dim3(2), 0, s, c.status);
-  if (l.n > 0) hipLaunchKernelGGL(cache_free_kernel, dim3(l.n), dim3(256), 0, s, c, l);
+  hipLaunchKernelGGL(cache_free_kernel, dim3(l.n > 0 ? l.n : 1), dim3(256), 0, s, c, l);
   return hipGetLastError();
 }
 
 hipError_t launch_cache_compact(const CacheArg& c, int32_t* work, hipStream_t s) {
   hipLaunchKernelGGL(cache_compact_plan_kernel, dim3(1), dim3(kT), 0, s, c, work);
   hipLaunchKernelGGL(cache_compact_kernel, dim3(2048), dim3(256), 0, s, c, work);
-  hipLaunchKernelGGL(cache_compact_refs_kernel, dim3(64), dim3(256), 0, s, c, work);
   return hipGetLastError();
 }
 

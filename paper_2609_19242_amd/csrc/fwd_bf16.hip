@@ -51,11 +51,11 @@ constexpr float kSumLimit = 18446744073709551616.f;  // 2^64: a lane's tile sum 
 template <int D, int NW, int HM>
 constexpr int kWavesPerSimd = D == 64 && NW == 4 && HM == 0 ? 3 : 2;  // (NW: waves of all teams)
 
-template <int D, int NW, int NS, int HM, int NT, class Args>
+template <int D, int NW, int NS, int HM, int NT, class Args, int HP = 1>
 __global__ __launch_bounds__(NT * NW * 64)
     __attribute__((amdgpu_waves_per_eu(kWavesPerSimd<D, NT * NW, HM>, kWavesPerSimd<D, NT * NW, HM>))) void fwd_bf16_kernel(
         const Args args) {
-  constexpr int BM = NW * 32, BN = 64, KS = D / 16, DT = D / 32;
+  constexpr int BM = NW * 32 / HP, BN = 64, KS = D / 16, DT = D / 32;
   constexpr uint32_t RB = D * 2, TB = BN * RB;  // row and tile bytes in LDS
   constexpr int STAGE = 2 * BN * D;             // K tile + V tile (elements), swizzled rows
   // Copies: each tile is BN * D / 8 16-byte slots, TI instructions of 64 lanes;
@@ -71,10 +71,11 @@ __global__ __launch_bounds__(NT * NW * 64)
   const int G = lane >> 4, sl = lane & 15;
 
   QTileItem it;
-  if (!q_tile_item(args, blockIdx.x, it)) return;
+  if (!q_tile_item<HP>(args, blockIdx.x, it)) return;
   auto&& a = call_view(args, it.item, 2);
   const QRangeArg& qr = a.qr[it.r];
   const int kvh = it.h / a.group;
+  const int h = HP == 1 ? it.h : it.h + w % HP, wrow = w / HP * 32;  // this wave's head and rows of the tile
   const int row0 = it.t * BM;
   const int nvalid = imin(BM, qr.len - row0);
   const int64_t H = a.heads, HKV = a.kv_heads;
@@ -83,13 +84,13 @@ __global__ __launch_bounds__(NT * NW * 64)
   // This wave's 32 query rows as MFMA B fragments (rows past the range read as zero).
   bf16x8 qf[KS];
   {
-    const bf16* qbase = (const bf16*)qr.q + row_elem<D>(a, it.b, qr.bstride, row0, H, it.h, QS);
+    const bf16* qbase = (const bf16*)qr.q + row_elem<D>(a, it.b, qr.bstride, row0, H, h, QS);
     const auto rs = make_rsrc(qbase, (uint32_t)(((int64_t)(nvalid - 1) * QS + D) * 2));
-    const uint32_t off = (uint32_t)(((int64_t)(w * 32 + l32) * QS + 8 * half) * 2);
+    const uint32_t off = (uint32_t)(((int64_t)(wrow + l32) * QS + 8 * half) * 2);
 #pragma unroll
     for (int s = 0; s < KS; ++s) qf[s] = __builtin_bit_cast(bf16x8, buf_load16(rs, off + s * 32));
   }
-  const int my_row = row0 + w * 32 + l32;
+  const int my_row = row0 + wrow + l32;
   const int pq = qr.pos0 + imin(my_row, qr.len - 1);
   const int pq0 = qr.pos0 + row0, pq1 = qr.pos0 + row0 + nvalid - 1;
 
@@ -412,7 +413,7 @@ __global__ __launch_bounds__(NT * NW * 64)
   const float inv = empty ? 0.f : 1.f / l_tot;
   if (a.out_f32) {
     if (my_row < qr.len) {
-      float* op = (float*)qr.o + row_elem<D>(a, it.b, qr.bstride, my_row, H, it.h, OS);
+      float* op = (float*)qr.o + row_elem<D>(a, it.b, qr.bstride, my_row, H, h, OS);
 #pragma unroll
       for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -427,14 +428,14 @@ __global__ __launch_bounds__(NT * NW * 64)
     // bf16 O through LDS (the stages are free: every wave's copies have landed
     // and every wave has left the walk once all meet this barrier).
     if constexpr (NT == 1) asm volatile("s_barrier" ::: "memory");  // (teams have met)
-    const int wrow0 = row0 + w * 32;
+    const int wrow0 = row0 + wrow;
     store_rows_bf16_via_lds<D>(
         lds_addr(lds) + (uint32_t)w * (D * 64), [&](int d, int g4, int e) { return acc[d][g4 * 4 + e] * inv; },
-        (bf16*)qr.o + row_elem<D>(a, it.b, qr.bstride, wrow0, H, it.h, OS), OS, qr.len - wrow0, lane);
+        (bf16*)qr.o + row_elem<D>(a, it.b, qr.bstride, wrow0, H, h, OS), OS, qr.len - wrow0, lane);
   }
   if (my_row < qr.len) {
     if (half == 0)
-      qr.lse[((int64_t)it.b * H + it.h) * qr.bstride + my_row] =
+      qr.lse[((int64_t)it.b * H + h) * qr.bstride + my_row] =
           empty ? -INFINITY : (m_run + log2f(l_tot)) * kLn2;
   }
 }
@@ -479,19 +480,25 @@ hipError_t launch_fwd_bf16(const AttnArgs& a, int head_dim, QTile q, hipStream_t
 
 }  // namespace
 
-// Packed calls: 128-row tiles, shared by two teams when there are few.
-hipError_t launch_fwd_bf16(const PackedArgs& a, int head_dim, int teams, hipStream_t s) {
-  const int n = workgroups_for(a.n_items * a.heads);
-  if (n == 0) return hipSuccess;
+template <int D, int NT, int HP>
+void launch_packed(const PackedArgs& a, int n, hipStream_t s) {
   constexpr int NW = kQRowsShortBf16 / 32;
-  const dim3 grid(n), threads(teams * NW * 64);
-  if (head_dim == 128) {
-    if (teams == 2) hipLaunchKernelGGL((fwd_bf16_kernel<128, NW, 2, 0, 2, PackedArgs>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((fwd_bf16_kernel<128, NW, 2, 0, 1, PackedArgs>), grid, threads, 0, s, a);
-  } else {
-    if (teams == 2) hipLaunchKernelGGL((fwd_bf16_kernel<64, NW, 2, 0, 2, PackedArgs>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((fwd_bf16_kernel<64, NW, 2, 0, 1, PackedArgs>), grid, threads, 0, s, a);
-  }
+  hipLaunchKernelGGL((fwd_bf16_kernel<D, NW, 2, 0, NT, PackedArgs, HP>), dim3(n), dim3(NT * NW * 64), 0, s, a);
+}
+template <int D, int NT>
+void launch_packed_heads(const PackedArgs& a, int n, hipStream_t s) {
+  const int hp = packed_tile_heads(a.group);
+  if (hp == 4) launch_packed<D, NT, 4>(a, n, s);
+  else if (hp == 2) launch_packed<D, NT, 2>(a, n, s);
+  else launch_packed<D, NT, 1>(a, n, s);
+}
+
+// Packed calls: four waves per tile (packed_tile_heads in packed.hpp), two teams of them when there are few tiles.
+hipError_t launch_fwd_bf16(const PackedArgs& a, int head_dim, int teams, hipStream_t s) {
+  const int n = workgroups_for(a.n_items * (a.heads / packed_tile_heads(a.group)));
+  if (n == 0) return hipSuccess;
+  if (head_dim == 128) teams == 2 ? launch_packed_heads<128, 2>(a, n, s) : launch_packed_heads<128, 1>(a, n, s);
+  else teams == 2 ? launch_packed_heads<64, 2>(a, n, s) : launch_packed_heads<64, 1>(a, n, s);
   return hipGetLastError();
 }
 

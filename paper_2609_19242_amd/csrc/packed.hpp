@@ -45,6 +45,12 @@ __host__ __device__ inline int packed_shift(int q_len, int k_len, int M) {
   return d <= 0 ? 0 : (d + M - 1) / M * M;
 }
 
+// Query heads of a KV head that the four waves of a bf16 forward or dQ tile
+// take side by side: the tile is then 128 / heads rows of each.  They read the
+// same keys as 128 rows of one head would, but the rows' causal ends lie closer
+// together, so fewer pairs are computed in vain and the waves end together.
+inline int packed_tile_heads(int group) { return group % 4 == 0 ? 4 : group % 2 == 0 ? 2 : 1; }
+
 // One sequence of a packed call, with the members of AttnArgs that the kernels read.
 struct PackedView {
   static constexpr int n_q = 1, n_k = 1, batch = 1, out_f32 = 0, hilo = 0;

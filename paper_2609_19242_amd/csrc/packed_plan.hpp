@@ -27,7 +27,8 @@ constexpr size_t kMaxPackedPartials = (size_t)256 << 20;
 
 // Work items, heaviest first: a workgroup that starts late should be short.
 //
-// Query tiles: 128 rows (16 in fp32) of one sequence, by the keys they walk.
+// Query tiles: 128 rows (16 in fp32) of one sequence, or as many fewer as a
+// tile has heads (packed_tile_heads), by the keys they walk.
 //
 // Key tiles: 128 keys (16), by the steps of their walks.  The longest walk,
 // the first keys' of the longest sequence, sets the time when there are few;
@@ -37,7 +38,8 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
   PackedPlanItems out;
   const bool f32 = p.dtype == BDLM_F32;
   const int M = (int)p.block_size, group = p.heads / p.kv_heads;
-  const int q_tile = f32 ? kRowsF32 : kQRowsShortBf16, k_tile = f32 ? kRowsF32 : kBwdKeysBf16;
+  const int tile_heads = f32 ? 1 : packed_tile_heads(group);
+  const int q_tile = f32 ? kRowsF32 : kQRowsShortBf16 / tile_heads, k_tile = f32 ? kRowsF32 : kBwdKeysBf16;
   const int step = packed_step_rows(f32, group);
   const int64_t per_block = f32 || group % 2 ? group : group / 2;
   const MaskRule rule{M, kIntraBlock, (int)p.window, 1, kBig, nullptr};
@@ -77,7 +79,7 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
   std::stable_sort(q.begin(), q.end(), heavier);
   std::stable_sort(k.begin(), k.end(), heavier);
   for (const Cost& c : q) out.q.push_back(c.it);
-  if (!f32 && (int64_t)out.q.size() * p.heads <= kTeamWgs) out.teams = 2;
+  if (!f32 && (int64_t)out.q.size() * (p.heads / tile_heads) <= kTeamWgs) out.teams = 2;
 
   // Chunks of the key tiles' walks.
   const int64_t longest = k.empty() ? 0 : k[0].cost;

@@ -24,6 +24,7 @@ struct QTileItem {
 // The items of a (batch, KV head) pair meet in one XCD group (xcd_pair_item);
 // within a pair the query heads of the group are interleaved, and the tiles of
 // each range run from the last (longest key prefix) to the first.
+template <int HP = 1>
 __device__ inline bool q_tile_item(const AttnArgs& a, int wg, QTileItem& it) {
   int bk, rank;
   if (!xcd_pair_item(wg, a.kv_heads * a.batch, a.group * a.total_tiles, false, bk, rank)) return false;
@@ -43,12 +44,15 @@ __device__ inline bool q_tile_item(const AttnArgs& a, int wg, QTileItem& it) {
   return true;
 }
 
-// The same of a packed call, whose items lie heaviest first in the plan.
+// The same of a packed call, whose items lie heaviest first in the plan; h is
+// the first of the HP query heads that a tile's waves take.
+template <int HP = 1>
 __device__ inline bool q_tile_item(const PackedArgs& a, int wg, QTileItem& it) {
   int rank;
-  if (!xcd_pair_item(wg, a.kv_heads, a.group * a.n_items, false, it.b, rank)) return false;
-  it.item = rank / a.group;
-  it.h = it.b * a.group + (rank - it.item * a.group);
+  const int per = a.group / HP;
+  if (!xcd_pair_item(wg, a.kv_heads, per * a.n_items, false, it.b, rank)) return false;
+  it.item = rank / per;
+  it.h = it.b * a.group + (rank - it.item * per) * HP;
   it.b = it.r = 0;
   it.t = a.items[it.item].tile;
   return true;

@@ -11,7 +11,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from . import _check, _dtype_code, _expect, _on_device, _torch_stream, device_stream, lib
+from . import _check, _dtype_code, _expect, _launch, _on_device, _torch_stream, lib
 
 __all__ = ["PackedPlan", "packed_plan", "packed_fwd", "packed_bwd"]
 
@@ -54,6 +54,7 @@ class PackedPlan:
 
     def __init__(self, record: _Plan, items: torch.Tensor, dtype: torch.dtype):
         self._record, self._items, self.dtype = record, items, dtype
+        self._ref, self._at = ctypes.byref(record), items.data_ptr()
         p = record.problem
         self.heads, self.kv_heads, self.head_dim = p.heads, p.kv_heads, p.head_dim
         self.q_rows, self.k_rows = record.q_rows, record.k_rows
@@ -110,26 +111,32 @@ def packed_plan(q_lens: Sequence[int], k_lens: Optional[Sequence[int]] = None, *
     return PackedPlan(rec, host.to(device), dtype)
 
 
-def _rows(plan, name, t, heads, at_least):
-    """A ``[rows][heads][head_dim]`` tensor whose rows may lie further apart than they are long."""
+def _rows(like, name, t, heads, at_least):
+    """A ``[rows][heads][head_dim]`` tensor whose rows may lie further apart than they are long, in the dtype and on the
+    device of ``like`` (a plan or a cache)."""
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
-    if t.dtype != plan.dtype:
-        raise TypeError(f"{name} must be {plan.dtype}, got {t.dtype}")
-    D = plan.head_dim
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != D:
-        raise ValueError(f"{name} must have shape (rows, {heads}, {D}), got {tuple(t.shape)}")
-    n, st = t.shape[0], t.stride()
+    if t.dtype is not like.dtype:
+        raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
+    D, shape = like.head_dim, t.shape
+    if len(shape) != 3 or shape[1] != heads or shape[2] != D:
+        raise ValueError(f"{name} must have shape (rows, {heads}, {D}), got {tuple(shape)}")
+    n = shape[0]
     if n < at_least:
-        raise ValueError(f"{name} has {n} rows, the plan's sequences end at row {at_least}")
-    if n and (st[2] != 1 or (heads > 1 and st[1] != D) or (n > 1 and st[0] < heads * D)):
+        raise ValueError(f"{name} has {n} rows, {at_least} are needed")
+    s0, s1, s2 = t.stride()
+    if n and (s2 != 1 or (heads > 1 and s1 != D) or (n > 1 and s0 < heads * D)):
         raise ValueError(f"{name} must hold each row's heads contiguously (only rows may lie apart)")
-    return _Rows(t.data_ptr(), st[0] if n > 1 else heads * D)
+    if t.device != like.device:
+        raise ValueError(f"{name} must be on {like.device}, got {t.device}")
+    return _Rows(t.data_ptr(), s0 if n > 1 else heads * D)
 
 
 def _check_plan(plan):
     if not isinstance(plan, PackedPlan):
         raise TypeError(f"plan must be a PackedPlan, got {type(plan).__name__}")
+    if plan.device.type != "cuda":
+        raise ValueError(f"the plan's items are on {plan.device}, not on a GPU")
 
 
 def _like(t, rows, heads, D):
@@ -141,27 +148,20 @@ def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, stream=No
     as in a fused projection).  Returns ``(o, lse)`` with ``lse [heads][rows]`` fp32, or writes into ``out``; rows of
     no sequence are left as they are (in new outputs: undefined)."""
     _check_plan(plan)
-    H, KV, D = plan.heads, plan.kv_heads, plan.head_dim
-    rq, rk, rv = (_rows(plan, *a) for a in (("q", q, H, plan.q_rows), ("k", k, KV, plan.k_rows),
-                                            ("v", v, KV, plan.k_rows)))
+    H, KV = plan.heads, plan.kv_heads
+    rq, rk, rv = (_rows(plan, "q", q, H, plan.q_rows), _rows(plan, "k", k, KV, plan.k_rows),
+                  _rows(plan, "v", v, KV, plan.k_rows))
     n = q.shape[0]
-    if out is not None:
+    if out is None:
+        o, lse = _like(q, n, H, plan.head_dim), torch.empty((H, n), dtype=torch.float32, device=q.device)
+        ro = _Rows(o.data_ptr(), H * plan.head_dim)
+    else:
         if len(out) != 2:
             raise ValueError("out must be (o, lse)")
         o, lse = out
-        _rows(plan, "o", o, H, n)
-        if o.shape[0] != n:
-            raise ValueError(f"o must have as many rows as q ({n}), got {o.shape[0]}")
-        _expect("lse", lse, torch.float32, (H, n))
-    _on_device(plan.device, q=q, k=k, v=v)
-    if out is None:
-        o, lse = _like(q, n, H, D), torch.empty((H, n), dtype=torch.float32, device=q.device)
-    else:
-        _on_device(plan.device, o=o, lse=lse)
-    ro = _rows(plan, "o", o, H, plan.q_rows)
-    with device_stream(plan.device, stream) as s:
-        _check(lib().bdlm_packed_fwd(ctypes.byref(plan._record), plan._items.data_ptr(), rq, rk, rv, ro,
-                                     lse.data_ptr(), n, s))
+        ro = _as_long(plan, "o", o, H, n)
+        _lse(plan, lse, n)
+    _launch(plan.device, stream, lib().bdlm_packed_fwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n)
     return o, lse
 
 
@@ -171,33 +171,35 @@ def packed_bwd(plan: PackedPlan, q, k, v, o, lse, do, out: Optional[tuple] = Non
     tensor of ``plan.workspace_bytes`` bytes (calls that may overlap in time need one each); allocated if not given."""
     _check_plan(plan)
     H, KV, D = plan.heads, plan.kv_heads, plan.head_dim
-    n, nk = (t.shape[0] if isinstance(t, torch.Tensor) and t.dim() else 0 for t in (q, k))
-    ins = [("q", q, H, plan.q_rows), ("k", k, KV, plan.k_rows), ("v", v, KV, plan.k_rows), ("o", o, H, n),
-           ("do", do, H, n)]
-    rq, rk, rv, ro, rdo = (_rows(plan, *a) for a in ins)
-    for name, t in (("o", o), ("do", do)):
-        if t.shape[0] != n:
-            raise ValueError(f"{name} must have as many rows as q ({n}), got {t.shape[0]}")
-    _expect("lse", lse, torch.float32, (H, n))
-    if out is not None:
+    rq, rk, rv = (_rows(plan, "q", q, H, plan.q_rows), _rows(plan, "k", k, KV, plan.k_rows),
+                  _rows(plan, "v", v, KV, plan.k_rows))
+    n, nk, nv = q.shape[0], k.shape[0], v.shape[0]
+    ro, rdo = _as_long(plan, "o", o, H, n), _as_long(plan, "do", do, H, n)
+    _lse(plan, lse, n)
+    if out is None:
+        dq, dk, dv = _like(q, n, H, D), _like(k, nk, KV, D), _like(v, nv, KV, D)
+    else:
         if len(out) != 3:
             raise ValueError("out must be (dq, dk, dv)")
-        for name, t, h, m in (("dq", out[0], H, n), ("dk", out[1], KV, nk), ("dv", out[2], KV, v.shape[0])):
-            _rows(plan, name, t, h, m)
-    _on_device(plan.device, q=q, k=k, v=v, o=o, lse=lse, do=do)
-    if out is None:
-        out = _like(q, n, H, D), _like(k, nk, KV, D), _like(v, v.shape[0], KV, D)
-    else:
-        _on_device(plan.device, dq=out[0], dk=out[1], dv=out[2])
-    dq, dk, dv = out
-    outs = [_rows(plan, "dq", dq, H, plan.q_rows), _rows(plan, "dk", dk, KV, plan.k_rows),
-            _rows(plan, "dv", dv, KV, plan.k_rows)]
+        dq, dk, dv = out
+    outs = [_as_long(plan, "dq", dq, H, n), _as_long(plan, "dk", dk, KV, nk), _as_long(plan, "dv", dv, KV, nv)]
     workspace = _workspace(workspace, plan.workspace_bytes, plan.device, stream)
-    with device_stream(plan.device, stream) as s:
-        _check(lib().bdlm_packed_bwd(ctypes.byref(plan._record), plan._items.data_ptr(), rq, rk, rv, ro,
-                                     lse.data_ptr(), n, rdo, *outs, workspace.data_ptr(),
-                                     workspace.numel() * workspace.element_size(), s))
+    _launch(plan.device, stream, lib().bdlm_packed_bwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n, rdo,
+            *outs, workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return dq, dk, dv
+
+
+def _as_long(plan, name, t, heads, n):
+    r = _rows(plan, name, t, heads, n)
+    if t.shape[0] != n:
+        raise ValueError(f"{name} must have {n} rows, got {t.shape[0]}")
+    return r
+
+
+def _lse(plan, lse, n):
+    _expect("lse", lse, torch.float32, (plan.heads, n))
+    if lse.device != plan.device:
+        raise ValueError(f"lse must be on {plan.device}, got {lse.device}")
 
 
 def _workspace(workspace, nbytes, device, stream):
