@@ -15,7 +15,7 @@ namespace {
 
 constexpr int64_t kMaxSeqs = (int64_t)1 << 19;  // a bit each in the bookkeeping's LDS
 constexpr int64_t kMaxPages = ((int64_t)1 << 30) - 1;
-constexpr int kMaxParts_ = 1024;  // chunks of keys of one attention call
+constexpr int kMaxKeyChunks = 1 << 20;  // chunks of keys of one attention call
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
 
@@ -73,40 +73,51 @@ bdlm_status done(hipError_t e, const char* what) { return e == hipSuccess ? BDLM
 
 // How the keys of an attention call are cut into chunks and its rows into tiles.
 //
-// A workgroup runs alone on a CU (its LDS), so the work is cut into about as
-// many equal pieces as there are CUs, by keys walked; chunks below kMinChunk keys cost
-// more in partial sums than they save.
-constexpr int64_t kMinChunk = 256;
+// The prefix: chunks of kPrefixChunk keys, longer ones where its tiles of rows
+// alone give every workgroup slot kItemsPerSlot items (64 requests behind 8K
+// tokens, 32/8 heads, one row each: 3,328 keys 110 us, 2,048 76, 1,024 58, 512
+// 71: partial sums cost what balance gains).
+// A request's own keys: chunks of at least kOwnChunk keys, their number limited
+// by the workgroups that find nothing to do where a sequence is shorter than
+// its table (kMaxOwnItems).
+// A prefix that would save less than kFoldBytes of reading is not kept apart:
+// the requests' own keys then start at 0, and short ones need no partial sums.
+constexpr int64_t kSlots = 2 * kCus, kItemsPerSlot = 2, kPrefixChunk = 1024, kOwnChunk = 768, kMaxOwnItems = 4096;
+constexpr int64_t kFoldBytes = 8 << 20;
 
 bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int32_t heads, int64_t prefix,
                         PrefixArgs& a, size_t& part_bytes) {
   const bool f32 = c->dtype == BDLM_F32;
   const int64_t group = heads / c->kv_heads, per = rows * group, all = requests * per;
-  const int64_t cap = c->max_pages * c->page_size;
+  const int64_t row_bytes = (int64_t)2 * c->kv_heads * c->head_dim * (f32 ? 4 : 2);
+  if ((requests - 1) * prefix * row_bytes <= kFoldBytes) prefix = 0;
+  a.prefix = (int32_t)prefix;
   a.prefix_shared = !f32 && all > 2 * kPrefixWaveRows;
   a.own_shared = !f32 && per > 2 * kPrefixWaveRows;
   auto tile = [&](bool shared) { return f32 ? kPrefixRowsF32 : shared ? kPrefixSharedRows : kPrefixWaveRows; };
   const int64_t pt = (all + tile(a.prefix_shared) - 1) / tile(a.prefix_shared);
   const int64_t ot = (per + tile(a.own_shared) - 1) / tile(a.own_shared);
-  const int64_t own = cap - prefix;
+  const int64_t own = c->max_pages * c->page_size - prefix;
   const int64_t limit = (kPrefixTableEntries - 2) * c->page_size;  // keys whose pages a workgroup can hold
-  const int64_t total = c->kv_heads * (pt * prefix + requests * ot * own);
-  int64_t chunk = std::max<int64_t>(kMinChunk, (total / kCus + 63) / 64 * 64);
-  chunk = std::min(chunk, std::max<int64_t>(limit / 64 * 64 - 64, std::min<int64_t>(limit, 64)));
-  a.prefix_chunk = (int32_t)chunk;
-  a.prefix_chunks = (int32_t)((prefix + chunk - 1) / chunk);
-  a.own_min = (int32_t)chunk;
-  a.own_chunks = (int32_t)std::max<int64_t>((own + chunk - 1) / chunk, own > 0 ? 1 : 0);
-  if (a.own_chunks == 0 && a.prefix_chunks == 0) a.own_chunks = 1;
+  auto up64 = [](int64_t x) { return (x + 63) / 64 * 64; };
+  const int64_t pc = std::min(std::max(kPrefixChunk, up64(c->kv_heads * pt * prefix / (kSlots * kItemsPerSlot))),
+                              std::min(limit, up64(prefix + 1)));
+  a.prefix_chunk = (int32_t)pc;
+  a.prefix_chunks = (int32_t)((prefix + pc - 1) / pc);
+  const int64_t base = c->kv_heads * requests * ot;
+  int64_t oc = std::min((own + kOwnChunk - 1) / kOwnChunk, std::max<int64_t>(kMaxOwnItems / base, 1));
+  oc = std::max(oc, (own + limit - 65) / (limit - 64));
+  if (oc == 0 && a.prefix_chunks == 0) oc = 1;
+  a.own_chunks = (int32_t)oc;
+  a.own_min = (int32_t)std::max<int64_t>(oc > 0 ? (own + oc - 1) / oc : 1, 1);
   a.prefix_tiles = (int32_t)pt;
   a.own_tiles = (int32_t)ot;
-  const int64_t pi = c->kv_heads * pt * a.prefix_chunks, oi = c->kv_heads * requests * ot * a.own_chunks;
-  if (pi + oi >= (int64_t)1 << 31 || a.prefix_chunks + a.own_chunks > kMaxParts_)
-    return fail(BDLM_ERR_UNSUPPORTED, "attention over the cache needs %lld workgroups and %d chunks (limits 2^31, %d)",
-                (long long)(pi + oi), a.prefix_chunks + a.own_chunks, kMaxParts_);
+  const int64_t parts = a.prefix_chunks + oc, pi = c->kv_heads * pt * a.prefix_chunks, oi = base * oc;
+  if (pi + oi >= (int64_t)1 << 31 || parts > kMaxKeyChunks)
+    return fail(BDLM_ERR_UNSUPPORTED, "attention over the cache needs %lld workgroups and %lld chunks (limits 2^31, %d)",
+                (long long)(pi + oi), (long long)parts, kMaxKeyChunks);
   a.prefix_items = (int32_t)pi;
   a.own_items = (int32_t)oi;
-  const int64_t parts = a.prefix_chunks + a.own_chunks;
   part_bytes = parts == 1 ? 0 : (size_t)parts * requests * rows * heads * c->head_dim * sizeof(float);
   return BDLM_OK;
 }
@@ -260,7 +271,6 @@ bdlm_status bdlm_prefix_attn(const bdlm_cache* c, int64_t layer, int64_t request
   a.heads = heads;
   a.kv_heads = c->kv_heads;
   a.group = heads / c->kv_heads;
-  a.prefix = (int32_t)prefix;
   a.block = block;
   a.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)c->head_dim)) * 1.44269504088896340736f;
   const int bf16 = c->dtype == BDLM_BF16;

@@ -4,12 +4,13 @@
 //
 // Per chunk of keys and tile of rows: S^T = K Q^T, an online softmax, and
 // O^T += V^T P^T with v_mfma_f32_32x32x16_bf16, the products, layouts and LDS
-// swizzle of the forward (fwd_bf16.hip).  A workgroup of eight waves runs an
-// item in one of two forms:
-//  * shared: 256 rows, 32 per wave; the waves share 64-key tiles in three LDS
-//    stages, copied two tiles ahead.  For the prefix of a batch and for blocks
-//    of query rows: bound by the matrix cores from some 300 rows on.
-//  * by waves: 32 rows; every wave takes every eighth 32-key tile through its
+// swizzle of the forward (fwd_bf16.hip).  A workgroup of four waves (two fit a
+// CU, so that one's start-up overlaps the other's products) runs an item in one
+// of two forms:
+//  * shared: 128 rows, 32 per wave; the waves share 64-key tiles in two LDS
+//    stages.  For the prefix of a batch and for blocks of query rows: bound by
+//    the matrix cores from some 300 rows on.
+//  * by waves: 32 rows; every wave takes every fourth 32-key tile through its
 //    own 16 KB of LDS, without barriers, and the waves' sums are merged at the
 //    end.  For single tokens (few rows): bound by reading K and V.  A wave asks
 //    for the next tile's keys as soon as its scores are there, and for its
@@ -24,9 +25,9 @@ namespace bdlm {
 
 namespace {
 
-constexpr int kNW = 8;
+constexpr int kNW = 4;
 constexpr float kLn2 = 0.69314718055994530942f;
-constexpr float kLimit = 64.f;  // the running max moves when a score passes it by this much (powers of two)
+constexpr float kSumLimit = 18446744073709551616.f;  // 2^64: a lane's tile sum of p above which the running max moves
 
 __device__ __attribute__((aligned(256))) const uint32_t zero_row[64] = {};
 
@@ -58,35 +59,46 @@ struct RowState {
   }
 };
 
-// P of U 32-key steps from the scores (in place in s), as bf16 operands;
-// rounding P to bf16 is off by at most 2^-9 relative, as in the forward.
+// P of U 32-key steps from the scores, as bf16 operands (off by at most 2^-9
+// relative, as in the forward).  The running max of a row moves on its first
+// visible tile, and when a lane's sum over a tile passes 2^64: see fwd_bf16.hip.
 template <int D, int U>
-__device__ __forceinline__ void softmax_step(RowState<D>& st, f32x16 (&s)[U], bf16x8 (&pb)[2 * U], float c) {
-  float mx = s[0][0];
+__device__ __forceinline__ void softmax_step(RowState<D>& st, const f32x16 (&s)[U], bf16x8 (&pb)[2 * U], float c) {
+  float psum;
+  auto probs = [&](float m) __attribute__((always_inline)) {
+    psum = 0.f;
 #pragma unroll
-  for (int u = 0; u < U; ++u)
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);
-  mx = fmaxf(mx, partner(mx)) * c;
-  if (__builtin_amdgcn_ballot_w64(mx > st.m + kLimit || (st.m == -INFINITY && mx > -INFINITY)) != 0) {
-    const float mn = fmaxf(st.m, mx);
-    const float al = st.m == -INFINITY ? 0.f : exp2f_fast(st.m - mn);
+      for (int i = 0; i < 16; ++i) {
+        const float p = exp2f_fast(fmaf(s[u][i], c, -m));
+        psum += p;
+        pb[2 * u + (i >> 3)][i & 7] = to_bf16(p);
+      }
+  };
+  bool rescale = __builtin_amdgcn_ballot_w64(st.m == -INFINITY) != 0;
+  if (!rescale) {
+    probs(st.m);
+    rescale = __builtin_amdgcn_ballot_w64(psum > kSumLimit) != 0;
+  }
+  if (rescale) {
+    float mx = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[u][i]);
+    mx = fmaxf(mx, partner(mx));
+    const float mn = fmaxf(st.m, mx * c);
+    const float al = exp2f_fast(st.m - (mn == -INFINITY ? 0.f : mn));
     st.l *= al;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int i = 0; i < 16; ++i) st.acc[d][i] *= al;
     st.m = mn;
+    probs(mn == -INFINITY ? 0.f : mn);
   }
-  const float m = st.m == -INFINITY ? 0.f : st.m;
-#pragma unroll
-  for (int u = 0; u < U; ++u)
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-      const float p = exp2f_fast(fmaf(s[u][i], c, -m));
-      st.l += p;
-      pb[2 * u + (i >> 3)][i & 7] = to_bf16(p);
-    }
+  st.l += psum;
 }
 
 template <int D>
@@ -94,7 +106,7 @@ struct Lds {
   static constexpr uint32_t RB = D * 2;
   static constexpr uint32_t Stage = 2 * 64 * RB;     // K and V of 64 keys
   static constexpr uint32_t Wave = 2 * 32 * RB;      // K and V of 32 keys; later 32 rows of sums
-  static constexpr uint32_t Tiles = kNW * Wave > 3 * Stage ? kNW * Wave : 3 * Stage;
+  static constexpr uint32_t Tiles = kNW * Wave > 2 * Stage ? kNW * Wave : 2 * Stage;
   static constexpr uint32_t Pages = Tiles;
   static constexpr uint32_t Ml = Pages + kPrefixTableEntries * 4;
   static constexpr uint32_t Bytes = Ml + kNW * 32 * 8;
@@ -170,14 +182,14 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   st.init();
 
   if (it.shared) {
-    // ---- eight waves share 64-key tiles; waves 0-3 copy K, 4-7 V, 16 rows each
-    constexpr int NS = 3, IPW = 16 / RPI;
+    // ---- the waves share 64-key tiles; waves 0 and 1 copy K, 2 and 3 V, 32 rows each
+    constexpr int IPW = 32 / RPI;
     const int ntiles = (nkeys + 63) / 64;
-    const char* const base = w < 4 ? kb : vb;
-    const int crow = (w & 3) * 16;
+    const char* const base = w < 2 ? kb : vb;
+    const int crow = (w & 1) * 32;
     auto copy_tile = [&](int t, int stage) __attribute__((always_inline)) {
-      const int64_t mine = key_offset(t < ntiles ? it.k0 + t * 64 + crow + (lane & 15) : it.k1);
-      const uint32_t dst = L0 + stage * L::Stage + (w < 4 ? 0u : 64 * RB) + crow * RB;
+      const int64_t mine = key_offset(t < ntiles ? it.k0 + t * 64 + crow + l32 : it.k1);
+      const uint32_t dst = L0 + stage * L::Stage + (w < 2 ? 0u : 64 * RB) + crow * RB;
 #pragma unroll
       for (int i = 0; i < IPW; ++i) {
         const int r = i * RPI + lane / CH;
@@ -187,25 +199,39 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
       }
     };
     const bool any = __builtin_amdgcn_ballot_w64(row_ok && end > it.k0) != 0;
-#pragma unroll
-    for (int s = 0; s < NS - 1; ++s) copy_tile(s, s);
-    vm_wait_barrier<IPW*(NS - 2)>();
-    int cur = 0;
+    copy_tile(0, 0);
+    vm_wait_barrier<0>();
     for (int t = 0; t < ntiles; ++t) {
-      copy_tile(t + NS - 1, cur == 0 ? NS - 1 : cur - 1);
+      copy_tile(t + 1, (t + 1) & 1);
       const int key0 = it.k0 + t * 64;
       if (any && __builtin_amdgcn_ballot_w64(end > key0) != 0) {
-        const uint32_t sb = L0 + cur * L::Stage;
+        const uint32_t sb = L0 + (t & 1) * L::Stage;
         const uint32_t zr = sb + yrow;
         f32x16 s[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[u][i] = 0.f;
+        {
+          // key fragments LA k-steps ahead of their products, as in the forward
+          constexpr int LA = 3;
+          bf16x8 kf[LA + 1][2];
 #pragma unroll
-        for (int k = 0; k < KS; ++k)
+          for (int k = 0; k < LA; ++k)
 #pragma unroll
-          for (int u = 0; u < 2; ++u) s[u] = mfma32(lds_load16((zr ^ (32u * k)) + u * 32 * RB), qf[k], s[u]);
+            for (int u = 0; u < 2; ++u) kf[k][u] = lds_load16((zr ^ (32u * k)) + u * 32 * RB);
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int k = 0; k < KS; ++k) {
+            if (k + LA < KS) {
+#pragma unroll
+              for (int u = 0; u < 2; ++u) kf[(k + LA) % (LA + 1)][u] = lds_load16((zr ^ (32u * (k + LA))) + u * 32 * RB);
+            }
+#pragma unroll
+            for (int u = 0; u < 2; ++u) s[u] = mfma32(kf[k % (LA + 1)][u], qf[k], s[u]);
+            __builtin_amdgcn_sched_barrier(0);
+          }
+        }
         if (__builtin_amdgcn_ballot_w64(end < key0 + 64) != 0) {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
@@ -213,19 +239,27 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
             for (int i = 0; i < 16; ++i)
               if (key0 + u * 32 + (i >> 2) * 8 + 4 * half + (i & 3) >= end) s[u][i] = -INFINITY;
         }
+        // value fragments PA products ahead, the first ones under the softmax
+        const uint32_t zt0 = sb + 64 * RB + ytr0, zt1 = sb + 64 * RB + ytr1;
+        auto vop = [&](int n) {
+          const int u = n / DT, d = n % DT;
+          return cat(lds_read_tr_at((zt0 ^ (64u * d)) + u * 16 * RB), lds_read_tr_at((zt1 ^ (64u * d)) + u * 16 * RB));
+        };
+        constexpr int PA = 4, NP = 4 * DT;
+        bf16x8 vr[PA + 1];
+#pragma unroll
+        for (int n = 0; n < PA; ++n) vr[n] = vop(n);
         bf16x8 pb[4];
         softmax_step<D, 2>(st, s, pb, c);
-        const uint32_t zt0 = sb + 64 * RB + ytr0, zt1 = sb + 64 * RB + ytr1;
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-#pragma unroll
-          for (int d = 0; d < DT; ++d)
-            st.acc[d] = mfma32(cat(lds_read_tr_at((zt0 ^ (64u * d)) + u * 16 * RB),
-                                   lds_read_tr_at((zt1 ^ (64u * d)) + u * 16 * RB)),
-                               pb[u], st.acc[d]);
+        for (int n = 0; n < NP; ++n) {
+          if (n + PA < NP) vr[(n + PA) % (PA + 1)] = vop(n + PA);
+          st.acc[n % DT] = mfma32(vr[n % (PA + 1)], pb[n / DT], st.acc[n % DT]);
+          __builtin_amdgcn_sched_barrier(0);
+        }
       }
-      vm_wait_barrier<IPW*(NS - 2)>();
-      cur = cur == NS - 1 ? 0 : cur + 1;
+      vm_wait_barrier<0>();
     }
     vm_wait<0>();  // copies in flight land before the LDS is released
     const float l = st.l + partner(st.l);
@@ -264,7 +298,7 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
     return;
   }
 
-  // ---- by waves: tile t of 32 keys to wave t % 8
+  // ---- by waves: tile t of 32 keys to wave t % 4
   constexpr int NI = 32 / RPI;  // copies per tensor and tile
   const int ntiles = (nkeys + 31) / 32;
   const uint32_t wb = L0 + w * L::Wave, wv = wb + 32 * RB;

@@ -1,7 +1,7 @@
 // Attention of decoding requests over a paged cache, fp32, gfx950: as
 // prefix_bf16.hip, with scores, exponentials and sums in fp64 on the fp64
 // matrix cores (f64tile.hpp), like the fp32 forward (fwd_f32.hip).  A workgroup
-// of four waves owns 16 query rows of a KV head and a chunk of keys, whose
+// of eight waves owns 16 query rows of a KV head and a chunk of keys, whose
 // 16-key tiles the waves take in turn; K and V rows go straight from global
 // memory into registers, rows past the chunk from a row of zeros.  Bound by
 // the fp64 matrix rate (16 rows share a tile's products however few they are)
@@ -13,7 +13,7 @@ namespace bdlm {
 
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = 8;
 constexpr double kRescale = 256.0;  // as in fwd_f32.hip
 
 __device__ __attribute__((aligned(256))) const float zero_row_f32[128] = {};
@@ -65,15 +65,16 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   acc.zero();
   double m = -INFINITY, l = 0.0;
   const int ntiles = (nkeys + 15) / 16;
+  fl4 kx[NC];
+  auto load_keys = [&](int64_t mine) __attribute__((always_inline)) {
+    const float* p = row_of(kb, mine) + 4 * g;
+#pragma unroll
+    for (int k = 0; k < NC; ++k) kx[k] = *(const fl4*)(p + 16 * k);
+  };
+  int64_t mine = key_offset(it.k0 + w * 16 + i);
+  if (w < ntiles) load_keys(mine);
   for (int t = w; t < ntiles; t += kWaves) {
     const int key0 = it.k0 + t * 16;
-    const int64_t mine = key_offset(key0 + i);
-    fl4 kx[NC];
-    {
-      const float* p = row_of(kb, mine) + 4 * g;
-#pragma unroll
-      for (int k = 0; k < NC; ++k) kx[k] = *(const fl4*)(p + 16 * k);
-    }
     ColOps<D> vx;
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
@@ -84,6 +85,9 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
       for (int h = 0; h < D / 64; ++h) vx.x[kk][h] = *(const fl4*)(p + 64 * h);
     }
     f64x4 s = row_product<D>(kx, lds, lane) * c;
+    // the next tile's keys are loaded under the softmax and the products below
+    mine = key_offset(key0 + kWaves * 16 + i);
+    load_keys(mine);
     bool grow = false;
 #pragma unroll
     for (int r = 0; r < 4; ++r) grow |= key0 + 4 * r + g < end && !(s[r] <= m + kRescale);
@@ -119,8 +123,8 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   acc.scale(m == -INFINITY ? 0.0 : exp2_f64(m - mt));
   acc_to_lds<D>(acc, lds + w * 16 * kRedRow<D>, i, g);
   __syncthreads();
-  constexpr int EPT = 16 * D / (kWaves * 64);
-  const int q = tid / (D / EPT), d0 = (tid % (D / EPT)) * EPT;
+  // four elements of a row per thread
+  const int q = tid / (D / 4), d0 = (tid % (D / 4)) * 4;
   if (q >= it.nrows) return;
   double M = red_m[0][q], lt = 0.0;
 #pragma unroll
@@ -133,18 +137,15 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   const int64_t orow = (int64_t)pr.token * a.heads + pr.head;
   const int64_t at = (int64_t)it.part * a.requests * a.rows * a.heads + orow;
   float* op = (single ? (float*)a.o + orow * D : a.part_o + at * D) + d0;
+  fl4 out;
 #pragma unroll
-  for (int e4 = 0; e4 < EPT / 4; ++e4) {
-    fl4 o;
+  for (int e = 0; e < 4; ++e) {
+    double x = 0.0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      double x = 0.0;
-#pragma unroll
-      for (int k = 0; k < kWaves; ++k) x += lds[(k * 16 + q) * kRedRow<D> + d0 + 4 * e4 + e];
-      o[e] = (float)(x * inv);
-    }
-    *(fl4*)(op + 4 * e4) = o;
+    for (int k = 0; k < kWaves; ++k) x += lds[(k * 16 + q) * kRedRow<D> + d0 + e];
+    out[e] = (float)(x * inv);
   }
+  *(fl4*)op = out;
   if (d0 == 0) {
     const double z = M + log2(lt);
     if (single) a.lse[prefix_lse_at(a, pr)] = empty ? -INFINITY : (float)(z * kLn2D);

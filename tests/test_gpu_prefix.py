@@ -137,6 +137,20 @@ def test_long_prefix_in_chunks(dtype):
     run([2100, 2071, 2600], 2064, 1, 4, 2, 64 if dtype == F32 else 128, dtype, seed=15)
 
 
+# Prefixes long enough to be kept apart (shorter ones are read with each request's own keys): few rows and many, pages
+# that the prefix ends in, rows that lie in the prefix themselves, requests that are not longer than it.
+@pytest.mark.parametrize("ps", [16, 24, 100])
+@pytest.mark.parametrize("dtype,R,P,n,H,KV,D,block", [
+    (BF, 9, 2003, 1, 16, 4, 128, False), (BF, 9, 2003, 1, 4, 4, 64, False), (BF, 24, 1100, 1, 8, 2, 128, False),
+    (BF, 8, 2500, 5, 8, 2, 128, False), (BF, 8, 2500, 5, 8, 2, 128, True), (BF, 6, 3001, 32, 16, 2, 128, True),
+    (BF, 33, 1025, 9, 4, 2, 64, False), (F32, 7, 1200, 1, 4, 2, 128, False), (F32, 9, 1601, 6, 6, 2, 64, False)])
+def test_prefixes_kept_apart(ps, dtype, R, P, n, H, KV, D, block):
+    lens = [P + (0 if r == 3 else 1 + (r * 37) % 130) for r in range(R)]
+    c, q, o, lse = run(lens, P, n, H, KV, D, dtype, ps=ps, block=block, seed=33)
+    parts = bd.prefix_attn_workspace_bytes(q, c, P) // (R * n * H * (D + 1) * 4)
+    assert parts >= 2
+
+
 def test_one_long_request():
     run([5000], 0, 1, 8, 1, 128, BF, seed=17)
     run([5000], 4999, 1, 8, 1, 128, BF, seed=17)
