@@ -73,16 +73,20 @@ bdlm_status done(hipError_t e, const char* what) { return e == hipSuccess ? BDLM
 
 // How the keys of an attention call are cut into chunks and its rows into tiles.
 //
-// The prefix: chunks of kPrefixChunk keys, longer ones where its tiles of rows
-// alone give every workgroup slot kItemsPerSlot items (64 requests behind 8K
-// tokens, 32/8 heads, one row each: 3,328 keys 110 us, 2,048 76, 1,024 58, 512
-// 71: partial sums cost what balance gains).
-// A request's own keys: chunks of at least kOwnChunk keys, their number limited
-// by the workgroups that find nothing to do where a sequence is shorter than
-// its table (kMaxOwnItems).
+// Chunks trade balance against partial sums, whose cost grows with the query
+// rows (all heads of all requests), so few rows take shorter chunks.
+// The prefix: long enough that its tiles of rows give every workgroup slot one
+// item, at least half a key per query row within [256, 1024] (2,048 rows, 8K
+// tokens, 8 KV heads: chunks of 2,048 keys 56 us, 1,024 44, 512 54; 16,384 rows, 16K
+// tokens, 4 KV heads, one item per slot: 4,096 keys 173 us, 2,048 185, 8,192 197).
+// A request's own keys: as many keys per query row, at least kOwnPerBase per
+// (KV head, request, tile), within [256, 1536] (512 of those, up to 1,500 keys:
+// chunks of 384 51 us, 768 46, whole 44), their number limited by the workgroups
+// that find nothing to do where a sequence is shorter than its table
+// (kMaxOwnItems).  Tables of up to kOwnWhole keys: one chunk, which needs no sums.
 // A prefix that would save less than kFoldBytes of reading is not kept apart:
 // the requests' own keys then start at 0, and short ones need no partial sums.
-constexpr int64_t kSlots = 2 * kCus, kItemsPerSlot = 2, kPrefixChunk = 1024, kOwnChunk = 768, kMaxOwnItems = 4096;
+constexpr int64_t kSlots = 2 * kCus, kOwnPerBase = 3, kOwnWhole = 512, kMaxOwnItems = 4096;
 constexpr int64_t kFoldBytes = 8 << 20;
 
 bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int32_t heads, int64_t prefix,
@@ -98,18 +102,23 @@ bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int
   const int64_t pt = (all + tile(a.prefix_shared) - 1) / tile(a.prefix_shared);
   const int64_t ot = (per + tile(a.own_shared) - 1) / tile(a.own_shared);
   const int64_t own = c->max_pages * c->page_size - prefix;
-  const int64_t limit = (kPrefixTableEntries - 2) * c->page_size;  // keys whose pages a workgroup can hold
+  // keys whose pages (or groups) a workgroup can hold, with a chunk that starts inside one
+  const int64_t limit = !f32 && c->page_size % 16 == 0 ? (kPrefixGroups - 2) * 16 : (kPrefixTableEntries - 2) * c->page_size;
   auto up64 = [](int64_t x) { return (x + 63) / 64 * 64; };
-  const int64_t pc = std::min(std::max(kPrefixChunk, up64(c->kv_heads * pt * prefix / (kSlots * kItemsPerSlot))),
+  auto within = [](int64_t x, int64_t lo, int64_t hi) { return std::min(std::max(x, lo), hi); };
+  const int64_t base = c->kv_heads * requests * ot;
+  const int64_t row_min = requests * rows * heads / 2;
+  const int64_t pc = std::min(std::max(up64(within(row_min, 256, 1024)),
+                                       up64(c->kv_heads * pt * prefix / kSlots)),
                               std::min(limit, up64(prefix + 1)));
   a.prefix_chunk = (int32_t)pc;
   a.prefix_chunks = (int32_t)((prefix + pc - 1) / pc);
-  const int64_t base = c->kv_heads * requests * ot;
-  int64_t oc = std::min((own + kOwnChunk - 1) / kOwnChunk, std::max<int64_t>(kMaxOwnItems / base, 1));
+  const int64_t own_min = own <= kOwnWhole ? kOwnWhole : within(std::max(kOwnPerBase * base, row_min), 256, 1536);
+  int64_t oc = std::min((own + own_min - 1) / own_min, std::max<int64_t>(kMaxOwnItems / base, 1));
   oc = std::max(oc, (own + limit - 65) / (limit - 64));
   if (oc == 0 && a.prefix_chunks == 0) oc = 1;
   a.own_chunks = (int32_t)oc;
-  a.own_min = (int32_t)std::max<int64_t>(oc > 0 ? (own + oc - 1) / oc : 1, 1);
+  a.own_min = (int32_t)std::min(own_min, limit - 64);
   a.prefix_tiles = (int32_t)pt;
   a.own_tiles = (int32_t)ot;
   const int64_t parts = a.prefix_chunks + oc, pi = c->kv_heads * pt * a.prefix_chunks, oi = base * oc;

@@ -15,9 +15,14 @@
 //    end.  For single tokens (few rows): bound by reading K and V.  A wave asks
 //    for the next tile's keys as soon as its scores are there, and for its
 //    values after P V, so that it always has copies in flight.
-// Keys come by LDS-DMA copies with a 64-bit address per lane (a cache may be
-// larger than 4 GB), rows past the chunk from a row of zeros; the page numbers
-// of a chunk wait in LDS.
+// Keys come by LDS-DMA copies (a cache may be larger than 4 GB).  Where pages
+// are whole groups of 16 tokens (GROUPS), tiles start at groups, the groups'
+// byte offsets wait in LDS, and a copy takes a wave-uniform 64-bit base and
+// constant lane offsets: no vector work per copy (with an address per lane, the
+// shuffles and 64-bit sums of which took as long as the softmax, 16 requests of
+// 32 rows behind 16K tokens took 184 us).  Other page sizes, and tiles with
+// rows past the chunk or in no page, which come from a row of zeros, take an
+// address per lane.
 #include "cache.hpp"
 #include "device.hpp"
 
@@ -37,6 +42,12 @@ __device__ __attribute__((aligned(256))) const uint32_t zero_row[64] = {};
 __device__ __forceinline__ void dma16(const char* src, uint32_t lds_byte) {
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(src), "{m0}"(lds_byte) : "memory");
 }
+// The same at a wave-uniform base and a 32-bit lane offset.
+__device__ __forceinline__ void dma16(const char* base, uint32_t voff, uint32_t lds_byte) {
+  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(voff), "s"(base), "{m0}"(lds_byte) : "memory");
+}
+// (a base from readlane, a vector instruction writing scalar registers, needs five wait states before a copy reads it)
+__device__ __forceinline__ void base_ready(const char* a, const char* b) { asm volatile("s_nop 4" ::"s"(a), "s"(b)); }
 __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void vm_wait() {
@@ -108,12 +119,12 @@ struct Lds {
   static constexpr uint32_t Wave = 2 * 32 * RB;      // K and V of 32 keys; later 32 rows of sums
   static constexpr uint32_t Tiles = kNW * Wave > 2 * Stage ? kNW * Wave : 2 * Stage;
   static constexpr uint32_t Pages = Tiles;
-  static constexpr uint32_t Ml = Pages + kPrefixTableEntries * 4;
+  static constexpr uint32_t Ml = Pages + kPrefixTableEntries * 4;  // (or kPrefixGroups * 8)
   static constexpr uint32_t Bytes = Ml + kNW * 32 * 8;
   static_assert(Wave == 32 * D * 4, "a wave's sums fit its tiles");
 };
 
-template <int D>
+template <int D, bool GROUPS>
 __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void prefix_bf16_kernel(
     const PrefixArgs a) {
   using L = Lds<D>;
@@ -122,6 +133,7 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   __shared__ __attribute__((aligned(1024))) unsigned char lds[L::Bytes];
   const uint32_t L0 = lds_addr(lds);
   int* const pages = (int*)(lds + L::Pages);
+  int64_t* const groups = (int64_t*)(lds + L::Pages);
   float* const red_m = (float*)(lds + L::Ml);  // [wave][32], the sums behind it
   float* const red_l = red_m + kNW * 32;
 
@@ -134,15 +146,23 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
     return;
   const bool single = a.prefix_chunks + a.own_chunks == 1;
   const float c = a.scale_log2;
-  const int nkeys = it.k1 - it.k0;
+  // Tiles start at the chunk's first key, or at the group of 16 that holds it (the keys before it are hidden).
+  const int start = GROUPS ? it.k0 & ~15 : it.k0;
+  const int nkeys = it.k1 > it.k0 ? it.k1 - start : 0;
+  const int64_t row_bytes = (int64_t)a.kv_heads * RB;
 
-  // The chunk's page numbers; those outside the cache become -1, whose rows read as zeros.
+  // The byte offsets of the chunk's groups, or its page numbers; -1 for pages
+  // outside the cache, whose rows read as zeros.
   const int page0 = it.k0 / a.page_size;
   if (nkeys > 0) {
-    const int n = (it.k1 - 1) / a.page_size - page0 + 1;
+    const int32_t* const table = a.table + (int64_t)it.seq * a.max_pages;
+    const int n = GROUPS ? (nkeys + 15) / 16 : (it.k1 - 1) / a.page_size - page0 + 1;
     for (int e = tid; e < n; e += kNW * 64) {
-      const int p = a.table[(int64_t)it.seq * a.max_pages + page0 + e];
-      pages[e] = (unsigned)p < (unsigned)a.pages ? p : -1;
+      const int key = start + e * 16, pe = GROUPS ? key / a.page_size : page0 + e;
+      const int p = table[pe];
+      const bool ok = (unsigned)p < (unsigned)a.pages;
+      if constexpr (GROUPS) groups[e] = ok ? ((int64_t)p * a.page_size + (key - pe * a.page_size)) * row_bytes : -1;
+      else pages[e] = ok ? p : -1;
     }
   }
 
@@ -161,49 +181,88 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
   for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(qf[s]));
 
-  const int64_t row_bytes = (int64_t)a.kv_heads * RB;
   const char* const kb = a.k + (int64_t)it.kvh * RB;
   const char* const vb = a.v + (int64_t)it.kvh * RB;
   const char* const zero = (const char*)zero_row;
   // Byte offset of a key's row in K (and V), -1: a row of zeros.
   auto key_offset = [&](int key) __attribute__((always_inline)) -> int64_t {
     if (key >= it.k1) return -1;
-    const int e = key / a.page_size;
-    const int p = pages[e - page0];
-    return p < 0 ? -1 : ((int64_t)p * a.page_size + (key - e * a.page_size)) * row_bytes;
+    if constexpr (GROUPS) {
+      const int64_t g = groups[(key - start) >> 4];
+      return g < 0 ? -1 : g + (key & 15) * row_bytes;
+    } else {
+      const int e = key / a.page_size;
+      const int p = pages[e - page0];
+      return p < 0 ? -1 : ((int64_t)p * a.page_size + (key - e * a.page_size)) * row_bytes;
+    }
+  };
+  // Copies of 32 rows from key `first` (a multiple of 16 with GROUPS) on to LDS.
+  constexpr int RPI = 64 / CH, NI = 32 / RPI, GI = 16 / RPI;  // rows per copy; copies of 32 rows, of a group
+  uint32_t voff[GI];
+#pragma unroll
+  for (int i = 0; i < GI; ++i) {
+    const int r = i * RPI + lane / CH;
+    voff[i] = (uint32_t)(r * (int)row_bytes) + (uint32_t)((lane % CH) ^ chunk_swz<D>(r)) * 16u;
+  }
+  // Their two groups' offsets, read ahead of the copies (any value where there is no such pair of groups).
+  struct Pair {
+    int64_t g0, g1;
+  };
+  auto pair_at = [&](int first) __attribute__((always_inline)) -> Pair {
+    if constexpr (!GROUPS) return Pair{-1, -1};
+    const int e = imin((first - start) >> 4, kPrefixGroups - 2);
+    return Pair{groups[e], groups[e + 1]};
+  };
+  auto copy32 = [&](const char* base, int first, const Pair& ahead, uint32_t dst) __attribute__((always_inline)) {
+    if constexpr (GROUPS) {
+      if (first + 32 <= it.k1) {
+        auto uniform = [](int64_t x) __attribute__((always_inline)) {
+          return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
+                           (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
+        };
+        const int64_t g0 = uniform(ahead.g0), g1 = uniform(ahead.g1);
+        if ((g0 | g1) >= 0) {
+          const char *b0 = base + g0, *b1 = base + g1;
+          lds_done();  // the rows there have been read
+          base_ready(b0, b1);
+#pragma unroll
+          for (int i = 0; i < NI; ++i) dma16(i < GI ? b0 : b1, voff[i % GI], dst + i * 1024);
+          return;
+        }
+      }
+    }
+    const int64_t mine = key_offset(first + l32);
+    lds_done();
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int r = i * RPI + lane / CH;
+      const int lo = __shfl((int)(uint32_t)mine, r), hi = __shfl((int)(mine >> 32), r);
+      const int64_t off = ((int64_t)hi << 32) | (uint32_t)lo;
+      dma16((off < 0 ? zero : base + off) + (uint32_t)((lane % CH) ^ chunk_swz<D>(r)) * 16u, dst + i * 1024);
+    }
   };
   const uint32_t yrow = swz_row_part<D>(l32, half);
   const uint32_t ytr0 = swz_tr_part<D>(G, sl, 0), ytr1 = swz_tr_part<D>(G, sl, 8);
-  // The 16-byte chunk of its row that lane `lane` fetches when the copy's first row is row0 of a tile.
-  constexpr int RPI = 64 / CH;  // rows per copy
-  auto copy_chunk = [&](int row0) { return (uint32_t)((lane % CH) ^ chunk_swz<D>(row0 + lane / CH)) * 16u; };
-
   RowState<D> st;
   st.init();
 
   if (it.shared) {
     // ---- the waves share 64-key tiles; waves 0 and 1 copy K, 2 and 3 V, 32 rows each
-    constexpr int IPW = 32 / RPI;
     const int ntiles = (nkeys + 63) / 64;
     const char* const base = w < 2 ? kb : vb;
     const int crow = (w & 1) * 32;
-    auto copy_tile = [&](int t, int stage) __attribute__((always_inline)) {
-      const int64_t mine = key_offset(t < ntiles ? it.k0 + t * 64 + crow + l32 : it.k1);
-      const uint32_t dst = L0 + stage * L::Stage + (w < 2 ? 0u : 64 * RB) + crow * RB;
-#pragma unroll
-      for (int i = 0; i < IPW; ++i) {
-        const int r = i * RPI + lane / CH;
-        const int lo = __shfl((int)(uint32_t)mine, r), hi = __shfl((int)(mine >> 32), r);
-        const int64_t off = ((int64_t)hi << 32) | (uint32_t)lo;
-        dma16((off < 0 ? zero : base + off) + copy_chunk(crow + i * RPI), dst + i * 1024);
-      }
+    auto first_of = [&](int t) { return t < ntiles ? start + t * 64 + crow : it.k1; };
+    auto copy_tile = [&](int t, const Pair& ahead, int stage) __attribute__((always_inline)) {
+      copy32(base, first_of(t), ahead, L0 + stage * L::Stage + (w < 2 ? 0u : 64 * RB) + crow * RB);
     };
     const bool any = __builtin_amdgcn_ballot_w64(row_ok && end > it.k0) != 0;
-    copy_tile(0, 0);
+    copy_tile(0, pair_at(first_of(0)), 0);
+    Pair ahead = pair_at(first_of(1));
     vm_wait_barrier<0>();
     for (int t = 0; t < ntiles; ++t) {
-      copy_tile(t + 1, (t + 1) & 1);
-      const int key0 = it.k0 + t * 64;
+      copy_tile(t + 1, ahead, (t + 1) & 1);
+      ahead = pair_at(first_of(t + 2));
+      const int key0 = start + t * 64;
       if (any && __builtin_amdgcn_ballot_w64(end > key0) != 0) {
         const uint32_t sb = L0 + (t & 1) * L::Stage;
         const uint32_t zr = sb + yrow;
@@ -232,12 +291,14 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
             __builtin_amdgcn_sched_barrier(0);
           }
         }
-        if (__builtin_amdgcn_ballot_w64(end < key0 + 64) != 0) {
+        if (key0 < it.k0 || __builtin_amdgcn_ballot_w64(end < key0 + 64) != 0) {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int i = 0; i < 16; ++i)
-              if (key0 + u * 32 + (i >> 2) * 8 + 4 * half + (i & 3) >= end) s[u][i] = -INFINITY;
+            for (int i = 0; i < 16; ++i) {
+              const int key = key0 + u * 32 + (i >> 2) * 8 + 4 * half + (i & 3);
+              if (key >= end || (GROUPS && key < it.k0)) s[u][i] = -INFINITY;
+            }
         }
         // value fragments PA products ahead, the first ones under the softmax
         const uint32_t zt0 = sb + 64 * RB + ytr0, zt1 = sb + 64 * RB + ytr1;
@@ -299,38 +360,28 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
 
   // ---- by waves: tile t of 32 keys to wave t % 4
-  constexpr int NI = 32 / RPI;  // copies per tensor and tile
   const int ntiles = (nkeys + 31) / 32;
   const uint32_t wb = L0 + w * L::Wave, wv = wb + 32 * RB;
-  auto row_offset = [&](int t) { return key_offset(it.k0 + t * 32 + l32); };
-  auto copy = [&](const char* base, int64_t mine, uint32_t dst) __attribute__((always_inline)) {
-    lds_done();  // the tile there has been read
-#pragma unroll
-    for (int i = 0; i < NI; ++i) {
-      const int r = i * RPI + lane / CH;
-      const int lo = __shfl((int)(uint32_t)mine, r), hi = __shfl((int)(mine >> 32), r);
-      const int64_t off = ((int64_t)hi << 32) | (uint32_t)lo;
-      dma16((off < 0 ? zero : base + off) + copy_chunk(i * RPI), dst + i * 1024);
-    }
-  };
   if (w < ntiles) {
-    int64_t mine = row_offset(w);
-    copy(kb, mine, wb);
-    copy(vb, mine, wv);
+    Pair ahead = pair_at(start + w * 32);
+    copy32(kb, start + w * 32, ahead, wb);
+    copy32(vb, start + w * 32, ahead, wv);
     for (int t = w; t < ntiles; t += kNW) {
-      const int key0 = it.k0 + t * 32;
-      const int64_t next = row_offset(t + kNW);  // (past the chunk: zeros)
-      vm_wait<NI>();                             // the keys are there, the values in flight
+      const int key0 = start + t * 32, next = key0 + kNW * 32;  // (past the chunk: zeros)
+      ahead = pair_at(next);
+      vm_wait<NI>();  // the keys are there, the values in flight
       f32x16 s[1];
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[0][i] = 0.f;
 #pragma unroll
       for (int k = 0; k < KS; ++k) s[0] = mfma32(lds_load16((wb + yrow) ^ (32u * k)), qf[k], s[0]);
-      copy(kb, next, wb);
-      if (__builtin_amdgcn_ballot_w64(end < key0 + 32) != 0) {
+      copy32(kb, next, ahead, wb);
+      if (key0 < it.k0 || __builtin_amdgcn_ballot_w64(end < key0 + 32) != 0) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          if (key0 + (i >> 2) * 8 + 4 * half + (i & 3) >= end) s[0][i] = -INFINITY;
+        for (int i = 0; i < 16; ++i) {
+          const int key = key0 + (i >> 2) * 8 + 4 * half + (i & 3);
+          if (key >= end || (GROUPS && key < it.k0)) s[0][i] = -INFINITY;
+        }
       }
       bf16x8 pb[2];
       softmax_step<D, 1>(st, s, pb, c);
@@ -342,7 +393,7 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
           st.acc[d] = mfma32(cat(lds_read_tr_at(((wv + ytr0) ^ (64u * d)) + u * 16 * RB),
                                  lds_read_tr_at(((wv + ytr1) ^ (64u * d)) + u * 16 * RB)),
                              pb[u], st.acc[d]);
-      copy(vb, next, wv);
+      copy32(vb, next, ahead, wv);
     }
     vm_wait<0>();
   }
@@ -399,13 +450,18 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   }
 }
 
+template <int D>
+void launch(const PrefixArgs& a, int n, hipStream_t s) {
+  if (a.page_size % 16 == 0) hipLaunchKernelGGL((prefix_bf16_kernel<D, true>), dim3(n), dim3(kNW * 64), 0, s, a);
+  else hipLaunchKernelGGL((prefix_bf16_kernel<D, false>), dim3(n), dim3(kNW * 64), 0, s, a);
+}
+
 }  // namespace
 
 hipError_t launch_prefix_bf16(const PrefixArgs& a, int head_dim, hipStream_t s) {
   const int n = a.prefix_items + a.own_items;
   if (n == 0) return hipSuccess;
-  if (head_dim == 128) hipLaunchKernelGGL((prefix_bf16_kernel<128>), dim3(n), dim3(kNW * 64), 0, s, a);
-  else hipLaunchKernelGGL((prefix_bf16_kernel<64>), dim3(n), dim3(kNW * 64), 0, s, a);
+  head_dim == 128 ? launch<128>(a, n, s) : launch<64>(a, n, s);
   return hipGetLastError();
 }
 

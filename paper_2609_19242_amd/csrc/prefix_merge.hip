@@ -2,9 +2,11 @@
 // added up, gfx950: with z_j the log2-sum-exp of chunk j of a row,
 //   m = max z_j,  w_j = 2^(z_j - m),  O = sum w_j O_j / sum w_j,
 //   LSE = ln 2 (m + log2 sum w_j)
-// in fp32, chunk by chunk in order: the same sums on every run.  Chunks that a
-// row does not see (z_j = -inf) are not read.  A wave per row, a lane per D / 64
-// elements.  Bound by reading the partials (mostly from L2).
+// in fp32, in an order that depends on the number of chunks only.  A wave per
+// row: D / 4 lanes hold 16 bytes each of one chunk's output, the wave takes
+// 256 / D chunks at a time, four such rounds in flight.  Chunks that a row does
+// not see (z_j = -inf) have left no output; what lies there takes no part.
+// Bound by reading the partials (mostly from L2).
 #include "cache.hpp"
 #include "device.hpp"
 
@@ -16,8 +18,8 @@ constexpr float kLn2 = 0.69314718055994530942f;
 
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void prefix_merge_kernel(const PrefixArgs a) {
-  constexpr int E = D / 64;
-  const int lane = threadIdx.x & 63;
+  constexpr int LPR = D / 4, PP = 64 / LPR;  // lanes per chunk, chunks at a time
+  const int lane = threadIdx.x & 63, part = lane / LPR, col = lane % LPR;
   const int64_t total = (int64_t)a.requests * a.rows * a.heads;
   const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (row >= total) return;
@@ -26,23 +28,42 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(const PrefixArgs a) {
   for (int j = lane; j < parts; j += 64) m = fmaxf(m, a.part_lse[j * total + row]);
 #pragma unroll
   for (int s = 32; s > 0; s >>= 1) m = fmaxf(m, __shfl_xor(m, s));
-  float sum = 0.f, x[E] = {};
-  if (m > -INFINITY) {
-    for (int j = 0; j < parts; ++j) {
-      const float z = a.part_lse[j * total + row];
-      if (z == -INFINITY) continue;
-      const float w = exp2f_fast(z - m);
-      sum += w;
-      const float* p = a.part_o + (j * total + row) * D + lane * E;
+  const float ref = m == -INFINITY ? 0.f : m;
+  float sum = 0.f;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+  for (int j0 = part; j0 < parts; j0 += 4 * PP) {
+    float z[4];
+    f32x4 p[4];
 #pragma unroll
-      for (int e = 0; e < E; ++e) x[e] = fmaf(w, p[e], x[e]);
+    for (int k = 0; k < 4; ++k) {
+      const int64_t at = imin(j0 + k * PP, parts - 1) * total + row;
+      z[k] = a.part_lse[at];
+      p[k] = *(const f32x4*)(a.part_o + at * D + col * 4);
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const bool seen = j0 + k * PP < parts && z[k] > -INFINITY;
+      const float w = seen ? exp2f_fast(z[k] - ref) : 0.f;
+      sum += w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = seen ? fmaf(w, p[k][e], x[e]) : x[e];
     }
   }
-  const float inv = sum > 0.f ? 1.f / sum : 0.f;
 #pragma unroll
-  for (int e = 0; e < E; ++e) {
-    if constexpr (BF16) ((bf16*)a.o)[row * D + lane * E + e] = to_bf16(x[e] * inv);
-    else ((float*)a.o)[row * D + lane * E + e] = x[e] * inv;
+  for (int s = LPR; s < 64; s <<= 1) {
+    sum += __shfl_xor(sum, s);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += __shfl_xor(x[e], s);
+  }
+  if (part != 0) return;
+  const float inv = sum > 0.f ? 1.f / sum : 0.f;
+  if constexpr (BF16) {
+    bf16x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = to_bf16(x[e] * inv);
+    *(bf16x4*)((bf16*)a.o + row * D + col * 4) = y;
+  } else {
+    *(f32x4*)((float*)a.o + row * D + col * 4) = x * inv;
   }
   if (lane == 0) {
     PrefixRow pr;
