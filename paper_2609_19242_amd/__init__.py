@@ -79,6 +79,8 @@ class BdlmError(RuntimeError):
 
 
 _LIB = None
+_current_gpu = torch._C._cuda_getDevice
+_raw_stream = torch._C._cuda_getCurrentRawStream
 _VP = ctypes.c_void_p
 _PP = ctypes.POINTER(ctypes.c_void_p)
 
@@ -172,13 +174,12 @@ def _torch_stream(stream, device) -> torch.cuda.Stream:
 
 
 def _launch(device, stream, call, *args):
-    """``call(*args, handle)``, with the handle of ``stream`` (default: the current stream of ``device``) and with
-    ``device`` current meanwhile; raises if it fails."""
-    if device.index != torch._C._cuda_getDevice():
+    """``call(*args, handle)``, with the handle of ``stream`` (default: the current stream of GPU ``device``) and with
+    that GPU current meanwhile; raises if it fails."""
+    if device != _current_gpu():
         with torch.cuda.device(device):
             return _launch(device, stream, call, *args)
-    handle = torch._C._cuda_getCurrentRawStream(device.index) if stream is None else _stream(stream)
-    status = call(*args, handle)
+    status = call(*args, _raw_stream(device) if stream is None else _stream(stream))
     if status != 0:
         _check(status)
 

@@ -70,7 +70,7 @@ class Cache:
         self.k, self.v, self.table, self.lens, self.refs, self.status = k, v, table, lens, refs, status
         self.layers, self.pages, self.page_size, self.kv_heads, self.head_dim = k.shape
         self.seqs, self.max_pages = seqs, max_pages
-        self.dtype, self.device = k.dtype, k.device
+        self.dtype, self.device, self.gpu = k.dtype, k.device, k.get_device()
         nbytes = lib().bdlm_cache_work_bytes(pages, seqs)
         self._work = torch.empty(max(64, nbytes) // 4, dtype=torch.int32, device=k.device)
         self._record = _Cache(k.data_ptr(), v.data_ptr(), table.data_ptr(), lens.data_ptr(), refs.data_ptr(),
@@ -101,15 +101,16 @@ def _cache(c):
 
 def _list(c, name, t, n=None):
     """An int32 list on the cache's device: its address."""
-    if not isinstance(t, torch.Tensor) or t.dim() != 1:
-        raise ValueError(f"{name} must be a one-dimensional int32 tensor")
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
     if t.dtype is not torch.int32:
         raise TypeError(f"{name} must be torch.int32, got {t.dtype}")
-    if n is not None and t.shape[0] != n:
-        raise ValueError(f"{name} has {t.shape[0]} entries, not {n}")
+    shape = t.shape
+    if len(shape) != 1 or (n is not None and shape[0] != n):
+        raise ValueError(f"{name} must have shape ({'n' if n is None else n},), got {tuple(shape)}")
     if not t.is_contiguous():
         raise ValueError(f"{name} must be contiguous")
-    if t.device != c.device:
+    if t.get_device() != c.gpu:
         raise ValueError(f"{name} must be on {c.device}, got {t.device}")
     return t.data_ptr()
 
@@ -119,7 +120,7 @@ def cache_grow(cache: Cache, seqs, counts, stream=None):
     c = _cache(cache)
     a = _list(c, "seqs", seqs)
     b = _list(c, "counts", counts, seqs.shape[0])
-    _launch(c.device, stream, lib().bdlm_cache_grow, c._ref, seqs.shape[0], a, b)
+    _launch(c.gpu, stream, lib().bdlm_cache_grow, c._ref, seqs.shape[0], a, b)
 
 
 def cache_fork(cache: Cache, parents, children, stream=None):
@@ -127,20 +128,20 @@ def cache_fork(cache: Cache, parents, children, stream=None):
     c = _cache(cache)
     a = _list(c, "parents", parents)
     b = _list(c, "children", children, parents.shape[0])
-    _launch(c.device, stream, lib().bdlm_cache_fork, c._ref, parents.shape[0], a, b)
+    _launch(c.gpu, stream, lib().bdlm_cache_fork, c._ref, parents.shape[0], a, b)
 
 
 def cache_free(cache: Cache, seqs, stream=None):
     """Empties sequences and gives back the pages that no other sequence holds."""
     c = _cache(cache)
     a = _list(c, "seqs", seqs)
-    _launch(c.device, stream, lib().bdlm_cache_free, c._ref, seqs.shape[0], a)
+    _launch(c.gpu, stream, lib().bdlm_cache_free, c._ref, seqs.shape[0], a)
 
 
 def cache_compact(cache: Cache, stream=None):
     """Moves live pages into the holes below them, so that the free pages are the last ones."""
     c = _cache(cache)
-    _launch(c.device, stream, lib().bdlm_cache_compact, c._ref)
+    _launch(c.gpu, stream, lib().bdlm_cache_compact, c._ref)
 
 
 def cache_write(cache: Cache, layer: int, seqs, counts, k, v, starts: Optional[torch.Tensor] = None, stream=None):
@@ -155,7 +156,7 @@ def cache_write(cache: Cache, layer: int, seqs, counts, k, v, starts: Optional[t
     rows = k.shape[0]
     if rows != v.shape[0]:
         raise ValueError(f"k has {rows} rows, v has {v.shape[0]}")
-    _launch(c.device, stream, lib().bdlm_cache_write, c._ref, layer, n, a, b, at, rows, rk, rv)
+    _launch(c.gpu, stream, lib().bdlm_cache_write, c._ref, layer, n, a, b, at, rows, rk, rv)
 
 
 def _check_q(c, q):
@@ -163,7 +164,7 @@ def _check_q(c, q):
         raise ValueError("q must be a [requests][rows][heads][head_dim] tensor")
     R, n, H, D = q.shape
     _expect("q", q, c.dtype, (R, n, H, c.head_dim))
-    if q.device != c.device:
+    if q.get_device() != c.gpu:
         raise ValueError(f"q must be on {c.device}, got {q.device}")
     return R, n, H
 
@@ -202,6 +203,6 @@ def prefix_attn(q, cache: Cache, layer: int, seqs, prefix: int = 0, block: bool 
     else:
         _workspace(workspace, 0, c.device, stream)
         nbytes = workspace.numel() * workspace.element_size()
-    _launch(c.device, stream, lib().bdlm_prefix_attn, c._ref, layer, R, a, n, H, prefix, 1 if block else 0, scale,
+    _launch(c.gpu, stream, lib().bdlm_prefix_attn, c._ref, layer, R, a, n, H, prefix, 1 if block else 0, scale,
             q.data_ptr(), o.data_ptr(), lse.data_ptr(), workspace.data_ptr(), nbytes)
     return o, lse

@@ -150,12 +150,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   };
   const bool kwave = w < NW / 2;
   const int64_t CS = kwave ? k_stride<D>(a) : v_stride<D>(a);  // of the tensor this wave copies
+  int u0, u1;
+  seen_keys(a, pq0, pq1, u0, u1);
   auto copy_seek = [&](CopyCur cc) -> CopyCur {
     if (cc.c.have) {
       const KRangeArg& kr = a.kr[cc.c.j];
       cc.src = (const bf16*)(kwave ? kr.k : kr.v) +
                row_elem<D>(a, it.b, kr.bstride, (int64_t)cc.c.t * BN, HKV, kvh, CS);
-      cc.rows_left = kr.len - cc.c.t * BN;
+      cc.rows_left = (kPacked ? u1 : kr.len) - cc.c.t * BN;
     }
     return cc;
   };
@@ -188,6 +190,19 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
       const int nr = nrows - 16 * k;
+      if constexpr (kPacked) {
+        // rows before the first seen key lie before the resource: their offsets wrap and read zeros too (as in
+        // the forward; no row of this copy's reach where the last seen key lies before it)
+        const int skip = cc.c.have ? u0 - cc.c.t * BN - 16 * k : 0;
+        if (skip > 0) {
+          const uint32_t ahead = (uint32_t)(skip * (int)CS * 2);
+          const auto r = make_rsrc(nr > skip ? cc.src + (int64_t)(16 * k + skip) * CS : any_src,
+                                   nr > skip ? (uint32_t)(((nr - skip - 1) * (int)CS + D) * 2) : 0u);
+#pragma unroll
+          for (int i = 0; i < PI; ++i) buf_to_lds<16>(r, dst + (k * PI + i) * 512, voff[i] - ahead, 0);
+          continue;
+        }
+      }
       const uint32_t bytes = nr > 0 ? (uint32_t)(((nr - 1) * (int)CS + D) * 2) : 0u;
       const auto r = make_rsrc(nr > 0 ? cc.src + (int64_t)16 * k * CS : any_src, bytes);
 #pragma unroll

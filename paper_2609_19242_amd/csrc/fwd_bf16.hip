@@ -130,12 +130,14 @@ __global__ __launch_bounds__(NT * NW * 64)
   };
   const bool kwave = w < NW / 2;
   const int64_t CS = kwave ? k_stride<D>(a) : v_stride<D>(a);  // of the tensor this wave copies
+  int u0, u1;
+  seen_keys(a, pq0, pq1, u0, u1);
   auto copy_seek = [&](CopyCur cc) -> CopyCur {
     if (cc.c.have) {
       const KRangeArg& kr = a.kr[cc.c.j];
       cc.src = (const bf16*)(kwave ? kr.k : kr.v) +
                row_elem<D>(a, it.b, kr.bstride, (int64_t)cc.c.t * BN, HKV, kvh, CS);
-      cc.rows_left = kr.len - cc.c.t * BN;
+      cc.rows_left = (kIsPacked<Args> ? u1 : kr.len) - cc.c.t * BN;
     }
     return cc;
   };
@@ -161,8 +163,19 @@ __global__ __launch_bounds__(NT * NW * 64)
   auto copy_tile = [&](bf16* st, const CopyCur& cc) __attribute__((always_inline)) {
     const int nrows = cc.c.have ? imin(BN, cc.rows_left) : 0;
     const uint32_t bytes = cc.c.have ? (uint32_t)(((nrows - 1) * (int)CS + D) * 2) : 0u;
-    const auto r = make_rsrc(cc.c.have ? cc.src : any_src, bytes);
     bf16* dst = st + (kwave ? 0 : BN * D) + cw * IPW * 512;
+    if constexpr (kIsPacked<Args>) {
+      // rows before the first seen key lie before the resource: their offsets wrap and read zeros too
+      const int skip = cc.c.have ? u0 - cc.c.t * BN : 0;
+      if (skip > 0) {
+        const uint32_t ahead = (uint32_t)(skip * (int)CS * 2);
+        const auto r = make_rsrc(cc.src + skip * CS, bytes - ahead);
+#pragma unroll
+        for (int i = 0; i < IPW; ++i) buf_to_lds<16>(r, dst + i * 512, voff[i] - ahead, 0);
+        return;
+      }
+    }
+    const auto r = make_rsrc(cc.c.have ? cc.src : any_src, bytes);
 #pragma unroll
     for (int i = 0; i < IPW; ++i) buf_to_lds<16>(r, dst + i * 512, voff[i], 0);
   };

@@ -98,6 +98,23 @@ __device__ inline bool find_key_tile(const A& a, int jj, int qs, int pq0, int pq
   return false;
 }
 
+// Packed calls: the keys [u0, u1) of the sequence that some row of the query
+// tile can see.  Only these are copied: what the others hold, an evicted or
+// unwritten part of a window's past, say, must not meet a probability of zero
+// as an infinity or NaN.
+__device__ inline void seen_keys(const AttnArgs&, int, int, int& u0, int& u1) {
+  u0 = 0;
+  u1 = kBig;
+}
+__device__ inline void seen_keys(const PackedView& a, int pq0, int pq1, int& u0, int& u1) {
+  const KRangeArg& kr = a.kr[0];
+  int lo0, hi0, lo1, hi1;
+  key_interval(kClean, pq0, kClean, rule_of(a), lo0, hi0);
+  key_interval(kClean, pq1, kClean, rule_of(a), lo1, hi1);
+  u0 = imax(lo0 - kr.pos0, 0);
+  u1 = imin(hi1 - kr.pos0, kr.len);
+}
+
 // Key tiles of all ranges that the query tile can see.
 template <class A>
 __device__ inline int count_key_tiles(const A& a, int qs, int pq0, int pq1, int BN) {

@@ -59,7 +59,7 @@ class PackedPlan:
         self.heads, self.kv_heads, self.head_dim = p.heads, p.kv_heads, p.head_dim
         self.q_rows, self.k_rows = record.q_rows, record.k_rows
         self.workspace_bytes = record.workspace_bytes
-        self.device = items.device
+        self.device, self.gpu = items.device, items.get_device()  # (gpu: -1 on the CPU)
 
     def __repr__(self):
         return (f"PackedPlan(q_rows={self.q_rows}, k_rows={self.k_rows}, heads={self.heads}, kv_heads={self.kv_heads}, "
@@ -118,24 +118,25 @@ def _rows(like, name, t, heads, at_least):
         raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
     if t.dtype is not like.dtype:
         raise TypeError(f"{name} must be {like.dtype}, got {t.dtype}")
-    D, shape = like.head_dim, t.shape
+    D, shape, st = like.head_dim, t.shape, t.stride()
     if len(shape) != 3 or shape[1] != heads or shape[2] != D:
         raise ValueError(f"{name} must have shape (rows, {heads}, {D}), got {tuple(shape)}")
-    n = shape[0]
+    n, s0 = shape[0], st[0]
     if n < at_least:
         raise ValueError(f"{name} has {n} rows, {at_least} are needed")
-    s0, s1, s2 = t.stride()
-    if n and (s2 != 1 or (heads > 1 and s1 != D) or (n > 1 and s0 < heads * D)):
+    if n <= 1:
+        s0 = heads * D
+    if n and (st[2] != 1 or (heads > 1 and st[1] != D) or s0 < heads * D):
         raise ValueError(f"{name} must hold each row's heads contiguously (only rows may lie apart)")
-    if t.device != like.device:
+    if t.get_device() != like.gpu:
         raise ValueError(f"{name} must be on {like.device}, got {t.device}")
-    return _Rows(t.data_ptr(), s0 if n > 1 else heads * D)
+    return _Rows(t.data_ptr(), s0)
 
 
 def _check_plan(plan):
     if not isinstance(plan, PackedPlan):
         raise TypeError(f"plan must be a PackedPlan, got {type(plan).__name__}")
-    if plan.device.type != "cuda":
+    if plan.gpu < 0:
         raise ValueError(f"the plan's items are on {plan.device}, not on a GPU")
 
 
@@ -161,7 +162,7 @@ def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, stream=No
         o, lse = out
         ro = _as_long(plan, "o", o, H, n)
         _lse(plan, lse, n)
-    _launch(plan.device, stream, lib().bdlm_packed_fwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n)
+    _launch(plan.gpu, stream, lib().bdlm_packed_fwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n)
     return o, lse
 
 
@@ -184,7 +185,7 @@ def packed_bwd(plan: PackedPlan, q, k, v, o, lse, do, out: Optional[tuple] = Non
         dq, dk, dv = out
     outs = [_as_long(plan, "dq", dq, H, n), _as_long(plan, "dk", dk, KV, nk), _as_long(plan, "dv", dv, KV, nv)]
     workspace = _workspace(workspace, plan.workspace_bytes, plan.device, stream)
-    _launch(plan.device, stream, lib().bdlm_packed_bwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n, rdo,
+    _launch(plan.gpu, stream, lib().bdlm_packed_bwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n, rdo,
             *outs, workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return dq, dk, dv
 
@@ -198,7 +199,7 @@ def _as_long(plan, name, t, heads, n):
 
 def _lse(plan, lse, n):
     _expect("lse", lse, torch.float32, (plan.heads, n))
-    if lse.device != plan.device:
+    if lse.get_device() != plan.gpu:
         raise ValueError(f"lse must be on {plan.device}, got {lse.device}")
 
 

@@ -7,7 +7,7 @@ import torch
 
 import paper_2609_19242_amd as bd
 import synth
-from tests.serving_util import check, packed
+from tests.serving_util import check, packed, visible
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda"
@@ -177,3 +177,50 @@ def test_two_streams_at_once():
     torch.cuda.synchronize()
     for a, b in zip(want, got):
         assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("what", [math.nan, math.inf, -math.inf])
+@pytest.mark.parametrize("ql,kl,block,window", [([20, 33], [300, 170], 1, 40), ([1, 5, 64], [129, 400, 200], 1, 1),
+                                                ([40, 100], [400, 333], 16, 70), ([10], [200], 64, 10)])
+def test_keys_that_no_row_sees_may_hold_anything(ql, kl, block, window, what, dtype):
+    """The past that a window has left behind: its keys and values, evicted or never written."""
+    H, KV, D = 4, 2, 64
+    qs, nq = rows_of(ql)
+    ks, nk = rows_of(kl)
+    q, do = (synth.normal((nq, H, D), 70 + i, dtype).to(DEV) for i in range(2))
+    k, v = (synth.normal((nk, KV, D), 80 + i, dtype).to(DEV) for i in range(2))
+    for s, (a, n, m) in enumerate(zip(ks, ql, kl)):
+        seen = visible(n, m, block, window).any(0).to(DEV)
+        assert not seen.all()
+        for t in (k, v):
+            t[a:a + m][~seen] = what
+    plan = bd.packed_plan(ql, kl, heads=H, kv_heads=KV, head_dim=D, dtype=dtype, block_size=block, window=window)
+    o, lse = bd.packed_fwd(plan, q, k, v)
+    dq, dk, dv = bd.packed_bwd(plan, q, k, v, o, lse, do)
+    torch.cuda.synchronize()
+    ref = packed(q, k, v, list(zip(qs, ql, ks, kl)), block=block, window=window, do=do)
+    for n, t in (("o", o), ("lse", lse), ("dq", dq), ("dk", dk), ("dv", dv)):
+        check(n, t, *ref[n])
+
+
+def test_padded_batch():
+    """[batch][longest] rows with lengths: the padding is read and written by nobody."""
+    B, S, H, KV, D = 3, 150, 4, 2, 64
+    lens = [150, 1, 77]
+    q, do = (synth.normal((B * S, H, D), 90 + i, BF).to(DEV) for i in range(2))
+    k, v = (synth.normal((B * S, KV, D), 95 + i, BF).to(DEV) for i in range(2))
+    starts = [b * S for b in range(B)]
+    for b, n in enumerate(lens):
+        for t in (q, k, v, do):
+            t[b * S + n:(b + 1) * S] = math.nan
+    plan = bd.packed_plan(lens, heads=H, kv_heads=KV, head_dim=D, dtype=BF, q_starts=starts)
+    out = torch.zeros_like(q), torch.zeros(H, B * S, device=DEV)
+    o, lse = bd.packed_fwd(plan, q, k, v, out=out)
+    grads = tuple(torch.zeros_like(t) for t in (q, k, v))
+    bd.packed_bwd(plan, q, k, v, o, lse, do, out=grads)
+    torch.cuda.synchronize()
+    ref = packed(q, k, v, [(s, n, s, n) for s, n in zip(starts, lens)], do=do)
+    for n, t in zip(("o", "lse", "dq", "dk", "dv"), (o, lse) + grads):
+        check(n, t, *ref[n])
+        assert not torch.isnan(t).any()
