@@ -337,21 +337,22 @@ __global__ __launch_bounds__(256) void cache_write_kernel(const CacheArg c, cons
   if ((unsigned)s >= (unsigned)c.seqs) return;
   const int per = r.rows / r.n;
   const int64_t first = r.starts ? r.starts[i] : (int64_t)i * per;
-  const int count = r.counts[i], n = clamped_len(c, s);
+  const int count = r.counts[i];
   const int64_t limit = r.starts ? r.rows : first + per;  // rows of this sequence in the new tensors end here
   // 16-byte pieces of several rows at a time
   const int pieces = c.row_bytes / 16;
-  const int64_t total = (int64_t)count * pieces;
-  for (int64_t x = (int64_t)blockIdx.y * 256 + threadIdx.x; x < total; x += (int64_t)gridDim.y * 256) {
-    const int j = (int)(x / pieces), b = (int)(x - (int64_t)j * pieces) * 16;
-    const int64_t row = first + j;
-    const int pos = n - count + j;
-    if (row < 0 || row >= limit || pos < 0) continue;
-    const int e = pos / c.page_size;
+  const int64_t j0 = first < 0 ? -first : 0, j1 = first + count < limit ? count : limit - first;
+  for (int64_t x = j0 * pieces + (int64_t)blockIdx.y * 256 + threadIdx.x; x < j1 * pieces; x += (int64_t)gridDim.y * 256) {
+    const int64_t j = x / pieces, row = first + j;
+    const int b = (int)(x - j * pieces) * 16;
+    // (loaded before the sequence's length and page are known: those take two loads in a row)
+    const u32x4 xk = *(const u32x4*)(r.k + row * r.k_stride + b), xv = *(const u32x4*)(r.v + row * r.v_stride + b);
+    const int64_t at_token = (int64_t)clamped_len(c, s) - count + j;
+    if (at_token < 0) continue;
+    const int pos = (int)at_token, e = pos / c.page_size;
     const int page = c.table[(int64_t)s * c.max_pages + e];
     if ((unsigned)page >= (unsigned)c.pages) continue;
     const int64_t at = r.layer * c.layer_bytes + page * c.page_bytes + (int64_t)(pos - e * c.page_size) * c.row_bytes + b;
-    const u32x4 xk = *(const u32x4*)(r.k + row * r.k_stride + b), xv = *(const u32x4*)(r.v + row * r.v_stride + b);
     *(u32x4*)(c.k + at) = xk;
     *(u32x4*)(c.v + at) = xv;
   }

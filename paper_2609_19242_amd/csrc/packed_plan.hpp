@@ -33,7 +33,10 @@ constexpr size_t kMaxPackedPartials = (size_t)256 << 20;
 // Key tiles: 128 keys (16), by the steps of their walks.  The longest walk,
 // the first keys' of the longest sequence, sets the time when there are few;
 // walks longer than the average load of a CU's workgroups are cut into chunks of
-// that load as in split_plan.hpp, whose reasons and limits hold here too.
+// that load as in split_plan.hpp, whose reasons and limits hold here too (fp32:
+// the whole load, not a quarter of it: 5 texts of 33 to 407 rows, 8/2 heads, d 64
+// 46 -> 43 us, of which the sums 10 -> 5; bf16, 8K of documents: 0.5, 0.75, 1 and
+// 1.5 loads 263, 252, 245 and 261 us).
 inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_packed_seq* seqs) {
   PackedPlanItems out;
   const bool f32 = p.dtype == BDLM_F32;
@@ -84,7 +87,7 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
   // Chunks of the key tiles' walks.
   const int64_t longest = k.empty() ? 0 : k[0].cost;
   const int64_t average = total / (f32 ? kCus : kCus * dkdv_wgs_per_cu(p.head_dim, 0, group));
-  int64_t unit = f32 ? std::max<int64_t>(kMinUnitF32, average / 4) : std::max<int64_t>(kMinUnitBf16, average);
+  int64_t unit = std::max<int64_t>(f32 ? kMinUnitF32 : kMinUnitBf16, average);
   if (!f32 && average < kMinUnitBf16) {  // a nearly idle card: as split_plan
     const int64_t u = std::max<int64_t>(kMinUnitBf16Idle, average);
     int64_t wgs = 0;

@@ -110,27 +110,27 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
     col_product<D>(acc, vx, p);
   }
 
-  // Merge the waves, as fwd_f32.hip.
+  // Merge the waves, as fwd_f32.hip; each wave also scales its own row sums.
   l = col_sum(l);
-  if (g == 0) {
-    red_m[w][i] = m;
-    red_l[w][i] = l;
-  }
+  if (g == 0) red_m[w][i] = m;
   __syncthreads();
   double mt = red_m[0][i];
 #pragma unroll
   for (int k = 1; k < kWaves; ++k) mt = fmax(mt, red_m[k][i]);
-  acc.scale(m == -INFINITY ? 0.0 : exp2_f64(m - mt));
+  const double al = m == -INFINITY ? 0.0 : exp2_f64(m - mt);
+  if (g == 0) red_l[w][i] = l * al;
+  acc.scale(al);
   acc_to_lds<D>(acc, lds + w * 16 * kRedRow<D>, i, g);
   __syncthreads();
   // four elements of a row per thread
   const int q = tid / (D / 4), d0 = (tid % (D / 4)) * 4;
   if (q >= it.nrows) return;
-  double M = red_m[0][q], lt = 0.0;
+  double M = red_m[0][q], lt = red_l[0][q];
 #pragma unroll
-  for (int k = 1; k < kWaves; ++k) M = fmax(M, red_m[k][q]);
-#pragma unroll
-  for (int k = 0; k < kWaves; ++k) lt += red_m[k][q] == -INFINITY ? 0.0 : red_l[k][q] * exp2_f64(red_m[k][q] - M);
+  for (int k = 1; k < kWaves; ++k) {
+    M = fmax(M, red_m[k][q]);
+    lt += red_l[k][q];
+  }
   const bool empty = !(lt > 0.0);
   const double inv = empty ? 0.0 : 1.0 / lt;
   const PrefixRow pr = prefix_row(a, it.kvh, it.row0 + q);
