@@ -351,7 +351,9 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
  * A paged cache of keys and values, and its pages' bookkeeping, all in device
  * memory owned by the caller.  Sequence s holds lens[s] tokens; token t is row
  * t % page_size of page table[s][t / page_size].  refs[p] counts the tables
- * that hold page p (0: free).  A page that is not full belongs to one sequence.
+ * that hold page p (0: free).  A page that is not full belongs to one sequence;
+ * full ones may be shared, and what is written into a shared page, all its
+ * sequences see.
  *
  * The page operations run in stream order and must not overlap in time with
  * each other or with attention over the same cache; they need no host round
@@ -415,9 +417,9 @@ bdlm_status bdlm_cache_write(const bdlm_cache* c, int64_t layer, int64_t n, cons
  * seqs[r], whose keys and values are in the cache, and its `rows` query rows
  * are its last tokens.  Row i sees the keys up to its own position, lens - rows
  * + i, or, with block = 1 (a block that is being denoised), all lens keys.  The
- * first `prefix` tokens are the same pages' in all requests and are read
- * through the first request's table, once for all; the result is that of
- * attention over each request's own tokens.
+ * first `prefix` tokens are the same in all requests; they may be read through
+ * the first request's table, once for all, which therefore has to hold them
+ * all.  The result is that of attention over each request's own tokens.
  *   q, o : [requests][rows][heads][head_dim] in the cache's dtype
  *   lse  : [requests][heads][rows] fp32, natural log
  * Rows that see nothing (also: of a sequence number out of range) get O = 0

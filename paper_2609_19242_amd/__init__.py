@@ -176,6 +176,8 @@ def _torch_stream(stream, device) -> torch.cuda.Stream:
 def _launch(device, stream, call, *args):
     """``call(*args, handle)``, with the handle of ``stream`` (default: the current stream of GPU ``device``) and with
     that GPU current meanwhile; raises if it fails."""
+    if device < 0:
+        raise ValueError("the tensors must be on a GPU")
     if device != _current_gpu():
         with torch.cuda.device(device):
             return _launch(device, stream, call, *args)

@@ -10,7 +10,7 @@ from typing import Optional
 
 import torch
 
-from . import _dtype_code, _expect, _launch, _on_device, lib
+from . import _dtype_code, _expect, _launch, lib
 from .packed import _Rows, _rows, _workspace
 
 __all__ = ["Cache", "cache_new", "cache_grow", "cache_write", "cache_fork", "cache_free", "cache_compact",
@@ -66,7 +66,9 @@ class Cache:
         _expect("lens", lens, torch.int32, (seqs,))
         _expect("refs", refs, torch.int32, (pages,))
         _expect("status", status, torch.int32, (2,))
-        _on_device(k.device, k=k, v=v, table=table, lens=lens, refs=refs, status=status)
+        for name, t in (("v", v), ("table", table), ("lens", lens), ("refs", refs), ("status", status)):
+            if t.device != k.device:
+                raise ValueError(f"{name} must be on {k.device}, got {t.device}")
         self.k, self.v, self.table, self.lens, self.refs, self.status = k, v, table, lens, refs, status
         self.layers, self.pages, self.page_size, self.kv_heads, self.head_dim = k.shape
         self.seqs, self.max_pages = seqs, max_pages
@@ -180,7 +182,8 @@ def prefix_attn(q, cache: Cache, layer: int, seqs, prefix: int = 0, block: bool 
                 out: Optional[tuple] = None, workspace: Optional[torch.Tensor] = None, stream=None):
     """Attention of the last ``rows`` tokens of the sequences ``seqs`` (int32 ``[requests]``) over their keys in the
     cache: q ``[requests][rows][heads][head_dim]``, causal, or, with ``block``, every row sees all of its sequence.
-    The first ``prefix`` tokens, which all requests share, are read once for all of them, through the first one's table.
+    The first ``prefix`` tokens, the same in all requests, may be read once for all of them, through the table of the
+    first one, which has to hold them all.
     Returns ``(o, lse)`` with ``lse [requests][heads][rows]`` fp32, or writes into ``out``.  ``workspace``: a device
     tensor of :func:`prefix_attn_workspace_bytes` (calls that may overlap in time need one each); allocated if not
     given."""
@@ -196,7 +199,8 @@ def prefix_attn(q, cache: Cache, layer: int, seqs, prefix: int = 0, block: bool 
         o, lse = out
         _expect("o", o, c.dtype, q.shape)
         _expect("lse", lse, torch.float32, (R, H, n))
-        _on_device(c.device, o=o, lse=lse)
+        if o.get_device() != c.gpu or lse.get_device() != c.gpu:
+            raise ValueError(f"o and lse must be on {c.device}")
     if workspace is None:
         nbytes = lib().bdlm_prefix_attn_workspace_bytes(c._ref, R, n, H, prefix)
         workspace = _workspace(None, nbytes, c.device, stream)

@@ -15,6 +15,8 @@ namespace {
 
 constexpr int64_t kMaxSeqs = (int64_t)1 << 19;  // a bit each in the bookkeeping's LDS
 constexpr int64_t kMaxPages = ((int64_t)1 << 30) - 1;
+constexpr int64_t kMaxRows = (int64_t)1 << 25;  // query rows x heads of one attention call (a grid dimension of the merge)
+constexpr int64_t kMaxWgs = (int64_t)1 << 22;
 constexpr int kMaxKeyChunks = 1 << 20;  // chunks of keys of one attention call
 
 bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
@@ -122,8 +124,8 @@ bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int
   a.prefix_tiles = (int32_t)pt;
   a.own_tiles = (int32_t)ot;
   const int64_t parts = a.prefix_chunks + oc, pi = c->kv_heads * pt * a.prefix_chunks, oi = base * oc;
-  if (pi + oi >= (int64_t)1 << 31 || parts > kMaxKeyChunks)
-    return fail(BDLM_ERR_UNSUPPORTED, "attention over the cache needs %lld workgroups and %lld chunks (limits 2^31, %d)",
+  if (pi + oi > kMaxWgs || parts > kMaxKeyChunks)
+    return fail(BDLM_ERR_UNSUPPORTED, "attention over the cache needs %lld workgroups and %lld chunks (limits 2^22, %d)",
                 (long long)(pi + oi), (long long)parts, kMaxKeyChunks);
   a.prefix_items = (int32_t)pi;
   a.own_items = (int32_t)oi;
@@ -134,9 +136,9 @@ bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int
 bdlm_status check_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int32_t heads, int64_t prefix) {
   if (heads < 1 || heads % c->kv_heads != 0)
     return fail(BDLM_ERR_INVALID, "heads (%d) must be a positive multiple of kv_heads (%d)", heads, c->kv_heads);
-  if (requests < 0 || rows < 0 || requests > kMaxPos || rows > kMaxPos ||
-      (requests > 0 && rows > 0 && requests * rows > kMaxPos / heads))
-    return fail(BDLM_ERR_INVALID, "requests %lld x rows %lld x heads %d outside [0, 2^30]", (long long)requests,
+  if (requests < 0 || rows < 0) return fail(BDLM_ERR_INVALID, "requests %lld x rows %lld", (long long)requests, (long long)rows);
+  if (requests > kMaxRows || rows > kMaxRows || (requests > 0 && rows > 0 && requests * rows > kMaxRows / heads))
+    return fail(BDLM_ERR_UNSUPPORTED, "requests %lld x rows %lld x heads %d exceeds 2^25", (long long)requests,
                 (long long)rows, heads);
   if (prefix < 0 || prefix > c->max_pages * c->page_size)
     return fail(BDLM_ERR_INVALID, "prefix %lld outside [0, %lld], what a table holds", (long long)prefix,

@@ -122,10 +122,13 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
   int64_t q_rows = 0, k_rows = 0;
   if ((st = check_seqs(n_seqs, seqs, q_rows, k_rows)) != BDLM_OK) return st;
   const PackedPlanItems it = packed_items(*p, n_seqs, seqs);
-  const int64_t q_wgs = (int64_t)it.q.size() * p->heads, k_wgs = (int64_t)it.k.size() * p->kv_heads;
-  if (std::max(q_wgs, k_wgs) >= ((int64_t)1 << 31) - 8 || (int64_t)it.sums.size() * p->kv_heads >= (int64_t)1 << 24)
-    return fail(BDLM_ERR_UNSUPPORTED, "packed problem needs %lld workgroups (limit 2^31)",
-                (long long)std::max(q_wgs, k_wgs));
+  // (a grid dimension holds fewer than 2^32 threads; the fp32 kernels' grids have two)
+  const bool f32 = p->dtype == BDLM_F32;
+  const int64_t q_wgs = (int64_t)it.q.size() * (p->heads / (f32 ? 1 : packed_tile_heads(p->heads / p->kv_heads)));
+  const int64_t wgs = std::max(q_wgs, (int64_t)it.k.size() * p->kv_heads), most = f32 ? (int64_t)1 << 30 : 1 << 22;
+  if (wgs > most || (int64_t)it.sums.size() * p->kv_heads > 1 << 18)
+    return fail(BDLM_ERR_UNSUPPORTED, "packed problem needs %lld workgroups (limit %lld)", (long long)wgs,
+                (long long)most);
   bdlm_packed_plan pl{};
   pl.problem = *p;
   pl.q_rows = q_rows;
@@ -138,8 +141,8 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
   const size_t qb = it.q.size() * sizeof(PackedItem), kb = it.k.size() * sizeof(PackedItem);
   pl.bytes = qb + kb + it.sums.size() * sizeof(PackedSum);
   pl.workspace_bytes = 2 * packed_stats_bytes(pl) + (size_t)it.slots * p->kv_heads *
-                                                        (p->dtype == BDLM_F32 ? kRowsF32 * sizeof(double)
-                                                                              : kBwdKeysBf16 * sizeof(float)) *
+                                                        (f32 ? kRowsF32 * sizeof(double)
+                                                             : kBwdKeysBf16 * sizeof(float)) *
                                                         2 * p->head_dim;
   if (items) {
     if (items_bytes < pl.bytes)

@@ -7,6 +7,7 @@ forward (:func:`packed_fwd`) and backward (:func:`packed_bwd`).  The rules and l
 from __future__ import annotations
 
 import ctypes
+import operator
 from typing import Optional, Sequence
 
 import torch
@@ -71,7 +72,7 @@ def _ints(name, xs, n=None):
         if xs.is_cuda or xs.dim() != 1 or xs.dtype not in (torch.int32, torch.int64):
             raise ValueError(f"{name} must be a one-dimensional integer tensor on the CPU, or a sequence of ints")
         xs = xs.tolist()
-    xs = [int(x) for x in xs]
+    xs = [operator.index(x) for x in xs]
     if n is not None and len(xs) != n:
         raise ValueError(f"{name} has {len(xs)} entries for {n} sequences")
     return xs
@@ -136,8 +137,6 @@ def _rows(like, name, t, heads, at_least):
 def _check_plan(plan):
     if not isinstance(plan, PackedPlan):
         raise TypeError(f"plan must be a PackedPlan, got {type(plan).__name__}")
-    if plan.gpu < 0:
-        raise ValueError(f"the plan's items are on {plan.device}, not on a GPU")
 
 
 def _like(t, rows, heads, D):

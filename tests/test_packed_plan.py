@@ -1,0 +1,103 @@
+"""The plan of packed calls: every tile of query rows once, every step of every key tile's walk once, partial sums in
+places of their own and added up, heaviest items first.  CPU only."""
+import random
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_19242_amd as bd
+
+BIG = 0x3fffffff
+
+
+def items(p):
+    r = p._record
+    a = np.frombuffer(p._items.numpy().tobytes(), dtype=np.int32)[:8 * (r.q_items + r.k_items + r.n_sums)].reshape(-1, 8)
+    return a[:r.q_items], a[r.q_items:r.q_items + r.k_items], a[r.q_items + r.k_items:]
+
+
+def steps_of(ql, kl, first, last, block, window, rows, per_block):
+    """Steps of the walk of keys [first, last]: blocks of `rows` query rows from the first that sees one of them to the last."""
+    seen = []
+    for i in range(ql):
+        x = kl - ql + i
+        e = (x // block + 1) * block
+        lo = e - window if window else 0
+        if x >= 0 and first < e and lo <= last:
+            seen.append(i)
+    return (seen[-1] // rows - seen[0] // rows + 1) * per_block if seen else 0
+
+
+def walked(ql, kl, a, b, block, window):
+    """Keys that rows [a, b) see, from the first to the last."""
+    lo, hi = kl, 0
+    for i in range(a, b):
+        x = kl - ql + i
+        if x < 0:
+            continue
+        e = (x // block + 1) * block
+        lo, hi = min(lo, max(0, e - window) if window else 0), max(hi, min(e, kl))
+    return max(0, hi - lo)
+
+
+def check(ql, kl, H, KV, D, dtype, block, window):
+    p = bd.packed_plan(ql, kl, heads=H, kv_heads=KV, head_dim=D, dtype=dtype, block_size=block, window=window, device="cpu")
+    q, k, sums = items(p)
+    f32, group = dtype == torch.float32, H // KV
+    heads = 1 if f32 else 4 if group % 4 == 0 else 2 if group % 2 == 0 else 1
+    qt, kt = (16, 16) if f32 else (128 // heads, 128)
+    rows = 16 if f32 else 64 if group % 2 else 32
+    per_block = group if f32 or group % 2 else group // 2
+    q0 = np.cumsum([0] + list(ql))
+    k0 = np.cumsum([0] + list(kl))
+    want = [(q0[i], n, k0[i], kl[i], t) for i, n in enumerate(ql) for t in range(-(-n // qt))]
+    assert sorted(map(tuple, q[:, :5].tolist())) == sorted(want)
+    cost = [walked(n, m, t * qt, min(n, (t + 1) * qt), block, window) for _, n, _, m, t in q[:, :5].tolist()]
+    assert all(a >= b for a, b in zip(cost, cost[1:]))
+    chunks = {}
+    for a in k.tolist():
+        chunks.setdefault(tuple(a[:5]), []).append(a[5:])
+    assert sorted(chunks) == sorted((q0[i], ql[i], k0[i], m, t) for i, m in enumerate(kl) for t in range(-(-m // kt)))
+    slots, longest = [], []
+    for (_, n, kk, m, t), parts in chunks.items():
+        parts.sort()
+        total = steps_of(n, m, t * kt, min(m, (t + 1) * kt) - 1, block, window, rows, per_block)
+        assert parts[0][0] == 0 and parts[-1][1] == BIG and all(a[1] == b[0] for a, b in zip(parts, parts[1:]))
+        assert parts[-1][0] < total or total == 0 == parts[-1][0]
+        if len(parts) == 1:
+            assert parts[0][2] == -1
+        else:
+            mine = [a[2] for a in parts]
+            assert mine == list(range(mine[0], mine[0] + len(mine)))
+            assert [kk, m, t, mine[0], len(mine)] in sums[:, :5].tolist()
+            slots += mine
+        longest += [b - a for a, b, _ in parts[:-1]]
+    assert sorted(slots) == list(range(p._record.slots)) and len(sums) == sum(len(x) > 1 for x in chunks.values())
+    assert not longest or len(set(longest)) == 1
+    return p
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("H,KV", [(4, 4), (4, 2), (8, 2), (6, 2), (3, 1)])
+def test_items_cover_the_work_once(H, KV, dtype):
+    rng = random.Random(7 * H + KV)
+    for _ in range(12):
+        n = rng.randint(1, 5)
+        ql = [rng.choice([0, 1, rng.randint(1, 400)]) for _ in range(n)]
+        kl = [max(0, x + rng.choice([0, 0, rng.randint(-50, 300)])) for x in ql]
+        check(ql, kl, H, KV, rng.choice([64, 128]), dtype, rng.choice([1, 1, 7, 32, 300]), rng.choice([0, 0, 1, 30, 200]))
+
+
+def test_long_walks_are_cut():
+    p = check([900, 40], [900, 40], 4, 1, 128, torch.bfloat16, 1, 0)
+    assert p._record.n_sums > 0 and p.workspace_bytes > 4 * 2 * 940 * 4
+
+
+def test_a_full_card_is_not_cut():
+    p = check([130] * 160, [130] * 160, 8, 8, 128, torch.bfloat16, 1, 0)
+    assert p._record.n_sums == 0 and p._record.teams == 1
+
+
+def test_few_tiles_take_two_teams():
+    assert check([64], [64], 4, 2, 128, torch.bfloat16, 1, 0)._record.teams == 2
