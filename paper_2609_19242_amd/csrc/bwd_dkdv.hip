@@ -189,7 +189,7 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const Args args) {
   const int64_t H = a.heads, HKV = a.kv_heads;
   const int64_t RS = w < 2 ? q_stride<D>(a) : do_stride<D>(a);  // of the tensor this wave copies
   const int b = it.b, kvh = it.kvh, r = it.r, t = it.t;
-  const KRangeArg& kr = a.kr[r];
+  const KRangeArg& kr = k_range(a, r);
   const int key0 = t * BN;
   const int nk = imin(BN, kr.len - key0);
   const bool ragged = nk < BN;
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(256) void dkdv_kernel(const Args args) {
   auto make_span = [&](int q) __attribute__((always_inline)) -> Span {
     Span sp{0, 0, 0, 0, 0, 0, 0, 0, nullptr, nullptr, 0u};
     if (q >= a.n_q) return sp;
-    const QRangeArg& qr = a.qr[q];
+    const QRangeArg& qr = q_range(a, q);
     sp.pos0 = qr.pos0;
     sp.len = qr.len;
     const int h0 = kvh * a.group;

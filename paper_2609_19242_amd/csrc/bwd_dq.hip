@@ -44,7 +44,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   QTileItem it;
   if (!q_tile_item<HP>(args, blockIdx.x, it)) return;
   auto&& a = call_view(args, it.item, 2);
-  const QRangeArg& qr = a.qr[it.r];
+  const QRangeArg& qr = q_range(a, it.r);
   const int kvh = it.h / a.group;
   const int h = HP == 1 ? it.h : it.h + w % HP, wrow = w / HP * 32;  // this wave's head and rows of the tile
   const int row0 = it.t * BM;
@@ -154,7 +154,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   seen_keys(a, pq0, pq1, u0, u1);
   auto copy_seek = [&](CopyCur cc) -> CopyCur {
     if (cc.c.have) {
-      const KRangeArg& kr = a.kr[cc.c.j];
+      const KRangeArg& kr = k_range(a, cc.c.j);
       cc.src = (const bf16*)(kwave ? kr.k : kr.v) +
                row_elem<D>(a, it.b, kr.bstride, (int64_t)cc.c.t * BN, HKV, kvh, CS);
       cc.rows_left = (kPacked ? u1 : kr.len) - cc.c.t * BN;
@@ -238,7 +238,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     // tile's keys skips it (it still copies and meets the barrier).
     bool skip = false;
     if (!(t >= f0 && t < f1)) {
-      const int kstart = a.kr[j].pos0 + t * BN - lane_lo;
+      const int kstart = k_range(a, j).pos0 + t * BN - lane_lo;
       skip = __builtin_amdgcn_ballot_w64(lane_w > 0 && kstart < lane_w && kstart + BN > 0) == 0;
     }
     if (!skip) {
@@ -280,7 +280,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       }
 
       if (!(t >= f0 && t < f1)) {
-        const int base = a.kr[j].pos0 + t * BN + 4 * half - lane_lo;
+        const int base = k_range(a, j).pos0 + t * BN + 4 * half - lane_lo;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
@@ -293,7 +293,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         // the rounded O misses it by up to 2^-9 |dO||O|, which is much of dS where
         // a row has few keys (one key: all of it).  (D lies in dpacc already.)
         if constexpr (kPacked) {
-          const int kstart = a.kr[j].pos0 + t * BN - lane_lo;
+          const int kstart = k_range(a, j).pos0 + t * BN - lane_lo;
           float rest = 0.f, z = lse2;
           asm volatile("" : "+v"(z));  // (or the compiler keeps these exponentials for the ones below, and spills)
 #pragma unroll

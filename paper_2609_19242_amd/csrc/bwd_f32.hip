@@ -46,7 +46,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   QTileItem it;
   if (!q_tile_item(args, workgroup_id(), it)) return;
   auto&& a = call_view(args, it.item, 4);
-  const QRangeArg& qr = a.qr[it.r];
+  const QRangeArg& qr = q_range(a, it.r);
   const int kvh = it.h / a.group;
   const int64_t H = a.heads, HKV = a.kv_heads;
   const int row0 = it.t * 16, nvalid = imin(16, qr.len - row0);
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   };
   t = t1 = -kWaves;
   while (advance()) {
-    const KRangeArg& kr = a.kr[j];
+    const KRangeArg& kr = k_range(a, j);
     const int krows = imin(16, kr.len - t * 16);
     auto tile_of = [&](const void* base, int64_t stride) __attribute__((always_inline)) {
       return row_tile<D>(base, row_elem<D>(a, it.b, kr.bstride, t * 16, HKV, kvh, stride), krows, stride);
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   KeyTileItem it;
   if (!key_tile_item(args, workgroup_id(), it)) return;
   auto&& a = call_view(args, it.item, 4);
-  const KRangeArg& kr = a.kr[it.r];
+  const KRangeArg& kr = k_range(a, it.r);
   const int64_t H = a.heads, HKV = a.kv_heads;
   const int row0 = it.t * 16, nvalid = imin(16, kr.len - row0);
   const int ki = imin(i, nvalid - 1), pk = kr.pos0 + row0 + ki;
@@ -181,7 +181,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   auto span = [&](int q) __attribute__((always_inline)) -> Span {
     Span s{0, 0, 0, 0};
     if (q >= a.n_q) return s;
-    const QRangeArg& qr = a.qr[q];
+    const QRangeArg& qr = q_range(a, q);
     int lo0, hi0, lo1, hi1;
     query_interval(qr.stream, kr.stream, kp0, rule_of(a), lo0, hi0);
     query_interval(qr.stream, kr.stream, kp1, rule_of(a), lo1, hi1);
@@ -236,7 +236,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
       t = sp.t0 + m / a.group;
       hq = m % a.group;
     }
-    const QRangeArg& qr = a.qr[q];
+    const QRangeArg& qr = q_range(a, q);
     const int h = it.kvh * a.group + hq;
     int qlo, qhi;  // the queries of the range that see this lane's key
     query_interval(qr.stream, kr.stream, pk, rule_of(a), qlo, qhi);

@@ -73,7 +73,7 @@ __global__ __launch_bounds__(NT * NW * 64)
   QTileItem it;
   if (!q_tile_item<HP>(args, blockIdx.x, it)) return;
   auto&& a = call_view(args, it.item, 2);
-  const QRangeArg& qr = a.qr[it.r];
+  const QRangeArg& qr = q_range(a, it.r);
   const int kvh = it.h / a.group;
   const int h = HP == 1 ? it.h : it.h + w % HP, wrow = w / HP * 32;  // this wave's head and rows of the tile
   const int row0 = it.t * BM;
@@ -134,7 +134,7 @@ __global__ __launch_bounds__(NT * NW * 64)
   seen_keys(a, pq0, pq1, u0, u1);
   auto copy_seek = [&](CopyCur cc) -> CopyCur {
     if (cc.c.have) {
-      const KRangeArg& kr = a.kr[cc.c.j];
+      const KRangeArg& kr = k_range(a, cc.c.j);
       cc.src = (const bf16*)(kwave ? kr.k : kr.v) +
                row_elem<D>(a, it.b, kr.bstride, (int64_t)cc.c.t * BN, HKV, kvh, CS);
       cc.rows_left = (kIsPacked<Args> ? u1 : kr.len) - cc.c.t * BN;
@@ -218,7 +218,7 @@ __global__ __launch_bounds__(NT * NW * 64)
     // tile's keys skips it (it still copies and meets the barrier).
     bool skip = NT > 1 && !c0.have;
     if (!skip && !(t >= f0 && t < f1)) {
-      const int kstart = a.kr[j].pos0 + t * BN - lane_lo;
+      const int kstart = k_range(a, j).pos0 + t * BN - lane_lo;
       skip = __builtin_amdgcn_ballot_w64(lane_w > 0 && kstart < lane_w && kstart + BN > 0) == 0;
     }
     if (!skip) {
@@ -255,7 +255,7 @@ __global__ __launch_bounds__(NT * NW * 64)
       }
 
       if (!(t >= f0 && t < f1)) {
-        const int base = a.kr[j].pos0 + t * BN + 4 * half - lane_lo;
+        const int base = k_range(a, j).pos0 + t * BN + 4 * half - lane_lo;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll

@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   QTileItem it;
   if (!q_tile_item(args, workgroup_id(), it)) return;
   auto&& a = call_view(args, it.item, 4);
-  const QRangeArg& qr = a.qr[it.r];
+  const QRangeArg& qr = q_range(a, it.r);
   const int kvh = it.h / a.group;
   const int64_t H = a.heads, HKV = a.kv_heads;
   const int row0 = it.t * 16, nvalid = imin(16, qr.len - row0);
@@ -75,15 +75,15 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
     return true;
   };
   auto tile_of = [&](const void* base, int64_t stride) __attribute__((always_inline)) {
-    const KRangeArg& kr = a.kr[j];
+    const KRangeArg& kr = k_range(a, j);
     return row_tile<D>(base, row_elem<D>(a, it.b, kr.bstride, t * 16, HKV, kvh, stride), imin(16, kr.len - t * 16),
                        stride);
   };
   t = t1 = -kWaves;  // the first call starts with range 0
   bool have = advance();
-  if (have) load_rows<D>(kx, tile_of(a.kr[j].k, k_stride<D>(a)), i, g);
+  if (have) load_rows<D>(kx, tile_of(k_range(a, j).k, k_stride<D>(a)), i, g);
   while (have) {
-    const KRangeArg& kr = a.kr[j];
+    const KRangeArg& kr = k_range(a, j);
     const int tt = t;
     const bool full = tt >= f0 && tt < f1;
     const RowTile vt = tile_of(kr.v, v_stride<D>(a));
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
     f64x4 s = row_product<D>(kx, lds, lane) * c;
     // the next tile's K loads run under the softmax and the products below
     have = advance();
-    if (have) load_rows<D>(kx, tile_of(a.kr[j].k, k_stride<D>(a)), i, g);
+    if (have) load_rows<D>(kx, tile_of(k_range(a, j).k, k_stride<D>(a)), i, g);
 
     bool grow = false;
 #pragma unroll

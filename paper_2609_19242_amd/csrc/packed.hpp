@@ -142,6 +142,13 @@ __device__ __forceinline__ int64_t row_elem(const PackedView&, int, int64_t, int
   return row * stride + h * D;
 }
 
+// Query and key ranges by number; a packed sequence has one of each (indexed by
+// a variable, its copy would live in scratch memory).
+__device__ __forceinline__ const QRangeArg& q_range(const AttnArgs& a, int i) { return a.qr[i]; }
+__device__ __forceinline__ const KRangeArg& k_range(const AttnArgs& a, int j) { return a.kr[j]; }
+__device__ __forceinline__ const QRangeArg& q_range(const PackedView& a, int) { return a.qr[0]; }
+__device__ __forceinline__ const KRangeArg& k_range(const PackedView& a, int) { return a.kr[0]; }
+
 // What a kernel reads its call through: the arguments themselves, or the sequence of a packed item.
 __device__ __forceinline__ const AttnArgs& call_view(const AttnArgs& a, int, int) { return a; }
 __device__ __forceinline__ PackedView call_view(const PackedArgs& a, int item, int elem) {

@@ -63,7 +63,7 @@ __device__ inline bool q_tile_item(const PackedArgs& a, int wg, QTileItem& it) {
 template <class A>
 __device__ inline void key_tile_span(const A& a, int j, int qs, int pq0, int pq1, int BN,
                                      int& t0, int& t1, int& f0, int& f1) {
-  const KRangeArg& kr = a.kr[j];
+  const KRangeArg& kr = k_range(a, j);
   int lo0, hi0, lo1, hi1;
   key_interval(qs, pq0, kr.stream, rule_of(a), lo0, hi0);
   key_interval(qs, pq1, kr.stream, rule_of(a), lo1, hi1);
@@ -130,7 +130,7 @@ __device__ inline int count_key_tiles(const A& a, int qs, int pq0, int pq1, int 
 // This lane's visible key interval [lo, lo + w) inside key range j (w may be 0).
 template <class A>
 __device__ inline void lane_key_interval(const A& a, int j, int qs, int pq, int& lo, int& w) {
-  const KRangeArg& kr = a.kr[j];
+  const KRangeArg& kr = k_range(a, j);
   int l, h;
   key_interval(qs, pq, kr.stream, rule_of(a), l, h);
   l = imax(l, kr.pos0);
