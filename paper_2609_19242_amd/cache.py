@@ -192,7 +192,7 @@ def prefix_attn(q, cache: Cache, layer: int, seqs, prefix: int = 0, block: bool 
     a = _list(c, "seqs", seqs, R)
     if out is None:
         o = torch.empty_like(q)
-        lse = torch.empty((R, H, n), dtype=torch.float32, device=q.device)
+        lse = q.new_empty((R, H, n), dtype=torch.float32)
     else:
         if len(out) != 2:
             raise ValueError("out must be (o, lse)")

@@ -139,10 +139,6 @@ def _check_plan(plan):
         raise TypeError(f"plan must be a PackedPlan, got {type(plan).__name__}")
 
 
-def _like(t, rows, heads, D):
-    return torch.empty((rows, heads, D), dtype=t.dtype, device=t.device)
-
-
 def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, stream=None):
     """Attention of the plan's sequences: q ``[rows][heads][D]``, k and v ``[rows][kv_heads][D]`` (rows may lie apart,
     as in a fused projection).  Returns ``(o, lse)`` with ``lse [heads][rows]`` fp32, or writes into ``out``; rows of
@@ -153,7 +149,7 @@ def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, stream=No
                   _rows(plan, "v", v, KV, plan.k_rows))
     n = q.shape[0]
     if out is None:
-        o, lse = _like(q, n, H, plan.head_dim), torch.empty((H, n), dtype=torch.float32, device=q.device)
+        o, lse = q.new_empty((n, H, plan.head_dim)), q.new_empty((H, n), dtype=torch.float32)
         ro = _Rows(o.data_ptr(), H * plan.head_dim)
     else:
         if len(out) != 2:
@@ -177,12 +173,13 @@ def packed_bwd(plan: PackedPlan, q, k, v, o, lse, do, out: Optional[tuple] = Non
     ro, rdo = _as_long(plan, "o", o, H, n), _as_long(plan, "do", do, H, n)
     _lse(plan, lse, n)
     if out is None:
-        dq, dk, dv = _like(q, n, H, D), _like(k, nk, KV, D), _like(v, nv, KV, D)
+        dq, dk, dv = q.new_empty((n, H, D)), k.new_empty((nk, KV, D)), v.new_empty((nv, KV, D))
+        outs = _Rows(dq.data_ptr(), H * D), _Rows(dk.data_ptr(), KV * D), _Rows(dv.data_ptr(), KV * D)
     else:
         if len(out) != 3:
             raise ValueError("out must be (dq, dk, dv)")
         dq, dk, dv = out
-    outs = [_as_long(plan, "dq", dq, H, n), _as_long(plan, "dk", dk, KV, nk), _as_long(plan, "dv", dv, KV, nv)]
+        outs = _as_long(plan, "dq", dq, H, n), _as_long(plan, "dk", dk, KV, nk), _as_long(plan, "dv", dv, KV, nv)
     workspace = _workspace(workspace, plan.workspace_bytes, plan.device, stream)
     _launch(plan.gpu, stream, lib().bdlm_packed_bwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n, rdo,
             *outs, workspace.data_ptr(), workspace.numel() * workspace.element_size())
