@@ -76,14 +76,18 @@ bdlm_status done(hipError_t e, const char* what) { return e == hipSuccess ? BDLM
 // How the keys of an attention call are cut into chunks and its rows into tiles.
 //
 // Chunks trade balance against partial sums, whose cost grows with the query
-// rows (all heads of all requests), so few rows take shorter chunks.
+// rows (all heads of all requests), so few rows take shorter chunks.  Times below
+// with keys that no cache holds yet, 32 heads on 8 KV heads, where not said otherwise.
 // The prefix: long enough that its tiles of rows give every workgroup slot one
-// item, at least half a key per query row within [256, 1024] (2,048 rows, 8K
-// tokens, 8 KV heads: chunks of 2,048 keys 56 us, 1,024 44, 512 54; 16,384 rows, 16K
-// tokens, 4 KV heads, one item per slot: 4,096 keys 173 us, 2,048 185, 8,192 197).
+// item, at least half a key per query row within [512, 1024] (one request, 16,000
+// tokens: chunks of 256 keys 25 us, 512 23, 1,024 29; 64 requests, 8,192 tokens, read
+// again: 2,048 keys 56 us, 1,024 44, 512 54; 16,384 rows, 16K tokens, 4 KV heads, one
+// item per slot: 4,096 keys 173 us, 2,048 185, 8,192 197).
 // A request's own keys: as many keys per query row, at least kOwnPerBase per
-// (KV head, request, tile), within [256, 1536] (512 of those, up to 1,500 keys:
-// chunks of 384 51 us, 768 46, whole 44), their number limited by the workgroups
+// (KV head, request, tile), within [512, 1536] (one request of 32,000 keys: chunks of
+// 256 43 us, 512 35, 768 39; 8 of 300 to 6,000: 33, 28, 30; 16 of 100 to 2,000 take
+// 384 sooner, 22 us, than 512, 24; 512 of up to 1,500 keys, read again: chunks of
+// 384 51 us, 768 46, whole 44), their number limited by the workgroups
 // that find nothing to do where a sequence is shorter than its table
 // (kMaxOwnItems).  Tables of up to kOwnWhole keys: one chunk, which needs no sums.
 // A prefix that would save less than kFoldBytes of reading is not kept apart:
@@ -110,12 +114,12 @@ bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int
   auto within = [](int64_t x, int64_t lo, int64_t hi) { return std::min(std::max(x, lo), hi); };
   const int64_t base = c->kv_heads * requests * ot;
   const int64_t row_min = requests * rows * heads / 2;
-  const int64_t pc = std::min(std::max(up64(within(row_min, 256, 1024)),
+  const int64_t pc = std::min(std::max(up64(within(row_min, 512, 1024)),
                                        up64(c->kv_heads * pt * prefix / kSlots)),
                               std::min(limit, up64(prefix + 1)));
   a.prefix_chunk = (int32_t)pc;
   a.prefix_chunks = (int32_t)((prefix + pc - 1) / pc);
-  const int64_t own_min = own <= kOwnWhole ? kOwnWhole : within(std::max(kOwnPerBase * base, row_min), 256, 1536);
+  const int64_t own_min = own <= kOwnWhole ? kOwnWhole : within(std::max(kOwnPerBase * base, row_min), 512, 1536);
   int64_t oc = std::min((own + own_min - 1) / own_min, std::max<int64_t>(kMaxOwnItems / base, 1));
   oc = std::max(oc, (own + limit - 65) / (limit - 64));
   if (oc == 0 && a.prefix_chunks == 0) oc = 1;
