@@ -84,14 +84,23 @@ bdlm_status done(hipError_t e, const char* what) { return e == hipSuccess ? BDLM
 // again: 2,048 keys 56 us, 1,024 44, 512 54; 16,384 rows, 16K tokens, 4 KV heads, one
 // item per slot: 4,096 keys 173 us, 2,048 185, 8,192 197).
 // A request's own keys: as many keys per query row, at least kOwnPerBase per
-// (KV head, request, tile), within [512, 1536] (one request of 32,000 keys: chunks of
+// (KV head, request, tile), within [512, 1024] (one request of 32,000 keys: chunks of
 // 256 43 us, 512 35, 768 39; 8 of 300 to 6,000: 33, 28, 30; 16 of 100 to 2,000 take
-// 384 sooner, 22 us, than 512, 24; 512 of up to 1,500 keys, read again: chunks of
-// 384 51 us, 768 46, whole 44), their number limited by the workgroups
+// 384 sooner, 22 us, than 512, 24; 16 of 32 rows and up to 2,000 keys, 32/4 heads:
+// 1,024 39 us, 1,536 47; 64 of 4,000 keys: 196, 193), their number limited by the workgroups
 // that find nothing to do where a sequence is shorter than its table
 // (kMaxOwnItems).  Tables of up to kOwnWhole keys: one chunk, which needs no sums.
 // A prefix that would save less than kFoldBytes of reading is not kept apart:
 // the requests' own keys then start at 0, and short ones need no partial sums.
+// Nor is one whose requests fill tiles of rows by themselves, since each tile
+// reads the prefix anyway, if it is at least half of what a table holds and the
+// tiles leave slots free: every sequence is cut into the same number of equal
+// chunks, so that no short item of a request's own keys runs after the prefix's
+// long ones.  Their number: the least of rounds of items times keys per chunk plus
+// the partial sums (at 128 rows and head_dim 128, three quarters of a key's time
+// per item).  4 requests of 64 rows, 32/8 heads, behind 16K tokens, with up to
+// 4,000 more: 111 -> 101 us; 20 of 32 rows behind 9,000 with 2,000: 145 -> 135;
+// 10 of 24 behind 5,000 with 1,000: 51 -> 51.
 constexpr int64_t kSlots = 2 * kCus, kOwnPerBase = 3, kOwnWhole = 512, kMaxOwnItems = 4096;
 constexpr int64_t kFoldBytes = 8 << 20;
 
@@ -100,27 +109,41 @@ bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int
   const bool f32 = c->dtype == BDLM_F32;
   const int64_t group = heads / c->kv_heads, per = rows * group, all = requests * per;
   const int64_t row_bytes = (int64_t)2 * c->kv_heads * c->head_dim * (f32 ? 4 : 2);
+  const int64_t common = prefix;
   if ((requests - 1) * prefix * row_bytes <= kFoldBytes) prefix = 0;
-  a.prefix = (int32_t)prefix;
   a.prefix_shared = !f32 && all > 2 * kPrefixWaveRows;
   a.own_shared = !f32 && per > 2 * kPrefixWaveRows;
   auto tile = [&](bool shared) { return f32 ? kPrefixRowsF32 : shared ? kPrefixSharedRows : kPrefixWaveRows; };
   const int64_t pt = (all + tile(a.prefix_shared) - 1) / tile(a.prefix_shared);
   const int64_t ot = (per + tile(a.own_shared) - 1) / tile(a.own_shared);
+  const int64_t base = c->kv_heads * requests * ot;
+  const bool full = a.own_shared && requests * ot * 8 <= pt * 9 && base <= kSlots &&
+                    2 * common >= c->max_pages * c->page_size;
+  if (full) prefix = 0;
+  a.prefix = (int32_t)prefix;
   const int64_t own = c->max_pages * c->page_size - prefix;
   // keys whose pages (or groups) a workgroup can hold, with a chunk that starts inside one
   const int64_t limit = !f32 && c->page_size % 16 == 0 ? (kPrefixGroups - 2) * 16 : (kPrefixTableEntries - 2) * c->page_size;
   auto up64 = [](int64_t x) { return (x + 63) / 64 * 64; };
   auto within = [](int64_t x, int64_t lo, int64_t hi) { return std::min(std::max(x, lo), hi); };
-  const int64_t base = c->kv_heads * requests * ot;
   const int64_t row_min = requests * rows * heads / 2;
   const int64_t pc = std::min(std::max(up64(within(row_min, 512, 1024)),
                                        up64(c->kv_heads * pt * prefix / kSlots)),
                               std::min(limit, up64(prefix + 1)));
   a.prefix_chunk = (int32_t)pc;
   a.prefix_chunks = (int32_t)((prefix + pc - 1) / pc);
-  const int64_t own_min = own <= kOwnWhole ? kOwnWhole : within(std::max(kOwnPerBase * base, row_min), 512, 1536);
+  int64_t own_min = own <= kOwnWhole ? kOwnWhole : within(std::max(kOwnPerBase * base, row_min), 512, 1024);
+  int64_t whole = 0;  // chunks of every request where whole sequences are cut up
+  if (full) {
+    int64_t best = INT64_MAX;
+    for (int64_t n = 1; n <= 2 * kSlots / base && (n == 1 || own / n >= 512); ++n) {
+      const int64_t cost = (base * n + kSlots - 1) / kSlots * own / n + n * base * 3 / 4;
+      if (own / n <= limit - 128 && cost < best) best = cost, whole = n;
+    }
+    if (whole > 0) own_min = 512;
+  }
   int64_t oc = std::min((own + own_min - 1) / own_min, std::max<int64_t>(kMaxOwnItems / base, 1));
+  if (whole > 0) oc = whole;
   oc = std::max(oc, (own + limit - 65) / (limit - 64));
   if (oc == 0 && a.prefix_chunks == 0) oc = 1;
   a.own_chunks = (int32_t)oc;

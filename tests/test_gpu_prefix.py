@@ -151,6 +151,18 @@ def test_prefixes_kept_apart(ps, dtype, R, P, n, H, KV, D, block):
     assert parts >= 2
 
 
+# Requests whose rows fill tiles by themselves, cut up whole into equal chunks (the last two tables hold too much beside
+# the prefix, or the tiles too few rows, for that): ragged, one without tokens, one in the prefix, one out of range.
+@pytest.mark.parametrize("ps", [16, 24])
+@pytest.mark.parametrize("P,n,H,KV,D,block,spare", [
+    (3001, 32, 16, 2, 128, True, 2), (3001, 33, 8, 1, 128, False, 2), (2500, 120, 2, 2, 64, False, 2),
+    (3001, 32, 16, 2, 128, False, 300), (3001, 9, 16, 2, 128, False, 2)])
+def test_requests_that_fill_tiles(P, n, H, KV, D, block, spare, ps):
+    lens = [P + 40, P + 513, 0, P - 700, P + 128, P + 1]
+    c, q, o, lse = run(lens, P, n, H, KV, D, BF, ps=ps, block=block, seed=35, spare=spare, seqs=[0, 1, 2, 3, 4, 5, 77])
+    assert bd.prefix_attn_workspace_bytes(q, c, P) >= 2 * 7 * n * H * (D + 1) * 4
+
+
 def test_one_long_request():
     run([5000], 0, 1, 8, 1, 128, BF, seed=17)
     run([5000], 4999, 1, 8, 1, 128, BF, seed=17)
