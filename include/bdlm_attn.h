@@ -365,7 +365,7 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
 typedef enum {
   BDLM_CACHE_OK = 0,
   BDLM_CACHE_BAD_LIST = 1, /* a number out of range or listed twice, or against the call's rules */
-  BDLM_CACHE_NO_PAGES = 2  /* too few free pages: status[1] more are needed */
+  BDLM_CACHE_NO_PAGES = 2  /* too few free pages: status[1] more are needed (at most 2^31 - 1 are told) */
 } bdlm_cache_status;
 
 typedef struct {

@@ -7,8 +7,11 @@
 //
 // Bookkeeping runs in one workgroup (a few microseconds: the work is a scan of
 // the reference counts up to the pages needed and of the list); it checks the
-// list first and changes nothing but the status if it does not hold.  Page data
-// is moved by a second kernel, 16 bytes per lane, at the speed of a copy.
+// list first and changes nothing but the status if it does not hold.  It is bound
+// by the scan's steps, each a round of loads and two barriers, so a step takes 16
+// pages per thread (of 100,000 pages the last ones free: grow 22 us, with one page
+// per thread 69; compact with nothing to move 45 us, 199).  Page data is moved by a
+// second kernel, 16 bytes per lane, at the speed of a copy.
 #include "cache.hpp"
 #include "device.hpp"
 
@@ -22,26 +25,46 @@ constexpr int kWordsLds = 16384; // a bit per sequence: 2^19 sequences
 // Outcomes (bdlm_cache_status).
 enum : int { kOk = 0, kBadList = 1, kNoPages = 2 };
 
+constexpr int kPer = 16;         // pages per thread of a scan's step, their counts in flight together
+
 // Exclusive prefix sum over the workgroup's threads; total of all.
-__device__ __forceinline__ int block_scan(int x, int& total, int* wsum) {
+template <class T>
+__device__ __forceinline__ T block_scan(T x, T& total, int64_t* wsum) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int v = x;
+  T v = x;
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) {
-    const int y = __shfl_up(v, s);
+    const T y = __shfl_up(v, s);
     if (lane >= s) v += y;
   }
   __syncthreads();  // (the sums of a scan before are read)
   if (lane == 63) wsum[w] = v;
   __syncthreads();
-  int base = 0, t = 0;
+  T base = 0, t = 0;
   for (int k = 0; k < kT / 64; ++k) {
-    const int y = wsum[k];
+    const T y = (T)wsum[k];
     if (k < w) base += y;
     t += y;
   }
   total = t;
   return base + v - x;
+}
+
+// Reference counts of the kPer pages from p on, 0 past the last (out: pages there are).
+__device__ __forceinline__ int load_refs(const CacheArg& c, int64_t p, int (&refs)[kPer]) {
+  typedef int32_t quad __attribute__((ext_vector_type(4), aligned(4)));
+  const int64_t left = c.pages - p;
+  if (left >= kPer) {
+#pragma unroll
+    for (int k = 0; k < kPer / 4; ++k) {
+      const quad x = *(const quad*)(c.refs + p + 4 * k);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) refs[4 * k + e] = x[e];
+    }
+    return kPer;
+  }
+  for (int k = 0; k < kPer; ++k) refs[k] = k < left ? c.refs[p + k] : 0;
+  return left < 0 ? 0 : (int)left;
 }
 
 __device__ __forceinline__ int clamped_len(const CacheArg& c, int seq) {
@@ -55,14 +78,21 @@ __device__ __forceinline__ int pages_of(const CacheArg& c, int64_t tokens) {
 
 // The first `need` free pages in ascending order into list[0 .. need); false:
 // fewer are free (found: how many).
-__device__ bool take_free(const CacheArg& c, int64_t need, int32_t* list, int* wsum, int& found) {
+__device__ bool take_free(const CacheArg& c, int64_t need, int32_t* list, int64_t* wsum, int& found) {
   found = 0;
-  for (int64_t p0 = 0; p0 < c.pages && found < need; p0 += kT) {
-    const int64_t p = p0 + threadIdx.x;
-    const bool is_free = p < c.pages && c.refs[p] == 0;
-    int total;
-    const int at = found + block_scan(is_free ? 1 : 0, total, wsum);
-    if (is_free && at < need) list[at] = (int32_t)p;
+  for (int64_t p0 = 0; p0 < c.pages && found < need; p0 += kT * kPer) {
+    const int64_t p = p0 + threadIdx.x * kPer;
+    int refs[kPer], mine = 0, total;
+    const int n = load_refs(c, p, refs);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) mine += k < n && refs[k] == 0;
+    int at = found + block_scan(mine, total, wsum);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k)
+      if (k < n && refs[k] == 0) {
+        if (at < need) list[at] = (int32_t)(p + k);
+        ++at;
+      }
     found += total;
   }
   __syncthreads();  // the list is read by other threads
@@ -80,13 +110,16 @@ __device__ bool mark(const CacheArg& c, const int32_t* list, int n, unsigned* bi
     else if (atomicOr(&bits[s >> 5], 1u << (s & 31)) >> (s & 31) & 1) *bad = 1;
   }
   __syncthreads();
-  return *bad == 0;
+  const bool ok = *bad == 0;
+  __syncthreads();  // (read by all before the caller's own checks write it)
+  return ok;
 }
 
 // work: [0] 1 if the operation goes ahead, [1] moves; then a list of pages.
 __global__ __launch_bounds__(kT) void cache_grow_kernel(const CacheArg c, const CacheList l, int32_t* work) {
-  __shared__ unsigned bits[kWordsLds];
-  __shared__ int wsum[kT / 64], bad;
+  __shared__ __attribute__((aligned(16))) unsigned bits[kWordsLds];
+  __shared__ int64_t wsum[kT / 64];
+  __shared__ int bad;
   int32_t* const list = work + kCacheHead;
   bool ok = mark(c, l.a, l.n, bits, &bad);
   if (ok) {
@@ -103,12 +136,11 @@ __global__ __launch_bounds__(kT) void cache_grow_kernel(const CacheArg c, const 
   if (ok) {
     for (int i0 = 0; i0 < l.n; i0 += kT) {
       const int i = i0 + threadIdx.x;
-      int pages = 0;
+      int64_t pages = 0, total;  // (the pages asked for may pass 32 bits)
       if (i < l.n) {
         const int n = clamped_len(c, l.a[i]);
         pages = pages_of(c, (int64_t)n + l.b[i]) - pages_of(c, n);
       }
-      int total;
       block_scan(pages, total, wsum);
       need += total;
     }
@@ -116,38 +148,48 @@ __global__ __launch_bounds__(kT) void cache_grow_kernel(const CacheArg c, const 
   }
   if (threadIdx.x == 0) {
     c.status[0] = !ok ? kBadList : enough ? kOk : kNoPages;
-    c.status[1] = ok && !enough ? (int32_t)(need - found) : 0;
+    c.status[1] = ok && !enough ? (int32_t)(need - found < 0x7fffffff ? need - found : 0x7fffffff) : 0;
   }
   if (!ok || !enough) return;
+  // Sequence i of a round gets the pages list[given + first[i] ..]: thread by
+  // thread for every page, so that a long prompt's pages take no longer than a
+  // batch's (one sequence, 2,048 pages: 257 us by one thread, 10 by all).
+  int* const first = (int*)bits;                      // [kT]
+  int64_t* const entry = (int64_t*)(bits + kT);       // [kT]: where its first new page stands in the table, less first[i]
   int64_t given = 0;
   for (int i0 = 0; i0 < l.n; i0 += kT) {
     const int i = i0 + threadIdx.x;
-    int n = 0, add = 0, first = 0, pages = 0;
+    int n = 0, add = 0, held = 0, pages = 0, s = 0, total;
     if (i < l.n) {
-      n = clamped_len(c, l.a[i]);
+      s = l.a[i];
+      n = clamped_len(c, s);
       add = l.b[i];
-      first = pages_of(c, n);
-      pages = pages_of(c, (int64_t)n + add) - first;
+      held = pages_of(c, n);
+      pages = pages_of(c, (int64_t)n + add) - held;
     }
-    int total;
-    const int64_t at = given + block_scan(pages, total, wsum);
+    const int at = block_scan(pages, total, wsum);
+    first[threadIdx.x] = at;
+    entry[threadIdx.x] = (int64_t)s * c.max_pages + held - at;
+    __syncthreads();
+    for (int k = threadIdx.x; k < total; k += kT) {
+      int lo = 0;  // the last with first[lo] <= k
+#pragma unroll
+      for (int step = kT / 2; step > 0; step >>= 1)
+        if (first[lo + step] <= k) lo += step;
+      const int32_t p = list[given + k];
+      c.table[entry[lo] + k] = p;
+      c.refs[p] = 1;
+    }
     given += total;
-    if (i < l.n) {
-      const int s = l.a[i];
-      for (int k = 0; k < pages; ++k) {
-        const int32_t p = list[at + k];
-        c.table[(int64_t)s * c.max_pages + first + k] = p;
-        c.refs[p] = 1;
-      }
-      c.lens[s] = n + add;
-    }
+    if (i < l.n) c.lens[s] = n + add;
   }
 }
 
 // Pages for the children's partial last pages: list[i] = child i's page or -1.
 __global__ __launch_bounds__(kT) void cache_fork_plan_kernel(const CacheArg c, const CacheList l, int32_t* work) {
-  __shared__ unsigned bits[kWordsLds];
-  __shared__ int wsum[kT / 64], bad;
+  __shared__ __attribute__((aligned(16))) unsigned bits[kWordsLds];
+  __shared__ int64_t wsum[kT / 64];
+  __shared__ int bad;
   int32_t* const of_child = work + kCacheHead;
   int32_t* const list = of_child + l.n;
   bool ok = mark(c, l.b, l.n, bits, &bad);
@@ -176,7 +218,7 @@ __global__ __launch_bounds__(kT) void cache_fork_plan_kernel(const CacheArg c, c
   }
   if (threadIdx.x == 0) {
     c.status[0] = !ok ? kBadList : enough ? kOk : kNoPages;
-    c.status[1] = ok && !enough ? (int32_t)(need - found) : 0;
+    c.status[1] = ok && !enough ? (int32_t)(need - found < 0x7fffffff ? need - found : 0x7fffffff) : 0;
     work[0] = ok && enough;
   }
   if (!ok || !enough) return;
@@ -274,28 +316,42 @@ __global__ __launch_bounds__(256) void cache_free_kernel(const CacheArg c, const
 // list[2 pages + p]: where page p >= live goes, -1 for a page that no table
 // should hold.  The references move here, before the data.
 __global__ __launch_bounds__(kT) void cache_compact_plan_kernel(const CacheArg c, int32_t* work) {
-  __shared__ int wsum[kT / 64];
+  __shared__ int64_t wsum[kT / 64];
   int32_t* const dst = work + kCacheHead;
   int32_t* const src = dst + c.pages;
   int64_t live = 0;
-  for (int64_t p0 = 0; p0 < c.pages; p0 += kT) {
-    const int64_t p = p0 + threadIdx.x;
-    int total;
-    block_scan(p < c.pages && c.refs[p] > 0 ? 1 : 0, total, wsum);
-    live += total;
+  for (int64_t p = threadIdx.x * kPer; p < c.pages; p += kT * kPer) {
+    int refs[kPer];
+    load_refs(c, p, refs);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) live += refs[k] > 0;
   }
+  int64_t all;
+  block_scan(live, all, wsum);
+  live = all;
   int64_t holes = 0, moves = 0;
-  for (int64_t p0 = 0; p0 < c.pages; p0 += kT) {
-    const int64_t p = p0 + threadIdx.x;
-    const bool in = p < c.pages, used = in && c.refs[p] > 0;
-    const bool hole = in && !used && p < live, move = used && p >= live;
-    int th, tm;
-    const int64_t ah = holes + block_scan(hole ? 1 : 0, th, wsum), am = moves + block_scan(move ? 1 : 0, tm, wsum);
-    if (hole) dst[ah] = (int32_t)p;
-    if (move) src[am] = (int32_t)p;
-    if (in && p >= live) src[c.pages + p] = move ? (int32_t)am : -1;
-    holes += th;
-    moves += tm;
+  for (int64_t p0 = 0; p0 < c.pages; p0 += kT * kPer) {
+    const int64_t p = p0 + threadIdx.x * kPer;
+    int refs[kPer];
+    const int n = load_refs(c, p, refs);
+    int64_t mine = 0, total;  // holes, and from bit 32 on moves
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      if (k < n && refs[k] <= 0 && p + k < live) mine += 1;
+      if (k < n && refs[k] > 0 && p + k >= live) mine += (int64_t)1 << 32;
+    }
+    const int64_t at = block_scan(mine, total, wsum);
+    int64_t ah = holes + (int32_t)at, am = moves + (at >> 32);
+#pragma unroll
+    for (int k = 0; k < kPer; ++k) {
+      if (k >= n) break;
+      const bool move = refs[k] > 0 && p + k >= live;
+      if (refs[k] <= 0 && p + k < live) dst[ah++] = (int32_t)(p + k);
+      if (p + k >= live) src[c.pages + p + k] = move ? (int32_t)am : -1;
+      if (move) src[am++] = (int32_t)(p + k);
+    }
+    holes += (int32_t)total;
+    moves += total >> 32;
   }
   if (threadIdx.x == 0) {
     work[0] = (int32_t)live;

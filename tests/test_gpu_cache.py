@@ -222,3 +222,27 @@ def test_graph_replays():
         g.replay()
         host()
         o.compare(c)
+
+
+@pytest.mark.parametrize("pages", [16384, 40007])
+def test_many_pages(pages):
+    """More pages than a step of the scans takes, sequences that grow by thousands of pages, more than a round of them."""
+    S = 1500
+    c, o = fresh(layers=1, pages=pages, ps=2, KV=1, seqs=S, max_pages=9000)
+    both_grow(c, o, [3], [17001])
+    both_grow(c, o, [7, 3, 9], [2000, 0, 1])
+    rng = random.Random(pages)
+    order = [s for s in rng.sample(range(S), S) if s not in (3, 7, 9)]
+    both_grow(c, o, order, [rng.choice([0, 0, 1, 2, 3, 5]) for _ in order])
+    gone = [3] + order[::3]
+    bd.cache_free(c, i32(gone))
+    o.free(gone)
+    o.compare(c)
+    both_grow(c, o, order[:40], [rng.randrange(0, 300) for _ in range(40)])
+    bd.cache_compact(c)
+    o.compact()
+    o.compare(c)
+    both_grow(c, o, [3], [4001])
+    both_grow(c, o, [order[0]], [9000])
+    both_grow(c, o, [order[1], order[2], order[4]], [16000] * 3)
+    both_grow(c, o, [order[5], order[7], order[8]], [17000] * 3)

@@ -75,3 +75,15 @@ def test_packed_rows_past_2_31_elements():
     for n, t in (("o", o), ("dq", dq), ("dk", dk), ("dv", dv)):
         check(n, torch.cat([t[s:s + m] for s, m in zip(starts, ql)]), *ref[n])
     check("lse", torch.cat([lse[:, s:s + m] for s, m in zip(starts, ql)], 1), *ref["lse"])
+
+
+def test_more_pages_asked_for_than_32_bits_hold():
+    S, mp = 1024, 1 << 21
+    k, v = (torch.zeros((1, 100, 1, 1, 64), dtype=BF, device=DEV) for _ in range(2))
+    table = torch.full((S, mp), -1, dtype=torch.int32, device=DEV)
+    c = bd.Cache(k, v, table, i32([0] * S), i32([0] * 100), i32([0, 0]))
+    for n in (S, S - 1):
+        bd.cache_grow(c, i32(range(n)), i32([mp] * n))
+        torch.cuda.synchronize()
+        assert c.status.tolist() == [2, min(n * mp - 100, 2 ** 31 - 1)]
+        assert int(c.lens.sum()) == 0 and int(c.refs.sum()) == 0 and bool((table[::128] == -1).all())
