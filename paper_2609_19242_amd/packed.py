@@ -7,6 +7,7 @@ forward (:func:`packed_fwd`) and backward (:func:`packed_bwd`).  The rules and l
 from __future__ import annotations
 
 import ctypes
+import math
 import operator
 from typing import Optional, Sequence
 
@@ -53,8 +54,9 @@ def declare(L: ctypes.CDLL):
 class PackedPlan:
     """The work items of packed calls over some sequences, on ``device`` (see :func:`packed_plan`)."""
 
-    def __init__(self, record: _Plan, items: torch.Tensor, dtype: torch.dtype):
+    def __init__(self, record: _Plan, items: torch.Tensor, dtype: torch.dtype, held=(0, 0)):
         self._record, self._items, self.dtype = record, items, dtype
+        self._held = held  # query and key rows that belong to a sequence
         self._ref, self._at = ctypes.byref(record), items.data_ptr()
         p = record.problem
         self.heads, self.kv_heads, self.head_dim = p.heads, p.kv_heads, p.head_dim
@@ -109,7 +111,7 @@ def packed_plan(q_lens: Sequence[int], k_lens: Optional[Sequence[int]] = None, *
     _check(lib().bdlm_packed_plan_make(ctypes.byref(p), n, seqs, None, 0, ctypes.byref(rec)))
     host = torch.empty(max(16, rec.bytes), dtype=torch.uint8)
     _check(lib().bdlm_packed_plan_make(ctypes.byref(p), n, seqs, host.data_ptr(), host.numel(), ctypes.byref(rec)))
-    return PackedPlan(rec, host.to(device), dtype)
+    return PackedPlan(rec, host.to(device), dtype, (sum(ql), sum(kl)))
 
 
 def _rows(like, name, t, heads, at_least):
@@ -139,17 +141,30 @@ def _check_plan(plan):
         raise TypeError(f"plan must be a PackedPlan, got {type(plan).__name__}")
 
 
+def _filled(like, shape, stream, dtype=None, fill=0.0):
+    """A new output of which a call does not write all, filled on the call's stream."""
+    t = like.new_empty(shape, dtype=dtype)
+    if stream is None:
+        return t.fill_(fill)
+    with torch.cuda.stream(_torch_stream(stream, like.device)):
+        return t.fill_(fill)
+
+
 def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, stream=None):
     """Attention of the plan's sequences: q ``[rows][heads][D]``, k and v ``[rows][kv_heads][D]`` (rows may lie apart,
     as in a fused projection).  Returns ``(o, lse)`` with ``lse [heads][rows]`` fp32, or writes into ``out``; rows of
-    no sequence are left as they are (in new outputs: undefined)."""
+    no sequence are left as they are there, and are 0 (lse: -inf) in new outputs."""
     _check_plan(plan)
     H, KV = plan.heads, plan.kv_heads
     rq, rk, rv = (_rows(plan, "q", q, H, plan.q_rows), _rows(plan, "k", k, KV, plan.k_rows),
                   _rows(plan, "v", v, KV, plan.k_rows))
     n = q.shape[0]
     if out is None:
-        o, lse = q.new_empty((n, H, plan.head_dim)), q.new_empty((H, n), dtype=torch.float32)
+        if n == plan._held[0]:
+            o, lse = q.new_empty((n, H, plan.head_dim)), q.new_empty((H, n), dtype=torch.float32)
+        else:
+            o = _filled(q, (n, H, plan.head_dim), stream)
+            lse = _filled(q, (H, n), stream, torch.float32, -math.inf)
         ro = _Rows(o.data_ptr(), H * plan.head_dim)
     else:
         if len(out) != 2:
@@ -163,8 +178,9 @@ def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, stream=No
 
 def packed_bwd(plan: PackedPlan, q, k, v, o, lse, do, out: Optional[tuple] = None,
                workspace: Optional[torch.Tensor] = None, stream=None):
-    """Backward of :func:`packed_fwd`; returns ``(dq, dk, dv)``, or writes into ``out``.  ``workspace``: a device
-    tensor of ``plan.workspace_bytes`` bytes (calls that may overlap in time need one each); allocated if not given."""
+    """Backward of :func:`packed_fwd`; returns ``(dq, dk, dv)``, or writes into ``out``; rows of no sequence are left as
+    they are there, and are 0 in new outputs.  ``workspace``: a device tensor of ``plan.workspace_bytes`` bytes (calls
+    that may overlap in time need one each); allocated if not given."""
     _check_plan(plan)
     H, KV, D = plan.heads, plan.kv_heads, plan.head_dim
     rq, rk, rv = (_rows(plan, "q", q, H, plan.q_rows), _rows(plan, "k", k, KV, plan.k_rows),
@@ -173,7 +189,9 @@ def packed_bwd(plan: PackedPlan, q, k, v, o, lse, do, out: Optional[tuple] = Non
     ro, rdo = _as_long(plan, "o", o, H, n), _as_long(plan, "do", do, H, n)
     _lse(plan, lse, n)
     if out is None:
-        dq, dk, dv = q.new_empty((n, H, D)), k.new_empty((nk, KV, D)), v.new_empty((nv, KV, D))
+        hq, hk = plan._held
+        dq = q.new_empty((n, H, D)) if n == hq else _filled(q, (n, H, D), stream)
+        dk, dv = (t.new_empty((m, KV, D)) if m == hk else _filled(t, (m, KV, D), stream) for t, m in ((k, nk), (v, nv)))
         outs = _Rows(dq.data_ptr(), H * D), _Rows(dk.data_ptr(), KV * D), _Rows(dv.data_ptr(), KV * D)
     else:
         if len(out) != 3:

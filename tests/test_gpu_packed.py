@@ -224,3 +224,25 @@ def test_padded_batch():
     for n, t in zip(("o", "lse", "dq", "dk", "dv"), (o, lse) + grads):
         check(n, t, *ref[n])
         assert not torch.isnan(t).any()
+
+
+@pytest.mark.parametrize("other", [False, True])
+def test_new_outputs_hold_zeros_in_rows_of_no_sequence(other):
+    q, k, v, do = (synth.normal((40, h, 64), 60 + i, BF).to(DEV) for i, h in enumerate((4, 2, 2, 4)))
+    stream = torch.cuda.Stream() if other else None
+    for starts, n in (([0, 20], 40), (None, 40), (None, 27)):  # gaps, rows behind the last, neither
+        plan = bd.packed_plan([10, 17], heads=4, kv_heads=2, head_dim=64, dtype=BF, q_starts=starts)
+        for _ in range(2):  # (memory that held something)
+            trash = [torch.full((n, h, 64), math.nan, dtype=BF, device=DEV) for h in (4, 4, 2, 2)]
+            trash.append(torch.full((4, n), math.nan, device=DEV))
+            del trash
+            torch.cuda.synchronize()
+            o, lse = bd.packed_fwd(plan, q[:n], k[:n], v[:n], stream=stream)
+            dq, dk, dv = bd.packed_bwd(plan, q[:n], k[:n], v[:n], o, lse, do[:n], stream=stream)
+            torch.cuda.synchronize()
+        mine = torch.zeros(n, dtype=torch.bool)
+        for a, m in zip(starts or (0, 10), (10, 17)):
+            mine[a:a + m] = True
+        for t in (o, dq, dk, dv):
+            assert torch.all(t.cpu()[~mine] == 0) and bool(torch.isfinite(t).all())
+        assert torch.all(lse.cpu()[:, ~mine] == -math.inf) and bool(torch.isfinite(lse.cpu()[:, mine]).all())
