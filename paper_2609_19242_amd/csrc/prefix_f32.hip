@@ -5,7 +5,8 @@
 // 16-key tiles the waves take in turn; K and V rows go straight from global
 // memory into registers, rows past the chunk from a row of zeros.  Bound by
 // the fp64 matrix rate (16 rows share a tile's products however few they are)
-// and, for few requests, by latency.
+// and, for few requests, by latency (4 requests of 290 keys, 8/2 heads, d 64: 13.5
+// us for three tiles a wave, behind the chain sequence, length, page, key).
 #include "cache.hpp"
 #include "f64tile.hpp"
 
