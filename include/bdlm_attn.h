@@ -312,9 +312,10 @@ typedef struct {
 typedef struct {
   bdlm_packed problem;
   int64_t q_rows, k_rows;    /* rows that the query and key tensors have at least */
-  int32_t q_items, k_items, n_sums, slots, teams, reserved;
-  size_t bytes;              /* of the items */
-  size_t workspace_bytes;    /* of bdlm_packed_bwd */
+  int32_t q_items, k_items, n_sums, slots, teams, fwd_items, fwd_sums, fwd_slots;
+  size_t bytes;               /* of the items */
+  size_t workspace_bytes;     /* of bdlm_packed_bwd */
+  size_t fwd_workspace_bytes; /* of bdlm_packed_fwd */
 } bdlm_packed_plan;
 
 /* A tensor's first row and the elements between its rows. */
@@ -333,9 +334,12 @@ typedef struct {
 bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bdlm_packed_seq* seqs, void* items,
                                   size_t items_bytes, bdlm_packed_plan* plan);
 
-/* O and LSE of a packed call.  items: the plan's items in device memory. */
+/* O and LSE of a packed call.  items: the plan's items in device memory.
+ * workspace: plan->fwd_workspace_bytes bytes (0 unless there are few query tiles with long walks), as in
+ * bdlm_packed_bwd.  Deterministic. */
 bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdlm_rows q, bdlm_rows k, bdlm_rows v,
-                            bdlm_rows o, float* lse, int64_t lse_pitch, hipStream_t stream);
+                            bdlm_rows o, float* lse, int64_t lse_pitch, void* workspace, size_t workspace_bytes,
+                            hipStream_t stream);
 
 /*
  * dQ, dK and dV of a packed call from its O and LSE (the formulas of

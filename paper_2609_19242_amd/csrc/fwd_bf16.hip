@@ -194,6 +194,12 @@ __global__ __launch_bounds__(NT * NW * 64)
   if constexpr (NT > 1) {
     if (team == 1) c0 = next_one(c0);
   }
+  if constexpr (kIsPacked<Args> && NT == 1) {  // a chunk of the walk
+    const PackedItem& p = args.items[it.item];
+    c0.t1 = imin(c0.t1, c0.t + p.n1);
+    c0.t += p.n0;
+    c0.have = c0.have && c0.t < c0.t1;
+  }
   // (teams: every wave runs as many rounds as team 0, the first to be dealt a tile, for the barriers)
   int rounds = NT > 1 ? (count_key_tiles(a, qr.stream, pq0, pq1, BN) + NT - 1) / NT : 0;
   CopyCur cp = copy_seek(CopyCur{c0, any_src, 0});
@@ -424,6 +430,26 @@ __global__ __launch_bounds__(NT * NW * 64)
   const float l_tot = l_run + partner(l_run);
   const bool empty = !(l_tot > 0.f);
   const float inv = empty ? 0.f : 1.f / l_tot;
+  if constexpr (kIsPacked<Args> && NT == 1) {
+    const int slot = args.items[it.item].slot;
+    if (slot >= 0) {  // a chunk's partial output, [slot][heads / HP][128 rows of the waves][D]
+      const int64_t at = ((int64_t)slot * (a.heads / HP) + it.h / HP) * (NW * 32) + w * 32 + l32;
+      if (!empty) {
+        float* op = (float*)args.partials + at * D;
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+          for (int g4 = 0; g4 < 4; ++g4) {
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = acc[d][g4 * 4 + e] * inv;
+            *(f32x4*)(op + 32 * d + 8 * g4 + 4 * half) = v;
+          }
+      }
+      if (half == 0) args.part_lse[at] = empty ? -INFINITY : m_run + log2f(l_tot);
+      return;
+    }
+  }
   if (a.out_f32) {
     if (my_row < qr.len) {
       float* op = (float*)qr.o + row_elem<D>(a, it.b, qr.bstride, my_row, H, h, OS);

@@ -140,11 +140,11 @@ __device__ inline SumTile<ROWS> sum_tile(const PackedArgs& a, int n) {
   const PackedSum& p = a.sums[n / a.kv_heads];
   s.kvh = n - n / a.kv_heads * a.kv_heads;
   s.n = p.n;
-  s.nk = imin(ROWS, p.k_len - p.tile * ROWS);
+  s.nk = imin(ROWS, p.len - p.tile * ROWS);
   s.dks = a.dks;
   s.dvs = a.dvs;
-  s.dk = ((int64_t)p.k0 + p.tile * ROWS) * a.dks + s.kvh * D;
-  s.dv = ((int64_t)p.k0 + p.tile * ROWS) * a.dvs + s.kvh * D;
+  s.dk = ((int64_t)p.row0 + p.tile * ROWS) * a.dks + s.kvh * D;
+  s.dv = ((int64_t)p.row0 + p.tile * ROWS) * a.dvs + s.kvh * D;
   s.row0 = ((int64_t)p.slot * a.kv_heads + s.kvh) * ROWS;
   s.step = (int64_t)a.kv_heads * ROWS;
   s.it = SumItem{};

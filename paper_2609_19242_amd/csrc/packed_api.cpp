@@ -77,11 +77,24 @@ size_t packed_stats_bytes(const bdlm_packed_plan& pl) {
   return align256((size_t)pl.q_rows * pl.problem.heads * sizeof(float));
 }
 
+bdlm_status check_workspace(size_t need, const void* p, size_t bytes) {
+  if (need > 0 && (!p || bytes < need || (reinterpret_cast<uintptr_t>(p) & 255u)))
+    return fail(BDLM_ERR_WORKSPACE, "workspace needs %zu bytes, 256-byte aligned (got %zu at %p)", need, bytes, p);
+  return BDLM_OK;
+}
+
+// Partial outputs of the forward's cut walks; their LSE lies behind them.
+size_t part_bytes(const bdlm_packed_plan& pl) {
+  const int per = pl.problem.heads / packed_tile_heads(pl.problem.heads / pl.problem.kv_heads);
+  return align256((size_t)pl.fwd_slots * per * kQRowsShortBf16 * pl.problem.head_dim * sizeof(float));
+}
+
 bdlm_status check_plan(const bdlm_packed_plan* pl, const void* items) {
   if (!pl) return fail(BDLM_ERR_INVALID, "plan is null");
   const bdlm_status st = check_packed(&pl->problem);
   if (st != BDLM_OK) return st;
-  if (pl->q_items < 0 || pl->k_items < 0 || pl->n_sums < 0 || pl->slots < 0 || pl->q_rows < 0 || pl->k_rows < 0 ||
+  if (pl->q_items < 0 || pl->k_items < 0 || pl->n_sums < 0 || pl->slots < 0 || pl->fwd_items < 0 || pl->fwd_sums < 0 ||
+      pl->fwd_slots < 0 || pl->q_rows < 0 || pl->k_rows < 0 ||
       pl->teams < 1 || pl->teams > 2)
     return fail(BDLM_ERR_INVALID, "plan was not made by bdlm_packed_plan_make");
   if (pl->bytes > 0 && (!items || !aligned16(items)))
@@ -124,9 +137,10 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
   const PackedPlanItems it = packed_items(*p, n_seqs, seqs);
   // (a grid dimension holds fewer than 2^32 threads; the fp32 kernels' grids have two)
   const bool f32 = p->dtype == BDLM_F32;
-  const int64_t q_wgs = (int64_t)it.q.size() * (p->heads / (f32 ? 1 : packed_tile_heads(p->heads / p->kv_heads)));
+  const int64_t per = p->heads / (f32 ? 1 : packed_tile_heads(p->heads / p->kv_heads));
+  const int64_t q_wgs = (int64_t)std::max(it.q.size(), it.fwd.size()) * per;
   const int64_t wgs = std::max(q_wgs, (int64_t)it.k.size() * p->kv_heads), most = f32 ? (int64_t)1 << 30 : 1 << 22;
-  if (wgs > most || (int64_t)it.sums.size() * p->kv_heads > 1 << 18)
+  if (wgs > most || (int64_t)it.sums.size() * p->kv_heads > 1 << 18 || (int64_t)it.fwd_sums.size() * per > 1 << 18)
     return fail(BDLM_ERR_UNSUPPORTED, "packed problem needs %lld workgroups (limit %lld)", (long long)wgs,
                 (long long)most);
   bdlm_packed_plan pl{};
@@ -138,8 +152,13 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
   pl.n_sums = (int32_t)it.sums.size();
   pl.slots = it.slots;
   pl.teams = it.teams;
-  const size_t qb = it.q.size() * sizeof(PackedItem), kb = it.k.size() * sizeof(PackedItem);
-  pl.bytes = qb + kb + it.sums.size() * sizeof(PackedSum);
+  pl.fwd_items = (int32_t)it.fwd.size();
+  pl.fwd_sums = (int32_t)it.fwd_sums.size();
+  pl.fwd_slots = it.fwd_slots;
+  pl.bytes = (it.q.size() + it.k.size() + it.fwd.size()) * sizeof(PackedItem) +
+             (it.sums.size() + it.fwd_sums.size()) * sizeof(PackedSum);
+  const size_t part_rows = (size_t)it.fwd_slots * per * kQRowsShortBf16;
+  pl.fwd_workspace_bytes = align256(part_rows * p->head_dim * sizeof(float)) + align256(part_rows * sizeof(float));
   pl.workspace_bytes = 2 * packed_stats_bytes(pl) + (size_t)it.slots * p->kv_heads *
                                                         (f32 ? kRowsF32 * sizeof(double)
                                                              : kBwdKeysBf16 * sizeof(float)) *
@@ -148,9 +167,15 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
     if (items_bytes < pl.bytes)
       return fail(BDLM_ERR_INVALID, "plan needs %zu bytes (got %zu)", pl.bytes, items_bytes);
     char* dst = static_cast<char*>(items);
-    if (qb) std::memcpy(dst, it.q.data(), qb);
-    if (kb) std::memcpy(dst + qb, it.k.data(), kb);
-    if (!it.sums.empty()) std::memcpy(dst + qb + kb, it.sums.data(), it.sums.size() * sizeof(PackedSum));
+    auto put = [&](const auto& v) {
+      if (!v.empty()) std::memcpy(dst, v.data(), v.size() * sizeof(v[0]));
+      dst += v.size() * sizeof(v[0]);
+    };
+    put(it.q);
+    put(it.k);
+    put(it.sums);
+    put(it.fwd);
+    put(it.fwd_sums);
   }
   *plan = pl;
   return BDLM_OK;
@@ -159,7 +184,8 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
 }
 
 bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdlm_rows q, bdlm_rows k, bdlm_rows v,
-                            bdlm_rows o, float* lse, int64_t lse_pitch, hipStream_t stream) {
+                            bdlm_rows o, float* lse, int64_t lse_pitch, void* workspace, size_t workspace_bytes,
+                            hipStream_t stream) {
   bdlm_status st;
   if ((st = check_plan(plan, items)) != BDLM_OK) return st;
   const bdlm_packed& p = plan->problem;
@@ -172,9 +198,19 @@ bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdl
   if ((st = check_rows(o, "o", rows, qe, elem)) != BDLM_OK) return st;
   if ((st = check_pitch(*plan, lse_pitch)) != BDLM_OK) return st;
   if (rows && !lse) return fail(BDLM_ERR_INVALID, "lse pointer is null");
+  if ((st = check_workspace(plan->fwd_workspace_bytes, workspace, workspace_bytes)) != BDLM_OK) return st;
   PackedArgs a = packed_args(*plan, lse_pitch);
   a.items = static_cast<const PackedItem*>(items);
   a.n_items = plan->q_items;
+  if (plan->fwd_items > 0) {
+    const PackedItem* const k_end = a.items + plan->q_items + plan->k_items;
+    a.items = reinterpret_cast<const PackedItem*>(reinterpret_cast<const PackedSum*>(k_end) + plan->n_sums);
+    a.n_items = plan->fwd_items;
+    a.sums = reinterpret_cast<const PackedSum*>(a.items + plan->fwd_items);
+    a.n_sums = plan->fwd_sums;
+    a.partials = workspace;
+    a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_bytes(*plan));
+  }
   a.q = q.ptr;
   a.qs = (int32_t)q.stride;
   a.k = k.ptr;
@@ -185,8 +221,9 @@ bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdl
   a.os = (int32_t)o.stride;
   a.lse = lse;
   const hipError_t e = timed(kKPackedFwd, stream, [&] {
-    return p.dtype == BDLM_BF16 ? launch_fwd_bf16(a, p.head_dim, plan->teams, stream)
-                                : launch_fwd_f32(a, p.head_dim, stream);
+    const hipError_t le = p.dtype == BDLM_BF16 ? launch_fwd_bf16(a, p.head_dim, plan->teams, stream)
+                                               : launch_fwd_f32(a, p.head_dim, stream);
+    return le != hipSuccess || a.n_sums == 0 ? le : launch_packed_fwd_sum(a, p.head_dim, stream);
   });
   return e == hipSuccess ? BDLM_OK : hip_fail(e, "packed forward launch");
 }
@@ -213,9 +250,7 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
   if (plan->q_rows * p.heads > ((int64_t)1 << 28))
     return fail(BDLM_ERR_UNSUPPORTED, "query rows x heads = %lld exceeds 2^28", (long long)(plan->q_rows * p.heads));
   const size_t need = plan->workspace_bytes, arr = packed_stats_bytes(*plan);
-  if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u)))
-    return fail(BDLM_ERR_WORKSPACE, "workspace needs %zu bytes, 256-byte aligned (got %zu at %p)", need,
-                workspace_bytes, workspace);
+  if ((st = check_workspace(need, workspace, workspace_bytes)) != BDLM_OK) return st;
   PackedArgs a = packed_args(*plan, lse_pitch);
   a.q = q.ptr;
   a.qs = (int32_t)q.stride;

@@ -14,9 +14,9 @@
 namespace bdlm {
 
 struct PackedPlanItems {
-  std::vector<PackedItem> q, k;
-  std::vector<PackedSum> sums;
-  int32_t slots = 0;
+  std::vector<PackedItem> q, k, fwd;  // fwd: the forward's, if some walks are cut (else q)
+  std::vector<PackedSum> sums, fwd_sums;
+  int32_t slots = 0, fwd_slots = 0;
   int32_t teams = 1;
 };
 
@@ -25,10 +25,24 @@ inline int packed_step_rows(bool f32, int group) { return f32 ? kRowsF32 : group
 // Partial sums of cut walks at most (per call); longer chunks where they would come to more.
 constexpr size_t kMaxPackedPartials = (size_t)256 << 20;
 
+// Key tiles of the forward's chunks at least; what partial outputs and their sums cost, in key tiles.
+constexpr int64_t kMinFwdUnit = 8, kFwdSumTiles = 10, kFwdSumTiles64 = 18;
+
 // Work items, heaviest first: a workgroup that starts late should be short.
 //
 // Query tiles: 128 rows (16 in fp32) of one sequence, or as many fewer as a
 // tile has heads (packed_tile_heads), by the keys they walk.
+//
+// Forward, bf16: where few tiles have long walks (a piece of a long prompt, few
+// heads), the busiest CU's walks, not the card, set the time.  If they are longer
+// than the average load of a CU by more than partial outputs cost, walks are cut
+// into equal chunks of at most that load, a chunk per CU, whose outputs
+// packed_fwd_sum.hip joins (the factor is what a chunk's tiles take longer without a
+// second team).  32/8 heads, d 128, without and with cuts: 1 row behind 2,048 keys 33
+// and 19 us, behind 8,192 109 and 22, behind 32,768 444 and 40; 256 rows 37 and 30, 119
+// and 59, 438 and 184; 512 rows behind 2,048 are left whole (42, 47 cut), 1,024 behind
+// 8,192 too (155, 193).  3,000 rows of 4/2 heads 45 and 31.  (Chunks that fill two
+// workgroups a CU write twice the partial outputs: 256 rows behind 8,192 65 us.)
 //
 // Key tiles: 128 keys (16), by the steps of their walks.  The longest walk,
 // the first keys' of the longest sequence, sets the time when there are few;
@@ -51,8 +65,8 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
     int64_t cost;
     PackedItem it;
   };
-  std::vector<Cost> q, k;
-  int64_t total = 0;
+  std::vector<Cost> q, k, walks;  // walks: the query tiles by 64-key tiles
+  int64_t total = 0, fwd_total = 0;
   for (int64_t i = 0; i < n; ++i) {
     const bdlm_packed_seq& s = seqs[i];
     const int ql = (int)s.q_len, kl = (int)s.k_len;
@@ -64,7 +78,10 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
       key_interval(kClean, qp + first, kClean, rule, lo, hi);
       key_interval(kClean, qp + last, kClean, rule, lo1, hi1);
       it.tile = t;
-      q.push_back({std::max(0, std::min(hi1, shift + kl) - std::max(lo, shift)), it});
+      const int u0 = std::max(lo - shift, 0), u1 = std::min(hi1 - shift, kl);
+      q.push_back({std::max(0, u1 - u0), it});
+      walks.push_back({u1 > u0 ? (u1 + 63) / 64 - u0 / 64 : 0, it});
+      fwd_total += walks.back().cost;
     }
     for (int t = 0; t * (int64_t)k_tile < kl; ++t) {
       const int first = t * k_tile, last = std::min(kl, first + k_tile) - 1;
@@ -82,7 +99,45 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
   std::stable_sort(q.begin(), q.end(), heavier);
   std::stable_sort(k.begin(), k.end(), heavier);
   for (const Cost& c : q) out.q.push_back(c.it);
-  if (!f32 && (int64_t)out.q.size() * (p.heads / tile_heads) <= kTeamWgs) out.teams = 2;
+  const int64_t per = p.heads / tile_heads;  // workgroups of a query tile
+
+  // Chunks of the query tiles' walks (bf16 forward).
+  std::stable_sort(walks.begin(), walks.end(), heavier);
+  const int64_t fwd_longest = walks.empty() ? 0 : walks[0].cost;
+  const int64_t wgs = (int64_t)walks.size() * per, fwd_average = (fwd_total * per + kCus - 1) / kCus;
+  int64_t fwd_unit = std::max(kMinFwdUnit, fwd_average);
+  // what the busiest CU walks without cuts: all workgroups resident, or dealt out as others end
+  int64_t busiest = 0;
+  if (wgs <= kCus * (p.head_dim == 64 ? 3 : 2))
+    for (int64_t i = 0; i < wgs; i += kCus) busiest += walks[i / per].cost;
+  else
+    busiest = std::max(fwd_longest, fwd_average);
+  if (!f32 && busiest > fwd_unit * 8 / 5 + (p.head_dim == 64 ? kFwdSumTiles64 : kFwdSumTiles)) {
+    const int64_t most = (int64_t)(kMaxPackedPartials / (per * kQRowsShortBf16 * p.head_dim * sizeof(float)));
+    for (;; fwd_unit *= 2) {
+      int64_t slots = 0;
+      for (const Cost& c : walks)
+        if (c.cost > fwd_unit) slots += (c.cost + fwd_unit - 1) / fwd_unit;
+      if (slots <= most) break;
+    }
+    std::vector<Cost> chunks;
+    for (const Cost& c : walks) {
+      const int64_t nch = std::max<int64_t>((c.cost + fwd_unit - 1) / fwd_unit, 1), size = (c.cost + nch - 1) / nch;
+      PackedItem it = c.it;
+      if (nch > 1) out.fwd_sums.push_back({it.q0, it.q_len, it.tile, out.fwd_slots, (int32_t)nch, 0, 0, 0});
+      for (int64_t j = 0; j < nch; ++j) {
+        it.n0 = (int32_t)(j * size);
+        it.n1 = j + 1 < nch ? (int32_t)((j + 1) * size) : kBig;
+        it.slot = nch > 1 ? out.fwd_slots++ : -1;
+        chunks.push_back({std::max<int64_t>(0, std::min(c.cost, (j + 1) * size) - j * size), it});
+      }
+    }
+    if (out.fwd_slots > 0) {
+      std::stable_sort(chunks.begin(), chunks.end(), heavier);
+      for (const Cost& c : chunks) out.fwd.push_back(c.it);
+    }
+  }
+  if (!f32 && out.fwd.empty() && (int64_t)out.q.size() * per <= kTeamWgs) out.teams = 2;
 
   // Chunks of the key tiles' walks.
   const int64_t longest = k.empty() ? 0 : k[0].cost;

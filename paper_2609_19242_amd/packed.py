@@ -32,8 +32,9 @@ class _Seq(ctypes.Structure):  # bdlm_packed_seq
 class _Plan(ctypes.Structure):  # bdlm_packed_plan
     _fields_ = [("problem", _Packed), ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64),
                 ("q_items", ctypes.c_int32), ("k_items", ctypes.c_int32), ("n_sums", ctypes.c_int32),
-                ("slots", ctypes.c_int32), ("teams", ctypes.c_int32), ("reserved", ctypes.c_int32),
-                ("bytes", ctypes.c_size_t), ("workspace_bytes", ctypes.c_size_t)]
+                ("slots", ctypes.c_int32), ("teams", ctypes.c_int32), ("fwd_items", ctypes.c_int32),
+                ("fwd_sums", ctypes.c_int32), ("fwd_slots", ctypes.c_int32),
+                ("bytes", ctypes.c_size_t), ("workspace_bytes", ctypes.c_size_t), ("fwd_workspace_bytes", ctypes.c_size_t)]
 
 
 class _Rows(ctypes.Structure):  # bdlm_rows
@@ -44,7 +45,7 @@ def declare(L: ctypes.CDLL):
     vp, sz = ctypes.c_void_p, ctypes.c_size_t
     L.bdlm_packed_plan_make.argtypes = [ctypes.POINTER(_Packed), ctypes.c_int64, ctypes.POINTER(_Seq), vp, sz,
                                         ctypes.POINTER(_Plan)]
-    L.bdlm_packed_fwd.argtypes = [ctypes.POINTER(_Plan), vp] + [_Rows] * 4 + [vp, ctypes.c_int64, vp]
+    L.bdlm_packed_fwd.argtypes = [ctypes.POINTER(_Plan), vp] + [_Rows] * 4 + [vp, ctypes.c_int64, vp, sz, vp]
     L.bdlm_packed_bwd.argtypes = [ctypes.POINTER(_Plan), vp] + [_Rows] * 4 + [vp, ctypes.c_int64] + [_Rows] * 4 + \
         [vp, sz, vp]
     for name in ("bdlm_packed_plan_make", "bdlm_packed_fwd", "bdlm_packed_bwd"):
@@ -61,7 +62,7 @@ class PackedPlan:
         p = record.problem
         self.heads, self.kv_heads, self.head_dim = p.heads, p.kv_heads, p.head_dim
         self.q_rows, self.k_rows = record.q_rows, record.k_rows
-        self.workspace_bytes = record.workspace_bytes
+        self.workspace_bytes, self.fwd_workspace_bytes = record.workspace_bytes, record.fwd_workspace_bytes
         self.device, self.gpu = items.device, items.get_device()  # (gpu: -1 on the CPU)
 
     def __repr__(self):
@@ -150,10 +151,12 @@ def _filled(like, shape, stream, dtype=None, fill=0.0):
         return t.fill_(fill)
 
 
-def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, stream=None):
+def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None):
     """Attention of the plan's sequences: q ``[rows][heads][D]``, k and v ``[rows][kv_heads][D]`` (rows may lie apart,
     as in a fused projection).  Returns ``(o, lse)`` with ``lse [heads][rows]`` fp32, or writes into ``out``; rows of
-    no sequence are left as they are there, and are 0 (lse: -inf) in new outputs."""
+    no sequence are left as they are there, and are 0 (lse: -inf) in new outputs.  ``workspace``: a device tensor of
+    ``plan.fwd_workspace_bytes`` bytes, if that is not 0 (as in :func:`packed_bwd`)."""
     _check_plan(plan)
     H, KV = plan.heads, plan.kv_heads
     rq, rk, rv = (_rows(plan, "q", q, H, plan.q_rows), _rows(plan, "k", k, KV, plan.k_rows),
@@ -172,7 +175,11 @@ def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, stream=No
         o, lse = out
         ro = _as_long(plan, "o", o, H, n)
         _lse(plan, lse, n)
-    _launch(plan.gpu, stream, lib().bdlm_packed_fwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n)
+    at = nbytes = 0
+    if plan.fwd_workspace_bytes:
+        workspace = _workspace(workspace, plan.fwd_workspace_bytes, plan.device, stream)
+        at, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    _launch(plan.gpu, stream, lib().bdlm_packed_fwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n, at, nbytes)
     return o, lse
 
 

@@ -246,3 +246,30 @@ def test_new_outputs_hold_zeros_in_rows_of_no_sequence(other):
         for t in (o, dq, dk, dv):
             assert torch.all(t.cpu()[~mine] == 0) and bool(torch.isfinite(t).all())
         assert torch.all(lse.cpu()[:, ~mine] == -math.inf) and bool(torch.isfinite(lse.cpu()[:, mine]).all())
+
+
+# Few query tiles with long walks: the walks are cut into chunks, whose partial outputs are joined.
+@pytest.mark.parametrize("H,KV,D", [(4, 1, 128), (4, 2, 64), (3, 1, 128), (2, 2, 64)])
+@pytest.mark.parametrize("ql,kl,block,window", [
+    ([1], [2500], 1, 0), ([70, 1, 3], [2000, 1700, 0], 1, 0), ([200], [2300], 32, 0), ([130, 40], [2400, 20], 1, 1900),
+    ([1800], [1700], 1, 0), ([65], [4000], 5000, 0)])
+def test_few_rows_with_long_walks(ql, kl, block, window, H, KV, D):
+    plan = bd.packed_plan(ql, kl, heads=H, kv_heads=KV, head_dim=D, dtype=BF, block_size=block, window=window)
+    # (27 key tiles are left whole at head_dim 64, where the products take half as long and the partial outputs do not)
+    assert plan.fwd_workspace_bytes > 0 or (D == 64 and ql == [1800])
+    run(ql, kl, H, KV, D, BF, block=block, window=window, gap=5, seed=41)
+
+
+def test_cut_walks_are_the_same_every_time_and_in_a_given_workspace():
+    plan = bd.packed_plan([90, 5], [3000, 2500], heads=8, kv_heads=2, head_dim=128, dtype=BF)
+    q, k, v = (synth.normal((n, h, 128), 70 + h, BF).to(DEV) for n, h in ((95, 8), (5500, 2), (5500, 2)))
+    ws = torch.full((plan.fwd_workspace_bytes,), 0xff, dtype=torch.uint8, device=DEV)
+    o, lse = bd.packed_fwd(plan, q, k, v)
+    for w in (None, ws, ws):
+        o1, lse1 = bd.packed_fwd(plan, q, k, v, workspace=w)
+        assert torch.equal(o, o1) and torch.equal(lse, lse1)
+    with pytest.raises(bd.BdlmError):
+        bd.packed_fwd(plan, q, k, v, workspace=ws[:-256])
+    ref = packed(q, k, v, [(0, 90, 0, 3000), (90, 5, 3000, 2500)])
+    check("o", o, *ref["o"])
+    check("lse", lse, *ref["lse"])

@@ -101,3 +101,52 @@ def test_a_full_card_is_not_cut():
 
 def test_few_tiles_take_two_teams():
     assert check([64], [64], 4, 2, 128, torch.bfloat16, 1, 0)._record.teams == 2
+
+
+def fwd_items(p):
+    r = p._record
+    a = np.frombuffer(p._items.numpy().tobytes(), dtype=np.int32)
+    at = r.q_items + r.k_items + r.n_sums
+    a = a[8 * at:8 * (at + r.fwd_items + r.fwd_sums)].reshape(-1, 8)
+    return a[:r.fwd_items].tolist(), a[r.fwd_items:].tolist()
+
+
+@pytest.mark.parametrize("ql,kl,H,KV,block,window", [
+    ([1], [2500], 4, 1, 1, 0), ([70, 1, 3, 300], [2000, 1700, 0, 300], 4, 2, 1, 0), ([130, 40], [2400, 20], 3, 1, 1, 1900),
+    ([1800], [1700], 2, 2, 7, 0), ([3000, 10], [3000, 5000], 8, 2, 1, 0)])
+def test_forward_chunks_cover_each_walk_once(ql, kl, H, KV, block, window):
+    p = check(ql, kl, H, KV, 128, torch.bfloat16, block, window)
+    chunks, sums = fwd_items(p)
+    r, group = p._record, H // KV
+    heads = 4 if group % 4 == 0 else 2 if group % 2 == 0 else 1
+    qt = 128 // heads
+    assert r.fwd_items > r.q_items and r.teams == 1 and len(sums) == r.fwd_sums > 0
+    by_tile = {}
+    for a in chunks:
+        by_tile.setdefault(tuple(a[:5]), []).append(a[5:])
+    whole = items(p)[0]
+    assert sorted(by_tile) == sorted(map(tuple, whole[:, :5].tolist()))
+    slots = []
+    for (q0, n, _, m, t), parts in by_tile.items():
+        parts.sort()
+        assert parts[0][0] == 0 and parts[-1][1] == BIG and all(a[1] == b[0] for a, b in zip(parts, parts[1:]))
+        keys = walked(n, m, t * qt, min(n, (t + 1) * qt), block, window)
+        assert parts[-1][0] * 64 < keys + 64 or len(parts) == 1
+        if len(parts) > 1:
+            mine = [a[2] for a in parts]
+            assert mine == list(range(mine[0], mine[0] + len(mine)))
+            assert [q0, n, t, mine[0], len(mine)] in [x[:5] for x in sums]
+            slots += mine
+        else:
+            assert parts[0][2] == -1
+    assert sorted(slots) == list(range(r.fwd_slots))
+    rows = r.fwd_slots * (H // heads) * 128
+    assert p.fwd_workspace_bytes >= rows * 129 * 4
+
+
+def test_walks_that_fill_the_card_or_are_short_are_not_cut():
+    for ql, H in (([4000] * 8, 16), ([1000], 4), ([30] * 100, 8)):
+        p = bd.packed_plan(ql, heads=H, kv_heads=4, head_dim=128, dtype=torch.bfloat16, device="cpu")
+        assert p.fwd_workspace_bytes == 0 and p._record.fwd_items == 0
+    p = bd.packed_plan([1], [2500], heads=4, kv_heads=4, head_dim=64, dtype=torch.float32, device="cpu")
+    assert p.fwd_workspace_bytes == 0

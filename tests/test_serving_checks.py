@@ -113,7 +113,7 @@ def _rec(**kw):
 def _fwd(r, q=FAKE, qs=256, k=FAKE, ks=128, o=FAKE, lse=FAKE, pitch=8, items=FAKE):
     R = pm._Rows
     return bd.lib().bdlm_packed_fwd(ctypes.byref(r) if r is not None else None, items, R(q, qs), R(k, ks), R(FAKE, 128),
-                                    R(o, 256), lse, pitch, None)
+                                    R(o, 256), lse, pitch, None, 0, None)
 
 
 @host_only
