@@ -18,7 +18,7 @@ CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libbdlm_attn.so")
 BUILD_DIR = os.path.join(HERE, "_build")
 SOURCES = ["api.cpp", "packed_api.cpp", "cache_api.cpp", "fwd_bf16.hip", "fwd_f32.hip", "merge.hip", "bwd_bf16.hip", "bwd_dkdv.hip", "bwd_dq.hip",
-           "bwd_f32.hip", "packed_fwd_bf16.hip", "packed_fwd_sum.hip", "packed_fwd_f32.hip", "packed_bwd_dq.hip", "packed_bwd_dkdv.hip",
+           "bwd_f32.hip", "packed_fwd_bf16.hip", "packed_q_sums.hip", "packed_fwd_f32.hip", "packed_bwd_dq.hip", "packed_bwd_dkdv.hip",
            "packed_bwd_f32.hip", "prefix_bf16.hip", "prefix_f32.hip", "prefix_merge.hip", "cache_pages.hip"]
 ARCH = os.environ.get("BDLM_OFFLOAD_ARCH", "gfx950")
 # Per-source code-generation options.  The dK/dV kernel runs one wave per SIMD,

@@ -107,7 +107,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   if (row_ok) {
     const float z = qr.lse[((int64_t)it.b * H + h) * qr.bstride + my_row];
     lse2 = (z == -INFINITY) ? INFINITY : z * kLog2e;
-    if (half == 0) {
+    if (half == 0 && first_chunk(args, it)) {
       const int64_t si = ((int64_t)it.b * H + h) * qr.len + my_row;
       if (a.stats_form) {
         if constexpr (!kPacked) qr.delta[si] = -dsum;  // (packed calls: behind the walk)
@@ -217,6 +217,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // and three stages on long walks, 4 waves and two on short ones).
   KCur c0;
   c0.have = find_key_tile(a, 0, qr.stream, pq0, pq1, BN, c0.j, c0.t, c0.t1, c0.f0, c0.f1);
+  cut_walk(args, it, c0.t, c0.t1, c0.have);
+  [[maybe_unused]] const int walk0 = c0.t, walk1 = c0.t1;
   CopyCur cp = copy_seek(CopyCur{c0, any_src, 0});
 #pragma unroll
   for (int s = 0; s < NST - 1; ++s) {
@@ -384,7 +386,26 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
 
   if constexpr (kPacked) {
-    if (row_ok && half == 0) qr.delta[((int64_t)it.b * H + h) * qr.len + my_row] = -dl;
+    // D, from the chunk of the walk that has the row's first key (which may have corrected it)
+    const PackedItem& p = args.items[it.item];
+    int lo, wid;
+    lane_key_interval(a, 0, qr.stream, pq, lo, wid);
+    const int first = (lo - k_range(a, 0).pos0) / BN;
+    const bool mine = p.slot < 0 || (wid > 0 ? first >= walk0 && first < walk1 : p.n0 == 0);
+    if (row_ok && half == 0 && mine) qr.delta[((int64_t)it.b * H + h) * qr.len + my_row] = -dl;
+    if (p.slot >= 0) {  // a chunk's share of dQ
+      float* op = (float*)args.partials + q_partial_row<NW, HP>(args, it, w, l32) * D;
+#pragma unroll
+      for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+          f32x4 v;
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[e] = acc[d][g4 * 4 + e] * a.scale;
+          *(f32x4*)(op + 32 * d + 8 * g4 + 4 * half) = v;
+        }
+      return;
+    }
   }
   if (a.out_f32) {
     if (row_ok) {

@@ -194,12 +194,7 @@ __global__ __launch_bounds__(NT * NW * 64)
   if constexpr (NT > 1) {
     if (team == 1) c0 = next_one(c0);
   }
-  if constexpr (kIsPacked<Args> && NT == 1) {  // a chunk of the walk
-    const PackedItem& p = args.items[it.item];
-    c0.t1 = imin(c0.t1, c0.t + p.n1);
-    c0.t += p.n0;
-    c0.have = c0.have && c0.t < c0.t1;
-  }
+  if constexpr (NT == 1) cut_walk(args, it, c0.t, c0.t1, c0.have);
   // (teams: every wave runs as many rounds as team 0, the first to be dealt a tile, for the barriers)
   int rounds = NT > 1 ? (count_key_tiles(a, qr.stream, pq0, pq1, BN) + NT - 1) / NT : 0;
   CopyCur cp = copy_seek(CopyCur{c0, any_src, 0});
@@ -431,9 +426,8 @@ __global__ __launch_bounds__(NT * NW * 64)
   const bool empty = !(l_tot > 0.f);
   const float inv = empty ? 0.f : 1.f / l_tot;
   if constexpr (kIsPacked<Args> && NT == 1) {
-    const int slot = args.items[it.item].slot;
-    if (slot >= 0) {  // a chunk's partial output, [slot][heads / HP][128 rows of the waves][D]
-      const int64_t at = ((int64_t)slot * (a.heads / HP) + it.h / HP) * (NW * 32) + w * 32 + l32;
+    if (args.items[it.item].slot >= 0) {  // a chunk's partial output
+      const int64_t at = q_partial_row<NW, HP>(args, it, w, l32);
       if (!empty) {
         float* op = (float*)args.partials + at * D;
 #pragma unroll

@@ -18,14 +18,14 @@
 
 namespace bdlm {
 
-// A work item: a tile of query rows, or a chunk of its walk (forward; key tiles
+// A work item: a tile of query rows, or a chunk of its walk (bf16; key tiles
 // [n0, n1) of those it sees), or a chunk of the walk of a tile of keys (dK/dV;
 // steps [n0, n1)).  slot >= 0: where its partial sums go.
 // Sequence: rows [q0, q0 + q_len) of the queries, [k0, k0 + k_len) of the keys.
 struct PackedItem {
   int32_t q0, q_len, k0, k_len, tile, n0, n1, slot;
 };
-// A tile whose walk was cut (row0, len: its sequence's keys, forward: queries):
+// A tile whose walk was cut (row0, len: its sequence's rows):
 // its partial sums in slots [slot, slot + n).
 struct PackedSum {
   int32_t row0, len, tile, slot, n, pad0, pad1, pad2;
@@ -169,6 +169,7 @@ template <> constexpr inline bool kIsPacked<PackedView> = true;
 
 hipError_t launch_fwd_bf16(const PackedArgs& a, int head_dim, int teams, hipStream_t s);
 hipError_t launch_packed_fwd_sum(const PackedArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_packed_dq_sum(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_fwd_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dq_bf16(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dkdv(const PackedArgs& a, int head_dim, hipStream_t s);

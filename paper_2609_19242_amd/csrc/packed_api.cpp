@@ -117,6 +117,15 @@ PackedArgs packed_args(const bdlm_packed_plan& pl, int64_t lse_pitch) {
   return a;
 }
 
+// The chunks of query tiles in place of the whole ones (a.items: the plan's).
+void take_chunks(const bdlm_packed_plan& pl, PackedArgs& a) {
+  const PackedItem* const k_end = a.items + pl.q_items + pl.k_items;
+  a.items = reinterpret_cast<const PackedItem*>(reinterpret_cast<const PackedSum*>(k_end) + pl.n_sums);
+  a.n_items = pl.fwd_items;
+  a.sums = reinterpret_cast<const PackedSum*>(a.items + pl.fwd_items);
+  a.n_sums = pl.fwd_sums;
+}
+
 bdlm_status check_pitch(const bdlm_packed_plan& pl, int64_t pitch) {
   if (pitch < pl.q_rows || pitch > kMaxLen)
     return fail(BDLM_ERR_INVALID, "lse pitch %lld outside [%lld, 2^28]", (long long)pitch, (long long)pl.q_rows);
@@ -159,10 +168,11 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
              (it.sums.size() + it.fwd_sums.size()) * sizeof(PackedSum);
   const size_t part_rows = (size_t)it.fwd_slots * per * kQRowsShortBf16;
   pl.fwd_workspace_bytes = align256(part_rows * p->head_dim * sizeof(float)) + align256(part_rows * sizeof(float));
-  pl.workspace_bytes = 2 * packed_stats_bytes(pl) + (size_t)it.slots * p->kv_heads *
-                                                        (f32 ? kRowsF32 * sizeof(double)
-                                                             : kBwdKeysBf16 * sizeof(float)) *
-                                                        2 * p->head_dim;
+  // (dQ's partial sums are added up before the first of dK and dV are written: in the same place)
+  pl.workspace_bytes = 2 * packed_stats_bytes(pl) +
+                       std::max((size_t)it.slots * p->kv_heads *
+                                    (f32 ? kRowsF32 * sizeof(double) : kBwdKeysBf16 * sizeof(float)) * 2 * p->head_dim,
+                                (size_t)it.fwd_slots * per * kQRowsShortBf16 * p->head_dim * sizeof(float));
   if (items) {
     if (items_bytes < pl.bytes)
       return fail(BDLM_ERR_INVALID, "plan needs %zu bytes (got %zu)", pl.bytes, items_bytes);
@@ -203,11 +213,7 @@ bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdl
   a.items = static_cast<const PackedItem*>(items);
   a.n_items = plan->q_items;
   if (plan->fwd_items > 0) {
-    const PackedItem* const k_end = a.items + plan->q_items + plan->k_items;
-    a.items = reinterpret_cast<const PackedItem*>(reinterpret_cast<const PackedSum*>(k_end) + plan->n_sums);
-    a.n_items = plan->fwd_items;
-    a.sums = reinterpret_cast<const PackedSum*>(a.items + plan->fwd_items);
-    a.n_sums = plan->fwd_sums;
+    take_chunks(*plan, a);
     a.partials = workspace;
     a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_bytes(*plan));
   }
@@ -275,12 +281,15 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
   a.partials = ws + 2 * arr;
   a.items = static_cast<const PackedItem*>(items);
   a.n_items = plan->q_items;
+  if (plan->fwd_items > 0) take_chunks(*plan, a);
   // dQ first: it leaves the row statistics for dK/dV.
   hipError_t e = timed(kKPackedDq, stream, [&] {
-    return p.dtype == BDLM_BF16 ? launch_bwd_dq_bf16(a, p.head_dim, stream) : launch_bwd_dq_f32(a, p.head_dim, stream);
+    const hipError_t le =
+        p.dtype == BDLM_BF16 ? launch_bwd_dq_bf16(a, p.head_dim, stream) : launch_bwd_dq_f32(a, p.head_dim, stream);
+    return le != hipSuccess || a.n_sums == 0 ? le : launch_packed_dq_sum(a, p.head_dim, stream);
   });
   if (e != hipSuccess) return hip_fail(e, "packed dQ launch");
-  a.items += plan->q_items;
+  a.items = static_cast<const PackedItem*>(items) + plan->q_items;
   a.n_items = plan->k_items;
   a.sums = reinterpret_cast<const PackedSum*>(a.items + plan->k_items);
   a.n_sums = plan->n_sums;

@@ -14,7 +14,7 @@
 namespace bdlm {
 
 struct PackedPlanItems {
-  std::vector<PackedItem> q, k, fwd;  // fwd: the forward's, if some walks are cut (else q)
+  std::vector<PackedItem> q, k, fwd;  // fwd: in place of q, if some of its walks are cut
   std::vector<PackedSum> sums, fwd_sums;
   int32_t slots = 0, fwd_slots = 0;
   int32_t teams = 1;
@@ -33,15 +33,16 @@ constexpr int64_t kMinFwdUnit = 8, kFwdSumTiles = 10, kFwdSumTiles64 = 18;
 // Query tiles: 128 rows (16 in fp32) of one sequence, or as many fewer as a
 // tile has heads (packed_tile_heads), by the keys they walk.
 //
-// Forward, bf16: where few tiles have long walks (a piece of a long prompt, few
+// Forward and dQ, bf16: where few tiles have long walks (a piece of a long prompt, few
 // heads), the busiest CU's walks, not the card, set the time.  If they are longer
 // than the average load of a CU by more than partial outputs cost, walks are cut
 // into equal chunks of at most that load, a chunk per CU, whose outputs
-// packed_fwd_sum.hip joins (the factor is what a chunk's tiles take longer without a
-// second team).  32/8 heads, d 128, without and with cuts: 1 row behind 2,048 keys 33
+// packed_q_sums.hip joins (the factor is what a chunk's tiles take longer without a
+// second team; dQ, which has none, takes the forward's chunks).  32/8 heads, d 128,
+// without and with cuts: 1 row behind 2,048 keys 33
 // and 19 us, behind 8,192 109 and 22, behind 32,768 444 and 40; 256 rows 37 and 30, 119
 // and 59, 438 and 184; 512 rows behind 2,048 are left whole (42, 47 cut), 1,024 behind
-// 8,192 too (155, 193).  3,000 rows of 4/2 heads 45 and 31.  (Chunks that fill two
+// 8,192 too (155, 193).  3,000 rows of 4/2 heads 45 and 32, dQ 74 and 39.  (Chunks that fill two
 // workgroups a CU write twice the partial outputs: 256 rows behind 8,192 65 us.)
 //
 // Key tiles: 128 keys (16), by the steps of their walks.  The longest walk,
@@ -101,7 +102,7 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
   for (const Cost& c : q) out.q.push_back(c.it);
   const int64_t per = p.heads / tile_heads;  // workgroups of a query tile
 
-  // Chunks of the query tiles' walks (bf16 forward).
+  // Chunks of the query tiles' walks (bf16).
   std::stable_sort(walks.begin(), walks.end(), heavier);
   const int64_t fwd_longest = walks.empty() ? 0 : walks[0].cost;
   const int64_t wgs = (int64_t)walks.size() * per, fwd_average = (fwd_total * per + kCus - 1) / kCus;

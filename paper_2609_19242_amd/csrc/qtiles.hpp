@@ -58,6 +58,22 @@ __device__ inline bool q_tile_item(const PackedArgs& a, int wg, QTileItem& it) {
   return true;
 }
 
+// The key tiles [t, t1) of a packed item's chunk of its tile's walk [t, t1).
+__device__ inline void cut_walk(const AttnArgs&, const QTileItem&, int&, int&, bool&) {}
+__device__ inline void cut_walk(const PackedArgs& a, const QTileItem& it, int& t, int& t1, bool& have) {
+  const PackedItem& p = a.items[it.item];
+  t1 = imin(t1, t + p.n1);
+  t += p.n0;
+  have = have && t < t1;
+}
+__device__ inline bool first_chunk(const AttnArgs&, const QTileItem&) { return true; }
+__device__ inline bool first_chunk(const PackedArgs& a, const QTileItem& it) { return a.items[it.item].n0 == 0; }
+// The row of its partial sums, [slot][heads / HP][row of the waves], for row l32 of wave w.
+template <int NW, int HP>
+__device__ inline int64_t q_partial_row(const PackedArgs& a, const QTileItem& it, int w, int l32) {
+  return ((int64_t)a.items[it.item].slot * (a.heads / HP) + it.h / HP) * (NW * 32) + w * 32 + l32;
+}
+
 // Key tiles [t0, t1) of key range j that any query position in [pq0, pq1]
 // can see, and the sub-span [f0, f1) every one of them sees completely.
 template <class A>

@@ -252,11 +252,11 @@ def test_new_outputs_hold_zeros_in_rows_of_no_sequence(other):
 @pytest.mark.parametrize("H,KV,D", [(4, 1, 128), (4, 2, 64), (3, 1, 128), (2, 2, 64)])
 @pytest.mark.parametrize("ql,kl,block,window", [
     ([1], [2500], 1, 0), ([70, 1, 3], [2000, 1700, 0], 1, 0), ([200], [2300], 32, 0), ([130, 40], [2400, 20], 1, 1900),
-    ([1800], [1700], 1, 0), ([65], [4000], 5000, 0)])
+    ([1800], [1700], 1, 0), ([65], [4000], 5000, 0), ([1600], [1500], 4000, 0)])
 def test_few_rows_with_long_walks(ql, kl, block, window, H, KV, D):
     plan = bd.packed_plan(ql, kl, heads=H, kv_heads=KV, head_dim=D, dtype=BF, block_size=block, window=window)
-    # (27 key tiles are left whole at head_dim 64, where the products take half as long and the partial outputs do not)
-    assert plan.fwd_workspace_bytes > 0 or (D == 64 and ql == [1800])
+    # (24 and 27 key tiles are left whole at head_dim 64, where the products take half as long and the partial outputs do not)
+    assert plan.fwd_workspace_bytes > 0 or (D == 64 and ql in ([1800], [1600]))
     run(ql, kl, H, KV, D, BF, block=block, window=window, gap=5, seed=41)
 
 

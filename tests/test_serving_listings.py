@@ -7,7 +7,7 @@ import pytest
 
 from tests.asm_listing import BF16, F64, functions, kernel_resources, listing, product_hazards, scalar_offset_accesses
 
-SOURCES = ["packed_fwd_bf16.hip", "packed_fwd_sum.hip", "packed_bwd_dq.hip", "packed_bwd_dkdv.hip", "packed_fwd_f32.hip", "packed_bwd_f32.hip",
+SOURCES = ["packed_fwd_bf16.hip", "packed_q_sums.hip", "packed_bwd_dq.hip", "packed_bwd_dkdv.hip", "packed_fwd_f32.hip", "packed_bwd_f32.hip",
            "prefix_bf16.hip", "prefix_f32.hip"]
 
 
