@@ -173,15 +173,22 @@ def _torch_stream(stream, device) -> torch.cuda.Stream:
     return torch.cuda.ExternalStream(handle, device=device)
 
 
-def _launch(device, stream, call, *args):
-    """``call(*args, handle)``, with the handle of ``stream`` (default: the current stream of GPU ``device``) and with
-    that GPU current meanwhile; raises if it fails."""
+def _launch(owner, stream, call, *args):
+    """``call(*args, handle)`` for a plan or cache, with the handle of ``stream`` (default: the current stream of its
+    GPU) and with that GPU current meanwhile; raises if it fails."""
+    device = owner.gpu
     if device < 0:
         raise ValueError("the tensors must be on a GPU")
     if device != _current_gpu():
         with torch.cuda.device(device):
-            return _launch(device, stream, call, *args)
-    status = call(*args, _raw_stream(device) if stream is None else _stream(stream))
+            return _launch(owner, stream, call, *args)
+    handle = _raw_stream(device) if stream is None else _stream(stream)
+    if handle not in owner._streams:
+        # the caller may drop the plan or cache while its kernels are still running there
+        for t in owner._tensors:
+            t.record_stream(_torch_stream(handle, owner.device))
+        owner._streams.add(handle)
+    status = call(*args, handle)
     if status != 0:
         _check(status)
 

@@ -79,6 +79,7 @@ class Cache:
                               status.data_ptr(), self._work.data_ptr(), layers, pages, page_size, seqs, max_pages,
                               kv_heads, head_dim, code, 0)
         self._ref = ctypes.byref(self._record)
+        self._tensors, self._streams = (k, v, table, lens, refs, status, self._work), set()
 
     def __repr__(self):
         return (f"Cache(layers={self.layers}, pages={self.pages} x {self.page_size}, seqs={self.seqs} x {self.max_pages} "
@@ -122,7 +123,7 @@ def cache_grow(cache: Cache, seqs, counts, stream=None):
     c = _cache(cache)
     a = _list(c, "seqs", seqs)
     b = _list(c, "counts", counts, seqs.shape[0])
-    _launch(c.gpu, stream, lib().bdlm_cache_grow, c._ref, seqs.shape[0], a, b)
+    _launch(c, stream, lib().bdlm_cache_grow, c._ref, seqs.shape[0], a, b)
 
 
 def cache_fork(cache: Cache, parents, children, stream=None):
@@ -130,20 +131,20 @@ def cache_fork(cache: Cache, parents, children, stream=None):
     c = _cache(cache)
     a = _list(c, "parents", parents)
     b = _list(c, "children", children, parents.shape[0])
-    _launch(c.gpu, stream, lib().bdlm_cache_fork, c._ref, parents.shape[0], a, b)
+    _launch(c, stream, lib().bdlm_cache_fork, c._ref, parents.shape[0], a, b)
 
 
 def cache_free(cache: Cache, seqs, stream=None):
     """Empties sequences and gives back the pages that no other sequence holds."""
     c = _cache(cache)
     a = _list(c, "seqs", seqs)
-    _launch(c.gpu, stream, lib().bdlm_cache_free, c._ref, seqs.shape[0], a)
+    _launch(c, stream, lib().bdlm_cache_free, c._ref, seqs.shape[0], a)
 
 
 def cache_compact(cache: Cache, stream=None):
     """Moves live pages into the holes below them, so that the free pages are the last ones."""
     c = _cache(cache)
-    _launch(c.gpu, stream, lib().bdlm_cache_compact, c._ref)
+    _launch(c, stream, lib().bdlm_cache_compact, c._ref)
 
 
 def cache_write(cache: Cache, layer: int, seqs, counts, k, v, starts: Optional[torch.Tensor] = None, stream=None):
@@ -158,7 +159,7 @@ def cache_write(cache: Cache, layer: int, seqs, counts, k, v, starts: Optional[t
     rows = k.shape[0]
     if rows != v.shape[0]:
         raise ValueError(f"k has {rows} rows, v has {v.shape[0]}")
-    _launch(c.gpu, stream, lib().bdlm_cache_write, c._ref, layer, n, a, b, at, rows, rk, rv)
+    _launch(c, stream, lib().bdlm_cache_write, c._ref, layer, n, a, b, at, rows, rk, rv)
 
 
 def _check_q(c, q):
@@ -207,6 +208,6 @@ def prefix_attn(q, cache: Cache, layer: int, seqs, prefix: int = 0, block: bool 
     else:
         _workspace(workspace, 0, c.device, stream)
         nbytes = workspace.numel() * workspace.element_size()
-    _launch(c.gpu, stream, lib().bdlm_prefix_attn, c._ref, layer, R, a, n, H, prefix, 1 if block else 0, scale,
+    _launch(c, stream, lib().bdlm_prefix_attn, c._ref, layer, R, a, n, H, prefix, 1 if block else 0, scale,
             q.data_ptr(), o.data_ptr(), lse.data_ptr(), workspace.data_ptr(), nbytes)
     return o, lse

@@ -58,6 +58,7 @@ class PackedPlan:
     def __init__(self, record: _Plan, items: torch.Tensor, dtype: torch.dtype, held=(0, 0)):
         self._record, self._items, self.dtype = record, items, dtype
         self._held = held  # query and key rows that belong to a sequence
+        self._tensors, self._streams = (items,), set()
         self._ref, self._at = ctypes.byref(record), items.data_ptr()
         p = record.problem
         self.heads, self.kv_heads, self.head_dim = p.heads, p.kv_heads, p.head_dim
@@ -179,7 +180,7 @@ def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, workspace
     if plan.fwd_workspace_bytes:
         workspace = _workspace(workspace, plan.fwd_workspace_bytes, plan.device, stream)
         at, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _launch(plan.gpu, stream, lib().bdlm_packed_fwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n, at, nbytes)
+    _launch(plan, stream, lib().bdlm_packed_fwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n, at, nbytes)
     return o, lse
 
 
@@ -206,7 +207,7 @@ def packed_bwd(plan: PackedPlan, q, k, v, o, lse, do, out: Optional[tuple] = Non
         dq, dk, dv = out
         outs = _as_long(plan, "dq", dq, H, n), _as_long(plan, "dk", dk, KV, nk), _as_long(plan, "dv", dv, KV, nv)
     workspace = _workspace(workspace, plan.workspace_bytes, plan.device, stream)
-    _launch(plan.gpu, stream, lib().bdlm_packed_bwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n, rdo,
+    _launch(plan, stream, lib().bdlm_packed_bwd, plan._ref, plan._at, rq, rk, rv, ro, lse.data_ptr(), n, rdo,
             *outs, workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return dq, dk, dv
 

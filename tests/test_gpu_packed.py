@@ -273,3 +273,23 @@ def test_cut_walks_are_the_same_every_time_and_in_a_given_workspace():
     ref = packed(q, k, v, [(0, 90, 0, 3000), (90, 5, 3000, 2500)])
     check("o", o, *ref["o"])
     check("lse", lse, *ref["lse"])
+
+
+def test_a_plan_dropped_while_its_kernels_run_elsewhere():
+    q, k, v = (synth.normal((4000, h, 128), 80 + h, BF).to(DEV) for h in (8, 2, 2))
+    kw = dict(heads=8, kv_heads=2, head_dim=128, dtype=BF)
+    o, lse = bd.packed_fwd(bd.packed_plan([4000], **kw), q, k, v)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    out = torch.zeros_like(o), torch.zeros_like(lse)
+    torch.cuda.synchronize()
+    for use in (dict(stream=side), dict(stream=side.cuda_stream)):
+        plan = bd.packed_plan([4000], **kw)
+        n = plan._items.numel()
+        for _ in range(20):  # (the last of these still waits when the plan is dropped)
+            bd.packed_fwd(plan, q, k, v, out=out, **use)
+        del plan
+        other = [torch.full((n,), 0xff, dtype=torch.uint8, device=DEV) for _ in range(8)]
+        torch.cuda.synchronize()
+        assert torch.equal(out[0], o) and torch.equal(out[1], lse)
+        del other
