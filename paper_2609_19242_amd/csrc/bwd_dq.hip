@@ -294,8 +294,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
         // here.  D = sum_j P_ij dP_ij, so that sum_j dS_ij = 0; the D formed from
         // the rounded O misses it by up to 2^-9 |dO||O|, which is much of dS where
         // a row has few keys (one key: all of it).  (D lies in dpacc already.)
-        if constexpr (kPacked) {
-          const int kstart = k_range(a, j).pos0 + t * BN - lane_lo;
+        const int kstart = k_range(a, j).pos0 + t * BN - lane_lo;
+        if (kPacked && __builtin_amdgcn_ballot_w64(lane_w > 0 && kstart <= 0 && kstart + BN >= lane_w) != 0) {
           float rest = 0.f, z = lse2;
           asm volatile("" : "+v"(z));  // (or the compiler keeps these exponentials for the ones below, and spills)
 #pragma unroll
