@@ -168,7 +168,7 @@ template <> constexpr inline bool kIsPacked<PackedArgs> = true;
 template <> constexpr inline bool kIsPacked<PackedView> = true;
 
 hipError_t launch_fwd_bf16(const PackedArgs& a, int head_dim, int teams, hipStream_t s);
-hipError_t launch_packed_fwd_sum(const PackedArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_packed_fwd_sum(const PackedArgs& a, int head_dim, int slots, hipStream_t s);
 hipError_t launch_packed_dq_sum(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_fwd_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dq_bf16(const PackedArgs& a, int head_dim, hipStream_t s);

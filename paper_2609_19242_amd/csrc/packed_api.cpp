@@ -229,7 +229,7 @@ bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdl
   const hipError_t e = timed(kKPackedFwd, stream, [&] {
     const hipError_t le = p.dtype == BDLM_BF16 ? launch_fwd_bf16(a, p.head_dim, plan->teams, stream)
                                                : launch_fwd_f32(a, p.head_dim, stream);
-    return le != hipSuccess || a.n_sums == 0 ? le : launch_packed_fwd_sum(a, p.head_dim, stream);
+    return le != hipSuccess || a.n_sums == 0 ? le : launch_packed_fwd_sum(a, p.head_dim, plan->fwd_slots, stream);
   });
   return e == hipSuccess ? BDLM_OK : hip_fail(e, "packed forward launch");
 }

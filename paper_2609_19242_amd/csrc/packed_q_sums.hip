@@ -1,6 +1,5 @@
 // The chunks' partial sums of query tiles whose walks were cut (packed_plan.hpp
-// says which), gfx950: the forward's outputs joined (partials.hpp), a wave per
-// row and head; dQ's shares added in the chunks' order, D / 4 lanes per row and
+// says which), gfx950: the forward's outputs joined (partials.hpp); dQ's shares added in the chunks' order, D / 4 lanes per row and
 // head.  Bound by the launch and by reading, 64 KB per chunk of 128 rows at d 128.
 #include "packed.hpp"
 #include "partials.hpp"
@@ -29,14 +28,18 @@ __device__ __forceinline__ CutRow cut_row(const PackedArgs& a, int tile_heads, i
   return x;
 }
 
-template <int D>
+template <int D, bool FEW>
 __global__ __launch_bounds__(256) void packed_fwd_sum_kernel(const PackedArgs a, const int tile_heads) {
-  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const CutRow c = cut_row(a, tile_heads, blockIdx.x >> 5, (blockIdx.x & 31) * 4 + w);
+  constexpr int LPR = JoinedRow<D>::LPR, ROWS = FEW ? 256 / LPR : 4, WGS = kQRowsShortBf16 / ROWS;
+  const int lane = FEW ? threadIdx.x % LPR : threadIdx.x & 63;
+  const int item = blockIdx.x / WGS, r = (blockIdx.x - item * WGS) * ROWS +
+                                         (FEW ? (int)threadIdx.x / LPR : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  const CutRow c = cut_row(a, tile_heads, item, r);
   if (c.row < 0) return;
-  const JoinedRow<D> x = join_partials<D>((const float*)a.partials, a.part_lse,
-                                          [&](int j) { return c.first + j * c.step; }, c.n, lane);
-  if (lane >= JoinedRow<D>::LPR) return;
+  auto at = [&](int j) { return c.first + j * c.step; };
+  const float* const o = (const float*)a.partials;
+  const JoinedRow<D> x = FEW ? join_few<D>(o, a.part_lse, at, c.n, lane) : join_partials<D>(o, a.part_lse, at, c.n, lane);
+  if (lane >= LPR) return;
   bf16x4 y;
 #pragma unroll
   for (int e = 0; e < 4; ++e) y[e] = to_bf16(x.x[e]);
@@ -70,13 +73,20 @@ __global__ __launch_bounds__(256) void packed_dq_sum_kernel(const PackedArgs a, 
   *(bf16x4*)((bf16*)a.dq + c.token * a.dqs + (int64_t)c.head * D + col) = y;
 }
 
+template <int D>
+void launch_fwd_sum(const PackedArgs& a, bool few, hipStream_t s) {
+  const int heads = packed_tile_heads(a.group), n = a.n_sums * (a.heads / heads);
+  const dim3 grid((unsigned)(n * (kQRowsShortBf16 / (few ? 256 / JoinedRow<D>::LPR : 4)))), threads(256);
+  if (few) hipLaunchKernelGGL((packed_fwd_sum_kernel<D, true>), grid, threads, 0, s, a, heads);
+  else hipLaunchKernelGGL((packed_fwd_sum_kernel<D, false>), grid, threads, 0, s, a, heads);
+}
+
 }  // namespace
 
-hipError_t launch_packed_fwd_sum(const PackedArgs& a, int head_dim, hipStream_t s) {
-  const int heads = packed_tile_heads(a.group);
-  const dim3 grid((unsigned)(a.n_sums * (a.heads / heads) * 32)), threads(256);
-  if (head_dim == 128) hipLaunchKernelGGL((packed_fwd_sum_kernel<128>), grid, threads, 0, s, a, heads);
-  else hipLaunchKernelGGL((packed_fwd_sum_kernel<64>), grid, threads, 0, s, a, heads);
+// slots: of all cut tiles together
+hipError_t launch_packed_fwd_sum(const PackedArgs& a, int head_dim, int slots, hipStream_t s) {
+  const bool few = slots <= (int64_t)a.n_sums * kFewParts;
+  head_dim == 128 ? launch_fwd_sum<128>(a, few, s) : launch_fwd_sum<64>(a, few, s);
   return hipGetLastError();
 }
 

@@ -1,7 +1,7 @@
 // The chunks' partial outputs of attention over a paged cache (cache.hpp)
 // joined (partials.hpp), gfx950.
-// Bound by reading the partials (16,384 rows of 128, 4 chunks: 10.7 us, 3.9 TB/s;
-// 2,048 rows, up to 10 chunks: 4.8 us).
+// Bound by reading the partials (16,384 rows of 128, 4 chunks: 8.1 us, 4.6 TB/s;
+// 2,048 rows, up to 10 chunks: 5.0 us).
 #include "cache.hpp"
 #include "partials.hpp"
 
@@ -9,15 +9,19 @@ namespace bdlm {
 
 namespace {
 
-template <int D, bool BF16>
+template <int D, bool BF16, bool FEW>
 __global__ __launch_bounds__(256) void prefix_merge_kernel(const PrefixArgs a) {
-  const int lane = threadIdx.x & 63;
+  constexpr int LPR = JoinedRow<D>::LPR, RPW = FEW ? 64 / LPR : 1;  // rows per wave
   const int64_t total = (int64_t)a.requests * a.rows * a.heads;
-  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = FEW ? threadIdx.x % LPR : threadIdx.x & 63;
+  const int64_t row = ((int64_t)blockIdx.x * 4 + w) * RPW + (FEW ? (threadIdx.x & 63) / LPR : 0);
   if (row >= total) return;
-  const JoinedRow<D> r = join_partials<D>(a.part_o, a.part_lse, [&](int j) { return j * total + row; },
-                                          a.prefix_chunks + a.own_chunks, lane);
-  if (lane >= JoinedRow<D>::LPR) return;
+  const int parts = a.prefix_chunks + a.own_chunks;
+  auto at = [&](int j) { return j * total + row; };
+  const JoinedRow<D> r = FEW ? join_few<D>(a.part_o, a.part_lse, at, parts, lane)
+                             : join_partials<D>(a.part_o, a.part_lse, at, parts, lane);
+  if (lane >= LPR) return;
   if constexpr (BF16) {
     bf16x4 y;
 #pragma unroll
@@ -35,19 +39,22 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(const PrefixArgs a) {
   }
 }
 
+template <int D, bool BF16>
+void launch(const PrefixArgs& a, int64_t rows, hipStream_t s) {
+  const bool few = a.prefix_chunks + a.own_chunks <= kFewParts;
+  const int per = few ? 4 * (64 / JoinedRow<D>::LPR) : 4;  // rows of a workgroup
+  const dim3 grid((unsigned)((rows + per - 1) / per)), threads(256);
+  if (few) hipLaunchKernelGGL((prefix_merge_kernel<D, BF16, true>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((prefix_merge_kernel<D, BF16, false>), grid, threads, 0, s, a);
+}
+
 }  // namespace
 
 hipError_t launch_prefix_merge(const PrefixArgs& a, int head_dim, int is_bf16, hipStream_t s) {
   const int64_t rows = (int64_t)a.requests * a.rows * a.heads;
-  const dim3 grid((unsigned)((rows + 3) / 4)), threads(256);
   if (rows == 0) return hipSuccess;
-  if (head_dim == 128) {
-    if (is_bf16) hipLaunchKernelGGL((prefix_merge_kernel<128, true>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((prefix_merge_kernel<128, false>), grid, threads, 0, s, a);
-  } else {
-    if (is_bf16) hipLaunchKernelGGL((prefix_merge_kernel<64, true>), grid, threads, 0, s, a);
-    else hipLaunchKernelGGL((prefix_merge_kernel<64, false>), grid, threads, 0, s, a);
-  }
+  if (head_dim == 128) is_bf16 ? launch<128, true>(a, rows, s) : launch<128, false>(a, rows, s);
+  else is_bf16 ? launch<64, true>(a, rows, s) : launch<64, false>(a, rows, s);
   return hipGetLastError();
 }
 
