@@ -9,7 +9,7 @@
 //
 // What bounds them is what bounds the joint calls.  Measured, 32/8 heads: 30K
 // rows of prompts with up to 9K earlier keys, d 128, forward 4.29 ms (1,115
-// TFLOP/s); 11 documents of 130 to 2,500 rows, forward 133 us (860), dQ 191 (900
+// TFLOP/s); 11 documents of 130 to 2,500 rows, forward 133 us (860), dQ 187 (920
 // with what it forms again), dK/dV 240 (955) and 5 for the sums; 48 prompts of up to
 // 2,013 rows at d 64 139 us (the vector units 88% busy).
 #pragma once
