@@ -293,3 +293,38 @@ def test_a_plan_dropped_while_its_kernels_run_elsewhere():
         torch.cuda.synchronize()
         assert torch.equal(out[0], o) and torch.equal(out[1], lse)
         del other
+
+
+def test_two_graphs_of_cut_walks_share_their_workspaces():
+    H, KV, D = 8, 2, 128
+    plans = [bd.packed_plan(ql, kl, heads=H, kv_heads=KV, head_dim=D, dtype=BF) for ql, kl in (([90, 5], [3000, 2500]),
+                                                                                              ([40], [4000]))]
+    assert all(p.fwd_workspace_bytes > 0 for p in plans)
+    ws = torch.empty(max(max(p.fwd_workspace_bytes, p.workspace_bytes) for p in plans), dtype=torch.uint8, device=DEV)
+    q, do = (synth.normal((95, H, D), 90 + i, BF).to(DEV) for i in range(2))
+    k, v = (synth.normal((5500, KV, D), 92 + i, BF).to(DEV) for i in range(2))
+
+    def step(p, w):
+        o, lse = bd.packed_fwd(p, q, k, v, workspace=w)
+        return (o, lse) + bd.packed_bwd(p, q, k, v, o, lse, do, workspace=w)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        for p in plans:
+            step(p, ws)
+    torch.cuda.current_stream().wait_stream(s)
+    graphs, outs = [], []
+    for p in plans:
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[-1]):
+            outs.append(step(p, ws))
+    for i in range(3):
+        q.copy_(synth.normal(q.shape, 95 + i, BF))
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        for p, out in zip(plans, outs):
+            want = step(p, None)
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, want))
