@@ -79,10 +79,12 @@ bdlm_status done(hipError_t e, const char* what) { return e == hipSuccess ? BDLM
 // rows (all heads of all requests), so few rows take shorter chunks.  Times below
 // with keys that no cache holds yet, 32 heads on 8 KV heads, where not said otherwise.
 // The prefix: long enough that its tiles of rows give every workgroup slot one
-// item, at least half a key per query row within [512, 1024] (one request, 16,000
-// tokens: chunks of 256 keys 25 us, 512 23, 1,024 29; 64 requests, 8,192 tokens, read
-// again: 2,048 keys 56 us, 1,024 44, 512 54; 16,384 rows, 16K tokens, 4 KV heads, one
-// item per slot: 4,096 keys 173 us, 2,048 185, 8,192 197).
+// item, at least half a key per query row up to 1,024, but no more than leave
+// kFewItems items, and at least a 24th of the prefix within [256, 512] (one request,
+// 16,000 tokens: chunks of 256 keys 25 us, 512 23, 1,024 29; 16 requests, 12/2 heads,
+// 2,000 tokens: 256 16.5 us, 512 20; 64 requests, 4,000 tokens: 512 27 us, 1,024 33;
+// 8,192 tokens and up to 1,500 of their own: 1,024 54.5, 512 59; 16,384 rows, 16K
+// tokens, 4 KV heads, one item per slot: 4,096 keys 173 us, 2,048 185, 8,192 197).
 // A request's own keys: as many keys per query row, at least kOwnPerBase per
 // (KV head, request, tile), within [512, 1024] (one request of 32,000 keys: chunks of
 // 256 43 us, 512 35, 768 39; 8 of 300 to 6,000: 33, 28, 30; 16 of 100 to 2,000 take
@@ -101,7 +103,7 @@ bdlm_status done(hipError_t e, const char* what) { return e == hipSuccess ? BDLM
 // per item).  4 requests of 64 rows, 32/8 heads, behind 16K tokens, with up to
 // 4,000 more: 111 -> 101 us; 20 of 32 rows behind 9,000 with 2,000: 145 -> 135;
 // 10 of 24 behind 5,000 with 1,000: 51 -> 51.
-constexpr int64_t kSlots = 2 * kCus, kOwnPerBase = 3, kOwnWhole = 512, kMaxOwnItems = 4096;
+constexpr int64_t kSlots = 2 * kCus, kFewItems = 128, kOwnPerBase = 3, kOwnWhole = 512, kMaxOwnItems = 4096;
 constexpr int64_t kFoldBytes = 8 << 20;
 
 bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int32_t heads, int64_t prefix,
@@ -127,8 +129,9 @@ bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int
   auto up64 = [](int64_t x) { return (x + 63) / 64 * 64; };
   auto within = [](int64_t x, int64_t lo, int64_t hi) { return std::min(std::max(x, lo), hi); };
   const int64_t row_min = requests * rows * heads / 2;
-  const int64_t pc = std::min(std::max(up64(within(row_min, 512, 1024)),
-                                       up64(c->kv_heads * pt * prefix / kSlots)),
+  const int64_t low = within(prefix / 24, 256, 512);
+  const int64_t want = std::min(within(row_min, low, 1024), std::max(low, c->kv_heads * pt * prefix / kFewItems));
+  const int64_t pc = std::min(std::max(up64(want), up64(c->kv_heads * pt * prefix / kSlots)),
                               std::min(limit, up64(prefix + 1)));
   a.prefix_chunk = (int32_t)pc;
   a.prefix_chunks = (int32_t)((prefix + pc - 1) / pc);
