@@ -287,7 +287,9 @@ int64_t bdlm_visible_pairs(const bdlm_problem* p, int32_t n_q, const bdlm_range*
  * j >= e - window.  Rows at negative positions (q_len > k_len) see nothing.
  * A row that sees no key gets O = 0, LSE = -inf and dQ = 0; a key that no row
  * sees gets dK = dV = 0.  Rows that belong to no sequence are neither read nor
- * written.
+ * written.  The other rows must be finite: hidden pairs enter products as 0 times
+ * their values, so a NaN or infinity in a key may reach rows of its sequence that
+ * do not see it (keys that no row sees may hold anything in bf16 and fp32 alike).
  *
  *   Q, O, dO, dQ : [rows][heads][head_dim], K, V, dK, dV : [rows][kv_heads][head_dim],
  *     rows `stride` elements apart (a multiple of 16 bytes, at most 2^20), so
@@ -427,7 +429,8 @@ bdlm_status bdlm_cache_write(const bdlm_cache* c, int64_t layer, int64_t n, cons
  *   q, o : [requests][rows][heads][head_dim] in the cache's dtype
  *   lse  : [requests][heads][rows] fp32, natural log
  * Rows that see nothing (also: of a sequence number out of range) get O = 0
- * and LSE = -inf.  A page number outside the cache reads as rows of zeros, and
+ * and LSE = -inf.  Keys and values of tokens that a sequence holds must be finite,
+ * as in packed calls; rows of pages behind its last token may hold anything.  A page number outside the cache reads as rows of zeros, and
  * lens are taken between 0 and what a table holds.
  * workspace: bdlm_prefix_attn_workspace_bytes() bytes, 256-byte aligned, contents ignored on
  * entry; calls that may overlap in time need one each.
