@@ -78,8 +78,9 @@ bdlm_status done(hipError_t e, const char* what) { return e == hipSuccess ? BDLM
 // Chunks trade balance against partial sums, whose cost grows with the query
 // rows (all heads of all requests), so few rows take shorter chunks.  Times below
 // with keys that no cache holds yet, 32 heads on 8 KV heads, where not said otherwise.
-// The prefix: long enough that its tiles of rows give every workgroup slot one
-// item, at least half a key per query row up to 1,024, but no more than leave
+// The prefix: long enough that its tiles of rows give every workgroup slot that the
+// requests' own items leave (half of them at least) one item (16 requests, 16,000
+// tokens: 40 us with one for every slot, 35; 40 requests 44, 41), at least half a key per query row up to 1,024, but no more than leave
 // kFewItems items, and at least a 24th of the prefix within [256, 512] (one request,
 // 16,000 tokens: chunks of 256 keys 25 us, 512 23, 1,024 29; 16 requests, 12/2 heads,
 // 2,000 tokens: 256 16.5 us, 512 20; 64 requests, 4,000 tokens: 512 27 us, 1,024 33;
@@ -131,7 +132,7 @@ bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int
   const int64_t row_min = requests * rows * heads / 2;
   const int64_t low = within(prefix / 24, 256, 512);
   const int64_t want = std::min(within(row_min, low, 1024), std::max(low, c->kv_heads * pt * prefix / kFewItems));
-  const int64_t pc = std::min(std::max(up64(want), up64(c->kv_heads * pt * prefix / kSlots)),
+  const int64_t pc = std::min(std::max(up64(want), up64(c->kv_heads * pt * prefix / std::max(kSlots - base, kSlots / 2))),
                               std::min(limit, up64(prefix + 1)));
   a.prefix_chunk = (int32_t)pc;
   a.prefix_chunks = (int32_t)((prefix + pc - 1) / pc);
