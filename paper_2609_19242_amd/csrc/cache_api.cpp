@@ -75,24 +75,28 @@ bdlm_status done(hipError_t e, const char* what) { return e == hipSuccess ? BDLM
 
 // How the keys of an attention call are cut into chunks and its rows into tiles.
 //
-// Chunks trade balance against partial sums, whose cost grows with the query
-// rows (all heads of all requests), so few rows take shorter chunks.  Times below
-// with keys that no cache holds yet, 32 heads on 8 KV heads, where not said otherwise.
-// The prefix: long enough that its tiles of rows give every workgroup slot that the
-// requests' own items leave (half of them at least) one item (16 requests, 16,000
-// tokens: 40 us with one for every slot, 35; 40 requests 44, 41), at least half a key per query row up to 1,024, but no more than leave
-// kFewItems items, and at least a 24th of the prefix within [256, 512] (one request,
+// Chunks trade balance against partial sums, whose cost grows with the query rows
+// (all heads of all requests), so few rows take shorter chunks.  Times below with
+// keys that no cache holds yet, 32 heads on 8 KV heads, where not said otherwise.
+//
+// The prefix: long enough that its tiles of rows give one item to every workgroup
+// slot that the requests' own items leave, half of them at least (16 requests, 16,000
+// tokens: one for every slot 40 us, so 35; 40 requests 44, 41; 16,384 rows, 16K
+// tokens, 4 KV heads: 4,096 keys, one item per slot, 173 us, 2,048 185, 8,192 197).
+// Below that, half a key per query row up to 1,024 keys, but no more than leave
+// kFewItems items, and a 24th of the prefix within [256, 512] at least (one request,
 // 16,000 tokens: chunks of 256 keys 25 us, 512 23, 1,024 29; 16 requests, 12/2 heads,
 // 2,000 tokens: 256 16.5 us, 512 20; 64 requests, 4,000 tokens: 512 27 us, 1,024 33;
-// 8,192 tokens and up to 1,500 of their own: 1,024 54.5, 512 59; 16,384 rows, 16K
-// tokens, 4 KV heads, one item per slot: 4,096 keys 173 us, 2,048 185, 8,192 197).
+// 8,192 tokens and up to 1,500 of their own: 1,024 54.5, 512 59).
+//
 // A request's own keys: as many keys per query row, at least kOwnPerBase per
 // (KV head, request, tile), within [512, 1024] (one request of 32,000 keys: chunks of
 // 256 43 us, 512 35, 768 39; 8 of 300 to 6,000: 33, 28, 30; 16 of 100 to 2,000 take
 // 384 sooner, 22 us, than 512, 24; 16 of 32 rows and up to 2,000 keys, 32/4 heads:
-// 1,024 39 us, 1,536 47; 64 of 4,000 keys: 196, 193), their number limited by the workgroups
-// that find nothing to do where a sequence is shorter than its table
+// 1,024 39 us, 1,536 47; 64 of 4,000 keys: 196, 193), their number limited by the
+// workgroups that find nothing to do where a sequence is shorter than its table
 // (kMaxOwnItems).  Tables of up to kOwnWhole keys: one chunk, which needs no sums.
+//
 // A prefix that would save less than kFoldBytes of reading is not kept apart:
 // the requests' own keys then start at 0, and short ones need no partial sums.
 // Nor is one whose requests fill tiles of rows by themselves, since each tile
@@ -101,9 +105,9 @@ bdlm_status done(hipError_t e, const char* what) { return e == hipSuccess ? BDLM
 // chunks, so that no short item of a request's own keys runs after the prefix's
 // long ones.  Their number: the least of rounds of items times keys per chunk plus
 // the partial sums (at 128 rows and head_dim 128, three quarters of a key's time
-// per item).  4 requests of 64 rows, 32/8 heads, behind 16K tokens, with up to
-// 4,000 more: 111 -> 101 us; 20 of 32 rows behind 9,000 with 2,000: 145 -> 135;
-// 10 of 24 behind 5,000 with 1,000: 51 -> 51.
+// per item).  4 requests of 64 rows behind 16K tokens, with up to 4,000 more: 111 ->
+// 101 us; 20 of 32 rows behind 9,000 with 2,000: 145 -> 135; 10 of 24 (40/8 heads)
+// behind 5,000 with 1,000: 51 -> 51.
 constexpr int64_t kSlots = 2 * kCus, kFewItems = 128, kOwnPerBase = 3, kOwnWhole = 512, kMaxOwnItems = 4096;
 constexpr int64_t kFoldBytes = 8 << 20;
 
