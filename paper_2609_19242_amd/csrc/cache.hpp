@@ -64,6 +64,7 @@ struct PrefixArgs {
 };
 constexpr int kPrefixTableEntries = 2048;  // pages of a chunk at most
 constexpr int kPrefixGroups = 1024;        // bf16, pages of whole groups of 16 tokens: groups of a chunk at most
+constexpr int kShortJoin = 16;             // parts whose outputs are joined the short way (kFewParts)
 constexpr int kPrefixSharedRows = 128, kPrefixWaveRows = 32, kPrefixRowsF32 = 16;
 
 hipError_t launch_prefix_bf16(const PrefixArgs& a, int head_dim, hipStream_t s);

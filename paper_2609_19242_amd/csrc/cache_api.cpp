@@ -80,9 +80,13 @@ bdlm_status done(hipError_t e, const char* what) { return e == hipSuccess ? BDLM
 // keys that no cache holds yet, 32 heads on 8 KV heads, where not said otherwise.
 //
 // The prefix: long enough that its tiles of rows give one item to every workgroup
-// slot that the requests' own items leave, half of them at least (16 requests, 16,000
+// slot that the requests' own items leave (items that tables of fewer than 512 keys
+// beside the prefix hold count for less), half of them at least (16 requests, 16,000
 // tokens: one for every slot 40 us, so 35; 40 requests 44, 41; 16,384 rows, 16K
-// tokens, 4 KV heads: 4,096 keys, one item per slot, 173 us, 2,048 185, 8,192 197).
+// tokens, 4 KV heads: 4,096 keys, one item per slot, 173 us, 2,048 185, 8,192 197);
+// and so few chunks, up to 1,024 keys each, that their sums take the short way
+// (kShortJoin) where that leaves half the slots an item (24 requests, 16/16 heads,
+// 16,000 tokens: 512 keys 43 us, 1,024 38).
 // Below that, half a key per query row up to 1,024 keys, but no more than leave
 // kFewItems items, and a 24th of the prefix within [256, 512] at least (one request,
 // 16,000 tokens: chunks of 256 keys 25 us, 512 23, 1,024 29; 16 requests, 12/2 heads,
@@ -136,7 +140,9 @@ bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int
   const int64_t row_min = requests * rows * heads / 2;
   const int64_t low = within(prefix / 24, 256, 512);
   const int64_t want = std::min(within(row_min, low, 1024), std::max(low, c->kv_heads * pt * prefix / kFewItems));
-  const int64_t pc = std::min(std::max(up64(want), up64(c->kv_heads * pt * prefix / std::max(kSlots - base, kSlots / 2))),
+  const int64_t slots = std::max(kSlots - base * std::min<int64_t>(own, 512) / 512, kSlots / 2);
+  const int64_t joins = c->kv_heads * pt * kShortJoin >= kSlots / 2 ? std::min<int64_t>(prefix / (kShortJoin - 2), 1024) : 0;
+  const int64_t pc = std::min(up64(std::max({want, c->kv_heads * pt * prefix / slots, joins})),
                               std::min(limit, up64(prefix + 1)));
   a.prefix_chunk = (int32_t)pc;
   a.prefix_chunks = (int32_t)((prefix + pc - 1) / pc);

@@ -9,6 +9,8 @@ namespace bdlm {
 
 namespace {
 
+static_assert(kShortJoin == kFewParts, "the plan's number is the kernel's");
+
 template <int D, bool BF16, bool FEW>
 __global__ __launch_bounds__(256) void prefix_merge_kernel(const PrefixArgs a) {
   constexpr int LPR = JoinedRow<D>::LPR, RPW = FEW ? 64 / LPR : 1;  // rows per wave
