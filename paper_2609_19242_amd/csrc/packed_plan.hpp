@@ -6,6 +6,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <functional>
 #include <vector>
 
 #include "packed.hpp"
@@ -27,6 +28,8 @@ constexpr size_t kMaxPackedPartials = (size_t)256 << 20;
 
 // Key tiles of the forward's chunks at least; what partial outputs and their sums cost, in key tiles.
 constexpr int64_t kMinFwdUnit = 8, kFwdSumTiles = 10, kFwdSumTiles64 = 18;
+// What a workgroup's start-up costs, in key tiles.
+constexpr int64_t kStartTiles = 3;
 
 // Work items, heaviest first: a workgroup that starts late should be short.
 //
@@ -44,6 +47,13 @@ constexpr int64_t kMinFwdUnit = 8, kFwdSumTiles = 10, kFwdSumTiles64 = 18;
 // and 59, 438 and 184; 512 rows behind 2,048 are left whole (42, 47 cut), 1,024 behind
 // 8,192 too (155, 193).  3,000 rows of 4/2 heads 45 and 32, dQ 74 and 39.  (Chunks that fill two
 // workgroups a CU write twice the partial outputs: 256 rows behind 8,192 65 us.)
+//
+// Two teams per workgroup (fwd_bf16.hip): up to a workgroup per CU, as in joint
+// calls, and up to two where a CU that takes them one after the other, as it gets
+// free, ends before one that holds two at once: with uneven walks (prompts of 1,355
+// rows, 24/8 heads, 288 workgroups 35 -> 27 us; 2,213, 600 and 152, 16/16 heads, 54
+// -> 41; 3,000, 16/4 heads, 69 -> 53; 2,048, 32/8 heads 51 -> 46), not with even or
+// short ones (8 of 500, 16/4 heads 20, 23; 1,000 and 800 behind 4,000 140, 149).
 //
 // Key tiles: 128 keys (16), by the steps of their walks.  The longest walk,
 // the first keys' of the longest sequence, sets the time when there are few;
@@ -113,6 +123,20 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
     for (int64_t i = 0; i < wgs; i += kCus) busiest += walks[i / per].cost;
   else
     busiest = std::max(fwd_longest, fwd_average);
+  bool teams = !f32 && wgs <= kTeamWgs;
+  if (!f32 && wgs > kTeamWgs && wgs <= 2 * kTeamWgs) {  // one workgroup of two teams per CU, the next when it ends
+    std::vector<int64_t> load(kCus, 0);  // (a heap, the least loaded CU first)
+    int64_t most = 0;
+    for (int64_t i = 0; i < wgs; ++i) {
+      std::pop_heap(load.begin(), load.end(), std::greater<int64_t>());
+      int64_t& cu = load.back();
+      cu += walks[i / per].cost + (cu > 0 ? kStartTiles : 0);
+      most = std::max(most, cu);
+      std::push_heap(load.begin(), load.end(), std::greater<int64_t>());
+    }
+    teams = most * 13 <= busiest * 12;
+    if (teams) busiest = most;
+  }
   if (!f32 && busiest > fwd_unit * 8 / 5 + (p.head_dim == 64 ? kFwdSumTiles64 : kFwdSumTiles)) {
     const int64_t most = (int64_t)(kMaxPackedPartials / (per * kQRowsShortBf16 * p.head_dim * sizeof(float)));
     for (;; fwd_unit *= 2) {
@@ -138,7 +162,7 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
       for (const Cost& c : chunks) out.fwd.push_back(c.it);
     }
   }
-  if (!f32 && out.fwd.empty() && (int64_t)out.q.size() * per <= kTeamWgs) out.teams = 2;
+  if (teams && out.fwd.empty()) out.teams = 2;
 
   // Chunks of the key tiles' walks.
   const int64_t longest = k.empty() ? 0 : k[0].cost;

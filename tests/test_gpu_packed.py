@@ -328,3 +328,11 @@ def test_two_graphs_of_cut_walks_share_their_workspaces():
             want = step(p, None)
             torch.cuda.synchronize()
             assert all(torch.equal(a, b) for a, b in zip(out, want))
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_more_workgroups_than_cus_in_two_teams(D):
+    ql = [1100, 130, 1]
+    plan = bd.packed_plan(ql, heads=28, kv_heads=28, head_dim=D, dtype=BF)
+    assert plan._record.teams == 2 and plan._record.q_items * 28 > 256
+    run(ql, ql, 28, 28, D, BF, gap=3, backward=False, seed=47)

@@ -150,3 +150,9 @@ def test_walks_that_fill_the_card_or_are_short_are_not_cut():
         assert p.fwd_workspace_bytes == 0 and p._record.fwd_items == 0
     p = bd.packed_plan([1], [2500], heads=4, kv_heads=4, head_dim=64, dtype=torch.float32, device="cpu")
     assert p.fwd_workspace_bytes == 0
+
+
+def test_two_teams_where_a_cu_ends_sooner_one_workgroup_at_a_time():
+    for ql, H, KV, teams in (([2213, 600, 152], 16, 16, 2), ([1355, 8], 24, 8, 2), ([500] * 8, 16, 4, 1), ([200] * 40, 8, 8, 1)):
+        p = bd.packed_plan(ql, heads=H, kv_heads=KV, head_dim=128, dtype=torch.bfloat16, device="cpu")
+        assert p._record.teams == teams and p._record.fwd_items == 0, (ql, H, KV)
