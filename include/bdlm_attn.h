@@ -310,11 +310,17 @@ typedef struct {
   int64_t q_start, q_len, k_start, k_len;
 } bdlm_packed_seq;
 
+/* Chunks of query tiles' walks, where those are cut. */
+typedef struct {
+  int32_t items, sums, slots, reserved;
+} bdlm_packed_chunks;
+
 /* What bdlm_packed_plan_make found: passed on to the calls unchanged. */
 typedef struct {
   bdlm_packed problem;
   int64_t q_rows, k_rows;    /* rows that the query and key tensors have at least */
-  int32_t q_items, k_items, n_sums, slots, teams, fwd_items, fwd_sums, fwd_slots;
+  int32_t q_items, k_items, n_sums, slots, teams, reserved;
+  bdlm_packed_chunks fwd, dq;
   size_t bytes;               /* of the items */
   size_t workspace_bytes;     /* of bdlm_packed_bwd */
   size_t fwd_workspace_bytes; /* of bdlm_packed_fwd */

@@ -86,15 +86,16 @@ bdlm_status check_workspace(size_t need, const void* p, size_t bytes) {
 // Partial outputs of the forward's cut walks; their LSE lies behind them.
 size_t part_bytes(const bdlm_packed_plan& pl) {
   const int per = pl.problem.heads / packed_tile_heads(pl.problem.heads / pl.problem.kv_heads);
-  return align256((size_t)pl.fwd_slots * per * kQRowsShortBf16 * pl.problem.head_dim * sizeof(float));
+  return align256((size_t)pl.fwd.slots * per * kQRowsShortBf16 * pl.problem.head_dim * sizeof(float));
 }
 
 bdlm_status check_plan(const bdlm_packed_plan* pl, const void* items) {
   if (!pl) return fail(BDLM_ERR_INVALID, "plan is null");
   const bdlm_status st = check_packed(&pl->problem);
   if (st != BDLM_OK) return st;
-  if (pl->q_items < 0 || pl->k_items < 0 || pl->n_sums < 0 || pl->slots < 0 || pl->fwd_items < 0 || pl->fwd_sums < 0 ||
-      pl->fwd_slots < 0 || pl->q_rows < 0 || pl->k_rows < 0 ||
+  auto bad = [](const bdlm_packed_chunks& c) { return c.items < 0 || c.sums < 0 || c.slots < 0 || c.reserved != 0; };
+  if (pl->q_items < 0 || pl->k_items < 0 || pl->n_sums < 0 || pl->slots < 0 || bad(pl->fwd) || bad(pl->dq) ||
+      pl->reserved != 0 || pl->q_rows < 0 || pl->k_rows < 0 ||
       pl->teams < 1 || pl->teams > 2)
     return fail(BDLM_ERR_INVALID, "plan was not made by bdlm_packed_plan_make");
   if (pl->bytes > 0 && (!items || !aligned16(items)))
@@ -117,13 +118,18 @@ PackedArgs packed_args(const bdlm_packed_plan& pl, int64_t lse_pitch) {
   return a;
 }
 
-// The chunks of query tiles in place of the whole ones (a.items: the plan's).
-void take_chunks(const bdlm_packed_plan& pl, PackedArgs& a) {
-  const PackedItem* const k_end = a.items + pl.q_items + pl.k_items;
-  a.items = reinterpret_cast<const PackedItem*>(reinterpret_cast<const PackedSum*>(k_end) + pl.n_sums);
-  a.n_items = pl.fwd_items;
-  a.sums = reinterpret_cast<const PackedSum*>(a.items + pl.fwd_items);
-  a.n_sums = pl.fwd_sums;
+// The chunks of query tiles in place of the whole ones, if there are any (a.items: the plan's).
+void take_chunks(const bdlm_packed_plan& pl, bool dq, PackedArgs& a) {
+  const bdlm_packed_chunks& c = dq ? pl.dq : pl.fwd;
+  if (c.items == 0) return;
+  auto behind = [](const PackedItem* items, int n_items, int n_sums) {  // items, then sums
+    return reinterpret_cast<const PackedItem*>(reinterpret_cast<const PackedSum*>(items + n_items) + n_sums);
+  };
+  a.items = behind(a.items, pl.q_items + pl.k_items, pl.n_sums);
+  if (dq) a.items = behind(a.items, pl.fwd.items, pl.fwd.sums);
+  a.n_items = c.items;
+  a.sums = reinterpret_cast<const PackedSum*>(a.items + c.items);
+  a.n_sums = c.sums;
 }
 
 bdlm_status check_pitch(const bdlm_packed_plan& pl, int64_t pitch) {
@@ -147,9 +153,9 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
   // (a grid dimension holds fewer than 2^32 threads; the fp32 kernels' grids have two)
   const bool f32 = p->dtype == BDLM_F32;
   const int64_t per = p->heads / (f32 ? 1 : packed_tile_heads(p->heads / p->kv_heads));
-  const int64_t q_wgs = (int64_t)std::max(it.q.size(), it.fwd.size()) * per;
+  const int64_t q_wgs = (int64_t)std::max({it.q.size(), it.fwd.items.size(), it.dq.items.size()}) * per;
   const int64_t wgs = std::max(q_wgs, (int64_t)it.k.size() * p->kv_heads), most = f32 ? (int64_t)1 << 30 : 1 << 22;
-  if (wgs > most || (int64_t)it.sums.size() * p->kv_heads > 1 << 18 || (int64_t)it.fwd_sums.size() * per > 1 << 18)
+  if (wgs > most || (int64_t)it.sums.size() * p->kv_heads > 1 << 18 || (int64_t)std::max(it.fwd.sums.size(), it.dq.sums.size()) * per > 1 << 18)
     return fail(BDLM_ERR_UNSUPPORTED, "packed problem needs %lld workgroups (limit %lld)", (long long)wgs,
                 (long long)most);
   bdlm_packed_plan pl{};
@@ -161,18 +167,20 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
   pl.n_sums = (int32_t)it.sums.size();
   pl.slots = it.slots;
   pl.teams = it.teams;
-  pl.fwd_items = (int32_t)it.fwd.size();
-  pl.fwd_sums = (int32_t)it.fwd_sums.size();
-  pl.fwd_slots = it.fwd_slots;
-  pl.bytes = (it.q.size() + it.k.size() + it.fwd.size()) * sizeof(PackedItem) +
-             (it.sums.size() + it.fwd_sums.size()) * sizeof(PackedSum);
-  const size_t part_rows = (size_t)it.fwd_slots * per * kQRowsShortBf16;
+  auto put_chunks = [](const PackedPlanItems::Chunks& c, bdlm_packed_chunks& to) {
+    to = {(int32_t)c.items.size(), (int32_t)c.sums.size(), c.slots, 0};
+  };
+  put_chunks(it.fwd, pl.fwd);
+  put_chunks(it.dq, pl.dq);
+  pl.bytes = (it.q.size() + it.k.size() + it.fwd.items.size() + it.dq.items.size()) * sizeof(PackedItem) +
+             (it.sums.size() + it.fwd.sums.size() + it.dq.sums.size()) * sizeof(PackedSum);
+  const size_t part_rows = (size_t)it.fwd.slots * per * kQRowsShortBf16;
   pl.fwd_workspace_bytes = align256(part_rows * p->head_dim * sizeof(float)) + align256(part_rows * sizeof(float));
   // (dQ's partial sums are added up before the first of dK and dV are written: in the same place)
   pl.workspace_bytes = 2 * packed_stats_bytes(pl) +
                        std::max((size_t)it.slots * p->kv_heads *
                                     (f32 ? kRowsF32 * sizeof(double) : kBwdKeysBf16 * sizeof(float)) * 2 * p->head_dim,
-                                (size_t)it.fwd_slots * per * kQRowsShortBf16 * p->head_dim * sizeof(float));
+                                (size_t)it.dq.slots * per * kQRowsShortBf16 * p->head_dim * sizeof(float));
   if (items) {
     if (items_bytes < pl.bytes)
       return fail(BDLM_ERR_INVALID, "plan needs %zu bytes (got %zu)", pl.bytes, items_bytes);
@@ -184,8 +192,10 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
     put(it.q);
     put(it.k);
     put(it.sums);
-    put(it.fwd);
-    put(it.fwd_sums);
+    for (const PackedPlanItems::Chunks* c : {&it.fwd, &it.dq}) {
+      put(c->items);
+      put(c->sums);
+    }
   }
   *plan = pl;
   return BDLM_OK;
@@ -212,8 +222,8 @@ bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdl
   PackedArgs a = packed_args(*plan, lse_pitch);
   a.items = static_cast<const PackedItem*>(items);
   a.n_items = plan->q_items;
-  if (plan->fwd_items > 0) {
-    take_chunks(*plan, a);
+  take_chunks(*plan, false, a);
+  if (a.n_sums > 0) {
     a.partials = workspace;
     a.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + part_bytes(*plan));
   }
@@ -229,7 +239,7 @@ bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdl
   const hipError_t e = timed(kKPackedFwd, stream, [&] {
     const hipError_t le = p.dtype == BDLM_BF16 ? launch_fwd_bf16(a, p.head_dim, plan->teams, stream)
                                                : launch_fwd_f32(a, p.head_dim, stream);
-    return le != hipSuccess || a.n_sums == 0 ? le : launch_packed_fwd_sum(a, p.head_dim, plan->fwd_slots, stream);
+    return le != hipSuccess || a.n_sums == 0 ? le : launch_packed_fwd_sum(a, p.head_dim, plan->fwd.slots, stream);
   });
   return e == hipSuccess ? BDLM_OK : hip_fail(e, "packed forward launch");
 }
@@ -281,7 +291,7 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
   a.partials = ws + 2 * arr;
   a.items = static_cast<const PackedItem*>(items);
   a.n_items = plan->q_items;
-  if (plan->fwd_items > 0) take_chunks(*plan, a);
+  take_chunks(*plan, true, a);
   // dQ first: it leaves the row statistics for dK/dV.
   hipError_t e = timed(kKPackedDq, stream, [&] {
     const hipError_t le =

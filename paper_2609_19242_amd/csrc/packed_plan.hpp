@@ -15,9 +15,14 @@
 namespace bdlm {
 
 struct PackedPlanItems {
-  std::vector<PackedItem> q, k, fwd;  // fwd: in place of q, if some of its walks are cut
-  std::vector<PackedSum> sums, fwd_sums;
-  int32_t slots = 0, fwd_slots = 0;
+  std::vector<PackedItem> q, k;
+  std::vector<PackedSum> sums;
+  int32_t slots = 0;
+  struct Chunks {  // in place of q, if some of its walks are cut
+    std::vector<PackedItem> items;
+    std::vector<PackedSum> sums;
+    int32_t slots = 0;
+  } fwd, dq;
   int32_t teams = 1;
 };
 
@@ -26,8 +31,8 @@ inline int packed_step_rows(bool f32, int group) { return f32 ? kRowsF32 : group
 // Partial sums of cut walks at most (per call); longer chunks where they would come to more.
 constexpr size_t kMaxPackedPartials = (size_t)256 << 20;
 
-// Key tiles of the forward's chunks at least; what partial outputs and their sums cost, in key tiles.
-constexpr int64_t kMinFwdUnit = 8, kFwdSumTiles = 10, kFwdSumTiles64 = 18;
+// Key tiles of a query tile's chunks at least; what partial sums cost, in key tiles.
+constexpr int64_t kMinFwdUnit = 8, kFwdSumTiles = 10, kFwdSumTiles64 = 18, kDqSumTiles = 8;
 // What a workgroup's start-up costs, in key tiles.
 constexpr int64_t kStartTiles = 3;
 
@@ -36,17 +41,19 @@ constexpr int64_t kStartTiles = 3;
 // Query tiles: 128 rows (16 in fp32) of one sequence, or as many fewer as a
 // tile has heads (packed_tile_heads), by the keys they walk.
 //
-// Forward and dQ, bf16: where few tiles have long walks (a piece of a long prompt, few
-// heads), the busiest CU's walks, not the card, set the time.  If they are longer
+// Forward and dQ, bf16: where few tiles have long walks (a piece of a long prompt,
+// few heads), the busiest CU's walks, not the card, set the time.  If they are longer
 // than the average load of a CU by more than partial outputs cost, walks are cut
 // into equal chunks of at most that load, a chunk per CU, whose outputs
 // packed_q_sums.hip joins (the factor is what a chunk's tiles take longer without a
-// second team; dQ, which has none, takes the forward's chunks).  32/8 heads, d 128,
-// without and with cuts: 1 row behind 2,048 keys 33
-// and 19 us, behind 8,192 109 and 22, behind 32,768 444 and 40; 256 rows 37 and 30, 119
-// and 59, 438 and 184; 512 rows behind 2,048 are left whole (42, 47 cut), 1,024 behind
-// 8,192 too (155, 193).  3,000 rows of 4/2 heads 45 and 32, dQ 74 and 39.  (Chunks that fill two
-// workgroups a CU write twice the partial outputs: 256 rows behind 8,192 65 us.)
+// second team; dQ has none in any case, and is cut sooner and, with more tiles than
+// CUs, into shorter chunks).  d 128, without and with cuts, 32/8 heads: 1 row behind
+// 2,048 keys 33 and 19 us, behind 8,192 109 and 22, behind 32,768 444 and 40; 256 rows
+// 37 and 30, 119 and 59, 438 and 184; 512 rows behind 2,048 are left whole (42, 47
+// cut), 1,024 behind 8,192 too (155, 193); 3,000 rows of 4/2 heads 45 and 32, dQ 74
+// and 39; dQ of 2,667, 200 and 15, 12/2 heads, 68 and 56, of 2,213, 600 and 152, 16/16,
+// 68 and 60.  (Chunks that fill two workgroups a CU write twice the partial outputs:
+// 256 rows behind 8,192 65 us.)
 //
 // Two teams per workgroup (fwd_bf16.hip): up to a workgroup per CU, as in joint
 // calls, and up to two where a CU that takes them one after the other, as it gets
@@ -116,13 +123,14 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
   std::stable_sort(walks.begin(), walks.end(), heavier);
   const int64_t fwd_longest = walks.empty() ? 0 : walks[0].cost;
   const int64_t wgs = (int64_t)walks.size() * per, fwd_average = (fwd_total * per + kCus - 1) / kCus;
-  int64_t fwd_unit = std::max(kMinFwdUnit, fwd_average);
+  const int64_t unit_q = std::max(kMinFwdUnit, fwd_average);
   // what the busiest CU walks without cuts: all workgroups resident, or dealt out as others end
   int64_t busiest = 0;
   if (wgs <= kCus * (p.head_dim == 64 ? 3 : 2))
     for (int64_t i = 0; i < wgs; i += kCus) busiest += walks[i / per].cost;
   else
     busiest = std::max(fwd_longest, fwd_average);
+  const int64_t busiest_dq = busiest;
   bool teams = !f32 && wgs <= kTeamWgs;
   if (!f32 && wgs > kTeamWgs && wgs <= 2 * kTeamWgs) {  // one workgroup of two teams per CU, the next when it ends
     std::vector<int64_t> load(kCus, 0);  // (a heap, the least loaded CU first)
@@ -137,32 +145,35 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
     teams = most * 13 <= busiest * 12;
     if (teams) busiest = most;
   }
-  if (!f32 && busiest > fwd_unit * 8 / 5 + (p.head_dim == 64 ? kFwdSumTiles64 : kFwdSumTiles)) {
+  auto cut = [&](int64_t unit, PackedPlanItems::Chunks& to) {
     const int64_t most = (int64_t)(kMaxPackedPartials / (per * kQRowsShortBf16 * p.head_dim * sizeof(float)));
-    for (;; fwd_unit *= 2) {
+    for (;; unit *= 2) {
       int64_t slots = 0;
       for (const Cost& c : walks)
-        if (c.cost > fwd_unit) slots += (c.cost + fwd_unit - 1) / fwd_unit;
+        if (c.cost > unit) slots += (c.cost + unit - 1) / unit;
       if (slots <= most) break;
     }
     std::vector<Cost> chunks;
     for (const Cost& c : walks) {
-      const int64_t nch = std::max<int64_t>((c.cost + fwd_unit - 1) / fwd_unit, 1), size = (c.cost + nch - 1) / nch;
+      const int64_t nch = std::max<int64_t>((c.cost + unit - 1) / unit, 1), size = (c.cost + nch - 1) / nch;
       PackedItem it = c.it;
-      if (nch > 1) out.fwd_sums.push_back({it.q0, it.q_len, it.tile, out.fwd_slots, (int32_t)nch, 0, 0, 0});
+      if (nch > 1) to.sums.push_back({it.q0, it.q_len, it.tile, to.slots, (int32_t)nch, 0, 0, 0});
       for (int64_t j = 0; j < nch; ++j) {
         it.n0 = (int32_t)(j * size);
         it.n1 = j + 1 < nch ? (int32_t)((j + 1) * size) : kBig;
-        it.slot = nch > 1 ? out.fwd_slots++ : -1;
+        it.slot = nch > 1 ? to.slots++ : -1;
         chunks.push_back({std::max<int64_t>(0, std::min(c.cost, (j + 1) * size) - j * size), it});
       }
     }
-    if (out.fwd_slots > 0) {
-      std::stable_sort(chunks.begin(), chunks.end(), heavier);
-      for (const Cost& c : chunks) out.fwd.push_back(c.it);
-    }
-  }
-  if (teams && out.fwd.empty()) out.teams = 2;
+    if (to.slots == 0) return;
+    std::stable_sort(chunks.begin(), chunks.end(), heavier);
+    for (const Cost& c : chunks) to.items.push_back(c.it);
+  };
+  const int64_t sum_tiles = p.head_dim == 64 ? kFwdSumTiles64 : kFwdSumTiles;
+  if (!f32 && busiest > unit_q * 8 / 5 + sum_tiles) cut(unit_q, out.fwd);
+  if (!f32 && busiest_dq > unit_q * 23 / 20 + kDqSumTiles)
+    cut(wgs > kCus ? std::max(kMinFwdUnit, unit_q * 3 / 4) : unit_q, out.dq);
+  if (teams && out.fwd.items.empty()) out.teams = 2;
 
   // Chunks of the key tiles' walks.
   const int64_t longest = k.empty() ? 0 : k[0].cost;

@@ -29,11 +29,15 @@ class _Seq(ctypes.Structure):  # bdlm_packed_seq
                 ("k_start", ctypes.c_int64), ("k_len", ctypes.c_int64)]
 
 
+class _Chunks(ctypes.Structure):  # bdlm_packed_chunks
+    _fields_ = [(n, ctypes.c_int32) for n in ("items", "sums", "slots", "reserved")]
+
+
 class _Plan(ctypes.Structure):  # bdlm_packed_plan
     _fields_ = [("problem", _Packed), ("q_rows", ctypes.c_int64), ("k_rows", ctypes.c_int64),
                 ("q_items", ctypes.c_int32), ("k_items", ctypes.c_int32), ("n_sums", ctypes.c_int32),
-                ("slots", ctypes.c_int32), ("teams", ctypes.c_int32), ("fwd_items", ctypes.c_int32),
-                ("fwd_sums", ctypes.c_int32), ("fwd_slots", ctypes.c_int32),
+                ("slots", ctypes.c_int32), ("teams", ctypes.c_int32), ("reserved", ctypes.c_int32),
+                ("fwd", _Chunks), ("dq", _Chunks),
                 ("bytes", ctypes.c_size_t), ("workspace_bytes", ctypes.c_size_t), ("fwd_workspace_bytes", ctypes.c_size_t)]
 
 

@@ -103,12 +103,13 @@ def test_few_tiles_take_two_teams():
     assert check([64], [64], 4, 2, 128, torch.bfloat16, 1, 0)._record.teams == 2
 
 
-def fwd_items(p):
+def chunk_items(p, dq):
     r = p._record
     a = np.frombuffer(p._items.numpy().tobytes(), dtype=np.int32)
-    at = r.q_items + r.k_items + r.n_sums
-    a = a[8 * at:8 * (at + r.fwd_items + r.fwd_sums)].reshape(-1, 8)
-    return a[:r.fwd_items].tolist(), a[r.fwd_items:].tolist()
+    at = r.q_items + r.k_items + r.n_sums + (r.fwd.items + r.fwd.sums if dq else 0)
+    c = r.dq if dq else r.fwd
+    a = a[8 * at:8 * (at + c.items + c.sums)].reshape(-1, 8)
+    return c, a[:c.items].tolist(), a[c.items:].tolist()
 
 
 @pytest.mark.parametrize("ql,kl,H,KV,block,window", [
@@ -116,11 +117,17 @@ def fwd_items(p):
     ([1800], [1700], 2, 2, 7, 0), ([3000, 10], [3000, 5000], 8, 2, 1, 0)])
 def test_forward_chunks_cover_each_walk_once(ql, kl, H, KV, block, window):
     p = check(ql, kl, H, KV, 128, torch.bfloat16, block, window)
-    chunks, sums = fwd_items(p)
+    for dq in (False, True):
+        check_chunks(p, dq, ql, H, KV, block, window)
+    assert p._record.teams == 1
+
+
+def check_chunks(p, dq, ql, H, KV, block, window):
+    c, chunks, sums = chunk_items(p, dq)
     r, group = p._record, H // KV
     heads = 4 if group % 4 == 0 else 2 if group % 2 == 0 else 1
     qt = 128 // heads
-    assert r.fwd_items > r.q_items and r.teams == 1 and len(sums) == r.fwd_sums > 0
+    assert c.items > r.q_items and len(sums) == c.sums > 0
     by_tile = {}
     for a in chunks:
         by_tile.setdefault(tuple(a[:5]), []).append(a[5:])
@@ -139,15 +146,18 @@ def test_forward_chunks_cover_each_walk_once(ql, kl, H, KV, block, window):
             slots += mine
         else:
             assert parts[0][2] == -1
-    assert sorted(slots) == list(range(r.fwd_slots))
-    rows = r.fwd_slots * (H // heads) * 128
-    assert p.fwd_workspace_bytes >= rows * 129 * 4
+    assert sorted(slots) == list(range(c.slots))
+    rows = c.slots * (H // heads) * 128
+    if dq:
+        assert p.workspace_bytes >= rows * 128 * 4 + 2 * p.q_rows * H * 4
+    else:
+        assert p.fwd_workspace_bytes >= rows * 129 * 4
 
 
 def test_walks_that_fill_the_card_or_are_short_are_not_cut():
     for ql, H in (([4000] * 8, 16), ([1000], 4), ([30] * 100, 8)):
         p = bd.packed_plan(ql, heads=H, kv_heads=4, head_dim=128, dtype=torch.bfloat16, device="cpu")
-        assert p.fwd_workspace_bytes == 0 and p._record.fwd_items == 0
+        assert p.fwd_workspace_bytes == 0 and p._record.fwd.items == 0
     p = bd.packed_plan([1], [2500], heads=4, kv_heads=4, head_dim=64, dtype=torch.float32, device="cpu")
     assert p.fwd_workspace_bytes == 0
 
@@ -155,4 +165,4 @@ def test_walks_that_fill_the_card_or_are_short_are_not_cut():
 def test_two_teams_where_a_cu_ends_sooner_one_workgroup_at_a_time():
     for ql, H, KV, teams in (([2213, 600, 152], 16, 16, 2), ([1355, 8], 24, 8, 2), ([500] * 8, 16, 4, 1), ([200] * 40, 8, 8, 1)):
         p = bd.packed_plan(ql, heads=H, kv_heads=KV, head_dim=128, dtype=torch.bfloat16, device="cpu")
-        assert p._record.teams == teams and p._record.fwd_items == 0, (ql, H, KV)
+        assert p._record.teams == teams and p._record.fwd.items == 0, (ql, H, KV)
