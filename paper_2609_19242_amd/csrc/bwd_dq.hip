@@ -228,12 +228,14 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   vm_wait_barrier<IPW * (NST - 2)>();
   int cur = 0;
   int lane_lo = 0, lane_w = 0, lane_j = -1;
+  [[maybe_unused]] bool few_keys = false;  // packed calls: some row of this wave has no more keys than a tile holds
   while (c0.have) {
     copy_tile(lds + (cur == 0 ? NST - 1 : cur - 1) * STAGE, cp);
     const int j = c0.j, t = c0.t, f0 = c0.f0, f1 = c0.f1;
     if (lane_j != j) {
       lane_key_interval(a, j, qr.stream, pq, lane_lo, lane_w);
       lane_j = j;
+      if constexpr (kPacked) few_keys = __builtin_amdgcn_ballot_w64(lane_w > 0 && lane_w <= BN) != 0;
     }
 
     // On a partly visible tile, a wave none of whose rows sees any of the
@@ -290,12 +292,15 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
             const int kk = base + u * 32 + (i >> 2) * 8 + (i & 3);
             if ((unsigned)kk >= (unsigned)lane_w) sacc[u][i] = -INFINITY;
           }
-        // Packed calls: a row all of whose keys lie in this tile gets its D from
-        // here.  D = sum_j P_ij dP_ij, so that sum_j dS_ij = 0; the D formed from
-        // the rounded O misses it by up to 2^-9 |dO||O|, which is much of dS where
-        // a row has few keys (one key: all of it).  (D lies in dpacc already.)
+      }
+
+      // Packed calls: a row all of whose keys lie in this tile, seen by all rows or
+      // not, gets its D from here.  D = sum_j P_ij dP_ij, so that sum_j dS_ij = 0; the
+      // D formed from the rounded O misses it by up to 2^-8 |dO||O|, which is much of
+      // dS where a row has few keys (one key: all of it).  (D lies in dpacc already.)
+      if (kPacked && few_keys) {
         const int kstart = k_range(a, j).pos0 + t * BN - lane_lo;
-        if (kPacked && __builtin_amdgcn_ballot_w64(lane_w > 0 && kstart <= 0 && kstart + BN >= lane_w) != 0) {
+        if (__builtin_amdgcn_ballot_w64(lane_w > 0 && kstart <= 0 && kstart + BN >= lane_w) != 0) {
           float rest = 0.f, z = lse2;
           asm volatile("" : "+v"(z));  // (or the compiler keeps these exponentials for the ones below, and spills)
 #pragma unroll
