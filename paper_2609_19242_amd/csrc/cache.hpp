@@ -43,15 +43,20 @@ hipError_t launch_cache_write(const CacheArg& c, const CacheRows& r, hipStream_t
 // tokens [request][row] and the query heads of its group.  They meet the
 // prefix's keys [0, prefix) all together, and their own request's keys
 // [prefix, len) by request; keys are cut into chunks, and every (chunk, row)
-// leaves a normalised partial output and its log2-sum-exp in `part_o`,
-// `part_lse` ([chunk][token][head]), which prefix_merge adds up.  With one
-// chunk in all, the kernels write O and LSE themselves.
+// leaves a normalised partial output (fp32) and its log2-sum-exp (fp32 in bf16
+// calls, fp64 in fp32 ones: partials.hpp) in `part_o`, `part_lse`
+// ([chunk][token][head]), which prefix_merge adds up.  With one chunk in all,
+// the kernels write O and LSE themselves.
+template <bool BF16> struct PartLseOf { typedef float type; };
+template <> struct PartLseOf<false> { typedef double type; };
+template <bool BF16> using PartLse = typename PartLseOf<BF16>::type;
 struct PrefixArgs {
   const char *k, *v;  // this layer's
   const int32_t *table, *lens, *seqs;
   const void* q;
   void* o;
-  float *lse, *part_o, *part_lse;
+  float *lse, *part_o;
+  void* part_lse;
   int32_t pages, page_size, seqs_in_cache, max_pages;
   int32_t requests, rows, heads, kv_heads, group;
   int32_t prefix, block;      // block: every row sees all len keys

@@ -174,6 +174,12 @@ bdlm_status plan_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int
   return BDLM_OK;
 }
 
+// Workspace: the partial outputs (`part` bytes), behind them their log2-sum-exp.
+size_t prefix_workspace(const bdlm_cache* c, size_t part) {
+  const size_t per = c->dtype == BDLM_F32 ? sizeof(PartLse<false>) : sizeof(PartLse<true>);
+  return part ? align256(part) + align256(part / (c->head_dim * sizeof(float)) * per) : 0;
+}
+
 bdlm_status check_prefix(const bdlm_cache* c, int64_t requests, int64_t rows, int32_t heads, int64_t prefix) {
   if (heads < 1 || heads % c->kv_heads != 0)
     return fail(BDLM_ERR_INVALID, "heads (%d) must be a positive multiple of kv_heads (%d)", heads, c->kv_heads);
@@ -278,9 +284,8 @@ size_t bdlm_prefix_attn_workspace_bytes(const bdlm_cache* c, int64_t requests, i
   PrefixArgs a{};
   size_t part = 0;
   if (check_cache(c) != BDLM_OK || check_prefix(c, requests, rows, heads, prefix) != BDLM_OK) return 0;
-  if (requests == 0 || rows == 0 || plan_prefix(c, requests, rows, heads, prefix, a, part) != BDLM_OK || part == 0)
-    return 0;
-  return align256(part) + align256(part / c->head_dim);
+  if (requests == 0 || rows == 0 || plan_prefix(c, requests, rows, heads, prefix, a, part) != BDLM_OK) return 0;
+  return prefix_workspace(c, part);
 }
 
 bdlm_status bdlm_prefix_attn(const bdlm_cache* c, int64_t layer, int64_t requests, const int32_t* seqs, int64_t rows,
@@ -299,7 +304,7 @@ bdlm_status bdlm_prefix_attn(const bdlm_cache* c, int64_t layer, int64_t request
   PrefixArgs a{};
   size_t part = 0;
   if ((st = plan_prefix(c, requests, rows, heads, prefix, a, part)) != BDLM_OK) return st;
-  const size_t need = part ? align256(part) + align256(part / c->head_dim) : 0;
+  const size_t need = prefix_workspace(c, part);
   if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u)))
     return fail(BDLM_ERR_WORKSPACE, "workspace needs %zu bytes, 256-byte aligned (got %zu at %p)", need,
                 workspace_bytes, workspace);
@@ -313,7 +318,7 @@ bdlm_status bdlm_prefix_attn(const bdlm_cache* c, int64_t layer, int64_t request
   a.o = o;
   a.lse = lse;
   a.part_o = static_cast<float*>(workspace);
-  a.part_lse = need ? reinterpret_cast<float*>(static_cast<char*>(workspace) + align256(part)) : nullptr;
+  a.part_lse = need ? static_cast<char*>(workspace) + align256(part) : nullptr;
   a.pages = ca.pages;
   a.page_size = ca.page_size;
   a.seqs_in_cache = ca.seqs;

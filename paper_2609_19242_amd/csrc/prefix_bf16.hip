@@ -359,7 +359,7 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
               *(f32x4*)(op + 32 * d + 8 * g4 + 4 * half) = x;
             }
         }
-        if (half == 0) a.part_lse[at] = empty ? -INFINITY : st.m + log2f(l);
+        if (half == 0) ((float*)a.part_lse)[at] = empty ? -INFINITY : st.m + log2f(l);
       }
     }
     return;
@@ -451,7 +451,7 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
     } else {
       const int64_t at = (int64_t)it.part * a.requests * a.rows * a.heads + orow;
       if (!empty) *(f32x4*)(a.part_o + at * D + piece * 4) = x;
-      if (piece == 0) a.part_lse[at] = empty ? -INFINITY : m + log2f(lt);
+      if (piece == 0) ((float*)a.part_lse)[at] = empty ? -INFINITY : m + log2f(lt);
     }
   }
 }

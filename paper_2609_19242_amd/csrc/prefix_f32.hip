@@ -150,7 +150,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
   if (d0 == 0) {
     const double z = M + log2(lt);
     if (single) a.lse[prefix_lse_at(a, pr)] = empty ? -INFINITY : (float)(z * kLn2D);
-    else a.part_lse[at] = empty ? -INFINITY : (float)z;
+    else ((double*)a.part_lse)[at] = empty ? -INFINITY : z;
   }
 }
 

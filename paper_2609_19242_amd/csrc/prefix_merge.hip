@@ -21,8 +21,9 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(const PrefixArgs a) {
   if (row >= total) return;
   const int parts = a.prefix_chunks + a.own_chunks;
   auto at = [&](int j) { return j * total + row; };
-  const JoinedRow<D> r = FEW ? join_few<D>(a.part_o, a.part_lse, at, parts, lane)
-                             : join_partials<D>(a.part_o, a.part_lse, at, parts, lane);
+  using Z = PartLse<BF16>;
+  const Z* const z = (const Z*)a.part_lse;
+  const JoinedRow<D, Z> r = FEW ? join_few<D>(a.part_o, z, at, parts, lane) : join_partials<D>(a.part_o, z, at, parts, lane);
   if (lane >= LPR) return;
   if constexpr (BF16) {
     bf16x4 y;
@@ -30,7 +31,10 @@ __global__ __launch_bounds__(256) void prefix_merge_kernel(const PrefixArgs a) {
     for (int e = 0; e < 4; ++e) y[e] = to_bf16(r.x[e]);
     *(bf16x4*)((bf16*)a.o + row * D + lane * 4) = y;
   } else {
-    *(f32x4*)((float*)a.o + row * D + lane * 4) = r.x;
+    f32x4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = (float)r.x[e];
+    *(f32x4*)((float*)a.o + row * D + lane * 4) = y;
   }
   if (lane == 0) {
     PrefixRow pr;
