@@ -12,6 +12,7 @@ there is no fallback path.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import functools
 import math
@@ -171,6 +172,25 @@ def _torch_stream(stream, device) -> torch.cuda.Stream:
     if handle == 0:  # the default stream, for which ExternalStream would take one from torch's pool
         return torch.cuda.default_stream(device)
     return torch.cuda.ExternalStream(handle, device=device)
+
+
+def _memory_of(stream, device):
+    """The context in which to make what a call on ``stream`` (None: the current one) writes: in that stream's own
+    memory, since what the current stream has given back may still be in use there, by work that ``stream`` does not
+    wait for."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream, device))
+
+
+def _made(stream, device, make, *args):
+    """``make(*args)``, the new tensors that a call on ``stream`` returns (:func:`_memory_of`), kept for the current
+    stream too, where the caller goes on with them."""
+    if stream is None:
+        return make(*args)
+    with _memory_of(stream, device):
+        tensors = make(*args)
+    for t in tensors:
+        t.record_stream(torch.cuda.current_stream(device))
+    return tensors
 
 
 def _launch(owner, stream, call, *args):

@@ -1,7 +1,8 @@
 """A paged cache of keys and values, operations on its pages, and the attention of decoding requests over it.
 
 :class:`Cache` holds the caller's tensors; the functions enqueue kernels on the current (or the given) stream and
-return without waiting.  The rules are those of ``bdlm_cache_*`` and ``bdlm_prefix_attn`` in ``include/bdlm_attn.h``.
+return without waiting; a given stream is not ordered against the current one.  The rules are those of
+``bdlm_cache_*`` and ``bdlm_prefix_attn`` in ``include/bdlm_attn.h``.
 """
 from __future__ import annotations
 
@@ -10,7 +11,7 @@ from typing import Optional
 
 import torch
 
-from . import _dtype_code, _expect, _launch, lib
+from . import _dtype_code, _expect, _launch, _made, lib
 from .packed import _Rows, _rows, _workspace
 
 __all__ = ["Cache", "cache_new", "cache_grow", "cache_write", "cache_fork", "cache_free", "cache_compact",
@@ -172,6 +173,11 @@ def _check_q(c, q):
     return R, n, H
 
 
+def _new_outputs(q):
+    R, n, H, _ = q.shape
+    return torch.empty_like(q), q.new_empty((R, H, n), dtype=torch.float32)
+
+
 def prefix_attn_workspace_bytes(q, cache: Cache, prefix: int = 0) -> int:
     """Workspace of :func:`prefix_attn` for queries like ``q``."""
     c = _cache(cache)
@@ -192,8 +198,7 @@ def prefix_attn(q, cache: Cache, layer: int, seqs, prefix: int = 0, block: bool 
     R, n, H = _check_q(c, q)
     a = _list(c, "seqs", seqs, R)
     if out is None:
-        o = torch.empty_like(q)
-        lse = q.new_empty((R, H, n), dtype=torch.float32)
+        o, lse = _made(stream, c.device, _new_outputs, q)
     else:
         if len(out) != 2:
             raise ValueError("out must be (o, lse)")

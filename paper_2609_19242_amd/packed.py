@@ -2,7 +2,8 @@
 
 A :class:`PackedPlan` (:func:`packed_plan`) is made once for a set of sequence lengths and serves every layer,
 forward (:func:`packed_fwd`) and backward (:func:`packed_bwd`).  The rules and layouts are those of
-``bdlm_packed_fwd`` in ``include/bdlm_attn.h``.
+``bdlm_packed_fwd`` in ``include/bdlm_attn.h``.  With ``stream``, a call runs there and is not ordered against the
+current stream: the caller orders what it reads before it and what uses its results behind it.
 """
 from __future__ import annotations
 
@@ -13,7 +14,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from . import _check, _dtype_code, _expect, _launch, _on_device, _torch_stream, lib
+from . import _check, _dtype_code, _expect, _launch, _made, _memory_of, _on_device, lib
 
 __all__ = ["PackedPlan", "packed_plan", "packed_fwd", "packed_bwd"]
 
@@ -147,13 +148,18 @@ def _check_plan(plan):
         raise TypeError(f"plan must be a PackedPlan, got {type(plan).__name__}")
 
 
-def _filled(like, shape, stream, dtype=None, fill=0.0):
-    """A new output of which a call does not write all, filled on the call's stream."""
-    t = like.new_empty(shape, dtype=dtype)
-    if stream is None:
-        return t.fill_(fill)
-    with torch.cuda.stream(_torch_stream(stream, like.device)):
-        return t.fill_(fill)
+# New outputs, filled where a call does not write all of them.
+def _fwd_outputs(plan, q):
+    n, H = q.shape[0], plan.heads
+    o, lse = q.new_empty((n, H, plan.head_dim)), q.new_empty((H, n), dtype=torch.float32)
+    return (o, lse) if n == plan._held[0] else (o.zero_(), lse.fill_(-math.inf))
+
+
+def _bwd_outputs(plan, q, k, v):
+    n, nk, nv, H, KV, D = q.shape[0], k.shape[0], v.shape[0], plan.heads, plan.kv_heads, plan.head_dim
+    hq, hk = plan._held
+    dq, dk, dv = q.new_empty((n, H, D)), k.new_empty((nk, KV, D)), v.new_empty((nv, KV, D))
+    return (dq if n == hq else dq.zero_(), dk if nk == hk else dk.zero_(), dv if nv == hk else dv.zero_())
 
 
 def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, workspace: Optional[torch.Tensor] = None,
@@ -168,11 +174,7 @@ def packed_fwd(plan: PackedPlan, q, k, v, out: Optional[tuple] = None, workspace
                   _rows(plan, "v", v, KV, plan.k_rows))
     n = q.shape[0]
     if out is None:
-        if n == plan._held[0]:
-            o, lse = q.new_empty((n, H, plan.head_dim)), q.new_empty((H, n), dtype=torch.float32)
-        else:
-            o = _filled(q, (n, H, plan.head_dim), stream)
-            lse = _filled(q, (H, n), stream, torch.float32, -math.inf)
+        o, lse = _made(stream, plan.device, _fwd_outputs, plan, q)
         ro = _Rows(o.data_ptr(), H * plan.head_dim)
     else:
         if len(out) != 2:
@@ -201,9 +203,7 @@ def packed_bwd(plan: PackedPlan, q, k, v, o, lse, do, out: Optional[tuple] = Non
     ro, rdo = _as_long(plan, "o", o, H, n), _as_long(plan, "do", do, H, n)
     _lse(plan, lse, n)
     if out is None:
-        hq, hk = plan._held
-        dq = q.new_empty((n, H, D)) if n == hq else _filled(q, (n, H, D), stream)
-        dk, dv = (t.new_empty((m, KV, D)) if m == hk else _filled(t, (m, KV, D), stream) for t, m in ((k, nk), (v, nv)))
+        dq, dk, dv = _made(stream, plan.device, _bwd_outputs, plan, q, k, v)
         outs = _Rows(dq.data_ptr(), H * D), _Rows(dk.data_ptr(), KV * D), _Rows(dv.data_ptr(), KV * D)
     else:
         if len(out) != 3:
@@ -235,7 +235,7 @@ def _workspace(workspace, nbytes, device, stream):
             raise ValueError("workspace must be a contiguous tensor")
         _on_device(device, workspace=workspace)
         return workspace
-    workspace = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
-    if stream is not None:  # used on that stream after this call has dropped it
-        workspace.record_stream(_torch_stream(stream, device))
-    return workspace
+    if stream is None:
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+    with _memory_of(stream, device):
+        return torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
