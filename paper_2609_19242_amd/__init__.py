@@ -439,8 +439,8 @@ def joint_fwd(q, k, v, block_size: int, clean_intra: int = CLEAN_INTRA_CAUSAL, s
         _expect("lse", lse, torch.float32, (B, Hq, n))
     _on_device(q.device, q=q, k=k, v=v)
     if out is None:
-        o = torch.empty(q.shape, dtype=odt, device=q.device)
-        lse = torch.empty((B, Hq, n), dtype=torch.float32, device=q.device)
+        o, lse = _made(stream, q.device, lambda: (torch.empty(q.shape, dtype=odt, device=q.device),
+                                                  torch.empty((B, Hq, n), dtype=torch.float32, device=q.device)))
     else:
         _on_device(q.device, o=o, lse=lse)
     r = _joint_range_array(L)
@@ -472,13 +472,14 @@ def joint_bwd(q, k, v, o, lse, do, block_size: int, clean_intra: int = CLEAN_INT
     _on_device(q.device, q=q, k=k, v=v, o=o, lse=lse, do=do)
     _check_ws(workspace, q.device)
     if out is None:
-        out = tuple(torch.empty(t.shape, dtype=odt, device=q.device) for t in (q, k, v))
+        out = _made(stream, q.device, lambda: tuple(torch.empty(t.shape, dtype=odt, device=q.device) for t in (q, k, v)))
     else:
         _on_device(q.device, dq=out[0], dk=out[1], dv=out[2])
     dq, dk, dv = out
     if workspace is None:
         nbytes = lib().bdlm_attn_bwd_workspace_bytes(ctypes.byref(p), 2, r)
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+        with _memory_of(stream, q.device):
+            workspace = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
         if stream is not None:  # used on that stream after this call has dropped it
             workspace.record_stream(_torch_stream(stream, q.device))
     else:

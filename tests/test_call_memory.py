@@ -84,6 +84,20 @@ def test_attention_over_the_cache(made):
     holds(made, bd.prefix_attn(q, c, 0, torch.tensor([0, 1], dtype=torch.int32), stream=SIDE), 1)
 
 
+def test_joint_calls(made, monkeypatch):
+    monkeypatch.setattr(bd, "_on_device", lambda *a, **kw: None)
+    monkeypatch.setattr(bd, "_stream", lambda s: 0)
+    ok = lambda *a: 0  # noqa: E731
+    monkeypatch.setattr(bd, "lib", lambda: types.SimpleNamespace(bdlm_attn_fwd=ok, bdlm_attn_bwd=ok,
+                                                                 bdlm_attn_bwd_workspace_bytes=lambda *a: 512))
+    q, k, v = (torch.ones(1, 64, h, 64, dtype=BF) for h in (4, 2, 2))
+    made.new.clear()
+    o, lse = bd.joint_fwd(q, k, v, 16, stream=SIDE)
+    holds(made, (o, lse), 0)
+    made.new.clear()
+    holds(made, bd.joint_bwd(q, k, v, o, lse, q, 16, stream=SIDE), 1)
+
+
 def test_calls_on_the_current_stream_record_nothing(made):
     plan = bd.packed_plan([5, 3], heads=4, kv_heads=2, head_dim=64, dtype=BF, device="cpu")
     q, k, v = (torch.ones(8, h, 64, dtype=BF) for h in (4, 2, 2))
@@ -116,4 +130,22 @@ def test_results_dropped_while_their_kernels_wait():
         others = [torch.full_like(t, 7) for t in (want[1], grads[1], grads[2], step[1], qs) for _ in range(3)]
         torch.cuda.synchronize()
         assert torch.equal(o, want[0]) and torch.equal(dq, grads[0]) and torch.equal(so, step[0])
+        assert all(bool((t == 7).all()) for t in others)
+
+
+@pytest.mark.gpu
+def test_joint_results_dropped_while_their_kernels_wait():
+    q, k, v, do = (torch.randn(1, 4096, h, 128, device="cuda").to(BF) for h in (8, 2, 2, 8))
+    want = bd.joint_fwd(q, k, v, 32)
+    grads = bd.joint_bwd(q, k, v, *want, do, 32)
+    side = torch.cuda.Stream()
+    for use in (side, side.cuda_stream):
+        torch.cuda.synchronize()
+        for _ in range(5):
+            bd.joint_bwd(q, k, v, *want, do, 32, stream=use)
+        o = bd.joint_fwd(q, k, v, 32, stream=use)[0]
+        dq = bd.joint_bwd(q, k, v, *want, do, 32, stream=use)[0]
+        others = [torch.full_like(t, 7) for t in (want[1], grads[1], grads[2]) for _ in range(3)]
+        torch.cuda.synchronize()
+        assert torch.equal(o, want[0]) and torch.equal(dq, grads[0])
         assert all(bool((t == 7).all()) for t in others)
