@@ -80,8 +80,9 @@ class BdlmError(RuntimeError):
 
 
 _LIB = None
-_current_gpu = torch._C._cuda_getDevice
-_raw_stream = torch._C._cuda_getCurrentRawStream
+# (None in a torch without GPU support, which can still make plans)
+_current_gpu = getattr(torch._C, "_cuda_getDevice", None)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 _VP = ctypes.c_void_p
 _PP = ctypes.POINTER(ctypes.c_void_p)
 
