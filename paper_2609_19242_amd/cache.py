@@ -12,7 +12,7 @@ from typing import Optional
 import torch
 
 from . import _dtype_code, _expect, _launch, _made, lib
-from .packed import _Rows, _rows, _workspace
+from .packed import _int, _Rows, _rows, _workspace
 
 __all__ = ["Cache", "cache_new", "cache_grow", "cache_write", "cache_fork", "cache_free", "cache_compact",
            "prefix_attn", "prefix_attn_workspace_bytes", "CACHE_OK", "CACHE_BAD_LIST", "CACHE_NO_PAGES"]
@@ -160,7 +160,7 @@ def cache_write(cache: Cache, layer: int, seqs, counts, k, v, starts: Optional[t
     rows = k.shape[0]
     if rows != v.shape[0]:
         raise ValueError(f"k has {rows} rows, v has {v.shape[0]}")
-    _launch(c, stream, lib().bdlm_cache_write, c._ref, layer, n, a, b, at, rows, rk, rv)
+    _launch(c, stream, lib().bdlm_cache_write, c._ref, _int("layer", layer), n, a, b, at, rows, rk, rv)
 
 
 def _check_q(c, q):
@@ -182,7 +182,7 @@ def prefix_attn_workspace_bytes(q, cache: Cache, prefix: int = 0) -> int:
     """Workspace of :func:`prefix_attn` for queries like ``q``."""
     c = _cache(cache)
     R, n, H = _check_q(c, q)
-    return int(lib().bdlm_prefix_attn_workspace_bytes(c._ref, R, n, H, prefix))
+    return int(lib().bdlm_prefix_attn_workspace_bytes(c._ref, R, n, H, _int("prefix", prefix)))
 
 
 def prefix_attn(q, cache: Cache, layer: int, seqs, prefix: int = 0, block: bool = False, scale: float = 0.0,
@@ -197,6 +197,7 @@ def prefix_attn(q, cache: Cache, layer: int, seqs, prefix: int = 0, block: bool 
     c = _cache(cache)
     R, n, H = _check_q(c, q)
     a = _list(c, "seqs", seqs, R)
+    layer, prefix = _int("layer", layer), _int("prefix", prefix)
     if out is None:
         o, lse = _made(stream, c.device, _new_outputs, q)
     else:

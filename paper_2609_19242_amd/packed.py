@@ -76,12 +76,22 @@ class PackedPlan:
                 f"head_dim={self.head_dim}, {self.dtype}, {self.device})")
 
 
+def _int(name, x, bits=64):
+    """``x`` as the C ABI's integer (which would take the low bits of a larger one)."""
+    x = operator.index(x)
+    if not -1 << bits - 1 <= x < 1 << bits - 1:
+        raise ValueError(f"{name} {x} does not fit {bits} bits")
+    return x
+
+
 def _ints(name, xs, n=None):
     if isinstance(xs, torch.Tensor):
         if xs.is_cuda or xs.dim() != 1 or xs.dtype not in (torch.int32, torch.int64):
             raise ValueError(f"{name} must be a one-dimensional integer tensor on the CPU, or a sequence of ints")
         xs = xs.tolist()
     xs = [operator.index(x) for x in xs]
+    if xs:
+        _int(name, min(xs)), _int(name, max(xs))
     if n is not None and len(xs) != n:
         raise ValueError(f"{name} has {len(xs)} entries for {n} sequences")
     return xs
@@ -112,7 +122,8 @@ def packed_plan(q_lens: Sequence[int], k_lens: Optional[Sequence[int]] = None, *
 
     qs = starts("q_starts", q_starts, ql)
     ks = starts("k_starts", k_starts, kl) if k_starts is not None or k_lens is not None or q_starts is None else qs
-    p = _Packed(heads, kv_heads, head_dim, _dtype_code(dtype), scale, 0, block_size, window)
+    p = _Packed(_int("heads", heads, 32), _int("kv_heads", kv_heads, 32), _int("head_dim", head_dim, 32), _dtype_code(dtype),
+                scale, 0, _int("block_size", block_size), _int("window", window))
     seqs = (_Seq * max(1, n))(*[_Seq(a, b, c, d) for a, b, c, d in zip(qs, ql, ks, kl)])
     rec = _Plan()
     _check(lib().bdlm_packed_plan_make(ctypes.byref(p), n, seqs, None, 0, ctypes.byref(rec)))
