@@ -296,6 +296,14 @@ int64_t bdlm_visible_pairs(const bdlm_problem* p, int32_t n_q, const bdlm_range*
  *     that q, k and v may be parts of one fused projection
  *   LSE          : [heads][lse_pitch] fp32, natural log
  * Everything is in the problem's dtype (LSE fp32).
+ *
+ * Rounding.  bf16: scores, softmax statistics, D and all sums are fp32; P (and,
+ * backward, dS) is rounded to bf16 for its second product, off by at most 2^-8 of
+ * itself, as in bdlm_attn_fwd and bdlm_attn_bwd without hilo, which packed calls do
+ * not have; outputs are rounded once.  fp32: fp64 between the inputs and the outputs,
+ * but for the LSE that backward reads and D between its kernels, which are fp32.  The
+ * same plan and inputs give the same bits.  In another batch a sequence's walks may
+ * be cut elsewhere, so that its sums run in another order.
  */
 typedef struct {
   int32_t heads, kv_heads, head_dim, dtype;
@@ -436,10 +444,17 @@ bdlm_status bdlm_cache_write(const bdlm_cache* c, int64_t layer, int64_t n, cons
  *   lse  : [requests][heads][rows] fp32, natural log
  * Rows that see nothing (also: of a sequence number out of range) get O = 0
  * and LSE = -inf.  Keys and values of tokens that a sequence holds must be finite,
- * as in packed calls; rows of pages behind its last token may hold anything.  A page number outside the cache reads as rows of zeros, and
- * lens are taken between 0 and what a table holds.
+ * as in packed calls; rows of pages behind its last token may hold anything.  A page
+ * number outside the cache reads as rows of zeros, and lens are taken between 0 and
+ * what a table holds.
+ * Rounding: as in packed calls, and where keys are cut into chunks their outputs are
+ * kept in fp32 in both dtypes; fp32 calls join them in fp64, bf16 ones in fp32.  The
+ * cuts follow the arguments and what a table can hold (the lengths are not known on
+ * the host), so bits may differ with `prefix`, the table's size and the batch.
  * workspace: bdlm_prefix_attn_workspace_bytes() bytes, 256-byte aligned, contents ignored on
- * entry; calls that may overlap in time need one each.
+ * entry; calls that may overlap in time need one each.  It grows with what a table can
+ * hold, by head_dim + 1 (fp32: + 2) words per chunk, row and head: 16 requests of 512
+ * rows of 32 heads take 258 MiB with tables of 9,700 tokens, 1.1 GiB with 131,072.
  */
 size_t bdlm_prefix_attn_workspace_bytes(const bdlm_cache* c, int64_t requests, int64_t rows, int32_t heads,
                                         int64_t prefix);

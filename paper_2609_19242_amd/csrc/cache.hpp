@@ -17,7 +17,7 @@ struct CacheArg {
   int32_t row_bytes;  // kv_heads * head_dim elements
 };
 
-// ---- page operations (cache_pages.hip).  work: kCacheWork words.
+// ---- page operations (cache_pages.hip)
 struct CacheList {
   int32_t n;
   const int32_t *a, *b;  // fork: parents, children; grow: sequences, counts; free: sequences
@@ -29,7 +29,10 @@ struct CacheRows {
   int64_t k_stride, v_stride;  // bytes between rows
   int64_t layer;
 };
-// Words of the page operations' workspace: a header, then a list of pages and one entry per listed sequence.
+// Words of the page operations' workspace (bdlm_cache_work_bytes): a header, then
+//   grow: the new pages (at most `pages`);
+//   fork: each child's page for its last rows (n <= seqs), then the new pages (at most `pages`);
+//   compact: the free pages to fill, the pages that move there, and each page's new number (`pages` words each).
 constexpr int kCacheHead = 16;
 hipError_t launch_cache_grow(const CacheArg& c, const CacheList& l, int32_t* work, hipStream_t s);
 hipError_t launch_cache_fork(const CacheArg& c, const CacheList& l, int32_t* work, hipStream_t s);

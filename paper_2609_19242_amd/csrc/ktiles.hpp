@@ -46,8 +46,8 @@ __device__ inline bool key_tile_item(const PackedArgs& a, int wg, KeyTileItem& i
   return true;
 }
 
-// A workgroup's chunk of its tile's walk: steps [n0, n1), and where its partial
-// sums go (null: it walks the whole tile and writes the gradients).  False: no such chunk.
+// A workgroup's chunk of its tile's walk: steps [n0, n1), and whether the walk is
+// cut (then it leaves partial sums, else it writes the gradients).  False: no such chunk.
 struct Chunk {
   int n0, n1;
   bool cut;

@@ -76,7 +76,7 @@ struct RowState {
   }
 };
 
-// P of U 32-key steps from the scores, as bf16 operands (off by at most 2^-9
+// P of U 32-key steps from the scores, as bf16 operands (off by at most 2^-8
 // relative, as in the forward).  The running max of a row moves on its first
 // visible tile, and when a lane's sum over a tile passes 2^64: see fwd_bf16.hip.
 template <int D, int U>
