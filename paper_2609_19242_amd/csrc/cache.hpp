@@ -63,7 +63,7 @@ struct PrefixArgs {
   int32_t pages, page_size, seqs_in_cache, max_pages;
   int32_t requests, rows, heads, kv_heads, group;
   int32_t prefix, block;      // block: every row sees all len keys
-  float scale_log2;
+  float scale, scale_log2;    // (scale: for the fp32 kernels, which multiply by log2(e) in 64 bits)
   int32_t prefix_chunks, prefix_chunk;  // chunks of the prefix, keys per chunk
   int32_t own_chunks, own_min;          // chunks of a request's own keys at most, keys per chunk at least
   int32_t prefix_tiles, own_tiles;      // tiles of query rows

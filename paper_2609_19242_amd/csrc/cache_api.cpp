@@ -329,7 +329,8 @@ bdlm_status bdlm_prefix_attn(const bdlm_cache* c, int64_t layer, int64_t request
   a.kv_heads = c->kv_heads;
   a.group = heads / c->kv_heads;
   a.block = block;
-  a.scale_log2 = (scale > 0.f ? scale : 1.0f / std::sqrt((float)c->head_dim)) * 1.44269504088896340736f;
+  a.scale = scale > 0.f ? scale : 1.0f / std::sqrt((float)c->head_dim);
+  a.scale_log2 = a.scale * 1.44269504088896340736f;
   const int bf16 = c->dtype == BDLM_BF16;
   hipError_t e = timed(kKPrefixAttn, stream, [&] {
     return bf16 ? launch_prefix_bf16(a, c->head_dim, stream) : launch_prefix_f32(a, c->head_dim, stream);

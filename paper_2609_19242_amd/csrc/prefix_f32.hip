@@ -60,7 +60,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
     return p < 0 ? -1 : ((int64_t)p * a.page_size + (key - e * a.page_size)) * row_elems;
   };
   auto row_of = [&](const float* base, int64_t off) { return off < 0 ? (const float*)zero_row_f32 : base + off; };
-  const double c = (double)a.scale_log2;
+  const double c = (double)a.scale * kLog2eD;
 
   AccTiles<D> acc;
   acc.zero();

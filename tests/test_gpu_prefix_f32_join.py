@@ -1,9 +1,8 @@
 """fp32 attention over the cache with scores that share a large offset: the log-sum-exps of a row's chunks are then large
 numbers that differ little, and what joins the chunks' outputs must not lose that difference.
 
-Scores are c s in 64 bits with c = scale log2(e) rounded to fp32 twice and the softmax scale once (u = 2^-24 each): a
-score s is off by 3 u |s|, of which only the differences within a row count for P, so P by 3 u (max s - min s).  A
-chunk's output is kept in fp32 (u of |O_j| <= sum P |V|), the joined one is rounded once (u |O|); everything else is in
+The softmax scale is an fp32 number, off by u = 2^-24 of itself at most: a score s is off by u |s|, of which only the
+differences within a row count for P, so P by u (max s - min s).  A chunk's output is kept in fp32 (u of |O_j| <= sum P |V|), the joined one is rounded once (u |O|); everything else is in
 64 bits.  Second-order terms: factor 1.05."""
 import math
 
@@ -54,9 +53,9 @@ def test_chunks_joined_at_large_log_sum_exps(lens, prefix, n, H, KV, D, spare, l
             z = torch.logsumexp(s, 1, keepdim=True)
             p = torch.exp(s - z)
             ref, spread = p @ vv[:, g], (s.amax(1) - s.masked_fill(~vis, math.inf).amin(1))[:, None]
-            bound = 1.05 * ((3 * U * spread + U) * (p @ vv[:, g].abs()) + U * ref.abs()) + 1e-30
+            bound = 1.05 * ((U * spread + U) * (p @ vv[:, g].abs()) + U * ref.abs()) + 1e-30
             used = float(((o[r, :, h].cpu().double() - ref).abs() / bound).max())
             worst = max(worst, used)
-            assert float((lse[r, h].cpu().double() - z[:, 0]).abs().max()) <= 4.2 * U * float(z.abs().max())
+            assert float((lse[r, h].cpu().double() - z[:, 0]).abs().max()) <= 2.1 * U * float(z.abs().max())
     print(f"{parts} parts: {worst:.3f} of the bound", flush=True)
     assert worst <= 1
