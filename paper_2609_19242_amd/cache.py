@@ -1,8 +1,9 @@
 """A paged cache of keys and values, operations on its pages, and the attention of decoding requests over it.
 
 :class:`Cache` holds the caller's tensors; the functions enqueue kernels on the current (or the given) stream and
-return without waiting; a given stream is not ordered against the current one.  The rules are those of
-``bdlm_cache_*`` and ``bdlm_prefix_attn`` in ``include/bdlm_attn.h``.
+return without waiting; a given stream is not ordered against the current one, and what a call reads there (lists and
+new rows too) is kept by the caller until it has run.  The rules are those of ``bdlm_cache_*`` and ``bdlm_prefix_attn`` in
+``include/bdlm_attn.h``.
 """
 from __future__ import annotations
 

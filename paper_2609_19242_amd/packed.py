@@ -3,7 +3,8 @@
 A :class:`PackedPlan` (:func:`packed_plan`) is made once for a set of sequence lengths and serves every layer,
 forward (:func:`packed_fwd`) and backward (:func:`packed_bwd`).  The rules and layouts are those of
 ``bdlm_packed_fwd`` in ``include/bdlm_attn.h``.  With ``stream``, a call runs there and is not ordered against the
-current stream: the caller orders what it reads before it and what uses its results behind it.
+current stream: the caller orders what it reads before it, keeps that until it has run, and orders what uses its results
+behind it.
 """
 from __future__ import annotations
 

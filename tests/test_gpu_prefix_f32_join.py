@@ -2,8 +2,8 @@
 numbers that differ little, and what joins the chunks' outputs must not lose that difference.
 
 The softmax scale is an fp32 number, off by u = 2^-24 of itself at most: a score s is off by u |s|, of which only the
-differences within a row count for P, so P by u (max s - min s).  A chunk's output is kept in fp32 (u of |O_j| <= sum P |V|), the joined one is rounded once (u |O|); everything else is in
-64 bits.  Second-order terms: factor 1.05."""
+differences within a row count for P, so P by u (max s - min s).  A chunk's output is kept in fp32 (u of |O_j| <= sum P
+|V|), the joined one is rounded once (u |O|); everything else is in 64 bits.  Second-order terms: factor 1.05."""
 import math
 
 import pytest
