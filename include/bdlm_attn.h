@@ -368,6 +368,50 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
                             bdlm_rows dv, void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /*
+ * Norms of queries and keys for each head with the position rotation, in one
+ * pass: what comes between the projections and any of the attention calls.
+ * For a head's row x with weight w (null: ones), at position p_a on axis a:
+ *   r = 1 / sqrt(mean x^2 + eps),  n = x r w     (eps 0: no norm, n = x),
+ * and of the first `dim` elements pair i, on axis axis[i], turns by
+ * t = p_axis[i] * freq[i]: (n1, n2) -> (n1 cos t - n2 sin t, n2 cos t + n1 sin t).
+ *   q, k, outputs : [rows][heads or kv_heads][head_dim], rows `stride` elements apart
+ *     (parts of one fused projection, say).  Outputs may be the inputs (the same
+ *     pointer and stride); other overlaps are the caller's error.
+ *   positions     : [axes][rows] int32 in device memory, of any sign
+ *   weights       : [head_dim] in `dtype`
+ * Rounding: angles are formed in 64 bits and reduced there; in bf16 sums and products are
+ * fp32 (|x| must be below 2^60), in fp32 the sums over a row are fp64; outputs are rounded
+ * once.  A NaN or infinity stays in its head's row (and reaches the weights' gradient).
+ */
+typedef struct {
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t dim;         /* elements that turn, a multiple of 16 in [16, head_dim] */
+  int32_t interleaved; /* pair i: 0: elements i and i + dim / 2, 1: elements 2 i and 2 i + 1 */
+  int32_t axes;        /* 1 to BDLM_MAX_AXES */
+  double freq[64];     /* radians per position of pairs 0 .. dim / 2 - 1 */
+  int32_t axis[64];
+} bdlm_rotary;
+#define BDLM_MAX_AXES 4
+
+bdlm_status bdlm_qk_rotate_fwd(const bdlm_rotary* r, int32_t dtype, int64_t rows, const int32_t* positions, int32_t heads,
+                               int32_t kv_heads, bdlm_rows q, bdlm_rows k, const void* q_weight, const void* k_weight,
+                               double eps, bdlm_rows q_out, bdlm_rows k_out, hipStream_t stream);
+
+/*
+ * Backward from the same inputs and the outputs' gradients dq_out, dk_out: dq and dk
+ * (which may be dq_out and dk_out), and the weights' gradients [head_dim] in fp32 (null:
+ * not wanted; without a norm they must be), the same bits in every call.  workspace:
+ * bdlm_qk_rotate_workspace_bytes(), 256-byte aligned, contents ignored on entry, one per call that may
+ * overlap in time; not needed where no weight's gradient is wanted.
+ */
+size_t bdlm_qk_rotate_workspace_bytes(int32_t head_dim);
+bdlm_status bdlm_qk_rotate_bwd(const bdlm_rotary* r, int32_t dtype, int64_t rows, const int32_t* positions, int32_t heads,
+                               int32_t kv_heads, bdlm_rows q, bdlm_rows k, const void* q_weight, const void* k_weight,
+                               double eps, bdlm_rows dq_out, bdlm_rows dk_out, bdlm_rows dq, bdlm_rows dk,
+                               float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
+
+/*
  * A paged cache of keys and values, and its pages' bookkeeping, all in device
  * memory owned by the caller.  Sequence s holds lens[s] tokens; token t is row
  * t % page_size of page table[s][t / page_size].  refs[p] counts the tables

@@ -15,7 +15,7 @@ bdlm_status hip_fail(hipError_t e, const char* what);
 // Kernels by id (bdlm_kernel_name).
 enum KernelId {
   kKFwdBf16 = 0, kKFwdF32, kKMerge, kKBwdDqF32, kKBwdBf16, kKBwdDq, kKBwdF32,
-  kKPackedFwd, kKPackedDq, kKPackedDkDv, kKPrefixAttn, kKPrefixMerge, kKCachePages, kKCacheWrite, kKCount
+  kKPackedFwd, kKPackedDq, kKPackedDkDv, kKPrefixAttn, kKPrefixMerge, kKCachePages, kKCacheWrite, kKQkRotate, kKCount
 };
 
 // Per-thread kernel timing (bdlm_timing_enable): events around a launch.

@@ -1,0 +1,179 @@
+// C ABI of rotated queries and keys: argument validation, how rows and heads
+// are dealt out, launches.  Declarations and contracts: include/bdlm_attn.h.
+#include "bdlm_attn.h"
+
+#include <algorithm>
+#include <cmath>
+
+#include "api_util.hpp"
+#include "rotate.hpp"
+
+using namespace bdlm;
+
+namespace {
+
+constexpr int64_t kMaxRows = (int64_t)1 << 28;
+constexpr int64_t kMaxStride = (int64_t)1 << 30;
+constexpr int64_t kWaves = 4;           // of a workgroup
+constexpr int64_t kFullWaves = 4096;    // waves from which on a row's heads stay with one wave
+constexpr int64_t kMaxFwdWgs = 1 << 20;
+constexpr int64_t kMaxBwdWgs = 1024;    // (each leaves its sums of the weights' gradients)
+
+bdlm_status check_rotary(const bdlm_rotary* r, int32_t dtype, int64_t rows, const int32_t* pos, int32_t heads,
+                         int32_t kv_heads, double eps) {
+  if (!r) return fail(BDLM_ERR_INVALID, "rotary is null");
+  if (r->head_dim != 64 && r->head_dim != 128)
+    return fail(BDLM_ERR_UNSUPPORTED, "head_dim %d not supported (64 or 128)", r->head_dim);
+  if (r->dim < 16 || r->dim > r->head_dim || r->dim % 16 != 0)
+    return fail(BDLM_ERR_INVALID, "dim %d is not a multiple of 16 in [16, head_dim]", r->dim);
+  if (r->interleaved != 0 && r->interleaved != 1) return fail(BDLM_ERR_INVALID, "interleaved must be 0 or 1");
+  if (r->axes < 1 || r->axes > BDLM_MAX_AXES)
+    return fail(BDLM_ERR_INVALID, "axes %d outside [1, %d]", r->axes, BDLM_MAX_AXES);
+  for (int i = 0; i < r->dim / 2; ++i) {
+    if (!(std::fabs(r->freq[i]) <= 1048576.0)) return fail(BDLM_ERR_INVALID, "frequency %d is not within 2^20", i);
+    if (r->axis[i] < 0 || r->axis[i] >= r->axes)
+      return fail(BDLM_ERR_INVALID, "pair %d: axis %d outside [0, %d)", i, r->axis[i], r->axes);
+  }
+  if (dtype != BDLM_BF16 && dtype != BDLM_F32) return fail(BDLM_ERR_UNSUPPORTED, "dtype %d not supported", dtype);
+  if (heads < 1 || kv_heads < 1 || heads > kMaxRows || kv_heads > kMaxRows)
+    return fail(BDLM_ERR_INVALID, "heads %d and kv_heads %d must be in [1, 2^28]", heads, kv_heads);
+  if (rows < 0 || rows > kMaxRows) return fail(BDLM_ERR_INVALID, "rows %lld outside [0, 2^28]", (long long)rows);
+  if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(BDLM_ERR_INVALID, "eps must be finite and not negative");
+  if (rows > 0 && (!pos || (reinterpret_cast<uintptr_t>(pos) & 3u)))
+    return fail(BDLM_ERR_INVALID, "positions are null or not 4-byte aligned");
+  return BDLM_OK;
+}
+
+bdlm_status check_rows(const bdlm_rows& r, const char* what, int64_t row_elems, int elem) {
+  if (!r.ptr || !aligned16(r.ptr)) return fail(BDLM_ERR_INVALID, "%s is null or not 16-byte aligned", what);
+  if (r.stride < row_elems || r.stride > kMaxStride || r.stride * elem % 16 != 0)
+    return fail(BDLM_ERR_INVALID, "%s row stride %lld outside [%lld, 2^30] or not a multiple of 16 bytes", what,
+                (long long)r.stride, (long long)row_elems);
+  return BDLM_OK;
+}
+
+bdlm_status check_weight(const void* w, const char* what, double eps) {
+  if (w && !aligned16(w)) return fail(BDLM_ERR_INVALID, "%s is not 16-byte aligned", what);
+  if (w && eps == 0.0) return fail(BDLM_ERR_INVALID, "%s without a norm", what);
+  return BDLM_OK;
+}
+
+// Rows of a wave, and waves that share a row's heads.
+void deal(const bdlm_rotary& r, int64_t rows, int32_t heads, int32_t kv_heads, int64_t max_wgs, RotateArgs& a) {
+  const int side = 64 / (r.head_dim / 16);  // heads of a wave
+  auto passes = [&](int64_t h, int per) { return (h + side / per - 1) / (side / per); };
+  // passes per row, of which one for the cosines and sines
+  auto cost = [&](int per) { return (double)(passes(heads, per) + passes(kv_heads, per) + 1) / per; };
+  int best = 1;
+  for (int per = 2; per <= side; per *= 2)
+    if (cost(per) < cost(best)) best = per;
+  a.rows_per = best;
+  a.t[0].passes = (int32_t)passes(heads, best);
+  a.t[1].passes = (int32_t)passes(kv_heads, best);
+  const int64_t sets = (rows + best - 1) / best, all = (int64_t)a.t[0].passes + a.t[1].passes;
+  a.split = (int32_t)std::min(std::max<int64_t>((kFullWaves + sets - 1) / sets, 1), all);
+  a.wgs = (int32_t)std::min((sets * a.split + kWaves - 1) / kWaves, max_wgs);
+}
+
+RotateArgs rotate_args(const bdlm_rotary& r, int64_t rows, const int32_t* pos, double eps) {
+  RotateArgs a{};
+  a.pos = pos;
+  a.rows = rows;
+  a.eps = eps;
+  a.axes = r.axes;
+  a.dim = r.dim;
+  for (int i = 0; i < r.dim / 2; ++i) {
+    a.quarters[i] = r.freq[i] * 0.63661977236758134308;  // 2 / pi
+    a.axis[i] = r.axis[i];
+  }
+  return a;
+}
+
+RotateTensor tensor(const bdlm_rows& x, const bdlm_rows& dy, const void* w, const bdlm_rows& out, int32_t heads) {
+  RotateTensor t{};
+  t.x = x.ptr;
+  t.xs = x.stride;
+  t.dy = dy.ptr;
+  t.dys = dy.stride;
+  t.w = w;
+  t.out = out.ptr;
+  t.outs = out.stride;
+  t.heads = heads;
+  return t;
+}
+
+}  // namespace
+
+extern "C" {
+
+bdlm_status bdlm_qk_rotate_fwd(const bdlm_rotary* r, int32_t dtype, int64_t rows, const int32_t* positions, int32_t heads,
+                               int32_t kv_heads, bdlm_rows q, bdlm_rows k, const void* q_weight, const void* k_weight,
+                               double eps, bdlm_rows q_out, bdlm_rows k_out, hipStream_t stream) {
+  bdlm_status st;
+  if ((st = check_rotary(r, dtype, rows, positions, heads, kv_heads, eps)) != BDLM_OK) return st;
+  if ((st = check_weight(q_weight, "q weight", eps)) != BDLM_OK || (st = check_weight(k_weight, "k weight", eps)) != BDLM_OK)
+    return st;
+  if (rows == 0) return BDLM_OK;
+  const int elem = dtype == BDLM_F32 ? 4 : 2;
+  const int64_t qe = (int64_t)heads * r->head_dim, ke = (int64_t)kv_heads * r->head_dim;
+  if ((st = check_rows(q, "q", qe, elem)) != BDLM_OK || (st = check_rows(k, "k", ke, elem)) != BDLM_OK ||
+      (st = check_rows(q_out, "q_out", qe, elem)) != BDLM_OK || (st = check_rows(k_out, "k_out", ke, elem)) != BDLM_OK)
+    return st;
+  RotateArgs a = rotate_args(*r, rows, positions, eps);
+  a.t[0] = tensor(q, bdlm_rows{}, q_weight, q_out, heads);
+  a.t[1] = tensor(k, bdlm_rows{}, k_weight, k_out, kv_heads);
+  deal(*r, rows, heads, kv_heads, kMaxFwdWgs, a);
+  const hipError_t e = timed(kKQkRotate, stream, [&] {
+    return launch_rotate_fwd(a, r->head_dim, dtype == BDLM_BF16, r->interleaved, stream);
+  });
+  return e == hipSuccess ? BDLM_OK : hip_fail(e, "rotation launch");
+}
+
+size_t bdlm_qk_rotate_workspace_bytes(int32_t head_dim) {
+  return head_dim == 64 || head_dim == 128 ? (size_t)kMaxBwdWgs * 2 * head_dim * sizeof(float) : 0;
+}
+
+bdlm_status bdlm_qk_rotate_bwd(const bdlm_rotary* r, int32_t dtype, int64_t rows, const int32_t* positions, int32_t heads,
+                               int32_t kv_heads, bdlm_rows q, bdlm_rows k, const void* q_weight, const void* k_weight,
+                               double eps, bdlm_rows dq_out, bdlm_rows dk_out, bdlm_rows dq, bdlm_rows dk,
+                               float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream) {
+  bdlm_status st;
+  if ((st = check_rotary(r, dtype, rows, positions, heads, kv_heads, eps)) != BDLM_OK) return st;
+  if ((st = check_weight(q_weight, "q weight", eps)) != BDLM_OK || (st = check_weight(k_weight, "k weight", eps)) != BDLM_OK)
+    return st;
+  float* const dw[2] = {dq_weight, dk_weight};
+  for (float* w : dw) {
+    if (w && (reinterpret_cast<uintptr_t>(w) & 3u)) return fail(BDLM_ERR_INVALID, "a weight's gradient is not 4-byte aligned");
+    if (w && eps == 0.0) return fail(BDLM_ERR_INVALID, "a weight's gradient without a norm");
+  }
+  const bool weights = dq_weight || dk_weight;
+  const size_t need = weights ? bdlm_qk_rotate_workspace_bytes(r->head_dim) : 0;
+  if (need > 0 && (!workspace || workspace_bytes < need || (reinterpret_cast<uintptr_t>(workspace) & 255u)))
+    return fail(BDLM_ERR_WORKSPACE, "workspace needs %zu bytes, 256-byte aligned (got %zu at %p)", need, workspace_bytes,
+                workspace);
+  if (rows == 0 && !weights) return BDLM_OK;
+  RotateArgs a = rotate_args(*r, rows, positions, eps);
+  a.partials = weights ? static_cast<float*>(workspace) : nullptr;
+  a.dw[0] = dq_weight;
+  a.dw[1] = dk_weight;
+  if (rows > 0) {
+    const int elem = dtype == BDLM_F32 ? 4 : 2;
+    const int64_t qe = (int64_t)heads * r->head_dim, ke = (int64_t)kv_heads * r->head_dim;
+    if (eps > 0.0 && ((st = check_rows(q, "q", qe, elem)) != BDLM_OK || (st = check_rows(k, "k", ke, elem)) != BDLM_OK))
+      return st;
+    if ((st = check_rows(dq_out, "dq_out", qe, elem)) != BDLM_OK || (st = check_rows(dk_out, "dk_out", ke, elem)) != BDLM_OK ||
+        (st = check_rows(dq, "dq", qe, elem)) != BDLM_OK || (st = check_rows(dk, "dk", ke, elem)) != BDLM_OK)
+      return st;
+    a.t[0] = tensor(q, dq_out, q_weight, dq, heads);
+    a.t[1] = tensor(k, dk_out, k_weight, dk, kv_heads);
+    deal(*r, rows, heads, kv_heads, kMaxBwdWgs, a);
+  }
+  // (no rows: no partial sums to add, zeros)
+  const hipError_t e = timed(kKQkRotate, stream, [&] {
+    return launch_rotate_bwd(a, r->head_dim, dtype == BDLM_BF16, r->interleaved, stream);
+  });
+  return e == hipSuccess ? BDLM_OK : hip_fail(e, "rotation backward launch");
+}
+
+}  // extern "C"
