@@ -284,7 +284,7 @@ int64_t bdlm_visible_pairs(const bdlm_problem* p, int32_t n_q, const bdlm_range*
  * queries are the last q_len tokens), key row j at position j.  With blocks of
  * block_size tokens and e = block_size * (floor(x / block_size) + 1), row x sees
  * the keys j < e (block_size 1: j <= x), with a window only those with
- * j >= e - window.  Rows at negative positions (q_len > k_len) see nothing.
+ * j >= e - window and the first ones, j < sinks.  Rows at negative positions (q_len > k_len) see nothing.
  * A row that sees no key gets O = 0, LSE = -inf and dQ = 0; a key that no row
  * sees gets dK = dV = 0.  Rows that belong to no sequence are neither read nor
  * written.  The other rows must be finite: hidden pairs enter products as 0 times
@@ -308,7 +308,7 @@ int64_t bdlm_visible_pairs(const bdlm_problem* p, int32_t n_q, const bdlm_range*
 typedef struct {
   int32_t heads, kv_heads, head_dim, dtype;
   float scale;         /* <= 0 selects 1 / sqrt(head_dim); positive scales below 2^-96 are unsupported */
-  int32_t reserved;    /* must be 0 */
+  int32_t sinks;       /* with a window: the first keys of a sequence that stay visible */
   int64_t block_size;  /* tokens per block, 1 for token-causal attention */
   int64_t window;      /* 0: no limit */
 } bdlm_packed;

@@ -863,6 +863,11 @@ hipError_t launch_bwd_dkdv(const AttnArgs& a, int head_dim, hipStream_t s) {
 
 #else
 
+#ifdef BDLM_SINK_CALLS
+using PackedK = SinkKArgs;
+#else
+using PackedK = PackedArgs;
+
 hipError_t launch_bwd_dkdv_sum(const PackedArgs& a, int head_dim, hipStream_t s) {
   const int n = a.n_sums * a.kv_heads;
   if (n == 0) return hipSuccess;
@@ -871,8 +876,9 @@ hipError_t launch_bwd_dkdv_sum(const PackedArgs& a, int head_dim, hipStream_t s)
   else hipLaunchKernelGGL((dkdv_sum_kernel<64, PackedArgs>), dim3(n * kSumWgs<64>), dim3(256), 0, s, a);
   return hipGetLastError();
 }
+#endif
 
-hipError_t launch_bwd_dkdv(const PackedArgs& a, int head_dim, hipStream_t s) {
+hipError_t launch_bwd_dkdv(const PackedK& a, int head_dim, hipStream_t s) {
   const int n = workgroups_for(a.n_items * a.kv_heads);
   if (n == 0) return hipSuccess;
   if (head_dim == 128) launch_rows<128, false>(a, n, s);

@@ -157,7 +157,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const KRangeArg& kr = k_range(a, cc.c.j);
       cc.src = (const bf16*)(kwave ? kr.k : kr.v) +
                row_elem<D>(a, it.b, kr.bstride, (int64_t)cc.c.t * BN, HKV, kvh, CS);
-      cc.rows_left = (kPacked ? u1 : kr.len) - cc.c.t * BN;
+      if constexpr (kHasSinks<Args>) cc.rows_left = imin(u1 - (cc.c.j ? a.split : 0), kr.len) - cc.c.t * BN;
+      else cc.rows_left = (kPacked ? u1 : kr.len) - cc.c.t * BN;
     }
     return cc;
   };
@@ -190,7 +191,20 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
     for (int k = 0; k < NB; ++k) {
       const int nr = nrows - 16 * k;
-      if constexpr (kPacked) {
+      if constexpr (kHasSinks<Args>) {
+        // rows between the sinks and the first seen key of the windows read zeros too
+        const int hole0 = (cc.c.j ? 0 : a.sinks - cc.c.t * BN) - 16 * k;
+        const int hole1 = u0 - (cc.c.j ? a.split : 0) - cc.c.t * BN - 16 * k;
+        if (cc.c.have && nr > 0 && hole1 > imax(hole0, 0)) {
+          const auto r = make_rsrc(cc.src + (int64_t)16 * k * CS, (uint32_t)(((nr - 1) * (int)CS + D) * 2));
+#pragma unroll
+          for (int i = 0; i < PI; ++i) {
+            const int row = ((cw * IPW + i) * 64 + lane) / (D / 8);
+            buf_to_lds<16>(r, dst + (k * PI + i) * 512, row >= hole0 && row < hole1 ? ~15u : voff[i], 0);
+          }
+          continue;
+        }
+      } else if constexpr (kPacked) {
         // rows before the first seen key lie before the resource: their offsets wrap and read zeros too (as in
         // the forward; no row of this copy's reach where the last seen key lies before it)
         const int skip = cc.c.have ? u0 - cc.c.t * BN - 16 * k : 0;
@@ -228,6 +242,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   vm_wait_barrier<IPW * (NST - 2)>();
   int cur = 0;
   int lane_lo = 0, lane_w = 0, lane_j = -1;
+  [[maybe_unused]] int lane_s = 0, lane_end = 0;  // with sinks: this lane's in range j; the end of its keys
   [[maybe_unused]] bool few_keys = false;  // packed calls: some row of this wave has no more keys than a tile holds
   while (c0.have) {
     copy_tile(lds + (cur == 0 ? NST - 1 : cur - 1) * STAGE, cp);
@@ -235,7 +250,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     if (lane_j != j) {
       lane_key_interval(a, j, qr.stream, pq, lane_lo, lane_w);
       lane_j = j;
-      if constexpr (kPacked) few_keys = __builtin_amdgcn_ballot_w64(lane_w > 0 && lane_w <= BN) != 0;
+      lane_sinks(a, j, qr.stream, pq, lane_s, lane_end);
+      if constexpr (kHasSinks<Args>) few_keys = j == 0 && __builtin_amdgcn_ballot_w64(lane_end > 0 && lane_end <= BN) != 0;
+      else if constexpr (kPacked) few_keys = __builtin_amdgcn_ballot_w64(lane_w > 0 && lane_w <= BN) != 0;
     }
 
     // On a partly visible tile, a wave none of whose rows sees any of the
@@ -243,7 +260,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     bool skip = false;
     if (!(t >= f0 && t < f1)) {
       const int kstart = k_range(a, j).pos0 + t * BN - lane_lo;
-      skip = __builtin_amdgcn_ballot_w64(lane_w > 0 && kstart < lane_w && kstart + BN > 0) == 0;
+      skip = __builtin_amdgcn_ballot_w64((lane_w > 0 && kstart < lane_w && kstart + BN > 0) ||
+                                         (kHasSinks<Args> && t * BN < lane_s)) == 0;
     }
     if (!skip) {
       // S^T = K Q^T and dP^T = V dO^T: K and V rows 32u + l32 by row reads.
@@ -290,7 +308,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int kk = base + u * 32 + (i >> 2) * 8 + (i & 3);
-            if ((unsigned)kk >= (unsigned)lane_w) sacc[u][i] = -INFINITY;
+            bool hidden = (unsigned)kk >= (unsigned)lane_w;
+            if constexpr (kHasSinks<Args>) hidden = hidden && t * BN + 4 * half + u * 32 + (i >> 2) * 8 + (i & 3) >= lane_s;
+            if (hidden) sacc[u][i] = -INFINITY;
           }
       }
 
@@ -300,7 +320,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       // dS where a row has few keys (one key: all of it).  (D lies in dpacc already.)
       if (kPacked && few_keys) {
         const int kstart = k_range(a, j).pos0 + t * BN - lane_lo;
-        if (__builtin_amdgcn_ballot_w64(lane_w > 0 && kstart <= 0 && kstart + BN >= lane_w) != 0) {
+        // (with sinks a row that sees anything sees key 0: all of its keys lie in the first tile or none of the tiles)
+        const bool whole = kHasSinks<Args> ? j == 0 && t == 0 && lane_end > 0 && lane_end <= BN
+                                           : lane_w > 0 && kstart <= 0 && kstart + BN >= lane_w;
+        if (__builtin_amdgcn_ballot_w64(whole) != 0) {
           float rest = 0.f, z = lse2;
           asm volatile("" : "+v"(z));  // (or the compiler keeps these exponentials for the ones below, and spills)
 #pragma unroll
@@ -311,7 +334,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
               if (i % 4 == 3) __builtin_amdgcn_sched_barrier(0);
             }
           rest += partner(rest);
-          if (kstart > 0 || kstart + BN < lane_w) rest = 0.f;
+          if (kHasSinks<Args> ? !whole : kstart > 0 || kstart + BN < lane_w) rest = 0.f;
           dl += rest;  // (no other tile has keys of the row)
 #pragma unroll
           for (int u = 0; u < 2; ++u)
@@ -396,7 +419,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     int lo, wid;
     lane_key_interval(a, 0, qr.stream, pq, lo, wid);
     const int first = (lo - k_range(a, 0).pos0) / BN;
-    const bool mine = p.slot < 0 || (wid > 0 ? first >= walk0 && first < walk1 : p.n0 == 0);
+    const bool mine = p.slot < 0 || (!kHasSinks<Args> && wid > 0 ? first >= walk0 && first < walk1 : p.n0 == 0);
     if (row_ok && half == 0 && mine) qr.delta[((int64_t)it.b * H + h) * qr.len + my_row] = -dl;
     if (p.slot >= 0) {  // a chunk's share of dQ
       float* op = (float*)args.partials + q_partial_row<NW, HP>(args, it, w, l32) * D;
@@ -484,17 +507,23 @@ hipError_t launch_bwd_dq_bf16(const AttnArgs& a, int head_dim, int rows, hipStre
 
 }  // namespace
 
+#ifdef BDLM_SINK_CALLS
+using PackedQ = SinkQArgs;
+#else
+using PackedQ = PackedArgs;
+#endif
+
 template <int D>
-void launch_packed(const PackedArgs& a, int n, hipStream_t s) {
+void launch_packed(const PackedQ& a, int n, hipStream_t s) {
   constexpr int NW = kQRowsShortBf16 / 32;
   const int hp = packed_tile_heads(a.group);
   const dim3 grid(n), threads(NW * 64);
-  if (hp == 4) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedArgs, 4>), grid, threads, 0, s, a);
-  else if (hp == 2) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedArgs, 2>), grid, threads, 0, s, a);
-  else hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedArgs, 1>), grid, threads, 0, s, a);
+  if (hp == 4) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedQ, 4>), grid, threads, 0, s, a);
+  else if (hp == 2) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedQ, 2>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedQ, 1>), grid, threads, 0, s, a);
 }
 
-hipError_t launch_bwd_dq_bf16(const PackedArgs& a, int head_dim, hipStream_t s) {
+hipError_t launch_bwd_dq_bf16(const PackedQ& a, int head_dim, hipStream_t s) {
   const int n = workgroups_for(a.n_items * (a.heads / packed_tile_heads(a.group)));
   if (n == 0) return hipSuccess;
   head_dim == 128 ? launch_packed<128>(a, n, s) : launch_packed<64>(a, n, s);

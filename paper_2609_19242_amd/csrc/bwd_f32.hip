@@ -393,21 +393,31 @@ hipError_t launch_bwd_sum_f32(const AttnArgs& a, int head_dim, hipStream_t s) {
 
 #else
 
-hipError_t launch_bwd_dq_f32(const PackedArgs& a, int head_dim, hipStream_t s) {
+#ifdef BDLM_SINK_CALLS
+using PackedQ = SinkQArgs;
+using PackedK = SinkKArgs;
+#else
+using PackedQ = PackedArgs;
+using PackedK = PackedArgs;
+#endif
+
+hipError_t launch_bwd_dq_f32(const PackedQ& a, int head_dim, hipStream_t s) {
   const int n = workgroups_for(a.n_items * a.heads);
   if (n == 0) return hipSuccess;
-  if (head_dim == 128) hipLaunchKernelGGL((bwd_dq_f32_kernel<128, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
-  else hipLaunchKernelGGL((bwd_dq_f32_kernel<64, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  if (head_dim == 128) hipLaunchKernelGGL((bwd_dq_f32_kernel<128, PackedQ>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  else hipLaunchKernelGGL((bwd_dq_f32_kernel<64, PackedQ>), grid_of(n), dim3(kWaves * 64), 0, s, a);
   return hipGetLastError();
 }
 
-hipError_t launch_bwd_dkv_f32(const PackedArgs& a, int head_dim, hipStream_t s) {
+hipError_t launch_bwd_dkv_f32(const PackedK& a, int head_dim, hipStream_t s) {
   const int n = workgroups_for(a.n_items * a.kv_heads);
   if (n == 0) return hipSuccess;
-  if (head_dim == 128) hipLaunchKernelGGL((bwd_dkv_f32_kernel<128, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
-  else hipLaunchKernelGGL((bwd_dkv_f32_kernel<64, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  if (head_dim == 128) hipLaunchKernelGGL((bwd_dkv_f32_kernel<128, PackedK>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+  else hipLaunchKernelGGL((bwd_dkv_f32_kernel<64, PackedK>), grid_of(n), dim3(kWaves * 64), 0, s, a);
   return hipGetLastError();
 }
+
+#ifndef BDLM_SINK_CALLS
 
 hipError_t launch_bwd_sum_f32(const PackedArgs& a, int head_dim, hipStream_t s) {
   const int n = a.n_sums * a.kv_heads;
@@ -417,6 +427,7 @@ hipError_t launch_bwd_sum_f32(const PackedArgs& a, int head_dim, hipStream_t s) 
   return hipGetLastError();
 }
 
+#endif
 #endif
 
 }  // namespace bdlm

@@ -137,7 +137,8 @@ __global__ __launch_bounds__(NT * NW * 64)
       const KRangeArg& kr = k_range(a, cc.c.j);
       cc.src = (const bf16*)(kwave ? kr.k : kr.v) +
                row_elem<D>(a, it.b, kr.bstride, (int64_t)cc.c.t * BN, HKV, kvh, CS);
-      cc.rows_left = (kIsPacked<Args> ? u1 : kr.len) - cc.c.t * BN;
+      if constexpr (kHasSinks<Args>) cc.rows_left = imin(u1 - (cc.c.j ? a.split : 0), kr.len) - cc.c.t * BN;
+      else cc.rows_left = (kIsPacked<Args> ? u1 : kr.len) - cc.c.t * BN;
     }
     return cc;
   };
@@ -164,7 +165,19 @@ __global__ __launch_bounds__(NT * NW * 64)
     const int nrows = cc.c.have ? imin(BN, cc.rows_left) : 0;
     const uint32_t bytes = cc.c.have ? (uint32_t)(((nrows - 1) * (int)CS + D) * 2) : 0u;
     bf16* dst = st + (kwave ? 0 : BN * D) + cw * IPW * 512;
-    if constexpr (kIsPacked<Args>) {
+    if constexpr (kHasSinks<Args>) {
+      // rows between the sinks and the first seen key of the windows read zeros too
+      const int hole0 = cc.c.j ? 0 : a.sinks - cc.c.t * BN, hole1 = u0 - (cc.c.j ? a.split : 0) - cc.c.t * BN;
+      if (cc.c.have && hole1 > imax(hole0, 0)) {
+        const auto r = make_rsrc(cc.src, bytes);
+#pragma unroll
+        for (int i = 0; i < IPW; ++i) {
+          const int row = ((cw * IPW + i) * 64 + lane) / (D / 8);
+          buf_to_lds<16>(r, dst + i * 512, row >= hole0 && row < hole1 ? ~15u : voff[i], 0);
+        }
+        return;
+      }
+    } else if constexpr (kIsPacked<Args>) {
       // rows before the first seen key lie before the resource: their offsets wrap and read zeros too
       const int skip = cc.c.have ? u0 - cc.c.t * BN : 0;
       if (skip > 0) {
@@ -206,12 +219,14 @@ __global__ __launch_bounds__(NT * NW * 64)
   vm_wait_barrier<IPW * (NS - 2)>();
   int cur = 0;
   int lane_lo = 0, lane_w = 0, lane_j = -1;
+  [[maybe_unused]] int lane_s = 0, lane_end = 0;  // with sinks: this lane's in range j
   while (NT > 1 ? rounds > 0 : c0.have) {
     if constexpr (NT > 1) --rounds;
     copy_tile(lds + (cur == 0 ? NS - 1 : cur - 1) * STAGE, cp);
     const int j = c0.j, t = c0.t, f0 = c0.f0, f1 = c0.f1;
     if (lane_j != j && (NT == 1 || c0.have)) {  // this lane's visible key interval inside range j
       lane_key_interval(a, j, qr.stream, pq, lane_lo, lane_w);
+      lane_sinks(a, j, qr.stream, pq, lane_s, lane_end);
       lane_j = j;
     }
 
@@ -220,7 +235,8 @@ __global__ __launch_bounds__(NT * NW * 64)
     bool skip = NT > 1 && !c0.have;
     if (!skip && !(t >= f0 && t < f1)) {
       const int kstart = k_range(a, j).pos0 + t * BN - lane_lo;
-      skip = __builtin_amdgcn_ballot_w64(lane_w > 0 && kstart < lane_w && kstart + BN > 0) == 0;
+      skip = __builtin_amdgcn_ballot_w64((lane_w > 0 && kstart < lane_w && kstart + BN > 0) ||
+                                         (kHasSinks<Args> && t * BN < lane_s)) == 0;
     }
     if (!skip) {
       // S^T = K Q^T: K rows 32u + l32 by row reads (K tile at the stage base).
@@ -262,7 +278,9 @@ __global__ __launch_bounds__(NT * NW * 64)
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
             const int kk = base + u * 32 + (i >> 2) * 8 + (i & 3);
-            if ((unsigned)kk >= (unsigned)lane_w) sacc[u][i] = -INFINITY;
+            bool hidden = (unsigned)kk >= (unsigned)lane_w;
+            if constexpr (kHasSinks<Args>) hidden = hidden && t * BN + 4 * half + u * 32 + (i >> 2) * 8 + (i & 3) >= lane_s;
+            if (hidden) sacc[u][i] = -INFINITY;
           }
       }
 
@@ -513,13 +531,19 @@ hipError_t launch_fwd_bf16(const AttnArgs& a, int head_dim, QTile q, hipStream_t
 
 }  // namespace
 
+#ifdef BDLM_SINK_CALLS
+using PackedQ = SinkQArgs;
+#else
+using PackedQ = PackedArgs;
+#endif
+
 template <int D, int NT, int HP>
-void launch_packed(const PackedArgs& a, int n, hipStream_t s) {
+void launch_packed(const PackedQ& a, int n, hipStream_t s) {
   constexpr int NW = kQRowsShortBf16 / 32;
-  hipLaunchKernelGGL((fwd_bf16_kernel<D, NW, 2, 0, NT, PackedArgs, HP>), dim3(n), dim3(NT * NW * 64), 0, s, a);
+  hipLaunchKernelGGL((fwd_bf16_kernel<D, NW, 2, 0, NT, PackedQ, HP>), dim3(n), dim3(NT * NW * 64), 0, s, a);
 }
 template <int D, int NT>
-void launch_packed_heads(const PackedArgs& a, int n, hipStream_t s) {
+void launch_packed_heads(const PackedQ& a, int n, hipStream_t s) {
   const int hp = packed_tile_heads(a.group);
   if (hp == 4) launch_packed<D, NT, 4>(a, n, s);
   else if (hp == 2) launch_packed<D, NT, 2>(a, n, s);
@@ -527,7 +551,7 @@ void launch_packed_heads(const PackedArgs& a, int n, hipStream_t s) {
 }
 
 // Packed calls: four waves per tile (packed_tile_heads in packed.hpp), two teams of them when there are few tiles.
-hipError_t launch_fwd_bf16(const PackedArgs& a, int head_dim, int teams, hipStream_t s) {
+hipError_t launch_fwd_bf16(const PackedQ& a, int head_dim, int teams, hipStream_t s) {
   const int n = workgroups_for(a.n_items * (a.heads / packed_tile_heads(a.group)));
   if (n == 0) return hipSuccess;
   if (head_dim == 128) teams == 2 ? launch_packed_heads<128, 2>(a, n, s) : launch_packed_heads<128, 1>(a, n, s);

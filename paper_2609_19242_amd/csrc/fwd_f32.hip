@@ -181,13 +181,19 @@ hipError_t launch_fwd_f32(const AttnArgs& a, int head_dim, hipStream_t s) {
 
 #else
 
-hipError_t launch_fwd_f32(const PackedArgs& a, int head_dim, hipStream_t s) {
+#ifdef BDLM_SINK_CALLS
+using PackedQ = SinkQArgs;
+#else
+using PackedQ = PackedArgs;
+#endif
+
+hipError_t launch_fwd_f32(const PackedQ& a, int head_dim, hipStream_t s) {
   const int n = workgroups_for(a.n_items * a.heads);
   if (n == 0) return hipSuccess;
   if (head_dim == 128)
-    hipLaunchKernelGGL((fwd_f32_kernel<128, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+    hipLaunchKernelGGL((fwd_f32_kernel<128, PackedQ>), grid_of(n), dim3(kWaves * 64), 0, s, a);
   else
-    hipLaunchKernelGGL((fwd_f32_kernel<64, PackedArgs>), grid_of(n), dim3(kWaves * 64), 0, s, a);
+    hipLaunchKernelGGL((fwd_f32_kernel<64, PackedQ>), grid_of(n), dim3(kWaves * 64), 0, s, a);
   return hipGetLastError();
 }
 

@@ -46,6 +46,13 @@ __device__ inline bool key_tile_item(const PackedArgs& a, int wg, KeyTileItem& i
   return true;
 }
 
+// With sinks: tile -1 - t is the t-th of the sinks (packed.hpp).
+__device__ inline bool key_tile_item(const SinkKArgs& a, int wg, KeyTileItem& it) {
+  if (!key_tile_item(static_cast<const PackedArgs&>(a), wg, it)) return false;
+  if (it.t < 0) it.t = -1 - it.t;
+  return true;
+}
+
 // A workgroup's chunk of its tile's walk: steps [n0, n1), and whether the walk is
 // cut (then it leaves partial sums, else it writes the gradients).  False: no such chunk.
 struct Chunk {

@@ -45,6 +45,7 @@ struct PackedArgs {
   float *lse, *l2, *delta;
   void* partials;
   float* part_lse;     // forward: log2-sum-exp of each partial row
+  int32_t sinks;       // with a window: first keys that stay visible (0: none, and without a window)
 };
 
 // Positions start at a multiple of M that leaves room for query rows before
@@ -151,6 +152,78 @@ __device__ __forceinline__ int64_t row_elem(const PackedView&, int, int64_t, int
   return row * stride + h * D;
 }
 
+// ---- sinks: a window, and the first S keys of a sequence stay visible.
+//
+// A row sees the keys [0, min(S, e)) and [e - W, e).  A call with sinks is the same
+// kernels over another view of the sequence (SinkQArgs, SinkKArgs):
+//  * forward and dQ: two key ranges, the keys below `split` and the others.  bf16:
+//    split is S rounded up to whole 64-key tiles, so that a sequence's tiles are
+//    those of a call without sinks; in the first range a lane tests a key against
+//    its sinks and its window.  fp32: split is S.  A query tile visits the first
+//    range's tiles that hold sinks (or its window) and then its window's: the keys in
+//    between cost nothing.
+//  * dK/dV: the sinks, which all rows from theirs on see, are keys of a call without a
+//    window, the others of one without sinks: items of two kinds, tile -1 - t the
+//    t-th of the sinks.
+struct SinkQArgs : PackedArgs {};
+struct SinkKArgs : PackedArgs {};
+
+struct SinkView : PackedView {
+  static constexpr int n_k = 2;
+  int32_t sinks, split;
+  int32_t n0, n1;          // tiles of its walk that the item takes
+  int64_t k_ahead, v_ahead;  // bytes from a sequence's first key to the second range
+};
+
+inline int __host__ __device__ sink_split(int sinks, int k_len, bool f32) {
+  return imin(f32 ? sinks : (sinks + 63) / 64 * 64, k_len);
+}
+
+__device__ __forceinline__ SinkView call_view(const SinkQArgs& p, int item, int elem) {
+  const PackedItem& it = p.items[item];
+  SinkView a;
+  static_cast<PackedView&>(a) = packed_view(p, it, elem);
+  a.sinks = imin(p.sinks, it.k_len);
+  a.split = sink_split(p.sinks, it.k_len, elem == 4);
+  a.n0 = it.n0;
+  a.n1 = it.n1;
+  a.k_ahead = (int64_t)a.split * p.ks * elem;
+  a.v_ahead = (int64_t)a.split * p.vs * elem;
+  a.kr[0].len = a.split;  // (the second range: k_range)
+  a.kr[0].ntiles = it.k_len;
+  return a;
+}
+__device__ __forceinline__ KRangeArg k_range(const SinkView& a, int j) {
+  KRangeArg r = a.kr[0];
+  if (j > 0) {
+    r.pos0 += a.split;
+    r.len = r.ntiles - a.split;
+    r.k = (const char*)r.k + a.k_ahead;
+    r.v = (const char*)r.v + a.v_ahead;
+  }
+  return r;
+}
+
+__device__ __forceinline__ PackedView call_view(const SinkKArgs& p, int item, int elem) {
+  const PackedItem& it = p.items[item];
+  PackedView a = packed_view(p, it, elem);
+  const int S = imin(p.sinks, it.k_len);
+  KRangeArg& kr = a.kr[0];
+  if (it.tile < 0) {
+    a.rule.window = 0;
+    kr.len = S;
+  } else {
+    kr.pos0 += S;
+    kr.len -= S;
+    auto on = [&](const void* x, int32_t stride) { return (void*)((char*)const_cast<void*>(x) + (int64_t)S * stride * elem); };
+    kr.k = on(kr.k, p.ks);
+    kr.v = on(kr.v, p.vs);
+    kr.dk = on(kr.dk, p.dks);
+    kr.dv = on(kr.dv, p.dvs);
+  }
+  return a;
+}
+
 // Query and key ranges by number; a packed sequence has one of each (indexed by
 // a variable, its copy would live in scratch memory).
 __device__ __forceinline__ const QRangeArg& q_range(const AttnArgs& a, int i) { return a.qr[i]; }
@@ -166,6 +239,11 @@ __device__ __forceinline__ PackedView call_view(const PackedArgs& a, int item, i
 template <class A> constexpr bool kIsPacked = false;
 template <> constexpr inline bool kIsPacked<PackedArgs> = true;
 template <> constexpr inline bool kIsPacked<PackedView> = true;
+template <> constexpr inline bool kIsPacked<SinkQArgs> = true;
+template <> constexpr inline bool kIsPacked<SinkKArgs> = true;
+template <class A> constexpr bool kHasSinks = false;
+template <> constexpr inline bool kHasSinks<SinkQArgs> = true;
+template <> constexpr inline bool kHasSinks<SinkView> = true;
 
 hipError_t launch_fwd_bf16(const PackedArgs& a, int head_dim, int teams, hipStream_t s);
 hipError_t launch_packed_fwd_sum(const PackedArgs& a, int head_dim, int slots, hipStream_t s);
@@ -177,5 +255,11 @@ hipError_t launch_bwd_dkdv_sum(const PackedArgs& a, int head_dim, hipStream_t s)
 hipError_t launch_bwd_dq_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dkv_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_sum_f32(const PackedArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_fwd_bf16(const SinkQArgs& a, int head_dim, int teams, hipStream_t s);
+hipError_t launch_fwd_f32(const SinkQArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_bwd_dq_bf16(const SinkQArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_bwd_dkdv(const SinkKArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_bwd_dq_f32(const SinkQArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_bwd_dkv_f32(const SinkKArgs& a, int head_dim, hipStream_t s);
 
 }  // namespace bdlm

@@ -30,7 +30,7 @@ bdlm_status check_packed(const bdlm_packed* p) {
   if (!std::isfinite(p->scale)) return fail(BDLM_ERR_INVALID, "scale is not finite");
   if (p->scale > 0.f && p->scale < kMinScheduledScale)
     return fail(BDLM_ERR_UNSUPPORTED, "scale %g is below 2^-96", (double)p->scale);
-  if (p->reserved != 0) return fail(BDLM_ERR_INVALID, "reserved field must be 0");
+  if (p->sinks < 0 || p->sinks > kMaxLen) return fail(BDLM_ERR_INVALID, "sinks must be in [0, 2^28] (got %d)", p->sinks);
   if (p->block_size < 1 || p->block_size > kMaxLen)
     return fail(BDLM_ERR_INVALID, "block_size must be in [1, 2^28] (got %lld)", (long long)p->block_size);
   if (p->window < 0 || p->window > kMaxLen)
@@ -111,6 +111,7 @@ PackedArgs packed_args(const bdlm_packed_plan& pl, int64_t lse_pitch) {
   a.group = p.heads / p.kv_heads;
   a.M = (int32_t)p.block_size;
   a.window = (int32_t)p.window;
+  a.sinks = p.sinks;
   a.scale = p.scale > 0.f ? p.scale : 1.0f / std::sqrt((float)p.head_dim);
   a.scale_log2 = a.scale * 1.44269504088896340736f;
   a.q_rows = (int32_t)lse_pitch;
@@ -132,6 +133,12 @@ void take_chunks(const bdlm_packed_plan& pl, bool dq, PackedArgs& a) {
   a.n_sums = c.sums;
 }
 
+// launch(a), as a call with sinks if it has some.
+template <class Sinks, class F>
+hipError_t with_sinks(const PackedArgs& a, F&& launch) {
+  return a.sinks > 0 ? launch(Sinks{a}) : launch(a);
+}
+
 bdlm_status check_pitch(const bdlm_packed_plan& pl, int64_t pitch) {
   if (pitch < pl.q_rows || pitch > kMaxLen)
     return fail(BDLM_ERR_INVALID, "lse pitch %lld outside [%lld, 2^28]", (long long)pitch, (long long)pl.q_rows);
@@ -149,7 +156,9 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
   if ((st = check_packed(p)) != BDLM_OK) return st;
   int64_t q_rows = 0, k_rows = 0;
   if ((st = check_seqs(n_seqs, seqs, q_rows, k_rows)) != BDLM_OK) return st;
-  const PackedPlanItems it = packed_items(*p, n_seqs, seqs);
+  bdlm_packed problem = *p;
+  if (problem.window == 0) problem.sinks = 0;  // (every earlier key is visible)
+  const PackedPlanItems it = packed_items(problem, n_seqs, seqs);
   // (a grid dimension holds fewer than 2^32 threads; the fp32 kernels' grids have two)
   const bool f32 = p->dtype == BDLM_F32;
   const int64_t per = p->heads / (f32 ? 1 : packed_tile_heads(p->heads / p->kv_heads));
@@ -159,7 +168,7 @@ bdlm_status bdlm_packed_plan_make(const bdlm_packed* p, int64_t n_seqs, const bd
     return fail(BDLM_ERR_UNSUPPORTED, "packed problem needs %lld workgroups (limit %lld)", (long long)wgs,
                 (long long)most);
   bdlm_packed_plan pl{};
-  pl.problem = *p;
+  pl.problem = problem;
   pl.q_rows = q_rows;
   pl.k_rows = k_rows;
   pl.q_items = (int32_t)it.q.size();
@@ -237,8 +246,10 @@ bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdl
   a.os = (int32_t)o.stride;
   a.lse = lse;
   const hipError_t e = timed(kKPackedFwd, stream, [&] {
-    const hipError_t le = p.dtype == BDLM_BF16 ? launch_fwd_bf16(a, p.head_dim, plan->teams, stream)
-                                               : launch_fwd_f32(a, p.head_dim, stream);
+    const hipError_t le = with_sinks<SinkQArgs>(a, [&](const auto& c) {
+      return p.dtype == BDLM_BF16 ? launch_fwd_bf16(c, p.head_dim, plan->teams, stream)
+                                  : launch_fwd_f32(c, p.head_dim, stream);
+    });
     return le != hipSuccess || a.n_sums == 0 ? le : launch_packed_fwd_sum(a, p.head_dim, plan->fwd.slots, stream);
   });
   return e == hipSuccess ? BDLM_OK : hip_fail(e, "packed forward launch");
@@ -294,8 +305,9 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
   take_chunks(*plan, true, a);
   // dQ first: it leaves the row statistics for dK/dV.
   hipError_t e = timed(kKPackedDq, stream, [&] {
-    const hipError_t le =
-        p.dtype == BDLM_BF16 ? launch_bwd_dq_bf16(a, p.head_dim, stream) : launch_bwd_dq_f32(a, p.head_dim, stream);
+    const hipError_t le = with_sinks<SinkQArgs>(a, [&](const auto& c) {
+      return p.dtype == BDLM_BF16 ? launch_bwd_dq_bf16(c, p.head_dim, stream) : launch_bwd_dq_f32(c, p.head_dim, stream);
+    });
     return le != hipSuccess || a.n_sums == 0 ? le : launch_packed_dq_sum(a, p.head_dim, stream);
   });
   if (e != hipSuccess) return hip_fail(e, "packed dQ launch");
@@ -304,8 +316,9 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
   a.sums = reinterpret_cast<const PackedSum*>(a.items + plan->k_items);
   a.n_sums = plan->n_sums;
   e = timed(kKPackedDkDv, stream, [&] {
-    hipError_t le = p.dtype == BDLM_BF16 ? launch_bwd_dkdv(a, p.head_dim, stream)
-                                         : launch_bwd_dkv_f32(a, p.head_dim, stream);
+    hipError_t le = with_sinks<SinkKArgs>(a, [&](const auto& c) {
+      return p.dtype == BDLM_BF16 ? launch_bwd_dkdv(c, p.head_dim, stream) : launch_bwd_dkv_f32(c, p.head_dim, stream);
+    });
     if (le != hipSuccess || a.n_sums == 0) return le;
     return p.dtype == BDLM_BF16 ? launch_bwd_dkdv_sum(a, p.head_dim, stream) : launch_bwd_sum_f32(a, p.head_dim, stream);
   });

@@ -69,6 +69,11 @@ constexpr int64_t kStartTiles = 3;
 // the whole load, not a quarter of it: 5 texts of 33 to 407 rows, 8/2 heads, d 64
 // 46 -> 43 us, of which the sums 10 -> 5; bf16, 8K of documents: 0.5, 0.75, 1 and
 // 1.5 loads 263, 252, 245 and 261 us).
+//
+// Sinks (packed.hpp): a query tile's walk has the tiles that hold sinks or windowed
+// keys in the first range, then its window's in the second; a sequence's key tiles
+// are those of its sinks, numbered -1 - t, which all rows from theirs on walk, and
+// those of its other keys.
 inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_packed_seq* seqs) {
   PackedPlanItems out;
   const bool f32 = p.dtype == BDLM_F32;
@@ -77,7 +82,7 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
   const int q_tile = f32 ? kRowsF32 : kQRowsShortBf16 / tile_heads, k_tile = f32 ? kRowsF32 : kBwdKeysBf16;
   const int step = packed_step_rows(f32, group);
   const int64_t per_block = f32 || group % 2 ? group : group / 2;
-  const MaskRule rule{M, kIntraBlock, (int)p.window, 1, kBig, nullptr};
+  const MaskRule rule{M, kIntraBlock, (int)p.window, 1, kBig, nullptr}, always{M, kIntraBlock, 0, 1, kBig, nullptr};
 
   struct Cost {
     int64_t cost;
@@ -97,21 +102,32 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
       key_interval(kClean, qp + last, kClean, rule, lo1, hi1);
       it.tile = t;
       const int u0 = std::max(lo - shift, 0), u1 = std::min(hi1 - shift, kl);
-      q.push_back({std::max(0, u1 - u0), it});
-      walks.push_back({u1 > u0 ? (u1 + 63) / 64 - u0 / 64 : 0, it});
+      if (p.sinks == 0) {
+        q.push_back({std::max(0, u1 - u0), it});
+        walks.push_back({u1 > u0 ? (u1 + 63) / 64 - u0 / 64 : 0, it});
+      } else {
+        const int B = sink_split(p.sinks, kl, f32), near = std::min(B, std::max(u1, 0)), far = std::max(u0, B);
+        q.push_back({near + std::max(0, u1 - far), it});
+        walks.push_back({(near + 63) / 64 + (u1 > far ? (u1 - B + 63) / 64 - (far - B) / 64 : 0), it});
+      }
       fwd_total += walks.back().cost;
     }
-    for (int t = 0; t * (int64_t)k_tile < kl; ++t) {
-      const int first = t * k_tile, last = std::min(kl, first + k_tile) - 1;
-      int lo, hi, lo1, hi1;
-      query_interval(kClean, kClean, shift + first, rule, lo, hi);
-      query_interval(kClean, kClean, shift + last, rule, lo1, hi1);
-      const int u0 = std::max(lo - qp, 0), u1 = std::min(hi1 - qp, ql);
-      const int64_t steps = u1 > u0 ? ((u1 + step - 1) / step - u0 / step) * per_block : 0;
-      it.tile = t;
-      k.push_back({steps, it});
-      total += steps * p.kv_heads;
-    }
+    const int sinks = std::min(p.sinks, kl);
+    auto key_tiles = [&](int from, int to, const MaskRule& seen, bool sink) {  // keys [from, to) of the sequence
+      for (int t = 0; from + t * (int64_t)k_tile < to; ++t) {
+        const int first = from + t * k_tile, last = std::min(to, first + k_tile) - 1;
+        int lo, hi, lo1, hi1;
+        query_interval(kClean, kClean, shift + first, seen, lo, hi);
+        query_interval(kClean, kClean, shift + last, seen, lo1, hi1);
+        const int u0 = std::max(lo - qp, 0), u1 = std::min(hi1 - qp, ql);
+        const int64_t steps = u1 > u0 ? ((u1 + step - 1) / step - u0 / step) * per_block : 0;
+        it.tile = sink ? -1 - t : t;
+        k.push_back({steps, it});
+        total += steps * p.kv_heads;
+      }
+    };
+    key_tiles(0, sinks, always, true);
+    key_tiles(sinks, kl, rule, false);
   }
   auto heavier = [](const Cost& a, const Cost& b) { return a.cost > b.cost; };
   std::stable_sort(q.begin(), q.end(), heavier);
@@ -198,7 +214,11 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
   for (const Cost& c : k) {
     const int64_t nch = c.cost > unit ? (c.cost + unit - 1) / unit : 1;
     PackedItem it = c.it;
-    if (nch > 1) out.sums.push_back({it.k0, it.k_len, it.tile, out.slots, (int32_t)nch, 0, 0, 0});
+    if (nch > 1) {
+      const int sinks = std::min(p.sinks, it.k_len);
+      out.sums.push_back(it.tile < 0 ? PackedSum{it.k0, sinks, -1 - it.tile, out.slots, (int32_t)nch, 0, 0, 0}
+                                     : PackedSum{it.k0 + sinks, it.k_len - sinks, it.tile, out.slots, (int32_t)nch, 0, 0, 0});
+    }
     for (int64_t j = 0; j < nch; ++j) {
       it.n0 = (int32_t)(j * unit);
       it.n1 = j + 1 < nch ? (int32_t)((j + 1) * unit) : kBig;

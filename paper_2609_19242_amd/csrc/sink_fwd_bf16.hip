@@ -1,0 +1,4 @@
+// The kernels of fwd_bf16.hip for packed calls with a window and sinks (packed.hpp).
+#define BDLM_PACKED_CALLS
+#define BDLM_SINK_CALLS
+#include "fwd_bf16.hip"

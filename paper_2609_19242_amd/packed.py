@@ -22,7 +22,7 @@ __all__ = ["PackedPlan", "packed_plan", "packed_fwd", "packed_bwd"]
 
 class _Packed(ctypes.Structure):  # bdlm_packed
     _fields_ = [("heads", ctypes.c_int32), ("kv_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
-                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("reserved", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("scale", ctypes.c_float), ("sinks", ctypes.c_int32),
                 ("block_size", ctypes.c_int64), ("window", ctypes.c_int64)]
 
 
@@ -99,15 +99,16 @@ def _ints(name, xs, n=None):
 
 
 def packed_plan(q_lens: Sequence[int], k_lens: Optional[Sequence[int]] = None, *, heads: int, kv_heads: int,
-                head_dim: int, dtype, block_size: int = 1, window: int = 0, scale: float = 0.0,
+                head_dim: int, dtype, block_size: int = 1, window: int = 0, scale: float = 0.0, sinks: int = 0,
                 q_starts: Optional[Sequence[int]] = None, k_starts: Optional[Sequence[int]] = None,
                 device="cuda") -> PackedPlan:
     """The plan of packed calls over sequences of ``q_lens`` query rows and ``k_lens`` keys (default: the same).
 
     A sequence's queries are its last ``q_len`` tokens; each sees the keys up to the end of its block of
-    ``block_size`` tokens (1: up to itself), with ``window`` only the last ``window`` of those.  Sequences lie one
-    after the other, or at the rows ``q_starts`` / ``k_starts`` (a padded batch, say): in order, without overlap.
-    The lengths are host values; the plan's items are copied to ``device`` (not while a graph is captured)."""
+    ``block_size`` tokens (1: up to itself), with ``window`` only the last ``window`` of those and the sequence's first
+    ``sinks`` tokens.  Sequences lie one after the other, or at the rows ``q_starts`` / ``k_starts`` (a padded batch,
+    say): in order, without overlap.  The lengths are host values; the plan's items are copied to ``device`` (not while
+    a graph is captured)."""
     ql = _ints("q_lens", q_lens)
     n = len(ql)
     kl = ql if k_lens is None else _ints("k_lens", k_lens, n)
@@ -124,7 +125,7 @@ def packed_plan(q_lens: Sequence[int], k_lens: Optional[Sequence[int]] = None, *
     qs = starts("q_starts", q_starts, ql)
     ks = starts("k_starts", k_starts, kl) if k_starts is not None or k_lens is not None or q_starts is None else qs
     p = _Packed(_int("heads", heads, 32), _int("kv_heads", kv_heads, 32), _int("head_dim", head_dim, 32), _dtype_code(dtype),
-                scale, 0, _int("block_size", block_size), _int("window", window))
+                scale, _int("sinks", sinks, 32), _int("block_size", block_size), _int("window", window))
     seqs = (_Seq * max(1, n))(*[_Seq(a, b, c, d) for a, b, c, d in zip(qs, ql, ks, kl)])
     rec = _Plan()
     _check(lib().bdlm_packed_plan_make(ctypes.byref(p), n, seqs, None, 0, ctypes.byref(rec)))

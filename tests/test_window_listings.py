@@ -1,0 +1,35 @@
+"""What the listings of the kernels with sinks show, as test_serving_listings does for those without: products in inline
+assembly are waited for, no row address sits in a scalar offset, bf16 kernels keep their vector registers."""
+import pytest
+
+from tests.asm_listing import BF16, F64, functions, kernel_resources, listing, product_hazards, scalar_offset_accesses
+
+
+def text_of(src):
+    text = listing(src)
+    if text is None:
+        pytest.skip("hipcc not available")
+    return text
+
+
+@pytest.mark.parametrize("src,product,file,n", [("sink_fwd_f32.hip", F64, "v", 2), ("sink_bwd_f32.hip", F64, "v", 4),
+                                                ("sink_bwd_dkdv.hip", BF16, "a", 4)])
+def test_products_are_waited_for(src, product, file, n):
+    kernels = {name: b for name, b in functions(text_of(src)).items()
+               if any(op == product and ops[0].startswith(file) for _, _, op, ops in b)}
+    assert len(kernels) == n, sorted(kernels)
+    bad = {name: product_hazards(b, product, file) for name, b in kernels.items()}
+    assert not any(bad.values()), bad
+
+
+@pytest.mark.parametrize("src", ["sink_fwd_f32.hip", "sink_bwd_f32.hip"])
+def test_no_row_address_in_a_scalar_offset(src):
+    found = {n: scalar_offset_accesses(b) for n, b in functions(text_of(src)).items()}
+    assert sum(n for n, _ in found.values()) > 0
+    assert not any(lines for _, lines in found.values()), {n: x[1] for n, x in found.items() if x[1]}
+
+
+@pytest.mark.parametrize("src", ["sink_fwd_bf16.hip", "sink_bwd_dq.hip", "sink_bwd_dkdv.hip"])
+def test_nothing_goes_to_scratch(src):
+    for name, r in kernel_resources(text_of(src)).items():
+        assert r["vgpr_spill_count"] == 0 and r["private_segment_fixed_size"] == 0, (name, r)
