@@ -289,7 +289,8 @@ int64_t bdlm_visible_pairs(const bdlm_problem* p, int32_t n_q, const bdlm_range*
  * sees gets dK = dV = 0.  Rows that belong to no sequence are neither read nor
  * written.  The other rows must be finite: hidden pairs enter products as 0 times
  * their values, so a NaN or infinity in a key may reach rows of its sequence that
- * do not see it (keys that no row sees may hold anything in bf16 and fp32 alike).
+ * do not see it (keys that no row sees may hold anything in bf16 and fp32 alike, but for
+ * those between the windows of blocks longer than a window).
  *
  *   Q, O, dO, dQ : [rows][heads][head_dim], K, V, dK, dV : [rows][kv_heads][head_dim],
  *     rows `stride` elements apart (a multiple of 16 bytes, at most 2^20), so
@@ -366,50 +367,6 @@ bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdl
 bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdlm_rows q, bdlm_rows k, bdlm_rows v,
                             bdlm_rows o, const float* lse, int64_t lse_pitch, bdlm_rows dO, bdlm_rows dq, bdlm_rows dk,
                             bdlm_rows dv, void* workspace, size_t workspace_bytes, hipStream_t stream);
-
-/*
- * Norms of queries and keys for each head with the position rotation, in one
- * pass: what comes between the projections and any of the attention calls.
- * For a head's row x with weight w (null: ones), at position p_a on axis a:
- *   r = 1 / sqrt(mean x^2 + eps),  n = x r w     (eps 0: no norm, n = x),
- * and of the first `dim` elements pair i, on axis axis[i], turns by
- * t = p_axis[i] * freq[i]: (n1, n2) -> (n1 cos t - n2 sin t, n2 cos t + n1 sin t).
- *   q, k, outputs : [rows][heads or kv_heads][head_dim], rows `stride` elements apart
- *     (parts of one fused projection, say).  Outputs may be the inputs (the same
- *     pointer and stride); other overlaps are the caller's error.
- *   positions     : [axes][rows] int32 in device memory, of any sign
- *   weights       : [head_dim] in `dtype`
- * Rounding: angles are formed in 64 bits and reduced there; in bf16 sums and products are
- * fp32 (|x| must be below 2^60), in fp32 the sums over a row are fp64; outputs are rounded
- * once.  A NaN or infinity stays in its head's row (and reaches the weights' gradient).
- */
-typedef struct {
-  int32_t head_dim;    /* 64 or 128 */
-  int32_t dim;         /* elements that turn, a multiple of 16 in [16, head_dim] */
-  int32_t interleaved; /* pair i: 0: elements i and i + dim / 2, 1: elements 2 i and 2 i + 1 */
-  int32_t axes;        /* 1 to BDLM_MAX_AXES */
-  double freq[64];     /* radians per position of pairs 0 .. dim / 2 - 1 */
-  int32_t axis[64];
-} bdlm_rotary;
-#define BDLM_MAX_AXES 4
-
-bdlm_status bdlm_qk_rotate_fwd(const bdlm_rotary* r, int32_t dtype, int64_t rows, const int32_t* positions, int32_t heads,
-                               int32_t kv_heads, bdlm_rows q, bdlm_rows k, const void* q_weight, const void* k_weight,
-                               double eps, bdlm_rows q_out, bdlm_rows k_out, hipStream_t stream);
-
-/*
- * Backward from the same inputs and the outputs' gradients dq_out, dk_out: dq and dk
- * (which may be dq_out and dk_out), and the weights' gradients [head_dim] in fp32 (null:
- * not wanted; without a norm they must be), the same bits in every call.  workspace:
- * bdlm_qk_rotate_workspace_bytes(), 256-byte aligned, contents ignored on entry, one per call that may
- * overlap in time; not needed where no weight's gradient is wanted.
- */
-size_t bdlm_qk_rotate_workspace_bytes(int32_t head_dim);
-bdlm_status bdlm_qk_rotate_bwd(const bdlm_rotary* r, int32_t dtype, int64_t rows, const int32_t* positions, int32_t heads,
-                               int32_t kv_heads, bdlm_rows q, bdlm_rows k, const void* q_weight, const void* k_weight,
-                               double eps, bdlm_rows dq_out, bdlm_rows dk_out, bdlm_rows dq, bdlm_rows dk,
-                               float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes,
-                               hipStream_t stream);
 
 /*
  * A paged cache of keys and values, and its pages' bookkeeping, all in device
@@ -505,6 +462,93 @@ size_t bdlm_prefix_attn_workspace_bytes(const bdlm_cache* c, int64_t requests, i
 bdlm_status bdlm_prefix_attn(const bdlm_cache* c, int64_t layer, int64_t requests, const int32_t* seqs, int64_t rows,
                              int32_t heads, int64_t prefix, int32_t block, float scale, const void* q, void* o,
                              float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Attention of chunks of new tokens over the cache: request r is sequence seqs[r],
+ * and its counts[r] new tokens are its last ones (after grow; their keys and values are in the
+ * cache): one for a decoding request, many for a piece of a prompt.  The requests'
+ * query rows lie one after the other in q, in the order of the list; rows behind
+ * the last request's belong to none.  With len the sequence's tokens, row i of request
+ * r is at position x = len - counts[r] + i; it sees the keys that a row at x sees in packed calls:
+ * with e = block_size * (floor(x / block_size) + 1), j < min(e, len), with a window only
+ * j >= e - window or j < sinks.  Rows that see nothing (negative positions, a sequence
+ * number out of range) get O = 0 and LSE = -inf.  Negative counts count as 0; rows past `rows` are passed over.
+ *
+ * A plan is made on the device from the lengths and counts, in stream order, for all
+ * layers of a step; it may be captured in a graph.  It holds while the lengths it was
+ * made from do; the table is read by the calls.  After BDLM_CHUNK_STARTS bytes it holds the requests'
+ * first rows (int32 [requests], at most `rows`), as bdlm_cache_write takes them.
+ *   q, o : [rows][heads][head_dim] in the cache's dtype, rows `stride` elements apart
+ *   lse  : [heads][lse_pitch] fp32, natural log
+ *   fill : 1: rows behind the last request's become 0 (LSE -inf), 0: they stay as they are
+ * Keys and values that no row of a request sees may hold anything (but for those between
+ * the windows of blocks longer than a window); the others of its sequence must be finite.  A page number outside the cache reads as rows of zeros, and lens are
+ * taken between 0 and what a table holds.  Rounding as in bdlm_prefix_attn; the cuts follow the
+ * plan, so bits may differ with the batch.
+ * workspace: bdlm_chunk_workspace_bytes() bytes, 256-byte aligned, contents ignored on
+ * entry; calls that may overlap in time need one each (they may share a plan).
+ */
+#define BDLM_CHUNK_STARTS 64
+typedef struct {
+  int64_t requests, rows;
+  int64_t block_size, window;
+  int32_t heads, sinks;
+  float scale;         /* <= 0 selects 1 / sqrt(head_dim) */
+  int32_t reserved;    /* must be 0 */
+} bdlm_chunk;
+
+size_t bdlm_chunk_plan_bytes(const bdlm_cache* c, const bdlm_chunk* p);
+size_t bdlm_chunk_workspace_bytes(const bdlm_cache* c, const bdlm_chunk* p);
+/* plan: bdlm_chunk_plan_bytes() bytes of device memory, 16-byte aligned. */
+bdlm_status bdlm_chunk_plan(const bdlm_cache* c, const bdlm_chunk* p, const int32_t* seqs, const int32_t* counts,
+                            void* plan, size_t plan_bytes, hipStream_t stream);
+bdlm_status bdlm_chunk_attn(const bdlm_cache* c, const bdlm_chunk* p, int64_t layer, const void* plan, size_t plan_bytes,
+                            bdlm_rows q, bdlm_rows o, float* lse, int64_t lse_pitch, int32_t fill, void* workspace,
+                            size_t workspace_bytes, hipStream_t stream);
+
+/*
+ * Norms of queries and keys for each head with the position rotation, in one
+ * pass: what comes between the projections and any of the attention calls.
+ * For a head's row x with weight w (null: ones), at position p_a on axis a:
+ *   r = 1 / sqrt(mean x^2 + eps),  n = x r w     (eps 0: no norm, n = x),
+ * and of the first `dim` elements pair i, on axis axis[i], turns by
+ * t = p_axis[i] * freq[i]: (n1, n2) -> (n1 cos t - n2 sin t, n2 cos t + n1 sin t).
+ *   q, k, outputs : [rows][heads or kv_heads][head_dim], rows `stride` elements apart
+ *     (parts of one fused projection, say).  Outputs may be the inputs (the same
+ *     pointer and stride); other overlaps are the caller's error.
+ *   positions     : [axes][rows] int32 in device memory, of any sign
+ *   weights       : [head_dim] in `dtype`
+ * Rounding: angles are formed in 64 bits and reduced there; in bf16 sums and products are
+ * fp32 (|x| must be below 2^60), in fp32 the sums over a row are fp64; outputs are rounded
+ * once.  A NaN or infinity stays in its head's row (and reaches the weights' gradient).
+ */
+typedef struct {
+  int32_t head_dim;    /* 64 or 128 */
+  int32_t dim;         /* elements that turn, a multiple of 16 in [16, head_dim] */
+  int32_t interleaved; /* pair i: 0: elements i and i + dim / 2, 1: elements 2 i and 2 i + 1 */
+  int32_t axes;        /* 1 to BDLM_MAX_AXES */
+  double freq[64];     /* radians per position of pairs 0 .. dim / 2 - 1 */
+  int32_t axis[64];
+} bdlm_rotary;
+#define BDLM_MAX_AXES 4
+
+bdlm_status bdlm_qk_rotate_fwd(const bdlm_rotary* r, int32_t dtype, int64_t rows, const int32_t* positions, int32_t heads,
+                               int32_t kv_heads, bdlm_rows q, bdlm_rows k, const void* q_weight, const void* k_weight,
+                               double eps, bdlm_rows q_out, bdlm_rows k_out, hipStream_t stream);
+
+/*
+ * Backward from the same inputs and the outputs' gradients dq_out, dk_out: dq and dk
+ * (which may be dq_out and dk_out), and the weights' gradients [head_dim] in fp32 (null:
+ * not wanted; without a norm they must be), the same bits in every call.  workspace:
+ * bdlm_qk_rotate_workspace_bytes(), 256-byte aligned, contents ignored on entry, one per call that may
+ * overlap in time; not needed where no weight's gradient is wanted.
+ */
+size_t bdlm_qk_rotate_workspace_bytes(int32_t head_dim);
+bdlm_status bdlm_qk_rotate_bwd(const bdlm_rotary* r, int32_t dtype, int64_t rows, const int32_t* positions, int32_t heads,
+                               int32_t kv_heads, bdlm_rows q, bdlm_rows k, const void* q_weight, const void* k_weight,
+                               double eps, bdlm_rows dq_out, bdlm_rows dk_out, bdlm_rows dq, bdlm_rows dk,
+                               float* dq_weight, float* dk_weight, void* workspace, size_t workspace_bytes,
+                               hipStream_t stream);
 
 /*
  * Kernel timing (observability).  While enabled for the calling thread, every

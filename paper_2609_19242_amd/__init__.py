@@ -31,6 +31,7 @@ __all__ = [
     "PackedPlan", "packed_plan", "packed_fwd", "packed_bwd",
     "Cache", "cache_new", "cache_grow", "cache_write", "cache_fork", "cache_free", "cache_compact",
     "prefix_attn", "prefix_attn_workspace_bytes", "CACHE_OK", "CACHE_BAD_LIST", "CACHE_NO_PAGES",
+    "ChunkPlan", "chunk_plan", "chunk_attn", "chunk_attn_workspace_bytes",
     "Rotary", "rotary", "qk_rotate_fwd", "qk_rotate_bwd",
 ]
 
@@ -127,6 +128,7 @@ def lib() -> ctypes.CDLL:
             getattr(L, name).restype = ctypes.c_int
         packed.declare(L)
         cache.declare(L)
+        chunk.declare(L)
         rotate.declare(L)
         _LIB = L
     return _LIB
@@ -510,5 +512,7 @@ from .packed import PackedPlan, packed_bwd, packed_fwd, packed_plan  # noqa: E40
 from . import cache  # noqa: E402
 from .cache import (CACHE_BAD_LIST, CACHE_NO_PAGES, CACHE_OK, Cache, cache_compact, cache_fork, cache_free,  # noqa: E402
                     cache_grow, cache_new, cache_write, prefix_attn, prefix_attn_workspace_bytes)
+from . import chunk  # noqa: E402
+from .chunk import ChunkPlan, chunk_attn, chunk_attn_workspace_bytes, chunk_plan  # noqa: E402
 from . import rotate  # noqa: E402
 from .rotate import Rotary, qk_rotate_bwd, qk_rotate_fwd, rotary  # noqa: E402

@@ -31,7 +31,8 @@ thread_local std::string g_err;
 const char* const kKernelNames[kKCount] = {"fwd_bf16",      "fwd_f32",     "lse_merge",    "bwd_dq_f32",
                                            "bwd_dkdv_bf16", "bwd_dq_bf16", "bwd_dkdv_f32", "packed_fwd",
                                            "packed_bwd_dq", "packed_bwd_dkdv",
-                                           "prefix_attn", "prefix_merge", "cache_pages", "cache_write", "qk_rotate"};
+                                           "prefix_attn", "prefix_merge", "cache_pages", "cache_write", "qk_rotate",
+                                           "chunk_plan", "chunk_attn", "chunk_merge"};
 struct TimingRec {
   int id;
   hipEvent_t a, b;

@@ -5,21 +5,18 @@
 #include <algorithm>
 #include <cmath>
 
-#include "api_util.hpp"
-#include "cache.hpp"
+#include "cache_check.hpp"
 #include "split_plan.hpp"
 
 using namespace bdlm;
 
 namespace {
 
-constexpr int64_t kMaxSeqs = (int64_t)1 << 19;  // a bit each in the bookkeeping's LDS
-constexpr int64_t kMaxPages = ((int64_t)1 << 30) - 1;
-constexpr int64_t kMaxRows = (int64_t)1 << 25;  // query rows x heads of one attention call (a grid dimension of the merge)
-constexpr int64_t kMaxWgs = (int64_t)1 << 22;
 constexpr int kMaxKeyChunks = 1 << 20;  // chunks of keys of one attention call
 
-bool aligned4(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 3u) == 0; }
+}  // namespace
+
+namespace bdlm {
 
 bdlm_status check_cache(const bdlm_cache* c) {
   if (!c) return fail(BDLM_ERR_INVALID, "cache is null");
@@ -63,6 +60,10 @@ CacheArg cache_arg(const bdlm_cache* c) {
   a.layer_bytes = a.page_bytes * c->pages;
   return a;
 }
+
+}  // namespace bdlm
+
+namespace {
 
 bdlm_status check_list(const bdlm_cache* c, int64_t n, const int32_t* a, const char* what) {
   if (n < 0 || n > c->seqs)

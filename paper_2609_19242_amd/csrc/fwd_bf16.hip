@@ -279,7 +279,7 @@ __global__ __launch_bounds__(NT * NW * 64)
           for (int i = 0; i < 16; ++i) {
             const int kk = base + u * 32 + (i >> 2) * 8 + (i & 3);
             bool hidden = (unsigned)kk >= (unsigned)lane_w;
-            if constexpr (kHasSinks<Args>) hidden = hidden && t * BN + 4 * half + u * 32 + (i >> 2) * 8 + (i & 3) >= lane_s;
+            if constexpr (kHasSinks<Args>) hidden &= t * BN + 4 * half + u * 32 + (i >> 2) * 8 + (i & 3) >= lane_s;
             if (hidden) sacc[u][i] = -INFINITY;
           }
       }

@@ -29,7 +29,7 @@
 // of 32 rows of 16 requests behind 16K, 4 KV heads, 156 us (0.9 PFLOP/s): operand
 // reads take LDS as long as the products take the matrix cores, and copies a quarter
 // more (without them 138 us; without the exponentials 145).
-#include "cache.hpp"
+#include "chunk.hpp"
 #include "device.hpp"
 
 namespace bdlm {
@@ -130,9 +130,9 @@ struct Lds {
   static_assert(Wave == 32 * D * 4, "a wave's sums fit its tiles");
 };
 
-template <int D, bool GROUPS>
+template <int D, bool GROUPS, class Args>
 __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void prefix_bf16_kernel(
-    const PrefixArgs a) {
+    const Args a) {
   using L = Lds<D>;
   constexpr int KS = D / 16, DT = D / 32, CH = D / 8;
   constexpr uint32_t RB = L::RB;
@@ -146,11 +146,12 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int l32 = lane & 31, half = lane >> 5, G = lane >> 4, sl = lane & 15;
 
-  PrefixItem it;
-  if (!prefix_item(a, blockIdx.x, a.prefix_shared ? kPrefixSharedRows : kPrefixWaveRows,
-                   a.own_shared ? kPrefixSharedRows : kPrefixWaveRows, it))
+  typename ItemOf<Args>::type it;
+  if (!attn_item<true>(a, blockIdx.x, it)) {
+    fill_rest<bf16, D>(a, blockIdx.x, gridDim.x);
     return;
-  const bool single = a.prefix_chunks + a.own_chunks == 1;
+  }
+  const bool single = writes_outputs(a, it);
   const float c = a.scale_log2;
   // Tiles start at the chunk's first key, or at the group of 16 that holds it (the keys before it are hidden).
   const int start = GROUPS ? it.k0 & ~15 : it.k0;
@@ -160,11 +161,16 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   // The byte offsets of the chunk's groups, or its page numbers; -1 for pages
   // outside the cache, whose rows read as zeros.
   const int page0 = it.k0 / a.page_size;
+  [[maybe_unused]] WalkPages wp;
+  if constexpr (kIsChunk<Args> && !GROUPS) wp = walk_pages(a, it);
   if (nkeys > 0) {
     const int32_t* const table = a.table + (int64_t)it.seq * a.max_pages;
-    const int n = GROUPS ? (nkeys + 15) / 16 : (it.k1 - 1) / a.page_size - page0 + 1;
+    int n = GROUPS ? (nkeys + 15) / 16 : (it.k1 - 1) / a.page_size - page0 + 1;
+    if constexpr (kIsChunk<Args> && !GROUPS) n = wp.n;
     for (int e = tid; e < n; e += kNW * 64) {
-      const int key = start + e * 16, pe = GROUPS ? key / a.page_size : page0 + e;
+      const int key = walk_key(it, start + e * 16);
+      int pe = GROUPS ? key / a.page_size : page0 + e;
+      if constexpr (kIsChunk<Args> && !GROUPS) pe = wp.page(e);
       const int p = table[pe];
       const bool ok = (unsigned)p < (unsigned)a.pages;
       if constexpr (GROUPS) groups[e] = ok ? ((int64_t)p * a.page_size + (key - pe * a.page_size)) * row_bytes : -1;
@@ -175,12 +181,11 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   // This wave's rows as MFMA B fragments.
   const int lrow = (it.shared ? w * 32 : 0) + l32;  // within the item's rows
   const bool row_ok = lrow < it.nrows;
-  const PrefixRow row = prefix_row(a, it.kvh, it.row0 + imin(lrow, it.nrows - 1));
-  const int64_t out_row = (int64_t)row.token * a.heads + row.head;
+  const auto row = item_row(a, it, imin(lrow, it.nrows - 1));
+  const int64_t q_row = q_elem<D>(a, row);
   bf16x8 qf[KS];
 #pragma unroll
-  for (int s = 0; s < KS; ++s)
-    qf[s] = *(const bf16x8*)((const bf16*)a.q + out_row * D + 16 * s + 8 * half);
+  for (int s = 0; s < KS; ++s) qf[s] = *(const bf16x8*)((const bf16*)a.q + q_row + 16 * s + 8 * half);
   const int end = imin(row.end, it.k1);
   __syncthreads();
   // (waited for here: the loops' own waits count copies that the compiler does not know of)
@@ -193,13 +198,18 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   // Byte offset of a key's row in K (and V), -1: a row of zeros.
   auto key_offset = [&](int key) __attribute__((always_inline)) -> int64_t {
     if (key >= it.k1) return -1;
+    if constexpr (kIsChunk<Args>) {
+      if (key >= a.sinks && key < it.w0) return -1;
+    }
     if constexpr (GROUPS) {
       const int64_t g = groups[(key - start) >> 4];
       return g < 0 ? -1 : g + (key & 15) * row_bytes;
     } else {
-      const int e = key / a.page_size;
-      const int p = pages[e - page0];
-      return p < 0 ? -1 : ((int64_t)p * a.page_size + (key - e * a.page_size)) * row_bytes;
+      const int kk = walk_key(it, key), e = kk / a.page_size;
+      int at = e - page0;
+      if constexpr (kIsChunk<Args>) at = key < it.gap_at ? e - wp.p0 : wp.n0 + (e - wp.p1);
+      const int p = pages[at];
+      return p < 0 ? -1 : ((int64_t)p * a.page_size + (kk - e * a.page_size)) * row_bytes;
     }
   };
   // Copies of 32 rows from key `first` (a multiple of 16 with GROUPS) on to LDS.
@@ -221,7 +231,9 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   };
   auto copy32 = [&](const char* base, int first, const Pair& ahead, uint32_t dst) __attribute__((always_inline)) {
     if constexpr (GROUPS) {
-      if (first + 32 <= it.k1) {
+      bool whole = first + 32 <= it.k1;
+      if constexpr (kIsChunk<Args>) whole = whole && (first >= it.w0 || first + 32 <= a.sinks);
+      if (whole) {
         auto uniform = [](int64_t x) __attribute__((always_inline)) {
           return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
                            (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
@@ -262,6 +274,15 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
       copy32(base, first_of(t), ahead, L0 + stage * L::Stage + (w < 2 ? 0u : 64 * RB) + crow * RB);
     };
     const bool any = __builtin_amdgcn_ballot_w64(row_ok && end > it.k0) != 0;
+    // some row sees a key of the 64 from key0 on; some row does not see all of them
+    auto some_seen = [&](int key0) __attribute__((always_inline)) {
+      if constexpr (kIsChunk<Args>) return (end > key0) & ((row.lo < key0 + 64) | (key0 < a.sinks));
+      else return end > key0;
+    };
+    auto some_hidden = [&](int key0) __attribute__((always_inline)) {
+      if constexpr (kIsChunk<Args>) return (end < key0 + 64) | ((row.lo > key0) & (key0 + 64 > a.sinks));
+      else return end < key0 + 64;
+    };
     copy_tile(0, pair_at(first_of(0)), 0);
     Pair ahead = pair_at(first_of(1));
     vm_wait_barrier<0>();
@@ -269,7 +290,7 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
       copy_tile(t + 1, ahead, (t + 1) & 1);
       ahead = pair_at(first_of(t + 2));
       const int key0 = start + t * 64;
-      if (any && __builtin_amdgcn_ballot_w64(end > key0) != 0) {
+      if (any && __builtin_amdgcn_ballot_w64(some_seen(key0)) != 0) {
         const uint32_t sb = L0 + (t & 1) * L::Stage;
         const uint32_t zr = sb + yrow;
         f32x16 s[2];
@@ -297,13 +318,16 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
             __builtin_amdgcn_sched_barrier(0);
           }
         }
-        if (key0 < it.k0 || __builtin_amdgcn_ballot_w64(end < key0 + 64) != 0) {
+        if (key0 < it.k0 || __builtin_amdgcn_ballot_w64(some_hidden(key0)) != 0) {
 #pragma unroll
           for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const int key = key0 + u * 32 + (i >> 2) * 8 + 4 * half + (i & 3);
-              if (key >= end || (GROUPS && key < it.k0)) s[u][i] = -INFINITY;
+              // (chunks: without branches; hipcc lost the write of a score in one, with && and ||)
+              bool hidden = kIsChunk<Args> ? key >= end : key >= end || (GROUPS && key < it.k0);
+              if constexpr (kIsChunk<Args>) hidden |= (key < row.lo) & (key >= a.sinks);
+              if (hidden) s[u][i] = -INFINITY;
             }
         }
         // value fragments PA products ahead, the first ones under the softmax
@@ -334,7 +358,7 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
     const float inv = empty ? 0.f : 1.f / l;
     if (row_ok) {
       if (single) {
-        bf16* op = (bf16*)a.o + out_row * D;
+        bf16* op = (bf16*)a.o + o_elem<D>(a, row);
 #pragma unroll
         for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -344,9 +368,9 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
             for (int e = 0; e < 4; ++e) x[e] = to_bf16(st.acc[d][4 * g4 + e] * inv);
             *(bf16x4*)(op + 32 * d + 8 * g4 + 4 * half) = x;
           }
-        if (half == 0) a.lse[prefix_lse_at(a, row)] = empty ? -INFINITY : (st.m + log2f(l)) * kLn2;
+        if (half == 0) a.lse[lse_elem(a, row)] = empty ? -INFINITY : (st.m + log2f(l)) * kLn2;
       } else {
-        const int64_t at = (int64_t)it.part * a.requests * a.rows * a.heads + out_row;
+        const int64_t at = part_row(a, it, row, lrow);
         if (!empty) {
           float* op = a.part_o + at * D;
 #pragma unroll
@@ -382,11 +406,15 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
       for (int k = 0; k < KS; ++k) s[0] = mfma32(lds_load16((wb + yrow) ^ (32u * k)), qf[k], s[0]);
       copy32(kb, next, ahead, wb);
-      if (key0 < it.k0 || __builtin_amdgcn_ballot_w64(end < key0 + 32) != 0) {
+      bool cut = end < key0 + 32;
+      if constexpr (kIsChunk<Args>) cut |= (row.lo > key0) & (key0 + 32 > a.sinks);
+      if (key0 < it.k0 || __builtin_amdgcn_ballot_w64(cut) != 0) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int key = key0 + (i >> 2) * 8 + 4 * half + (i & 3);
-          if (key >= end || (GROUPS && key < it.k0)) s[0][i] = -INFINITY;
+          bool hidden = kIsChunk<Args> ? key >= end : key >= end || (GROUPS && key < it.k0);
+          if constexpr (kIsChunk<Args>) hidden |= (key < row.lo) & (key >= a.sinks);
+          if (hidden) s[0][i] = -INFINITY;
         }
       }
       bf16x8 pb[2];
@@ -440,29 +468,39 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
     const bool empty = !(lt > 0.f);
     x *= empty ? 0.f : 1.f / lt;
-    const PrefixRow pr = prefix_row(a, it.kvh, it.row0 + r);
-    const int64_t orow = (int64_t)pr.token * a.heads + pr.head;
+    const auto pr = item_row(a, it, r);
     if (single) {
       bf16x4 y;
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = to_bf16(x[e]);
-      *(bf16x4*)((bf16*)a.o + orow * D + piece * 4) = y;
-      if (piece == 0) a.lse[prefix_lse_at(a, pr)] = empty ? -INFINITY : (m + log2f(lt)) * kLn2;
+      *(bf16x4*)((bf16*)a.o + o_elem<D>(a, pr) + piece * 4) = y;
+      if (piece == 0) a.lse[lse_elem(a, pr)] = empty ? -INFINITY : (m + log2f(lt)) * kLn2;
     } else {
-      const int64_t at = (int64_t)it.part * a.requests * a.rows * a.heads + orow;
+      const int64_t at = part_row(a, it, pr, r);
       if (!empty) *(f32x4*)(a.part_o + at * D + piece * 4) = x;
       if (piece == 0) ((float*)a.part_lse)[at] = empty ? -INFINITY : m + log2f(lt);
     }
   }
 }
 
-template <int D>
-void launch(const PrefixArgs& a, int n, hipStream_t s) {
-  if (a.page_size % 16 == 0) hipLaunchKernelGGL((prefix_bf16_kernel<D, true>), dim3(n), dim3(kNW * 64), 0, s, a);
-  else hipLaunchKernelGGL((prefix_bf16_kernel<D, false>), dim3(n), dim3(kNW * 64), 0, s, a);
+template <int D, class Args>
+void launch(const Args& a, int n, hipStream_t s) {
+  if (a.page_size % 16 == 0) hipLaunchKernelGGL((prefix_bf16_kernel<D, true, Args>), dim3(n), dim3(kNW * 64), 0, s, a);
+  else hipLaunchKernelGGL((prefix_bf16_kernel<D, false, Args>), dim3(n), dim3(kNW * 64), 0, s, a);
 }
 
 }  // namespace
+
+#ifdef BDLM_CHUNK_CALLS
+
+hipError_t launch_chunk_bf16(const ChunkArgs& a, int head_dim, hipStream_t s) {
+  const int n = a.max_items * a.kv_heads + (a.fill ? kFillWgs : 0);
+  if (n == 0) return hipSuccess;
+  head_dim == 128 ? launch<128>(a, n, s) : launch<64>(a, n, s);
+  return hipGetLastError();
+}
+
+#else
 
 hipError_t launch_prefix_bf16(const PrefixArgs& a, int head_dim, hipStream_t s) {
   const int n = a.prefix_items + a.own_items;
@@ -470,5 +508,7 @@ hipError_t launch_prefix_bf16(const PrefixArgs& a, int head_dim, hipStream_t s) 
   head_dim == 128 ? launch<128>(a, n, s) : launch<64>(a, n, s);
   return hipGetLastError();
 }
+
+#endif
 
 }  // namespace bdlm

@@ -1,5 +1,8 @@
-"""What the listings of the kernels with sinks show, as test_serving_listings does for those without: products in inline
-assembly are waited for, no row address sits in a scalar offset, bf16 kernels keep their vector registers."""
+"""What the listings of the kernels with sinks and of those for chunks over the cache show, as test_serving_listings does for those without: products in inline
+assembly are waited for, no row address sits in a scalar offset, bf16 kernels keep their vector registers, two workgroups
+of the kernel over the cache fit a CU."""
+import re
+
 import pytest
 
 from tests.asm_listing import BF16, F64, functions, kernel_resources, listing, product_hazards, scalar_offset_accesses
@@ -13,7 +16,7 @@ def text_of(src):
 
 
 @pytest.mark.parametrize("src,product,file,n", [("sink_fwd_f32.hip", F64, "v", 2), ("sink_bwd_f32.hip", F64, "v", 4),
-                                                ("sink_bwd_dkdv.hip", BF16, "a", 4)])
+                                                ("sink_bwd_dkdv.hip", BF16, "a", 4), ("chunk_f32.hip", F64, "v", 2)])
 def test_products_are_waited_for(src, product, file, n):
     kernels = {name: b for name, b in functions(text_of(src)).items()
                if any(op == product and ops[0].startswith(file) for _, _, op, ops in b)}
@@ -29,7 +32,31 @@ def test_no_row_address_in_a_scalar_offset(src):
     assert not any(lines for _, lines in found.values()), {n: x[1] for n, x in found.items() if x[1]}
 
 
-@pytest.mark.parametrize("src", ["sink_fwd_bf16.hip", "sink_bwd_dq.hip", "sink_bwd_dkdv.hip"])
+@pytest.mark.parametrize("src", ["sink_fwd_bf16.hip", "sink_bwd_dq.hip", "sink_bwd_dkdv.hip", "chunk_bf16.hip",
+                                 "chunk_merge.hip"])
 def test_nothing_goes_to_scratch(src):
     for name, r in kernel_resources(text_of(src)).items():
         assert r["vgpr_spill_count"] == 0 and r["private_segment_fixed_size"] == 0, (name, r)
+
+
+def test_two_workgroups_over_the_cache_fit_a_cu():
+    seen = 0
+    for name, r in kernel_resources(text_of("chunk_bf16.hip")).items():
+        assert 2 * r["group_segment_fixed_size"] <= 160 * 1024 and r["vgpr_count"] <= 256, (name, r)
+        seen += 1
+    assert seen == 4
+
+
+@pytest.mark.parametrize("src", ["sink_fwd_bf16.hip", "sink_bwd_dq.hip", "chunk_bf16.hip", "chunk_f32.hip", "prefix_bf16.hip",
+                                 "prefix_f32.hip"])
+def test_no_write_under_a_condition_is_lost(src):
+    """A mask of lanes that is set and given up with nothing between: hipcc left that of a hidden score whose write it had
+    moved in front of another one."""
+    lines = [x.split(";")[0].strip() for x in text_of(src).split("\n")]
+    lines = [x for x in lines if x]
+    found = 0
+    for a, b in zip(lines, lines[1:]):
+        m = re.match(r"s_and_saveexec_b64 (s\[\d+:\d+\]),", a)
+        found += m is not None
+        assert not (m and b.startswith(f"s_or_b64 exec, exec, {m.group(1)}")), a
+    assert found > 0
