@@ -14,9 +14,9 @@ from typing import Optional
 
 import torch
 
-from . import _launch, _made, lib
+from . import _launch, _made, _stream, _torch_stream, lib
 from .cache import _cache, _Cache, _list
-from .packed import _as_long, _int, _lse, _Rows, _rows, _workspace
+from .packed import _as_long, _int, _lse, _Rows, _workspace
 
 __all__ = ["ChunkPlan", "chunk_plan", "chunk_attn", "chunk_attn_workspace_bytes"]
 
@@ -44,12 +44,19 @@ class ChunkPlan:
     """The work of a step of attention over ``cache`` (see :func:`chunk_plan`).  ``starts``: the requests' first rows,
     int32 ``[requests]``, as :func:`cache_write` takes them."""
 
-    def __init__(self, cache, record: _Chunk, items: torch.Tensor, workspace_bytes: int):
-        self.cache, self._record, self._items, self.workspace_bytes = cache, record, items, workspace_bytes
+    def __init__(self, cache, record: _Chunk, items: torch.Tensor, stream):
+        self.cache, self._record, self._items, self._workspace_bytes = cache, record, items, None
         self._ref, self._at, self._bytes = ctypes.byref(record), items.data_ptr(), items.numel() * 4
         self.requests, self.rows, self.heads = record.requests, record.rows, record.heads
         self.dtype, self.device, self.gpu, self.head_dim = cache.dtype, cache.device, cache.gpu, cache.head_dim
-        self._tensors, self._streams = (items,) + cache._tensors, set()
+        # (the items come from the memory of the stream that makes them)
+        self._tensors, self._streams = (items,), {_stream(stream)} if self.gpu >= 0 else set()
+
+    @property
+    def workspace_bytes(self):
+        if self._workspace_bytes is None:
+            self._workspace_bytes = int(lib().bdlm_chunk_workspace_bytes(self.cache._ref, self._ref))
+        return self._workspace_bytes
 
     @property
     def starts(self):
@@ -57,6 +64,16 @@ class ChunkPlan:
 
     def __repr__(self):
         return f"ChunkPlan(requests={self.requests}, rows={self.rows}, heads={self.heads}, {self.cache!r})"
+
+
+def _launch_plan(plan, stream, call, *args):
+    """:func:`_launch`, of the plan's memory and the cache's."""
+    _launch(plan, stream, call, *args)
+    c = plan.cache
+    for handle in plan._streams - c._streams:
+        for t in c._tensors:
+            t.record_stream(_torch_stream(handle, c.device))
+        c._streams.add(handle)
 
 
 def chunk_plan(cache, seqs, counts, rows: int, heads: int, block_size: int = 1, window: int = 0, sinks: int = 0,
@@ -79,14 +96,14 @@ def chunk_plan(cache, seqs, counts, rows: int, heads: int, block_size: int = 1, 
     if out is None:
         # (0: refused, by the call below)
         items, = _made(stream, c.device, lambda: (torch.empty(max(64, nbytes // 4), dtype=torch.int32, device=c.device),))
-        plan = ChunkPlan(c, rec, items, int(lib().bdlm_chunk_workspace_bytes(c._ref, ref)))
+        plan = ChunkPlan(c, rec, items, stream)
     else:
         if not isinstance(out, ChunkPlan):
             raise TypeError(f"out must be a ChunkPlan, got {type(out).__name__}")
         if out.cache is not c or (out.requests, out.rows, out.heads) != (n, rec.rows, rec.heads):
             raise ValueError("out must be a plan of the same cache, requests, rows and heads")
         plan = out
-    _launch(plan, stream, lib().bdlm_chunk_plan, c._ref, ref, a, b, plan._at, plan._bytes)
+    _launch_plan(plan, stream, lib().bdlm_chunk_plan, c._ref, ref, a, b, plan._at, plan._bytes)
     if out is not None:
         ctypes.memmove(ctypes.byref(plan._record), ref, ctypes.sizeof(rec))
     return plan
@@ -121,13 +138,14 @@ def chunk_attn(plan: ChunkPlan, q, layer: int, out: Optional[tuple] = None, work
     layer = _int("layer", layer)
     if out is None:
         o, lse = _made(stream, plan.device, _new_outputs, q)
+        ro = _Rows(o.data_ptr(), H * plan.head_dim)
     else:
         if len(out) != 2:
             raise ValueError("out must be (o, lse)")
         o, lse = out
-    ro = _as_long(plan, "o", o, H, n)
-    _lse(plan, lse, n)
+        ro = _as_long(plan, "o", o, H, n)
+        _lse(plan, lse, n)
     workspace = _workspace(workspace, plan.workspace_bytes, plan.device, stream)
-    _launch(plan, stream, lib().bdlm_chunk_attn, plan.cache._ref, plan._ref, layer, plan._at, plan._bytes, rq, ro,
+    _launch_plan(plan, stream, lib().bdlm_chunk_attn, plan.cache._ref, plan._ref, layer, plan._at, plan._bytes, rq, ro,
             lse.data_ptr(), n, 1 if out is None else 0, workspace.data_ptr(), workspace.numel() * workspace.element_size())
     return o, lse

@@ -20,6 +20,7 @@ static_assert(BDLM_CHUNK_STARTS == kChunkHead * sizeof(int32_t), "the plan's lay
 
 // Workgroups' worth of chunks that the walks are cut into, and keys of a chunk at least.
 constexpr int64_t kShares = 4 * kCus, kLeast = 256;
+static_assert((kShares & (kShares - 1)) == 0, "the planner shifts by it");
 
 // What a plan and a call's partial outputs need, whatever the lengths are
 // (chunk_plan.hip says why it is enough).

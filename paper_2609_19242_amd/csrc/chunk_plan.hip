@@ -15,69 +15,78 @@ namespace bdlm {
 
 namespace {
 
-constexpr int kT = 1024;
-constexpr int kLdsTiles = 8192;  // first tiles of that many requests are searched in LDS
+constexpr int kT = 512;
+constexpr int kLdsRequests = 2048;  // requests that are kept in LDS (more are read again)
 
-template <class T>
-__device__ __forceinline__ T block_scan(T x, T& total, T* wsum) {
+// Exclusive prefix sums of x and y over the workgroup's threads; totals of all.
+__device__ __forceinline__ void block_scan(int64_t& x, int64_t& y, int64_t& all_x, int64_t& all_y, int64_t (*wsum)[2]) {
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  T v = x;
+  int64_t u = x, v = y;
 #pragma unroll
   for (int s = 1; s < 64; s <<= 1) {
-    const T y = __shfl_up(v, s);
-    if (lane >= s) v += y;
+    const int64_t a = __shfl_up(u, s), b = __shfl_up(v, s);
+    if (lane >= s) u += a, v += b;
   }
   __syncthreads();  // (the sums of a scan before are read)
-  if (lane == 63) wsum[w] = v;
+  if (lane == 63) wsum[w][0] = u, wsum[w][1] = v;
   __syncthreads();
-  T base = 0, t = 0;
+  all_x = all_y = 0;
+  u -= x;
+  v -= y;
 #pragma unroll
   for (int k = 0; k < kT / 64; ++k) {
-    const T y = wsum[k];
-    if (k < w) base += y;
-    t += y;
+    const int64_t a = wsum[k][0], b = wsum[k][1];
+    if (k < w) u += a, v += b;
+    all_x += a;
+    all_y += b;
   }
-  total = t;
-  return base + v - x;
+  x = u;
+  y = v;
 }
 
-__device__ __forceinline__ int tile_rows(const ChunkPlanArgs& a, int64_t per) {
+__device__ __forceinline__ int tile_rows(const ChunkPlanArgs& a, int per) {
   return a.f32 ? kPrefixRowsF32 : per > 2 * kPrefixWaveRows ? kPrefixSharedRows : kPrefixWaveRows;
 }
+// x / n for the uniform n of a call, mostly 1 or a power of two (x >= 0).
+__device__ __forceinline__ int over(int x, int n) { return (n & (n - 1)) == 0 ? x >> __builtin_ctz(n) : x / n; }
 
-// A request: its first row, rows in the call, position of the first, tokens.
+// A request: its first tile, its first row and rows in the call, the position of the first, tokens.
 struct Request {
-  int seq, token0, rows, pos0, len;
+  int tile0, token0, rows, pos0, len, seq;
 };
-__device__ __forceinline__ Request request_of(const ChunkPlanArgs& a, int r, int start) {
-  Request q;
+// The sequence of request r, its tokens and new ones.
+__device__ __forceinline__ void load_request(const ChunkPlanArgs& a, int r, Request& q, int& count) {
+  count = imax(a.counts[r], 0);
   q.seq = a.seqs[r];
   if ((unsigned)q.seq >= (unsigned)a.seqs_in_cache) q.seq = -1;
-  const int n = q.seq < 0 ? 0 : a.lens[q.seq], count = imax(a.counts[r], 0);
+  const int n = q.seq < 0 ? 0 : a.lens[q.seq];
   q.len = n < 0 ? 0 : (int64_t)n > a.top ? (int)a.top : n;
-  q.token0 = start;
-  q.rows = imin(count, a.rows - start);
-  q.pos0 = (int)((int64_t)q.len - count < -kBig ? -kBig : (int64_t)q.len - count);  // (then no row of the call sees anything)
-  return q;
+  const int64_t pos0 = (int64_t)q.len - count;
+  q.pos0 = pos0 < -kBig ? -kBig : (int)pos0;  // (then no row of the call sees anything)
+}
+__device__ __forceinline__ void place_request(const ChunkPlanArgs& a, int64_t start, int count, Request& q) {
+  q.token0 = start < a.rows ? (int)start : a.rows;
+  q.rows = imin(count, a.rows - q.token0);
 }
 
 // A tile's walk.
 struct Walk {
   int row0, nrows, n, gap_at, gap, w0;
+  bool shared;
 };
 __device__ __forceinline__ Walk walk_of(const ChunkPlanArgs& a, const Request& q, int tile) {
-  const int64_t per = (int64_t)q.rows * a.group;
-  const int tr = tile_rows(a, per);
+  const int per = q.rows * a.group, tr = tile_rows(a, per);
   Walk w;
+  w.shared = tr == kPrefixSharedRows;
   w.row0 = tile * tr;
-  w.nrows = imin(tr, (int)(per - w.row0));
+  w.nrows = imin(tr, per - w.row0);
   w.n = 0;
   w.gap_at = kBig;
   w.gap = w.w0 = 0;
-  const int x0 = q.pos0 + w.row0 / a.group, x1 = q.pos0 + (w.row0 + w.nrows - 1) / a.group;
+  const int x0 = q.pos0 + over(w.row0, a.group), x1 = q.pos0 + over(w.row0 + w.nrows - 1, a.group);
   if (x1 < 0) return w;
-  const int end = imin(a.M * (x1 / a.M + 1), q.len);
-  const int w0 = a.window > 0 ? imax(a.M * (imax(x0, 0) / a.M + 1) - a.window, 0) : 0;
+  const int end = imin(a.M * (over(x1, a.M) + 1), q.len);
+  const int w0 = a.window > 0 ? imax(a.M * (over(imax(x0, 0), a.M) + 1) - a.window, 0) : 0;
   const int sinks = (imin(a.sinks, end) + 15) & ~15, first = w0 & ~15;
   w.n = end;
   w.w0 = w0;
@@ -91,115 +100,134 @@ __device__ __forceinline__ Walk walk_of(const ChunkPlanArgs& a, const Request& q
 }
 
 __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
-  __shared__ int tile0_lds[kLdsTiles];
-  __shared__ int64_t wsum[kT / 64];
+  __shared__ int req[6][kLdsRequests];
+  __shared__ int64_t wsum[kT / 64][2];
+  __shared__ unsigned long long total_lds;
   __shared__ int longest_lds;
   const int tid = threadIdx.x;
   int32_t* const starts = a.plan + kChunkHead;
   int32_t* const tile0 = starts + a.requests;
   ChunkItemRec* const items = (ChunkItemRec*)(tile0 + a.requests + 1);
   ChunkJoin* const joins = (ChunkJoin*)(items + a.max_items);
-  if (tid == 0) longest_lds = 0;
+  if (tid == 0) longest_lds = 0, total_lds = 0;
 
-  // rows and tiles of the requests
+  // the requests' rows and tiles
   int64_t rows = 0, tiles = 0;
+#pragma unroll 1
   for (int r0 = 0; r0 < a.requests; r0 += kT) {
     const int r = r0 + tid;
-    const int64_t count = r < a.requests ? imax(a.counts[r], 0) : 0;
-    int64_t all;
-    const int64_t start = rows + block_scan(count, all, wsum);
+    Request q;
+    int count = 0;
+    if (r < a.requests) load_request(a, r, q, count);
+    int64_t start = count, none = 0, all, all_tiles;
+    block_scan(start, none, all, all_tiles, wsum);
+    place_request(a, rows + start, count, q);
     rows += all;
-    const int first = start < a.rows ? (int)start : a.rows;
-    const int64_t used = count < a.rows - first ? count : a.rows - first, per = used * a.group;
-    const int tr = tile_rows(a, per);
-    const int64_t at = tiles + block_scan((per + tr - 1) / tr, all, wsum);
-    tiles += all;
+    const int per = q.rows * a.group, tr = tile_rows(a, per);
+    int64_t at = (per + tr - 1) / tr;
+    block_scan(at, none, all_tiles, all, wsum);
+    q.tile0 = (int)(tiles + at);
+    tiles += all_tiles;
     if (r < a.requests) {
-      starts[r] = first;
-      tile0[r] = (int)at;
-      if (r < kLdsTiles) tile0_lds[r] = (int)at;
+      starts[r] = q.token0;
+      tile0[r] = q.tile0;
+      if (r < kLdsRequests) {
+        req[0][r] = q.tile0;
+        req[1][r] = q.token0;
+        req[2][r] = q.rows;
+        req[3][r] = q.pos0;
+        req[4][r] = q.len;
+        req[5][r] = q.seq;
+      }
     }
   }
   if (tid == 0) tile0[a.requests] = (int)tiles;
   __syncthreads();
   const int T = (int)tiles;
-  const bool in_lds = a.requests <= kLdsTiles;
-  // The request of tile g: the last one whose first tile is not behind it.
+  const bool in_lds = a.requests <= kLdsRequests;
+  // Tile g of all: its request is the last one whose first tile is not behind it.
   auto walk_at = [&](int g, Request& q) __attribute__((always_inline)) -> Walk {
-    int lo = 0, hi = a.requests;  // tile0[lo] <= g < tile0[hi]
+    int lo = 0, hi = a.requests;
+#pragma unroll 1
     while (hi - lo > 1) {
       const int mid = (lo + hi) >> 1;
-      if ((in_lds ? tile0_lds[mid] : tile0[mid]) <= g) lo = mid;
+      if ((in_lds ? req[0][mid] : tile0[mid]) <= g) lo = mid;
       else hi = mid;
     }
-    q = request_of(a, lo, starts[lo]);
-    return walk_of(a, q, g - (in_lds ? tile0_lds[lo] : tile0[lo]));
+    if (in_lds) {
+      q = Request{req[0][lo], req[1][lo], req[2][lo], req[3][lo], req[4][lo], req[5][lo]};
+    } else {
+      int count;
+      load_request(a, lo, q, count);
+      place_request(a, starts[lo], count, q);
+      q.tile0 = tile0[lo];
+    }
+    return walk_of(a, q, g - q.tile0);
   };
 
-  // what all walks come to, and the share of a workgroup
-  int64_t mine = 0;
-  int longest = 0;
-  for (int g = tid; g < T; g += kT) {
-    Request q;
-    const int n = walk_at(g, q).n;
-    mine += n;
-    longest = imax(longest, n);
-  }
-  int64_t total;
-  block_scan(mine, total, wsum);
-  atomicMax(&longest_lds, longest);
-  __syncthreads();
-  longest = longest_lds;
-  const int64_t share = (total * a.kv_heads + a.slots - 1) / a.slots;
-  const int unit = (int)(share < a.least ? a.least : share > a.limit - 64 ? a.limit - 64 : share);
-  const int half = imin(longest, unit) / 2;
-
-  // the items, those longer than half of the longest first
-  int64_t placed = 0, part_rows = 0;  // (items << 32 | cut tiles)
-  for (int pass = 0; pass < 2; ++pass)
+  // 0: what all walks come to, and the longest; 1 (more tiles than threads): items of the
+  // longer half of the walks; 2: the items, those first.
+  int unit = 0, half = 0;
+  int64_t longer = 0, placed = 0, parts = 0;  // (longer items << 32 | others; cut tiles << 32 | their partial rows)
+  Request q{};
+  Walk w{};
+#pragma unroll 1
+  for (int pass = 0; pass < 3; ++pass) {
+    if (pass == 1 && T <= kT) continue;
+#pragma unroll 1
     for (int g0 = 0; g0 < T; g0 += kT) {
       const int g = g0 + tid;
-      Request q;
-      Walk w{};
+      if (g < T && (pass == 0 || T > kT)) w = walk_at(g, q);
+      if (pass == 0) {
+        if (g < T) {
+          atomicAdd(&total_lds, (unsigned long long)w.n);
+          atomicMax(&longest_lds, w.n);
+        }
+        continue;
+      }
       int n = 0, size = 0;
       if (g < T) {
-        w = walk_at(g, q);
-        const int cut = imax((w.n + unit - 1) / unit, 1);
-        size = imax(((w.n + cut - 1) / cut + 63) & ~63, 64);
-        n = imax((w.n + size - 1) / size, 1);
-        if ((imin(size, w.n) > half) != (pass == 0)) n = 0;
+        const int cut = imax(over(w.n + unit - 1, unit), 1);
+        size = imax((over(w.n + cut - 1, cut) + 63) & ~63, 64);
+        n = imax(over(w.n + size - 1, size), 1);
       }
-      int64_t all;
-      const int64_t at = placed + block_scan((int64_t)n << 32 | (n > 1), all, wsum);
-      placed += all;
-      int64_t part = part_rows + block_scan((int64_t)(n > 1 ? n * w.nrows : 0), all, wsum);
-      part_rows += all;
-      if (n == 0) continue;
-      const int i0 = (int)(at >> 32), j = (int)(at & 0xffffffff);
-      const bool shared = !a.f32 && w.row0 + w.nrows > 0 && tile_rows(a, (int64_t)q.rows * a.group) == kPrefixSharedRows;
-      if (i0 + (int64_t)n > a.max_items || (n > 1 && (j >= a.max_joins || part + (int64_t)n * w.nrows > a.max_part_rows)))
-        continue;  // (never: the host made room)
+      const bool is_longer = imin(size, w.n) > half;
+      int64_t x = is_longer ? (int64_t)n << 32 : n, y = n > 1 ? (int64_t)1 << 32 | n * w.nrows : 0, all_x, all_y;
+      block_scan(x, y, all_x, all_y, wsum);
+      if (pass == 1) {
+        longer += all_x >> 32;
+        continue;
+      }
+      if (T <= kT) longer = all_x >> 32;
+      x += placed;
+      y += parts;
+      placed += all_x;
+      parts += all_y;
+      const int i0 = is_longer ? (int)(x >> 32) : (int)(longer + (x & 0xffffffff)), j = (int)(y >> 32);
+      const int64_t part = y & 0xffffffff;
+      // (never: the host made room)
+      if (i0 + (int64_t)n > a.max_items || (n > 1 && (j >= a.max_joins || part + (int64_t)n * w.nrows > a.max_part_rows))) continue;
+      ChunkItemRec rec{q.seq, q.token0, q.pos0, q.len, w.row0, w.nrows, 0, 0, w.gap_at, w.gap, w.w0, 0};
+      const int flag = w.shared ? kSharedTile : 0;
+#pragma unroll 1
       for (int c = 0; c < n; ++c) {
-        ChunkItemRec x;
-        x.seq = q.seq;
-        x.token0 = q.token0;
-        x.pos0 = q.pos0;
-        x.len = q.len;
-        x.row0 = w.row0;
-        x.nrows = w.nrows;
-        x.k0 = c * size;
-        x.k1 = imin((c + 1) * size, w.n);
-        x.gap_at = w.gap_at;
-        x.gap = w.gap;
-        x.w0 = w.w0;
-        x.part = n > 1 ? (int)part + c * w.nrows | (shared ? kSharedTile : 0) : ~(shared ? kSharedTile : 0);
-        items[i0 + c] = x;
+        rec.k0 = c * size;
+        rec.k1 = imin((c + 1) * size, w.n);
+        rec.part = n > 1 ? (int)part + c * w.nrows | flag : ~flag;
+        items[i0 + c] = rec;
       }
       if (n > 1) joins[j] = ChunkJoin{q.token0, w.row0, w.nrows, (int)part, n, 0, 0, 0};
     }
+    if (pass == 0) {
+      __syncthreads();
+      const int64_t share = ((int64_t)total_lds * a.kv_heads + a.slots - 1) >> __builtin_ctz(a.slots);  // (a power of two)
+      unit = (int)(share < a.least ? a.least : share > a.limit - 64 ? a.limit - 64 : share);
+      half = imin(longest_lds, unit) / 2;
+    }
+  }
   if (tid == 0) {
-    a.plan[kPlanItems] = (int)(placed >> 32);
-    a.plan[kPlanJoins] = (int)(placed & 0xffffffff);
+    a.plan[kPlanItems] = (int)((placed >> 32) + (placed & 0xffffffff));
+    a.plan[kPlanJoins] = (int)(parts >> 32);
     a.plan[kPlanRows] = (int)(rows < a.rows ? rows : a.rows);
   }
 }

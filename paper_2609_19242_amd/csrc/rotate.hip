@@ -31,17 +31,18 @@ namespace {
 
 constexpr int kWaves = 4;
 
-// 8 consecutive elements.
-__device__ __forceinline__ void load8(const bf16* p, float (&x)[8]) {
-  const bf16x8 v = *(const bf16x8*)p;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) x[e] = (float)v[e];
-}
-__device__ __forceinline__ void load8(const float* p, float (&x)[8]) {
-  const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
-#pragma unroll
-  for (int e = 0; e < 4; ++e) x[e] = a[e], x[4 + e] = b[e];
-}
+// 8 consecutive elements, as they lie in memory.
+template <class T> struct Raw8;
+template <> struct Raw8<bf16> {
+  bf16x8 v;
+  __device__ __forceinline__ void load(const bf16* p) { v = *(const bf16x8*)p; }
+  __device__ __forceinline__ float operator[](int e) const { return (float)v[e]; }
+};
+template <> struct Raw8<float> {
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *(const f32x4*)p, b = *(const f32x4*)(p + 4); }
+  __device__ __forceinline__ float operator[](int e) const { return e < 4 ? a[e & 3] : b[e & 3]; }
+};
 __device__ __forceinline__ void store8(bf16* p, const float (&x)[8]) {
   bf16x8 v;
 #pragma unroll
@@ -121,6 +122,8 @@ struct Lane {
     row = set * a.rows_per + sub;
     ok = row < a.rows;
     if (!ok) row = a.rows - 1;
+  }
+  __device__ __forceinline__ void angles(const RotateArgs& a) {
     if (16 * l < a.dim) {
       if (a.axes == 1) {
         const double p = (double)a.pos[row];
@@ -138,15 +141,32 @@ struct Lane {
   }
 };
 
+// A lane's elements of a head's row.
 template <class T>
-__device__ __forceinline__ void load_weight(const RotateTensor& t, int ra, int rb, float (&wa)[8], float (&wb)[8]) {
-  if (t.w) {
-    load8((const T*)t.w + ra, wa);
-    load8((const T*)t.w + rb, wb);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e) wa[e] = wb[e] = 1.f;
+struct Piece {
+  Raw8<T> a, b;
+  __device__ __forceinline__ void load(const void* base, int64_t at, int ra, int rb) {
+    a.load((const T*)base + at + ra);
+    b.load((const T*)base + at + rb);
   }
+};
+template <class T>
+__device__ __forceinline__ void load_weight(Piece<T>& w, const RotateTensor& t, int ra, int rb) {
+  if (t.w) {
+    w.load(t.w, 0, ra, rb);
+  } else {
+    float one[8] = {1, 1, 1, 1, 1, 1, 1, 1};
+    T ones[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (T)one[e];
+    w.a.load(ones);
+    w.b.load(ones);
+  }
+}
+
+// The passes of a wave over a row's heads, of both tensors: the keys' follow the queries' in the deal.
+__device__ __forceinline__ int first_pass(const RotateArgs& a, int i, int part) {
+  return i == 0 ? part : (part - a.t[0].passes % a.split + a.split) % a.split;
 }
 
 template <class T, int D, bool IL, bool NORM>
@@ -163,34 +183,39 @@ __global__ __launch_bounds__(kWaves * 64) void rotate_fwd_kernel(const RotateArg
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const RotateTensor& t = a.t[i];
-      float wa[8], wb[8];
-      if constexpr (NORM) load_weight<T>(t, me.ra, me.rb, wa, wb);
-      // (the keys' passes follow the queries' in the deal)
-      for (int p = i == 0 ? part : (part - a.t[0].passes % a.split + a.split) % a.split; p < t.passes; p += a.split) {
+      auto head_of = [&](int p) __attribute__((always_inline)) {  // (a lane without one reads the first)
         const int h = p * me.heads + me.head;
-        const bool mine = me.ok && h < t.heads;
-        const int64_t at = me.row * t.xs + (int64_t)(mine ? h : 0) * D;
-        float x[8], y[8];
-        load8((const T*)t.x + at + me.ra, x);
-        load8((const T*)t.x + at + me.rb, y);
+        return (int64_t)(me.ok && h < t.heads ? h : 0) * D;
+      };
+      Piece<T> w, x, next;
+      int p = first_pass(a, i, part);
+      if (p < t.passes) x.load(t.x, me.row * t.xs + head_of(p), me.ra, me.rb);
+      if constexpr (NORM) load_weight<T>(w, t, me.ra, me.rb);
+      if (i == 0) me.angles(a);  // (under the first loads)
+      for (; p < t.passes; p += a.split) {
+        const int after = p + a.split;
+        if (after < t.passes) next.load(t.x, me.row * t.xs + head_of(after), me.ra, me.rb);
+        float u[8], v[8];
+        float r = 1.f;
         if constexpr (NORM) {
           S ss = 0;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) ss += (S)x[e] * (S)x[e] + (S)y[e] * (S)y[e];
+          for (int e = 0; e < 8; ++e) ss += (S)x.a[e] * (S)x.a[e] + (S)x.b[e] * (S)x.b[e];
           ss = row_sum<D / 16>(ss);
-          const float r = inverse_root(ss * (S)(1.0 / D) + (S)a.eps);
+          r = inverse_root(ss * (S)(1.0 / D) + (S)a.eps);
+        }
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x[e] = x[e] * r * wa[e];
-            y[e] = y[e] * r * wb[e];
-          }
+        for (int e = 0; e < 8; ++e) {
+          u[e] = NORM ? x.a[e] * r * w.a[e] : x.a[e];
+          v[e] = NORM ? x.b[e] * r * w.b[e] : x.b[e];
         }
-        turn<IL>(x, y, me.c, me.s, false);
-        if (mine) {
-          T* o = (T*)t.out + me.row * t.outs + (int64_t)h * D;
-          store8(o + me.ra, x);
-          store8(o + me.rb, y);
+        turn<IL>(u, v, me.c, me.s, false);
+        if (me.ok && p * me.heads + me.head < t.heads) {
+          T* o = (T*)t.out + me.row * t.outs + head_of(p);
+          store8(o + me.ra, u);
+          store8(o + me.rb, v);
         }
+        x = next;
       }
     }
   }
@@ -215,49 +240,55 @@ __global__ __launch_bounds__(kWaves * 64) void rotate_bwd_kernel(const RotateArg
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const RotateTensor& t = a.t[i];
-      float wa[8], wb[8];
-      if constexpr (NORM) load_weight<T>(t, me.ra, me.rb, wa, wb);
-      for (int p = i == 0 ? part : (part - a.t[0].passes % a.split + a.split) % a.split; p < t.passes; p += a.split) {
+      auto head_of = [&](int p) __attribute__((always_inline)) {
         const int h = p * me.heads + me.head;
-        const bool mine = me.ok && h < t.heads;
-        const int64_t head = (int64_t)(mine ? h : 0) * D;
-        float g[8], k[8], x[8], y[8];
-        if constexpr (NORM) {
-          load8((const T*)t.x + me.row * t.xs + head + me.ra, x);
-          load8((const T*)t.x + me.row * t.xs + head + me.rb, y);
-        }
-        load8((const T*)t.dy + me.row * t.dys + head + me.ra, g);
-        load8((const T*)t.dy + me.row * t.dys + head + me.rb, k);
+        return (int64_t)(me.ok && h < t.heads ? h : 0) * D;
+      };
+      Piece<T> wt, x, d, next_x, next_d;
+      auto load = [&](Piece<T>& px, Piece<T>& pd, int p) __attribute__((always_inline)) {
+        pd.load(t.dy, me.row * t.dys + head_of(p), me.ra, me.rb);
+        if constexpr (NORM) px.load(t.x, me.row * t.xs + head_of(p), me.ra, me.rb);
+      };
+      int p = first_pass(a, i, part);
+      if (p < t.passes) load(x, d, p);
+      if constexpr (NORM) load_weight<T>(wt, t, me.ra, me.rb);
+      if (i == 0) me.angles(a);
+      for (; p < t.passes; p += a.split) {
+        const int after = p + a.split;
+        if (after < t.passes) load(next_x, next_d, after);
+        const bool mine = me.ok && p * me.heads + me.head < t.heads;
+        float g[8], k[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) g[e] = d.a[e], k[e] = d.b[e];
         turn<IL>(g, k, me.c, me.s, true);
         if constexpr (NORM) {
           S ss = 0, hx = 0;
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            ss += (S)x[e] * (S)x[e] + (S)y[e] * (S)y[e];
-            hx += (S)(g[e] * wa[e]) * (S)x[e] + (S)(k[e] * wb[e]) * (S)y[e];
+            ss += (S)x.a[e] * (S)x.a[e] + (S)x.b[e] * (S)x.b[e];
+            hx += (S)(g[e] * wt.a[e]) * (S)x.a[e] + (S)(k[e] * wt.b[e]) * (S)x.b[e];
           }
           ss = row_sum<LPR>(ss);
           hx = row_sum<LPR>(hx);
           const float r = inverse_root(ss * (S)(1.0 / D) + (S)a.eps);
           const float m = (float)(hx * (S)(1.0 / D) * (S)r);  // mean(h x r)
-          if (mine) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              dw[i][e] = fmaf(g[e], x[e] * r, dw[i][e]);
-              dw[i][8 + e] = fmaf(k[e], y[e] * r, dw[i][8 + e]);
-            }
-          }
 #pragma unroll
           for (int e = 0; e < 8; ++e) {
-            g[e] = r * fmaf(-(x[e] * r), m, g[e] * wa[e]);
-            k[e] = r * fmaf(-(y[e] * r), m, k[e] * wb[e]);
+            if (mine) {
+              dw[i][e] = fmaf(g[e], x.a[e] * r, dw[i][e]);
+              dw[i][8 + e] = fmaf(k[e], x.b[e] * r, dw[i][8 + e]);
+            }
+            g[e] = r * fmaf(-(x.a[e] * r), m, g[e] * wt.a[e]);
+            k[e] = r * fmaf(-(x.b[e] * r), m, k[e] * wt.b[e]);
           }
         }
         if (mine) {
-          T* o = (T*)t.out + me.row * t.outs + head;
+          T* o = (T*)t.out + me.row * t.outs + head_of(p);
           store8(o + me.ra, g);
           store8(o + me.rb, k);
         }
+        x = next_x;
+        d = next_d;
       }
     }
   }
@@ -278,24 +309,37 @@ __global__ __launch_bounds__(kWaves * 64) void rotate_bwd_kernel(const RotateArg
       float x = 0.f;
 #pragma unroll
       for (int k = 0; k < kWaves; ++k) x += sums[k][n / D][n % D];
-      a.partials[(int64_t)blockIdx.x * 2 * D + n] = x;
+      a.partials[((int64_t)(n / 16) * a.wgs + blockIdx.x) * 16 + n % 16] = x;
     }
   }
 }
 
-// The workgroups' sums added up: 16 columns a workgroup, 64 rows of partials at a time.
+// The workgroups' sums added up: 16 columns a workgroup, 4 of a workgroup's sums a lane.
 template <int D>
 __global__ __launch_bounds__(1024) void rotate_dw_kernel(const RotateArgs a) {
-  __shared__ double sums[64][16];
-  const int col = threadIdx.x & 15, at = threadIdx.x >> 4, n = blockIdx.x * 16 + col;
-  double x = 0.0;
-  for (int r = at; r < a.wgs; r += 64) x += (double)a.partials[(int64_t)r * 2 * D + n];
-  sums[at][col] = x;
+  __shared__ double sums[16][16];
+  const int lane = threadIdx.x & 63, col = lane & 3, at = threadIdx.x >> 2;
+  const float* const p = a.partials + (int64_t)blockIdx.x * a.wgs * 16 + col * 4;
+  double x[4] = {0, 0, 0, 0};
+  for (int r = at; r < a.wgs; r += 256) {
+    const f32x4 v = *(const f32x4*)(p + (int64_t)r * 16);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] += (double)v[e];
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+#pragma unroll
+    for (int m = 4; m < 64; m <<= 1) x[e] += shfl_x(x[e], m);
+    if (lane < 4) sums[threadIdx.x >> 6][col * 4 + e] = x[e];
+  }
   __syncthreads();
-  if (at == 0) {
-    for (int k = 1; k < 64; ++k) x += sums[k][col];
+  if (threadIdx.x < 16) {
+    double y = 0.0;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) y += sums[k][threadIdx.x];
+    const int n = blockIdx.x * 16 + threadIdx.x;
     float* const dw = a.dw[n / D];
-    if (dw) dw[n % D] = (float)x;
+    if (dw) dw[n % D] = (float)y;
   }
 }
 

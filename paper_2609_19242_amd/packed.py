@@ -137,6 +137,10 @@ def packed_plan(q_lens: Sequence[int], k_lens: Optional[Sequence[int]] = None, *
 def _rows(like, name, t, heads, at_least):
     """A ``[rows][heads][head_dim]`` tensor whose rows may lie further apart than they are long, in the dtype and on the
     device of ``like`` (a plan or a cache)."""
+    if isinstance(t, torch.Tensor) and t.dtype is like.dtype and t.is_contiguous() and t.get_device() == like.gpu:
+        shape = t.shape  # (the common case first: these checks are much of a small call's host time)
+        if len(shape) == 3 and shape[1] == heads and shape[2] == like.head_dim and shape[0] >= at_least:
+            return _Rows(t.data_ptr(), heads * like.head_dim)
     if not isinstance(t, torch.Tensor):
         raise TypeError(f"{name} must be a torch.Tensor, got {type(t).__name__}")
     if t.dtype is not like.dtype:

@@ -45,6 +45,7 @@ class Rotary:
         self._record, self._ref = record, ctypes.byref(record)
         self.head_dim, self.dim, self.axes = record.head_dim, record.dim, record.axes
         self.interleaved = bool(record.interleaved)
+        self._calls = {}
 
     @property
     def freqs(self):
@@ -92,18 +93,27 @@ def rotary(head_dim: int, dim: Optional[int] = None, base: float = 10000.0, sect
 
 
 class _Call:
-    """The dtype and device of a call's tensors: those of q."""
+    """The dtype and device of a call's tensors."""
 
     _tensors = ()
 
-    def __init__(self, rot, q):
-        if not isinstance(rot, Rotary):
-            raise TypeError(f"rot must be a Rotary, got {type(rot).__name__}")
-        if not isinstance(q, torch.Tensor) or q.dim() != 3:
-            raise ValueError(f"q must be a [rows][heads][{rot.head_dim}] tensor")
-        self.code = _dtype_code(q.dtype)
-        self.dtype, self.device, self.gpu, self.head_dim = q.dtype, q.device, q.get_device(), rot.head_dim
+    def __init__(self, dtype, device, gpu, head_dim):
+        self.code = _dtype_code(dtype)
+        self.dtype, self.device, self.gpu, self.head_dim = dtype, device, gpu, head_dim
         self._streams = set()
+
+
+def _call(rot, q):
+    """Those of q (kept with the rotation: a small call's host time is its launch)."""
+    if not isinstance(rot, Rotary):
+        raise TypeError(f"rot must be a Rotary, got {type(rot).__name__}")
+    if not isinstance(q, torch.Tensor) or q.dim() != 3:
+        raise ValueError(f"q must be a [rows][heads][{rot.head_dim}] tensor")
+    key = q.dtype, q.get_device()
+    c = rot._calls.get(key)
+    if c is None:
+        c = rot._calls[key] = _Call(q.dtype, q.device, key[1], rot.head_dim)
+    return c
 
 
 def _weight(c, name, w, eps):
@@ -119,8 +129,8 @@ def _weight(c, name, w, eps):
 
 def _inputs(rot, q, k, positions, q_weight, k_weight, eps):
     """The arguments that both directions share, and the call's numbers."""
-    c = _Call(rot, q)
-    n, H = q.shape[:2]
+    c = _call(rot, q)
+    n, H, _ = q.shape
     if not isinstance(k, torch.Tensor) or k.dim() != 3:
         raise ValueError(f"k must be a [rows][kv_heads][{rot.head_dim}] tensor")
     KV = k.shape[1]
@@ -129,7 +139,7 @@ def _inputs(rot, q, k, positions, q_weight, k_weight, eps):
         raise ValueError(f"eps must be finite and positive, or None for no norm, got {eps}")
     if not isinstance(positions, torch.Tensor) or positions.dim() not in (1, 2):
         raise ValueError("positions must be a [rows] or [axes][rows] tensor")
-    _expect("positions", positions, torch.int32, (n,) if rot.axes == 1 and positions.dim() == 1 else (rot.axes, n))
+    _expect("positions", positions, torch.int32, (n,) if positions.dim() == 1 and rot.axes == 1 else (rot.axes, n))
     if positions.get_device() != c.gpu:
         raise ValueError(f"positions must be on {c.device}, got {positions.device}")
     w = _weight(c, "q_weight", q_weight, eps), _weight(c, "k_weight", k_weight, eps)
@@ -140,14 +150,15 @@ def _new_rows(q, k):
     return q.new_empty(q.shape), k.new_empty(k.shape)
 
 
-def _out_rows(c, name, out, names, q, k, stream):
+def _out_rows(c, out, names, q, k, stream):
     """The two outputs, new ones or the caller's, and their records."""
     if out is None:
-        out = _made(stream, c.device, _new_rows, q, k)
-    elif len(out) != 2:
-        raise ValueError(f"{name} must be ({', '.join(names)})")
+        a, b = _made(stream, c.device, _new_rows, q, k)
+        return (a, b), (_Rows(a.data_ptr(), q.shape[1] * c.head_dim), _Rows(b.data_ptr(), k.shape[1] * c.head_dim))
+    if len(out) != 2:
+        raise ValueError(f"out must be ({', '.join(names)})")
     n = q.shape[0]
-    return out, [_as_long(c, x, t, like.shape[1], n) for x, t, like in zip(names, out, (q, k))]
+    return tuple(out), [_as_long(c, x, t, like.shape[1], n) for x, t, like in zip(names, out, (q, k))]
 
 
 def qk_rotate_fwd(rot: Rotary, q, k, positions, q_weight=None, k_weight=None, eps: Optional[float] = None,
@@ -157,9 +168,9 @@ def qk_rotate_fwd(rot: Rotary, q, k, positions, q_weight=None, k_weight=None, ep
     row's int32 ``positions`` (``[rows]``, with several axes ``[axes][rows]``).  Returns ``(q, k)``, or writes into
     ``out``, which may be the inputs."""
     c, n, H, KV, args = _inputs(rot, q, k, positions, q_weight, k_weight, eps)
-    out, rows = _out_rows(c, "out", out, ("q_out", "k_out"), q, k, stream)
+    out, rows = _out_rows(c, out, ("q_out", "k_out"), q, k, stream)
     _launch(c, stream, lib().bdlm_qk_rotate_fwd, *args, *rows)
-    return tuple(out)
+    return out
 
 
 def _new_weight_grads(c, q_weight, k_weight):
@@ -175,7 +186,7 @@ def qk_rotate_bwd(rot: Rotary, q, k, positions, dq_out, dk_out, q_weight=None, k
     overlap in time need one each); allocated if not given and there is a weight."""
     c, n, H, KV, args = _inputs(rot, q, k, positions, q_weight, k_weight, eps)
     rdq, rdk = _as_long(c, "dq_out", dq_out, H, n), _as_long(c, "dk_out", dk_out, KV, n)
-    out, rows = _out_rows(c, "out", out, ("dq", "dk"), q, k, stream)
+    out, rows = _out_rows(c, out, ("dq", "dk"), q, k, stream)
     weights, at, nbytes = [], 0, 0
     if q_weight is not None or k_weight is not None:
         weights = list(_made(stream, c.device, _new_weight_grads, c, q_weight, k_weight))
