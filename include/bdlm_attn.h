@@ -510,7 +510,7 @@ bdlm_status bdlm_chunk_attn(const bdlm_cache* c, const bdlm_chunk* p, int64_t la
  * Norms of queries and keys for each head with the position rotation, in one
  * pass: what comes between the projections and any of the attention calls.
  * For a head's row x with weight w (null: ones), at position p_a on axis a:
- *   r = 1 / sqrt(mean x^2 + eps),  n = x r w     (eps 0: no norm, n = x),
+ *   r = 1 / sqrt(mean x^2 + eps),  n = x r w     (eps 0: no norm, n = x; else within [2^-100, 2^100]),
  * and of the first `dim` elements pair i, on axis axis[i], turns by
  * t = p_axis[i] * freq[i]: (n1, n2) -> (n1 cos t - n2 sin t, n2 cos t + n1 sin t).
  *   q, k, outputs : [rows][heads or kv_heads][head_dim], rows `stride` elements apart

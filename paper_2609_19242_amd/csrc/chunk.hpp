@@ -24,9 +24,9 @@
 namespace bdlm {
 
 // Words of a plan in device memory: a header, the requests' first rows, their first
-// tiles (with the total behind), the items, the cut tiles.
+// tiles (with the total behind), the items, the merge's units.
 constexpr int kChunkHead = 16;
-enum : int { kPlanItems = 0, kPlanJoins = 1, kPlanRows = 2 };  // of the header
+enum : int { kPlanItems = 0, kPlanJoins = 1, kPlanRows = 2, kPlanRoom = 3 };  // of the header (room: for items)
 
 struct ChunkItemRec {
   int32_t seq, token0, pos0, len;  // (-1: none) the request's first row, its position, the sequence's tokens
@@ -37,9 +37,12 @@ struct ChunkItemRec {
 };
 constexpr int32_t kSharedTile = 1 << 30;
 constexpr int kFillWgs = 32;  // workgroups beside the items', for rows of no request
+// Rows of a cut tile whose parts a workgroup of the merge joins: `nrows` rows from
+// row0 on, their first parts from partial row `part` on, n parts `step` rows apart.
 struct ChunkJoin {
-  int32_t token0, row0, nrows, part, n, pad0, pad1, pad2;  // parts n, `nrows` partial rows apart
+  int32_t token0, row0, nrows, part, n, step, pad0, pad1;
 };
+constexpr int join_rows(int head_dim) { return 1024 / head_dim; }  // of a unit; one where there are many parts
 
 struct ChunkPlanArgs {
   const int32_t *lens, *seqs, *counts;
@@ -47,8 +50,8 @@ struct ChunkPlanArgs {
   int64_t top;  // tokens that a table holds
   int32_t requests, rows, seqs_in_cache, group, kv_heads, M, window, sinks;
   int32_t tile, f32;             // rows of a request's tiles where there are many; fp32
-  int32_t limit, least, slots;   // keys of a chunk at most, at least; workgroups to fill
-  int32_t max_items, max_joins;
+  int32_t limit, least, slots;   // keys of a chunk at most, at least; workgroups that run at once
+  int32_t join_rows, max_items, max_joins;
   int64_t max_part_rows;
 };
 

@@ -18,9 +18,9 @@ constexpr int64_t kMaxLen = (int64_t)1 << 28;     // blocks, windows, sinks
 constexpr int64_t kMaxStride = (int64_t)1 << 30;
 static_assert(BDLM_CHUNK_STARTS == kChunkHead * sizeof(int32_t), "the plan's layout is the header's");
 
-// Workgroups' worth of chunks that the walks are cut into, and keys of a chunk at least.
-constexpr int64_t kShares = 4 * kCus, kLeast = 256;
-static_assert((kShares & (kShares - 1)) == 0, "the planner shifts by it");
+// Workgroups that run at once, of which the planner fills up to two rounds by cutting, and keys of a chunk at least.
+constexpr int64_t kSlots = 2 * kCus, kSlotsF32 = kCus, kLeast = 256;
+static_assert((kSlots & (kSlots - 1)) == 0 && (kSlotsF32 & (kSlotsF32 - 1)) == 0, "the planner shifts by them");
 
 // What a plan and a call's partial outputs need, whatever the lengths are
 // (chunk_plan.hip says why it is enough).
@@ -60,10 +60,13 @@ bdlm_status check_chunk(const bdlm_cache* c, const bdlm_chunk* p, Room& room) {
                                           (int64_t)1 << 29);
   const int64_t top = c->max_pages * c->page_size;
   // chunks beyond the first of each tile: by the share, or by the limit (n_cut of a tile at most)
-  const int64_t by_share = kShares / c->kv_heads + 1, n_cut = top / (room.limit - 64), by_limit = tiles * n_cut;
+  const int64_t slots = f32 ? kSlotsF32 : kSlots;
+  const int64_t by_share = 2 * slots / c->kv_heads + 1, n_cut = top / (room.limit - 64), by_limit = tiles * n_cut;
   const int64_t more = std::max(by_share, by_limit);
   room.items = tiles > 0 ? tiles + more : 0;
-  room.joins = std::min(tiles, more);
+  // units of the merge, of cut tiles: of join_rows rows, or of one in those of more than kShortJoin chunks
+  room.joins = std::min(tiles, more) * ((kPrefixSharedRows + join_rows(c->head_dim) - 1) / join_rows(c->head_dim)) +
+               std::min(std::min(tiles, more / kShortJoin) * kPrefixSharedRows, all);
   // rows of cut tiles' chunks: at most a tile's of twice as many chunks, and as many as all rows have in that many chunks
   const int64_t tile = f32 ? kPrefixRowsF32 : all > 2 * kPrefixWaveRows ? kPrefixSharedRows : kPrefixWaveRows;
   room.part_rows = std::max(std::min(2 * by_share * tile, all * (by_share + 1)), std::min(2 * by_limit * tile, all * (n_cut + 1)));
@@ -130,7 +133,8 @@ bdlm_status bdlm_chunk_plan(const bdlm_cache* c, const bdlm_chunk* p, const int3
   a.f32 = c->dtype == BDLM_F32;
   a.limit = room.limit;
   a.least = (int32_t)std::min<int64_t>(kLeast, room.limit - 64);
-  a.slots = (int32_t)kShares;
+  a.slots = (int32_t)(a.f32 ? kSlotsF32 : kSlots);
+  a.join_rows = join_rows(c->head_dim);
   a.max_items = (int32_t)room.items;
   a.max_joins = (int32_t)room.joins;
   a.max_part_rows = room.part_rows;

@@ -1,6 +1,8 @@
 // The chunks' partial outputs of tiles whose keys were cut (chunk_plan.hip),
-// joined (partials.hpp), gfx950.  How many tiles that is only the device knows: a
-// grid of at most kMergeWgs workgroups takes groups of rows of (tile, KV head) in turn.
+// joined (partials.hpp), gfx950.  How many there are only the device knows: a grid of
+// at most kMergeWgs workgroups takes the plan's units for each KV head in turn.
+// Few parts: a row per D / 4 lanes.  Many (a long walk of one request): a workgroup
+// per row, whose waves take parts in turn and add up through LDS.
 // Bound by the launch and by reading.
 #include "chunk.hpp"
 #include "partials.hpp"
@@ -10,22 +12,71 @@ namespace bdlm {
 namespace {
 
 constexpr int kMergeWgs = 2048;
+static_assert(kShortJoin == kFewParts, "the plan's number is the kernel's");
+
+// The four waves' sums over their parts of a row, with maximum m of all, in wave 0's lanes < D / 4.
+template <int D, class Z>
+struct ManyParts {
+  static constexpr int LPR = JoinedRow<D>::LPR, PP = 64 / LPR;  // lanes per part, parts of a wave at a time
+  Joined4<Z> x[4][LPR];
+  Z sum[4];
+  __device__ __forceinline__ JoinedRow<D, Z> join(const float* o, const Z* z, int64_t first, int step, int parts, int w, int lane) {
+    const int part = lane / LPR, col = lane % LPR;
+    Z m = -INFINITY;
+    for (int j = lane; j < parts; j += 64) m = max_of(m, z[first + (int64_t)j * step]);
+#pragma unroll
+    for (int s = 32; s > 0; s >>= 1) m = max_of(m, xor_of(m, s));
+    const Z ref = m == -INFINITY ? Z(0) : m;
+    Z all = 0;
+    Joined4<Z> y = {0, 0, 0, 0};
+    for (int base = w * PP; base < parts; base += 16 * PP) {
+      Z zz[4];
+      f32x4 p[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const int64_t row = first + (int64_t)imin(base + 4 * k * PP + part, parts - 1) * step;
+        zz[k] = z[row];
+        p[k] = *(const f32x4*)(o + row * D + col * 4);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const bool seen = base + 4 * k * PP + part < parts && zz[k] > -INFINITY;
+        const Z f = seen ? pow2(zz[k] - ref) : Z(0);
+        all += f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = seen ? fma_of(f, Z(p[k][e]), y[e]) : y[e];
+      }
+    }
+#pragma unroll
+    for (int s = LPR; s < 64; s <<= 1) {
+      all += xor_of(all, s);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] += xor_of(y[e], s);
+    }
+    __syncthreads();  // (the sums of a row before are read)
+    if (lane < LPR) x[w][lane] = y;
+    if (lane == 0) sum[w] = all;
+    __syncthreads();
+    y = x[0][col] + x[1][col] + x[2][col] + x[3][col];
+    return joined<D, Z>(y, m, sum[0] + sum[1] + sum[2] + sum[3]);
+  }
+};
 
 template <int D, bool BF16>
 __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
   using Z = PartLse<BF16>;
-  constexpr int LPR = JoinedRow<D>::LPR, ROWS = 256 / LPR, GROUPS = (BF16 ? kPrefixSharedRows : kPrefixRowsF32) / ROWS;
+  constexpr int LPR = JoinedRow<D>::LPR;
+  static_assert(256 / LPR == join_rows(D), "a unit's rows");
+  __shared__ ManyParts<D, Z> many;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int joins = imin(a.plan[kPlanJoins], a.max_joins);
-  const int64_t units = (int64_t)joins * a.kv_heads * GROUPS;
+  const int64_t units = (int64_t)imin(a.plan[kPlanJoins], a.max_joins) * a.kv_heads;
   const Z* const z = (const Z*)a.part_lse;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
-    const int grp = (int)(u % GROUPS), kvh = (int)(u / GROUPS % a.kv_heads);
-    const ChunkJoin& t = a.joins[u / GROUPS / a.kv_heads];
-    if (grp * ROWS >= t.nrows) continue;
+    const int n = (int)(u / a.kv_heads), kvh = (int)(u - (int64_t)n * a.kv_heads);
+    const ChunkJoin t = a.joins[n];
     const int64_t first = kvh * a.part_rows + t.part;
     auto write = [&](int row, int col, const JoinedRow<D, Z>& r) __attribute__((always_inline)) {
-      const int n = t.row0 + row, i = n / a.group, h = kvh * a.group + (n - i * a.group);
+      const int q = t.row0 + row, i = q / a.group, h = kvh * a.group + (q - i * a.group);
       const int64_t token = t.token0 + i, at = token * a.os + (int64_t)h * D + col * 4;
       if constexpr (BF16) {
         bf16x4 y;
@@ -40,17 +91,16 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
       }
       if (col == 0) a.lse[h * a.pitch + token] = r.lse;
     };
-    if (t.n <= kFewParts) {  // a row per LPR lanes
-      const int row = grp * ROWS + threadIdx.x / LPR, col = threadIdx.x % LPR;
+    if (t.n <= kFewParts) {
+      const int row = threadIdx.x / LPR, col = threadIdx.x % LPR;
       if (row < t.nrows) {
-        auto at = [&](int j) { return first + (int64_t)j * t.nrows + row; };
+        auto at = [&](int j) { return first + (int64_t)j * t.step + row; };
         write(row, col, join_few<D>(a.part_o, z, at, t.n, col));
       }
-    } else {  // a wave per row
-      for (int row = grp * ROWS + w; row < imin(t.nrows, (grp + 1) * ROWS); row += 4) {
-        auto at = [&](int j) { return first + (int64_t)j * t.nrows + row; };
-        const JoinedRow<D, Z> r = join_partials<D>(a.part_o, z, at, t.n, lane);
-        if (lane < LPR) write(row, lane, r);
+    } else {
+      for (int row = 0; row < t.nrows; ++row) {
+        const JoinedRow<D, Z> r = many.join(a.part_o, z, first + row, t.step, t.n, w, lane);
+        if (w == 0 && lane < LPR) write(row, lane, r);
       }
     }
   }
@@ -59,8 +109,8 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
 }  // namespace
 
 hipError_t launch_chunk_merge(const ChunkArgs& a, int head_dim, int is_bf16, hipStream_t s) {
-  const int64_t rows = (int64_t)a.max_joins * a.kv_heads * (is_bf16 ? kPrefixSharedRows : kPrefixRowsF32);
-  const int n = (int)(rows / 4 < kMergeWgs ? rows / 4 : kMergeWgs);
+  const int64_t units = (int64_t)a.max_joins * a.kv_heads;
+  const int n = (int)(units < kMergeWgs ? units : kMergeWgs);
   if (n == 0) return hipSuccess;
   const dim3 grid(n), threads(256);
   if (head_dim == 128) {

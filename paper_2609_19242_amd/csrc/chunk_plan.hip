@@ -1,15 +1,22 @@
 // The work of a step of attention over a paged cache (chunk.hpp), laid out on the
 // device from the sequences' lengths and the numbers of new tokens, gfx950.
 //
-// One workgroup: a scan of the requests' rows and tiles, the walks' total and
-// longest, then the items.  Walks longer than a share of all of them (the walks of
-// all KV heads by the workgroups to fill) are cut into equal chunks; the longer half
-// of the items comes first.  The numbers do not depend on timing.
+// One workgroup: a scan of the requests' rows and tiles, the walks' lengths, the
+// unit, then the items.  Walks longer than the unit are cut into equal chunks; the
+// longer half of the items comes first.  The numbers do not depend on timing.
 //
-// Room.  With unit >= total / share, chunks beyond the first of each tile are at most
-// sum floor((n - 1) / unit) < share, or, where the chunk limit is what cuts, tiles times
-// what a table holds by the limit: the host makes that much room; a plan writes no more.
+// The unit.  Half of a workgroup's share of all walks to twice as much, in 32 steps:
+// the one with the least cost in keys, which is the longer of (rounds of longer items
+// times their size) and the share, and a start-up per item and what the partial sums
+// cost (4 x D bytes written and read per row, at 4.5 TB/s against 40 ns per key).  Rounds are
+// what matters: 4 requests of 64 rows behind 16,000 tokens, cut by the share alone,
+// came to 544 items for 512 places.
+//
+// Room.  With unit >= total / (2 slots / KV heads), chunks beyond the first of each tile
+// are at most sum floor((n - 1) / unit) <= 2 slots / KV heads, or, where the chunk limit is
+// what cuts, tiles times what a table holds by the limit: the host makes that much room.
 #include "chunk.hpp"
+#include "device.hpp"
 
 namespace bdlm {
 
@@ -17,6 +24,10 @@ namespace {
 
 constexpr int kT = 512;
 constexpr int kLdsRequests = 2048;  // requests that are kept in LDS (more are read again)
+constexpr int kLdsTiles = 2048;     // tiles for which the unit is looked for (with more, the share)
+constexpr int kUnits = 32;
+constexpr float kStartKeys = 64.f;  // a workgroup's start-up
+constexpr float kPartRows = 176.f;  // partial rows that take as long as a key of a slot
 
 // Exclusive prefix sums of x and y over the workgroup's threads; totals of all.
 __device__ __forceinline__ void block_scan(int64_t& x, int64_t& y, int64_t& all_x, int64_t& all_y, int64_t (*wsum)[2]) {
@@ -102,8 +113,11 @@ __device__ __forceinline__ Walk walk_of(const ChunkPlanArgs& a, const Request& q
 __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
   __shared__ int req[6][kLdsRequests];
   __shared__ int64_t wsum[kT / 64][2];
+  __shared__ int tile_n[kLdsTiles], tile_nrows[kLdsTiles];
   __shared__ unsigned long long total_lds;
   __shared__ int longest_lds;
+  __shared__ f32x4 sums[kT / kUnits][kUnits];
+  __shared__ int best_lds;
   const int tid = threadIdx.x;
   int32_t* const starts = a.plan + kChunkHead;
   int32_t* const tile0 = starts + a.requests;
@@ -182,6 +196,7 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
         if (g < T) {
           atomicAdd(&total_lds, (unsigned long long)w.n);
           atomicMax(&longest_lds, w.n);
+          if (T <= kLdsTiles) tile_n[g] = w.n, tile_nrows[g] = w.nrows;
         }
         continue;
       }
@@ -192,7 +207,9 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
         n = imax(over(w.n + size - 1, size), 1);
       }
       const bool is_longer = imin(size, w.n) > half;
-      int64_t x = is_longer ? (int64_t)n << 32 : n, y = n > 1 ? (int64_t)1 << 32 | n * w.nrows : 0, all_x, all_y;
+      // units of the merge: a row each where there are many parts
+      const int join = n > kShortJoin ? 1 : a.join_rows, units = n > 1 ? (w.nrows + join - 1) / join : 0;
+      int64_t x = is_longer ? (int64_t)n << 32 : n, y = n > 1 ? (int64_t)units << 32 | n * w.nrows : 0, all_x, all_y;
       block_scan(x, y, all_x, all_y, wsum);
       if (pass == 1) {
         longer += all_x >> 32;
@@ -206,7 +223,7 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
       const int i0 = is_longer ? (int)(x >> 32) : (int)(longer + (x & 0xffffffff)), j = (int)(y >> 32);
       const int64_t part = y & 0xffffffff;
       // (never: the host made room)
-      if (i0 + (int64_t)n > a.max_items || (n > 1 && (j >= a.max_joins || part + (int64_t)n * w.nrows > a.max_part_rows))) continue;
+      if (i0 + (int64_t)n > a.max_items || (n > 1 && (j + units > a.max_joins || part + (int64_t)n * w.nrows > a.max_part_rows))) continue;
       ChunkItemRec rec{q.seq, q.token0, q.pos0, q.len, w.row0, w.nrows, 0, 0, w.gap_at, w.gap, w.w0, 0};
       const int flag = w.shared ? kSharedTile : 0;
 #pragma unroll 1
@@ -216,12 +233,51 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
         rec.part = n > 1 ? (int)part + c * w.nrows | flag : ~flag;
         items[i0 + c] = rec;
       }
-      if (n > 1) joins[j] = ChunkJoin{q.token0, w.row0, w.nrows, (int)part, n, 0, 0, 0};
+#pragma unroll 1
+      for (int u = 0; u < units; ++u)
+        joins[j + u] = ChunkJoin{q.token0, w.row0 + u * join, imin(join, w.nrows - u * join), (int)part + u * join, n, w.nrows, 0, 0};
     }
     if (pass == 0) {
       __syncthreads();
-      const int64_t share = ((int64_t)total_lds * a.kv_heads + a.slots - 1) >> __builtin_ctz(a.slots);  // (a power of two)
-      unit = (int)(share < a.least ? a.least : share > a.limit - 64 ? a.limit - 64 : share);
+      const int64_t all = (int64_t)total_lds * a.kv_heads, least = (all + 2 * a.slots - 1) >> __builtin_ctz(2 * a.slots);
+      const float share = (float)all / (float)a.slots;
+      auto unit_of = [&](int k) __attribute__((always_inline)) {
+        const float u = 0.5f * share * exp2f_fast((float)k * (2.f / (kUnits - 1)));
+        const int64_t v = u < 1e9f ? (int64_t)u : (int64_t)1 << 30, x = v < least ? least : v;
+        return (int)(x < a.least ? a.least : x > a.limit - 64 ? a.limit - 64 : x);
+      };
+      if (T > kLdsTiles) {
+        unit = unit_of(kUnits / 2);
+      } else {  // a unit per lane, tiles dealt to groups of kUnits lanes
+        const int k = tid % kUnits, grp = tid / kUnits;
+        const float u = (float)unit_of(k), inv = 1.f / u;
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};  // longer items, their keys, items, partial rows
+#pragma unroll 2
+        for (int g = grp; g < T; g += kT / kUnits) {
+          const float n = (float)tile_n[g], cut = fmaxf(ceilf(n * inv), 1.f);
+          const bool is_longer = 2.f * n > u * cut;
+          x += f32x4{is_longer ? cut : 0.f, is_longer ? n : 0.f, cut, cut > 1.f ? cut * (float)tile_nrows[g] : 0.f};
+        }
+        sums[grp][k] = x;
+        __syncthreads();
+        if (tid < kUnits) {
+#pragma unroll
+          for (int j = 1; j < kT / kUnits; ++j) x += sums[j][k];
+          const float kvh = (float)a.kv_heads, slots = (float)a.slots;
+          const float rounds = x[0] > 0.f ? ceilf(x[0] * kvh / slots) * x[1] / x[0] : 0.f;
+          float cost = fmaxf(rounds, share) + x[2] * kvh / slots * kStartKeys + x[3] * kvh / kPartRows;
+          int best = k;
+#pragma unroll
+          for (int m = kUnits / 2; m > 0; m >>= 1) {  // the longest of the best
+            const float c = __shfl_xor(cost, m);
+            const int j = __shfl_xor(best, m);
+            if (c < cost || (c == cost && j > best)) cost = c, best = j;
+          }
+          if (tid == 0) best_lds = best;
+        }
+        __syncthreads();
+        unit = unit_of(best_lds);
+      }
       half = imin(longest_lds, unit) / 2;
     }
   }
@@ -229,6 +285,7 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
     a.plan[kPlanItems] = (int)((placed >> 32) + (placed & 0xffffffff));
     a.plan[kPlanJoins] = (int)(parts >> 32);
     a.plan[kPlanRows] = (int)(rows < a.rows ? rows : a.rows);
+    a.plan[kPlanRoom] = a.max_items;
   }
 }
 

@@ -14,6 +14,7 @@ namespace {
 
 constexpr int64_t kMaxRows = (int64_t)1 << 28;
 constexpr int64_t kMaxStride = (int64_t)1 << 30;
+constexpr double kMinEps = 0x1p-100;    // (a sum with it must be an fp32 number, and not 0)
 constexpr int64_t kWaves = 4;           // of a workgroup
 constexpr int64_t kFullWaves = 4096;    // waves from which on a row's heads stay with one wave
 constexpr int64_t kMaxFwdWgs = 1 << 20;
@@ -38,7 +39,8 @@ bdlm_status check_rotary(const bdlm_rotary* r, int32_t dtype, int64_t rows, cons
   if (heads < 1 || kv_heads < 1 || heads > kMaxRows || kv_heads > kMaxRows)
     return fail(BDLM_ERR_INVALID, "heads %d and kv_heads %d must be in [1, 2^28]", heads, kv_heads);
   if (rows < 0 || rows > kMaxRows) return fail(BDLM_ERR_INVALID, "rows %lld outside [0, 2^28]", (long long)rows);
-  if (!(eps >= 0.0) || !std::isfinite(eps)) return fail(BDLM_ERR_INVALID, "eps must be finite and not negative");
+  if (eps != 0.0 && !(eps >= kMinEps && eps <= 1.0 / kMinEps))
+    return fail(BDLM_ERR_INVALID, "eps %g is neither 0 nor within [2^-100, 2^100]", eps);
   if (rows > 0 && (!pos || (reinterpret_cast<uintptr_t>(pos) & 3u)))
     return fail(BDLM_ERR_INVALID, "positions are null or not 4-byte aligned");
   return BDLM_OK;

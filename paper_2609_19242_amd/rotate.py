@@ -135,8 +135,8 @@ def _inputs(rot, q, k, positions, q_weight, k_weight, eps):
         raise ValueError(f"k must be a [rows][kv_heads][{rot.head_dim}] tensor")
     KV = k.shape[1]
     rq, rk = _rows(c, "q", q, H, n), _as_long(c, "k", k, KV, n)
-    if eps is not None and not (math.isfinite(eps) and eps > 0):
-        raise ValueError(f"eps must be finite and positive, or None for no norm, got {eps}")
+    if eps is not None and not 2.0 ** -100 <= eps <= 2.0 ** 100:
+        raise ValueError(f"eps must be within [2^-100, 2^100], or None for no norm, got {eps}")
     if not isinstance(positions, torch.Tensor) or positions.dim() not in (1, 2):
         raise ValueError("positions must be a [rows] or [axes][rows] tensor")
     _expect("positions", positions, torch.int32, (n,) if positions.dim() == 1 and rot.axes == 1 else (rot.axes, n))

@@ -66,19 +66,18 @@ def oracle(cache, seqs, counts, q, layer=0, scale=None, block=1, window=0, sinks
 
 
 def items_of(plan):
-    """The plan's header, items [12] and joins [8]."""
+    """The plan's header, items [12] and units of the merge [8]."""
     a = plan._items.cpu().numpy()
-    n, j, rows = a[:3].tolist()
+    n, j, rows, room = a[:4].tolist()
     at = 16 + 2 * plan.requests + 1
-    room = (len(a) - at)
-    items = a[at:at + 12 * n].reshape(-1, 12)
-    assert 12 * n + 8 * j <= room
-    return n, j, rows, items, a
+    joins = at + 12 * room
+    assert n <= room and joins + 8 * j <= len(a)
+    return n, j, rows, a[at:at + 12 * n].reshape(-1, 12), a[joins:joins + 8 * j].reshape(-1, 8)
 
 
 def check_plan(plan, lens, seqs, counts, group, f32, block, window, sinks):
     """Every tile of rows once, its chunks in order over the keys that its rows see; partial rows apart."""
-    n, j, rows, items, _ = items_of(plan)
+    n, j, rows, items, joins = items_of(plan)
     starts = plan.starts.cpu().tolist()
     at, want = 0, {}
     for r, (s, c) in enumerate(zip(seqs, counts)):
@@ -124,7 +123,15 @@ def check_plan(plan, lens, seqs, counts, group, f32, block, window, sinks):
                 parts.append((p, p + nrows))
     parts.sort()
     assert all(a[1] <= b[0] for a, b in zip(parts, parts[1:]))
-    assert j == sum(len(xs) > 1 for xs in got.values())
+    # the merge's units: every row of the cut tiles once
+    joined = {}
+    for token0, row0, nrows, part, m, step, *_ in joins.tolist():
+        assert nrows >= 1
+        for i in range(nrows):
+            assert joined.setdefault((token0, row0 + i), (part + i, m, step)) == (part + i, m, step)
+    cut = {(key[0], key[1] + i): ((xs[0][11] & ~(1 << 30)) + i, len(xs), xs[0][5])
+           for key, xs in got.items() if len(xs) > 1 for i in range(xs[0][5])}
+    assert joined == cut and sum(x[2] for x in joins.tolist()) == len(cut)
     return n, j
 
 

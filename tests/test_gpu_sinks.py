@@ -3,7 +3,7 @@ import pytest
 import torch
 
 import paper_2609_19242_amd as bd
-from tests import window_util
+from tests import rotate_oracle, window_util
 from tests.serving_util import check
 
 pytestmark = pytest.mark.gpu
@@ -145,6 +145,36 @@ def test_few_keys_of_large_values():
     q, k, v, do = make(64, 64, 4, 2, 64, BF, 14)
     v = (v.float() * 0.01 + 20).to(BF)
     both([64], None, 4, 2, 64, BF, 1, 16, 3, tensors=(q, k, v, do))
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_training_step_of_a_layer(dtype):
+    """As it is used: rotated queries and keys, attention, and both backward passes, each against the oracle of what it
+    was given."""
+    ql, H, KV, D = [70, 1, 150], 4, 2, 64
+    n, rot = sum(ql), bd.rotary(64, sections=(16, 16))
+    g = torch.Generator().manual_seed(18)
+    qkv = torch.randn(n, H + 2 * KV, D, generator=g).to(dtype).to(DEV)
+    w = [(1 + 0.2 * torch.randn(D, generator=g)).to(dtype).to(DEV) for _ in range(2)]
+    do = torch.randn(n, H, D, generator=g).to(dtype).to(DEV)
+    pos = torch.cat([torch.arange(x) for x in ql]).to(torch.int32)
+    pos = torch.stack([pos // 12, pos % 12]).to(DEV)
+    q, k, v = qkv[:, :H], qkv[:, H:H + KV], qkv[:, H + KV:]
+    plan = bd.packed_plan(ql, heads=H, kv_heads=KV, head_dim=D, dtype=dtype, window=40, sinks=3)
+    qr, kr = bd.qk_rotate_fwd(rot, q, k, pos, *w, eps=1e-6)
+    o, lse = bd.packed_fwd(plan, qr, kr, v)
+    dqr, dkr, dv = bd.packed_bwd(plan, qr, kr, v, o, lse, do)
+    dq, dk, dqw, dkw = bd.qk_rotate_bwd(rot, q, k, pos, dqr, dkr, *w, eps=1e-6)
+    seqs = [(sum(ql[:i]), x, sum(ql[:i]), x) for i, x in enumerate(ql)]
+    ref = window_util.packed(qr, kr, v, seqs, None, 1, 40, 3, do)
+    for name, t in zip(("o", "lse", "dq", "dk", "dv"), (o, lse, dqr, dkr, dv)):
+        check(name, t, *ref[name])
+    t = rotate_oracle.angles(rot.freqs, rot.pair_axes, pos)
+    for x, y, dy, dx, ww, dw in ((q, qr, dqr, dq, w[0], dqw), (k, kr, dkr, dk, w[1], dkw)):
+        check("rotated", y, *rotate_oracle.forward(x, ww, t, 1e-6, False))
+        back = rotate_oracle.backward(x, ww, t, 1e-6, False, dy)
+        check("dx", dx, *back["dx"])
+        check("dw", dw, *back["dw"])
 
 
 def test_replays_of_a_graph_equal_eager_calls():

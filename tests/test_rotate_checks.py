@@ -102,7 +102,7 @@ def test_calls_need_a_gpu():
     (dict(positions=torch.zeros(2, 6, dtype=torch.int32)), ValueError, "shape"),
     (dict(positions=torch.zeros(12, dtype=torch.int32)[::2]), ValueError, "contiguous"),
     (dict(eps=0.0), ValueError, "eps"), (dict(eps=-1.0), ValueError, "eps"), (dict(eps=math.nan), ValueError, "eps"),
-    (dict(eps=math.inf), ValueError, "eps"), (dict(eps=None), ValueError, "needs a norm"),
+    (dict(eps=math.inf), ValueError, "eps"), (dict(eps=1e-40), ValueError, "eps"), (dict(eps=None), ValueError, "needs a norm"),
     (dict(q_weight=torch.ones(64)), TypeError, "q_weight"), (dict(k_weight=torch.ones(32, dtype=BF)), ValueError, "k_weight"),
 ])
 def test_both_directions_refuse(change, err, what):
@@ -149,7 +149,7 @@ def call(record=None, bwd=False, **kw):
     (dict(dtype=2), -2), (dict(rows=-1), -1), (dict(rows=1 << 29), -1), (dict(pos=0), -1), (dict(pos=FAKE + 2), -1), (dict(heads=0), -1),
     (dict(kv=0), -1), (dict(q=0), -1), (dict(q=FAKE + 8), -1), (dict(qs=255), -1), (dict(qs=260), -1), (dict(qs=(1 << 30) + 8), -1),
     (dict(ks=64), -1), (dict(qw=FAKE + 4), -1), (dict(eps=0.0), -1), (dict(eps=-1.0), -1), (dict(eps=math.nan), -1),
-    (dict(eps=math.inf), -1), (dict(o=0), -1), (dict(os=128), -1)])
+    (dict(eps=math.inf), -1), (dict(eps=1e-40), -1), (dict(eps=1e40), -1), (dict(o=0), -1), (dict(os=128), -1)])
 def test_the_c_abi_refuses(kw, status):
     assert call(**kw) == status and call(bwd=True, **kw) == status
     assert bd.lib().bdlm_last_error()
