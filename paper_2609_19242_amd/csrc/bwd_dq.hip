@@ -150,6 +150,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   };
   const bool kwave = w < NW / 2;
   const int64_t CS = kwave ? k_stride<D>(a) : v_stride<D>(a);  // of the tensor this wave copies
+  [[maybe_unused]] const auto sw = sink_walk_of(a, pq0, pq1);
   int u0, u1;
   seen_keys(a, pq0, pq1, u0, u1);
   auto copy_seek = [&](CopyCur cc) -> CopyCur {
@@ -157,8 +158,12 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       const KRangeArg& kr = k_range(a, cc.c.j);
       cc.src = (const bf16*)(kwave ? kr.k : kr.v) +
                row_elem<D>(a, it.b, kr.bstride, (int64_t)cc.c.t * BN, HKV, kvh, CS);
-      if constexpr (kHasSinks<Args>) cc.rows_left = imin(u1 - (cc.c.j ? a.split : 0), kr.len) - cc.c.t * BN;
-      else cc.rows_left = (kPacked ? u1 : kr.len) - cc.c.t * BN;
+      if constexpr (kHasSinks<Args>) {
+        cc.src += (int64_t)sw.gap * CS;
+        cc.rows_left = sw.n - cc.c.t * BN;
+        return cc;
+      }
+      cc.rows_left = (kPacked ? u1 : kr.len) - cc.c.t * BN;
     }
     return cc;
   };
@@ -192,15 +197,16 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
     for (int k = 0; k < NB; ++k) {
       const int nr = nrows - 16 * k;
       if constexpr (kHasSinks<Args>) {
-        // rows between the sinks and the first seen key of the windows read zeros too
-        const int hole0 = (cc.c.j ? 0 : a.sinks - cc.c.t * BN) - 16 * k;
-        const int hole1 = u0 - (cc.c.j ? a.split : 0) - cc.c.t * BN - 16 * k;
-        if (cc.c.have && nr > 0 && hole1 > imax(hole0, 0)) {
-          const auto r = make_rsrc(cc.src + (int64_t)16 * k * CS, (uint32_t)(((nr - 1) * (int)CS + D) * 2));
+        // rows below the gap lie that much earlier; those that no row of the tile sees read zeros too
+        const int v0 = cc.c.t * BN + 16 * k;
+        if (cc.c.have && nr > 0 && cc.c.t * BN < sw.w0) {
+          const uint32_t bytes = (uint32_t)(((nr - 1) * (int)CS + D) * 2);
 #pragma unroll
           for (int i = 0; i < PI; ++i) {
-            const int row = ((cw * IPW + i) * 64 + lane) / (D / 8);
-            buf_to_lds<16>(r, dst + (k * PI + i) * 512, row >= hole0 && row < hole1 ? ~15u : voff[i], 0);
+            const int first = v0 + (cw * IPW + i) * (512 / D), v = first + lane / (D / 8);  // of the instruction, the lane
+            const int64_t at = (int64_t)(16 * k - (first < sw.gap_at ? sw.gap : 0)) * CS;
+            buf_to_lds<16>(make_rsrc(cc.src + at, bytes), dst + (k * PI + i) * 512,
+                           (v >= a.sinks) & (v < sw.w0) ? ~15u : voff[i], 0);
           }
           continue;
         }
@@ -242,17 +248,21 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   vm_wait_barrier<IPW * (NST - 2)>();
   int cur = 0;
   int lane_lo = 0, lane_w = 0, lane_j = -1;
-  [[maybe_unused]] int lane_s = 0, lane_end = 0;  // with sinks: this lane's in range j; the end of its keys
+  [[maybe_unused]] int lane_s = 0, lane_end = 0;  // with sinks: the end of this lane's, and of its keys
   [[maybe_unused]] bool few_keys = false;  // packed calls: some row of this wave has no more keys than a tile holds
   while (c0.have) {
     copy_tile(lds + (cur == 0 ? NST - 1 : cur - 1) * STAGE, cp);
     const int j = c0.j, t = c0.t, f0 = c0.f0, f1 = c0.f1;
     if (lane_j != j) {
-      lane_key_interval(a, j, qr.stream, pq, lane_lo, lane_w);
+      if constexpr (kHasSinks<Args>) {
+        lane_walk(a, sw, pq, lane_lo, lane_w, lane_s);
+        lane_end = lane_w > 0 ? lane_lo - k_range(a, j).pos0 + lane_w : lane_s;
+        few_keys = __builtin_amdgcn_ballot_w64(lane_end > 0 && lane_end <= BN) != 0;
+      } else {
+        lane_key_interval(a, j, qr.stream, pq, lane_lo, lane_w);
+      }
       lane_j = j;
-      lane_sinks(a, j, qr.stream, pq, lane_s, lane_end);
-      if constexpr (kHasSinks<Args>) few_keys = j == 0 && __builtin_amdgcn_ballot_w64(lane_end > 0 && lane_end <= BN) != 0;
-      else if constexpr (kPacked) few_keys = __builtin_amdgcn_ballot_w64(lane_w > 0 && lane_w <= BN) != 0;
+      if constexpr (kPacked && !kHasSinks<Args>) few_keys = __builtin_amdgcn_ballot_w64(lane_w > 0 && lane_w <= BN) != 0;
     }
 
     // On a partly visible tile, a wave none of whose rows sees any of the
@@ -320,8 +330,8 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       // dS where a row has few keys (one key: all of it).  (D lies in dpacc already.)
       if (kPacked && few_keys) {
         const int kstart = k_range(a, j).pos0 + t * BN - lane_lo;
-        // (with sinks a row that sees anything sees key 0: all of its keys lie in the first tile or none of the tiles)
-        const bool whole = kHasSinks<Args> ? j == 0 && t == 0 && lane_end > 0 && lane_end <= BN
+        // (with sinks a row that sees anything sees key 0)
+        const bool whole = kHasSinks<Args> ? t == 0 && lane_end > 0 && lane_end <= BN
                                            : lane_w > 0 && kstart <= 0 && kstart + BN >= lane_w;
         if (__builtin_amdgcn_ballot_w64(whole) != 0) {
           float rest = 0.f, z = lse2;

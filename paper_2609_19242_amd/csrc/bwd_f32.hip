@@ -394,7 +394,7 @@ hipError_t launch_bwd_sum_f32(const AttnArgs& a, int head_dim, hipStream_t s) {
 #else
 
 #ifdef BDLM_SINK_CALLS
-using PackedQ = SinkQArgs;
+using PackedQ = SinkQArgsF32;
 using PackedK = SinkKArgs;
 #else
 using PackedQ = PackedArgs;

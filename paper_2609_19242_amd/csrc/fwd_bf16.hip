@@ -130,6 +130,7 @@ __global__ __launch_bounds__(NT * NW * 64)
   };
   const bool kwave = w < NW / 2;
   const int64_t CS = kwave ? k_stride<D>(a) : v_stride<D>(a);  // of the tensor this wave copies
+  [[maybe_unused]] const auto sw = sink_walk_of(a, pq0, pq1);
   int u0, u1;
   seen_keys(a, pq0, pq1, u0, u1);
   auto copy_seek = [&](CopyCur cc) -> CopyCur {
@@ -137,8 +138,12 @@ __global__ __launch_bounds__(NT * NW * 64)
       const KRangeArg& kr = k_range(a, cc.c.j);
       cc.src = (const bf16*)(kwave ? kr.k : kr.v) +
                row_elem<D>(a, it.b, kr.bstride, (int64_t)cc.c.t * BN, HKV, kvh, CS);
-      if constexpr (kHasSinks<Args>) cc.rows_left = imin(u1 - (cc.c.j ? a.split : 0), kr.len) - cc.c.t * BN;
-      else cc.rows_left = (kIsPacked<Args> ? u1 : kr.len) - cc.c.t * BN;
+      if constexpr (kHasSinks<Args>) {
+        cc.src += (int64_t)sw.gap * CS;
+        cc.rows_left = sw.n - cc.c.t * BN;
+        return cc;
+      }
+      cc.rows_left = (kIsPacked<Args> ? u1 : kr.len) - cc.c.t * BN;
     }
     return cc;
   };
@@ -166,14 +171,14 @@ __global__ __launch_bounds__(NT * NW * 64)
     const uint32_t bytes = cc.c.have ? (uint32_t)(((nrows - 1) * (int)CS + D) * 2) : 0u;
     bf16* dst = st + (kwave ? 0 : BN * D) + cw * IPW * 512;
     if constexpr (kHasSinks<Args>) {
-      // rows between the sinks and the first seen key of the windows read zeros too
-      const int hole0 = cc.c.j ? 0 : a.sinks - cc.c.t * BN, hole1 = u0 - (cc.c.j ? a.split : 0) - cc.c.t * BN;
-      if (cc.c.have && hole1 > imax(hole0, 0)) {
-        const auto r = make_rsrc(cc.src, bytes);
+      // rows below the gap lie that much earlier; those that no row of the tile sees read zeros too
+      const int v0 = cc.c.t * BN;
+      if (cc.c.have && v0 < sw.w0) {
 #pragma unroll
         for (int i = 0; i < IPW; ++i) {
-          const int row = ((cw * IPW + i) * 64 + lane) / (D / 8);
-          buf_to_lds<16>(r, dst + i * 512, row >= hole0 && row < hole1 ? ~15u : voff[i], 0);
+          const int first = v0 + (cw * IPW + i) * (512 / D), v = first + lane / (D / 8);  // of the instruction, the lane
+          const auto r = make_rsrc(first < sw.gap_at ? cc.src - (int64_t)sw.gap * CS : cc.src, bytes);
+          buf_to_lds<16>(r, dst + i * 512, (v >= a.sinks) & (v < sw.w0) ? ~15u : voff[i], 0);
         }
         return;
       }
@@ -219,14 +224,14 @@ __global__ __launch_bounds__(NT * NW * 64)
   vm_wait_barrier<IPW * (NS - 2)>();
   int cur = 0;
   int lane_lo = 0, lane_w = 0, lane_j = -1;
-  [[maybe_unused]] int lane_s = 0, lane_end = 0;  // with sinks: this lane's in range j
+  [[maybe_unused]] int lane_s = 0;  // with sinks: the end of this lane's
   while (NT > 1 ? rounds > 0 : c0.have) {
     if constexpr (NT > 1) --rounds;
     copy_tile(lds + (cur == 0 ? NS - 1 : cur - 1) * STAGE, cp);
     const int j = c0.j, t = c0.t, f0 = c0.f0, f1 = c0.f1;
     if (lane_j != j && (NT == 1 || c0.have)) {  // this lane's visible key interval inside range j
-      lane_key_interval(a, j, qr.stream, pq, lane_lo, lane_w);
-      lane_sinks(a, j, qr.stream, pq, lane_s, lane_end);
+      if constexpr (kHasSinks<Args>) lane_walk(a, sw, pq, lane_lo, lane_w, lane_s);
+      else lane_key_interval(a, j, qr.stream, pq, lane_lo, lane_w);
       lane_j = j;
     }
 

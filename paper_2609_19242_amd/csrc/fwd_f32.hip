@@ -182,7 +182,7 @@ hipError_t launch_fwd_f32(const AttnArgs& a, int head_dim, hipStream_t s) {
 #else
 
 #ifdef BDLM_SINK_CALLS
-using PackedQ = SinkQArgs;
+using PackedQ = SinkQArgsF32;
 #else
 using PackedQ = PackedArgs;
 #endif

@@ -155,49 +155,75 @@ __device__ __forceinline__ int64_t row_elem(const PackedView&, int, int64_t, int
 // ---- sinks: a window, and the first S keys of a sequence stay visible.
 //
 // A row sees the keys [0, min(S, e)) and [e - W, e).  A call with sinks is the same
-// kernels over another view of the sequence (SinkQArgs, SinkKArgs):
-//  * forward and dQ: two key ranges, the keys below `split` and the others.  bf16:
-//    split is S rounded up to whole 64-key tiles, so that a sequence's tiles are
-//    those of a call without sinks; in the first range a lane tests a key against
-//    its sinks and its window.  fp32: split is S.  A query tile visits the first
-//    range's tiles that hold sinks (or its window) and then its window's: the keys in
-//    between cost nothing.
+// kernels over another view of the sequence (SinkQArgs, SinkQArgsF32, SinkKArgs):
+//  * forward and dQ, bf16: a query tile's rows see [0, S) and [w0, end), w0 the first row's
+//    window's start.  They are walked as [0, n) with the gap between taken out, in multiples
+//    of 16 keys, so that a few sinks share the first tile with the window's first keys: v
+//    < gap_at is key v, the others are key v + gap.  Keys that no row of the tile sees (at
+//    most 15 before w0, and behind S) read as zeros.  (8 texts of 2,048, 32/8 heads, d 128,
+//    window 128: without sinks forward 96 us, dQ 149, with 4 of them 97 and 157, and 115 and
+//    170 with the sinks in a tile of their own.)
+//  * the same, fp32: two key ranges, the sinks and the others.
 //  * dK/dV: the sinks, which all rows from theirs on see, are keys of a call without a
 //    window, the others of one without sinks: items of two kinds, tile -1 - t the
-//    t-th of the sinks.
+//    t-th of the sinks.  A tile of 4 keys costs as much as one of 128 (the same texts:
+//    169 us without, 225 with them; 16K tokens of 3 documents, window 1,024: 633, 671).
 struct SinkQArgs : PackedArgs {};
+struct SinkQArgsF32 : PackedArgs {};
 struct SinkKArgs : PackedArgs {};
 
-struct SinkView : PackedView {
-  static constexpr int n_k = 2;
-  int32_t sinks, split;
-  int32_t n0, n1;          // tiles of its walk that the item takes
-  int64_t k_ahead, v_ahead;  // bytes from a sequence's first key to the second range
+struct SinkWalk {
+  int n, gap_at, gap, w0;
 };
-
-inline int __host__ __device__ sink_split(int sinks, int k_len, bool f32) {
-  return imin(f32 ? sinks : (sinks + 63) / 64 * 64, k_len);
+// The walk of the rows at positions [pq0, pq1] over len keys from position pos0 on.
+__host__ __device__ inline SinkWalk sink_walk(const MaskRule& rule, int sinks, int pq0, int pq1, int pos0, int len) {
+  int lo0, hi0, lo1, hi1;
+  key_interval(kClean, pq0, kClean, rule, lo0, hi0);
+  key_interval(kClean, pq1, kClean, rule, lo1, hi1);
+  const int end = imin(hi1 - pos0, len);
+  SinkWalk w{imax(end, 0), kBig, 0, imax(lo0 - pos0, 0)};
+  const int below = (imin(sinks, w.n) + 15) & ~15, first = w.w0 & ~15;
+  if (first > below) {
+    w.gap_at = below;
+    w.gap = first - below;
+    w.w0 -= w.gap;
+    w.n = end > first ? below + end - first : imin(below, w.n);  // (a block may end behind its window's start)
+  }
+  return w;
 }
 
+struct SinkView : PackedView {
+  int32_t sinks;
+};
 __device__ __forceinline__ SinkView call_view(const SinkQArgs& p, int item, int elem) {
   const PackedItem& it = p.items[item];
   SinkView a;
   static_cast<PackedView&>(a) = packed_view(p, it, elem);
   a.sinks = imin(p.sinks, it.k_len);
-  a.split = sink_split(p.sinks, it.k_len, elem == 4);
-  a.n0 = it.n0;
-  a.n1 = it.n1;
-  a.k_ahead = (int64_t)a.split * p.ks * elem;
-  a.v_ahead = (int64_t)a.split * p.vs * elem;
-  a.kr[0].len = a.split;  // (the second range: k_range)
+  return a;
+}
+
+struct SinkViewF32 : PackedView {
+  static constexpr int n_k = 2;
+  int32_t sinks;             // the first range's keys
+  int64_t k_ahead, v_ahead;  // bytes from a sequence's first key to the second range
+};
+__device__ __forceinline__ SinkViewF32 call_view(const SinkQArgsF32& p, int item, int elem) {
+  const PackedItem& it = p.items[item];
+  SinkViewF32 a;
+  static_cast<PackedView&>(a) = packed_view(p, it, elem);
+  a.sinks = imin(p.sinks, it.k_len);
+  a.k_ahead = (int64_t)a.sinks * p.ks * elem;
+  a.v_ahead = (int64_t)a.sinks * p.vs * elem;
+  a.kr[0].len = a.sinks;
   a.kr[0].ntiles = it.k_len;
   return a;
 }
-__device__ __forceinline__ KRangeArg k_range(const SinkView& a, int j) {
+__device__ __forceinline__ KRangeArg k_range(const SinkViewF32& a, int j) {
   KRangeArg r = a.kr[0];
   if (j > 0) {
-    r.pos0 += a.split;
-    r.len = r.ntiles - a.split;
+    r.pos0 += a.sinks;
+    r.len = r.ntiles - a.sinks;
     r.k = (const char*)r.k + a.k_ahead;
     r.v = (const char*)r.v + a.v_ahead;
   }
@@ -240,10 +266,10 @@ template <class A> constexpr bool kIsPacked = false;
 template <> constexpr inline bool kIsPacked<PackedArgs> = true;
 template <> constexpr inline bool kIsPacked<PackedView> = true;
 template <> constexpr inline bool kIsPacked<SinkQArgs> = true;
+template <> constexpr inline bool kIsPacked<SinkQArgsF32> = true;
 template <> constexpr inline bool kIsPacked<SinkKArgs> = true;
 template <class A> constexpr bool kHasSinks = false;
 template <> constexpr inline bool kHasSinks<SinkQArgs> = true;
-template <> constexpr inline bool kHasSinks<SinkView> = true;
 
 hipError_t launch_fwd_bf16(const PackedArgs& a, int head_dim, int teams, hipStream_t s);
 hipError_t launch_packed_fwd_sum(const PackedArgs& a, int head_dim, int slots, hipStream_t s);
@@ -256,10 +282,10 @@ hipError_t launch_bwd_dq_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dkv_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_sum_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_fwd_bf16(const SinkQArgs& a, int head_dim, int teams, hipStream_t s);
-hipError_t launch_fwd_f32(const SinkQArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_fwd_f32(const SinkQArgsF32& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dq_bf16(const SinkQArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dkdv(const SinkKArgs& a, int head_dim, hipStream_t s);
-hipError_t launch_bwd_dq_f32(const SinkQArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_bwd_dq_f32(const SinkQArgsF32& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dkv_f32(const SinkKArgs& a, int head_dim, hipStream_t s);
 
 }  // namespace bdlm

@@ -133,10 +133,11 @@ void take_chunks(const bdlm_packed_plan& pl, bool dq, PackedArgs& a) {
   a.n_sums = c.sums;
 }
 
-// launch(a), as a call with sinks if it has some.
-template <class Sinks, class F>
-hipError_t with_sinks(const PackedArgs& a, F&& launch) {
-  return a.sinks > 0 ? launch(Sinks{a}) : launch(a);
+// bf16(a) or f32(a), as a call with sinks if it has some.
+template <class SinksBf16, class SinksF32, class F, class G>
+hipError_t launch_as(const PackedArgs& a, int32_t dtype, F&& bf16, G&& f32) {
+  if (dtype == BDLM_BF16) return a.sinks > 0 ? bf16(SinksBf16{a}) : bf16(a);
+  return a.sinks > 0 ? f32(SinksF32{a}) : f32(a);
 }
 
 bdlm_status check_pitch(const bdlm_packed_plan& pl, int64_t pitch) {
@@ -246,10 +247,9 @@ bdlm_status bdlm_packed_fwd(const bdlm_packed_plan* plan, const void* items, bdl
   a.os = (int32_t)o.stride;
   a.lse = lse;
   const hipError_t e = timed(kKPackedFwd, stream, [&] {
-    const hipError_t le = with_sinks<SinkQArgs>(a, [&](const auto& c) {
-      return p.dtype == BDLM_BF16 ? launch_fwd_bf16(c, p.head_dim, plan->teams, stream)
-                                  : launch_fwd_f32(c, p.head_dim, stream);
-    });
+    const hipError_t le = launch_as<SinkQArgs, SinkQArgsF32>(
+        a, p.dtype, [&](const auto& c) { return launch_fwd_bf16(c, p.head_dim, plan->teams, stream); },
+        [&](const auto& c) { return launch_fwd_f32(c, p.head_dim, stream); });
     return le != hipSuccess || a.n_sums == 0 ? le : launch_packed_fwd_sum(a, p.head_dim, plan->fwd.slots, stream);
   });
   return e == hipSuccess ? BDLM_OK : hip_fail(e, "packed forward launch");
@@ -305,9 +305,9 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
   take_chunks(*plan, true, a);
   // dQ first: it leaves the row statistics for dK/dV.
   hipError_t e = timed(kKPackedDq, stream, [&] {
-    const hipError_t le = with_sinks<SinkQArgs>(a, [&](const auto& c) {
-      return p.dtype == BDLM_BF16 ? launch_bwd_dq_bf16(c, p.head_dim, stream) : launch_bwd_dq_f32(c, p.head_dim, stream);
-    });
+    const hipError_t le = launch_as<SinkQArgs, SinkQArgsF32>(
+        a, p.dtype, [&](const auto& c) { return launch_bwd_dq_bf16(c, p.head_dim, stream); },
+        [&](const auto& c) { return launch_bwd_dq_f32(c, p.head_dim, stream); });
     return le != hipSuccess || a.n_sums == 0 ? le : launch_packed_dq_sum(a, p.head_dim, stream);
   });
   if (e != hipSuccess) return hip_fail(e, "packed dQ launch");
@@ -316,9 +316,9 @@ bdlm_status bdlm_packed_bwd(const bdlm_packed_plan* plan, const void* items, bdl
   a.sums = reinterpret_cast<const PackedSum*>(a.items + plan->k_items);
   a.n_sums = plan->n_sums;
   e = timed(kKPackedDkDv, stream, [&] {
-    hipError_t le = with_sinks<SinkKArgs>(a, [&](const auto& c) {
-      return p.dtype == BDLM_BF16 ? launch_bwd_dkdv(c, p.head_dim, stream) : launch_bwd_dkv_f32(c, p.head_dim, stream);
-    });
+    hipError_t le = launch_as<SinkKArgs, SinkKArgs>(
+        a, p.dtype, [&](const auto& c) { return launch_bwd_dkdv(c, p.head_dim, stream); },
+        [&](const auto& c) { return launch_bwd_dkv_f32(c, p.head_dim, stream); });
     if (le != hipSuccess || a.n_sums == 0) return le;
     return p.dtype == BDLM_BF16 ? launch_bwd_dkdv_sum(a, p.head_dim, stream) : launch_bwd_sum_f32(a, p.head_dim, stream);
   });

@@ -70,10 +70,9 @@ constexpr int64_t kStartTiles = 3;
 // 46 -> 43 us, of which the sums 10 -> 5; bf16, 8K of documents: 0.5, 0.75, 1 and
 // 1.5 loads 263, 252, 245 and 261 us).
 //
-// Sinks (packed.hpp): a query tile's walk has the tiles that hold sinks or windowed
-// keys in the first range, then its window's in the second; a sequence's key tiles
-// are those of its sinks, numbered -1 - t, which all rows from theirs on walk, and
-// those of its other keys.
+// Sinks (packed.hpp): a query tile's walk is that of its sinks and its window; a
+// sequence's key tiles are those of its sinks, numbered -1 - t, which all rows from
+// theirs on walk, and those of its other keys.
 inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_packed_seq* seqs) {
   PackedPlanItems out;
   const bool f32 = p.dtype == BDLM_F32;
@@ -106,9 +105,9 @@ inline PackedPlanItems packed_items(const bdlm_packed& p, int64_t n, const bdlm_
         q.push_back({std::max(0, u1 - u0), it});
         walks.push_back({u1 > u0 ? (u1 + 63) / 64 - u0 / 64 : 0, it});
       } else {
-        const int B = sink_split(p.sinks, kl, f32), near = std::min(B, std::max(u1, 0)), far = std::max(u0, B);
-        q.push_back({near + std::max(0, u1 - far), it});
-        walks.push_back({(near + 63) / 64 + (u1 > far ? (u1 - B + 63) / 64 - (far - B) / 64 : 0), it});
+        const int n = sink_walk(rule, std::min(p.sinks, kl), qp + first, qp + last, shift, kl).n;
+        q.push_back({n, it});
+        walks.push_back({(n + 63) / 64, it});
       }
       fwd_total += walks.back().cost;
     }

@@ -58,8 +58,6 @@ __device__ inline bool q_tile_item(const PackedArgs& a, int wg, QTileItem& it) {
   return true;
 }
 
-// With sinks a view's key_tile_span leaves the chunk's tiles only.
-__device__ inline void cut_walk(const SinkQArgs&, const QTileItem&, int&, int&, bool&) {}
 // The key tiles [t, t1) of a packed item's chunk of its tile's walk [t, t1).
 __device__ inline void cut_walk(const AttnArgs&, const QTileItem&, int&, int&, bool&) {}
 __device__ inline void cut_walk(const PackedArgs& a, const QTileItem& it, int& t, int& t1, bool& have) {
@@ -97,42 +95,60 @@ __device__ inline void key_tile_span(const A& a, int j, int qs, int pq0, int pq1
   }
 }
 
-// A view with sinks: the tiles of the first range that hold sinks or keys of the
-// rows' windows, then the window's tiles in the second, of both those that the
-// item's chunk of the walk takes.  (Tiles between the sinks and the window in the first range, if the
-// window starts there, hold a sink each but the last: none is visited in vain.)
-__device__ inline void key_tile_span(const SinkView& a, int j, int qs, int pq0, int pq1, int BN, int& t0, int& t1,
-                                     int& f0, int& f1) {
-  const int pos0 = a.kr[0].pos0, n = a.kr[0].ntiles, B = a.split;
+// With sinks: the walk's tiles (packed.hpp), those that all rows see among them.
+struct NoSinks {};
+template <class A>
+__device__ inline NoSinks sink_walk_of(const A&, int, int) { return {}; }
+__device__ inline SinkWalk sink_walk_of(const SinkView& a, int pq0, int pq1) {
+  return sink_walk(a.rule, a.sinks, pq0, pq1, a.kr[0].pos0, a.kr[0].len);
+}
+__device__ inline void key_tile_span(const SinkView& a, int, int, int pq0, int pq1, int BN, int& t0, int& t1, int& f0,
+                                     int& f1) {
+  const SinkWalk w = sink_walk_of(a, pq0, pq1);
   int lo0, hi0, lo1, hi1;
-  key_interval(qs, pq0, kClean, rule_of(a), lo0, hi0);
-  key_interval(qs, pq1, kClean, rule_of(a), lo1, hi1);
-  lo0 = imax(lo0 - pos0, 0);
-  lo1 = imax(lo1 - pos0, 0);
-  hi0 = imin(hi0 - pos0, n);
-  hi1 = imin(hi1 - pos0, n);
-  t0 = t1 = f0 = f1 = 0;
-  if (hi1 <= 0) return;
-  const int first = (imin(B, hi1) + BN - 1) / BN;  // tiles of the first range
-  if (j == 0) {
-    t1 = first;
-    if (hi0 > 0) f1 = imin(hi0, lo1 <= a.sinks ? B : a.sinks) / BN;
-    t0 = imin(a.n0, t1);
-    t1 = imin(a.n1, t1);
-    return;
+  key_interval(kClean, pq0, kClean, a.rule, lo0, hi0);
+  key_interval(kClean, pq1, kClean, a.rule, lo1, hi1);
+  const int lo = imax(lo1 - a.kr[0].pos0, 0) - w.gap, hi = imin(hi0 - a.kr[0].pos0, a.kr[0].len) - w.gap;
+  t0 = f0 = f1 = 0;
+  t1 = (w.n + BN - 1) / BN;
+  if (hi > 0) {
+    f0 = lo <= a.sinks ? 0 : (lo + BN - 1) / BN;
+    f1 = hi / BN;
   }
-  const int u0 = imax(lo0 - B, 0), u1 = hi1 - B;
+}
+// This lane's part of it: its window at [lo, lo + w) (positions as if the walk were
+// the sequence), and the end of its sinks.
+__device__ inline void lane_walk(const SinkView& a, const SinkWalk& w, int pq, int& lo, int& wid, int& sinks) {
+  const int pos0 = a.kr[0].pos0;
+  int l, h;
+  key_interval(kClean, pq, kClean, a.rule, l, h);
+  l = imax(l - pos0, 0) - w.gap;
+  h = imin(h - pos0, a.kr[0].len);
+  h = h <= w.gap_at ? h : imax(h - w.gap, w.gap_at);
+  lo = pos0 + l;
+  wid = imax(h - l, 0);
+  sinks = imin(a.sinks, h);
+}
+
+// With sinks, fp32: the sinks, and the window's tiles among the other keys.
+__device__ inline void key_tile_span(const SinkViewF32& a, int j, int, int pq0, int pq1, int BN, int& t0, int& t1, int& f0,
+                                     int& f1) {
+  const int pos0 = a.kr[0].pos0, n = a.kr[0].ntiles, S = a.sinks;
+  int lo0, hi0, lo1, hi1;
+  key_interval(kClean, pq0, kClean, a.rule, lo0, hi0);
+  key_interval(kClean, pq1, kClean, a.rule, lo1, hi1);
+  // (the window's ends from key S on; of the sinks a row sees those before its end)
+  const int u0 = j == 0 ? 0 : imax(lo0 - pos0 - S, 0), i0 = j == 0 ? 0 : imax(lo1 - pos0 - S, 0);
+  const int u1 = j == 0 ? imin(hi1 - pos0, S) : imin(hi1 - pos0, n) - S;
+  const int i1 = j == 0 ? imin(hi0 - pos0, S) : imin(hi0 - pos0, n) - S;
+  t0 = t1 = f0 = f1 = 0;
   if (u1 <= u0) return;
   t0 = u0 / BN;
   t1 = (u1 + BN - 1) / BN;
-  const int i0 = imax(lo1 - B, 0), i1 = hi0 - B;
   if (i1 > i0) {
     f0 = (i0 + BN - 1) / BN;
     f1 = i1 / BN;
   }
-  const int at = t0 - first;  // (of the walk's tile n, in this range: t = at + n)
-  t1 = a.n1 >= t1 - at ? t1 : at + a.n1;
-  t0 = imax(t0, at + a.n0);
 }
 
 // First key tile at or after key range jj that the query tile can see.
@@ -171,15 +187,6 @@ __device__ inline void seen_keys(const PackedView& a, int pq0, int pq1, int& u0,
   u1 = imin(hi1 - kr.pos0, kr.len);
 }
 
-// With sinks: the keys [0, S) and [u0, u1).
-__device__ inline void seen_keys(const SinkView& a, int pq0, int pq1, int& u0, int& u1) {
-  int lo0, hi0, lo1, hi1;
-  key_interval(kClean, pq0, kClean, rule_of(a), lo0, hi0);
-  key_interval(kClean, pq1, kClean, rule_of(a), lo1, hi1);
-  u0 = imax(lo0 - a.kr[0].pos0, 0);
-  u1 = imin(hi1 - a.kr[0].pos0, a.kr[0].ntiles);
-}
-
 // Key tiles of all ranges that the query tile can see.
 template <class A>
 __device__ inline int count_key_tiles(const A& a, int qs, int pq0, int pq1, int BN) {
@@ -204,30 +211,12 @@ __device__ inline void lane_key_interval(const A& a, int j, int qs, int pq, int&
   w = imax(h - l, 0);
 }
 
-// With sinks: of its window; in a first range of sinks alone, of the sinks.  Its
-// sinks there (of any first range), and the end of its keys in the sequence.
-__device__ inline void lane_key_interval(const SinkView& a, int j, int qs, int pq, int& lo, int& w) {
-  const int pos0 = a.kr[0].pos0, n = a.kr[0].ntiles;
+__device__ inline void lane_key_interval(const SinkViewF32& a, int j, int, int pq, int& lo, int& w) {
+  const int pos0 = a.kr[0].pos0;
   int l, h;
-  key_interval(qs, pq, kClean, rule_of(a), l, h);
-  l = imax(l, pos0);
-  h = imin(h, pos0 + n);
-  if (j == 0) {
-    if (a.split == a.sinks) l = pos0;
-    h = imin(h, pos0 + a.split);
-  } else {
-    l = imax(l, pos0 + a.split);
-  }
-  lo = l;
-  w = imax(h - l, 0);
-}
-template <class A>
-__device__ inline void lane_sinks(const A&, int, int, int, int&, int&) {}
-__device__ inline void lane_sinks(const SinkView& a, int j, int qs, int pq, int& sinks, int& end) {
-  int l, h;
-  key_interval(qs, pq, kClean, rule_of(a), l, h);
-  end = imin(h - a.kr[0].pos0, a.kr[0].ntiles);
-  sinks = j == 0 ? imin(end, a.sinks) : 0;
+  key_interval(kClean, pq, kClean, a.rule, l, h);
+  lo = j == 0 ? pos0 : imax(l, pos0 + a.sinks);
+  w = imax(imin(h, pos0 + (j == 0 ? a.sinks : a.kr[0].ntiles)) - lo, 0);
 }
 
 }  // namespace bdlm

@@ -73,14 +73,13 @@ def test_items(dtype, ql, kl, block, window, sinks, H, KV, D):
             assert cs[0][0] == 0 and cs[-1][1] == BIG and all(a[1] == b[0] for a, b in zip(cs, cs[1:]))
             if len(cs) > 1:
                 assert sums[(key[0], key[4])] == (cs[0][2], len(cs)) and [c[2] for c in cs] == list(range(cs[0][2], cs[0][2] + len(cs)))
-                # no chunk is empty: the walk has the first range's tiles and the window's
+                # no chunk is empty: the walk has the sinks and the window, without the gap between in multiples of 16
                 i, t = which[key[0]], key[4]
-                rows = vis[i][t * qt:(t + 1) * qt]
-                split = min((sinks + 63) // 64 * 64, kl[i])
-                keys = torch.nonzero(rows.any(0)).flatten().tolist()
-                near = span([j for j in keys if j < split], lambda j: j // 64)
-                far = span([j for j in keys if j >= split], lambda j: (j - split) // 64)
-                assert cs[-1][0] < near[1] + far[1] - far[0]
+                keys = torch.nonzero(vis[i][t * qt:(t + 1) * qt].any(0)).flatten().tolist()
+                first = min(j for j in keys if j >= min(sinks, kl[i])) // 16 * 16
+                below = (min(sinks, kl[i]) + 15) // 16 * 16
+                walk = below + keys[-1] + 1 - first if first > below else keys[-1] + 1
+                assert cs[-1][0] < -(-walk // 64)
     # key tiles: the sinks' and the others'
     want_k = sorted((q0[i], ql[i], k0[i], m, t) for i, m in enumerate(kl) for s in [min(sinks, m)]
                     for t in [-1 - t for t in range(-(-s // kt))] + list(range(-(-(m - s) // kt))))
