@@ -16,9 +16,10 @@ constexpr int64_t kMaxRows = (int64_t)1 << 28;
 constexpr int64_t kMaxStride = (int64_t)1 << 30;
 constexpr double kMinEps = 0x1p-100;    // (a sum with it must be an fp32 number, and not 0)
 constexpr int64_t kWaves = 4;           // of a workgroup
-constexpr int64_t kFullWaves = 4096;    // waves from which on a row's heads stay with one wave
+constexpr int64_t kFullWaves = 2048;    // waves from which on a row's heads stay with one wave
+constexpr double kApart = 1.3;          // what a pass over heads of several rows takes longer
 constexpr int64_t kMaxFwdWgs = 1 << 20;
-constexpr int64_t kMaxBwdWgs = 1024;    // (each leaves its sums of the weights' gradients)
+constexpr int64_t kMaxBwdWgs = 512;     // (each leaves its sums of the weights' gradients)
 
 bdlm_status check_rotary(const bdlm_rotary* r, int32_t dtype, int64_t rows, const int32_t* pos, int32_t heads,
                          int32_t kv_heads, double eps) {
@@ -60,12 +61,21 @@ bdlm_status check_weight(const void* w, const char* what, double eps) {
   return BDLM_OK;
 }
 
-// Rows of a wave, and waves that share a row's heads.
+// Rows of a wave, and waves that share a row's heads.  Where one row's heads fill a
+// wave, one row at a time: its loads then are of one run of memory (30,011 rows of 32/8
+// heads, d 128, with 8 rows a wave 141 us, with one 117; 16,384 66 and 59).  Few heads, or a row whose
+// passes would be few beside its angles, take several (8,190 rows of 16/16 heads, d 64:
+// 16 rows a wave 19 us, one 22, backward 32 and 43; 2,000 of 12/2, d 128: 9.3 and 11.5).
+// More waves than 2,048 for the same rows cost more in angles than they hide (4,000 rows
+// of 32/8 heads, d 64, backward: 2,048 33 us, 4,096 35, 8,192 39).  Backward: up to 512 workgroups, two per
+// CU, go through the rows (1,024: 16,384 rows 119 us, 8,190 39, 512: 114, 33).
 void deal(const bdlm_rotary& r, int64_t rows, int32_t heads, int32_t kv_heads, int64_t max_wgs, RotateArgs& a) {
   const int side = 64 / (r.head_dim / 16);  // heads of a wave
   auto passes = [&](int64_t h, int per) { return (h + side / per - 1) / (side / per); };
-  // passes per row, of which one for the cosines and sines
-  auto cost = [&](int per) { return (double)(passes(heads, per) + passes(kv_heads, per) + 1) / per; };
+  // passes per row, of which one for the cosines and sines; heads of one row lie side by side, those of several do not
+  auto cost = [&](int per) {
+    return (double)(passes(heads, per) + passes(kv_heads, per) + 1) / per * (per > 1 ? kApart : 1.0);
+  };
   int best = 1;
   for (int per = 2; per <= side; per *= 2)
     if (cost(per) < cost(best)) best = per;
