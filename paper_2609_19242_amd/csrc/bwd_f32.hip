@@ -343,6 +343,8 @@ __global__ __launch_bounds__(256) void bwd_sum_f32_kernel(const Args a) {
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     double x[EPT] = {};
+    // (four chunks' loads in flight, added in their order)
+#pragma unroll 4
     for (int ch = 0; ch < st.n; ++ch) {
       const double* src = (const double*)partials_of(a) + partial_row(a, st, ch) * (2 * D) + (which * st.nk + k) * D + d0;
 #pragma unroll
