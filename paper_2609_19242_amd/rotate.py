@@ -100,7 +100,7 @@ class _Call:
     def __init__(self, dtype, device, gpu, head_dim):
         self.code = _dtype_code(dtype)
         self.dtype, self.device, self.gpu, self.head_dim = dtype, device, gpu, head_dim
-        self._streams = set()
+        self._streams, self.workspace_bytes = set(), None
 
 
 def _call(rot, q):
@@ -116,15 +116,12 @@ def _call(rot, q):
     return c
 
 
-def _weight(c, name, w, eps):
-    if w is None:
-        return None
-    if eps is None:
-        raise ValueError(f"{name} needs a norm (eps)")
-    _expect(name, w, c.dtype, (c.head_dim,))
-    if w.get_device() != c.gpu:
-        raise ValueError(f"{name} must be on {c.device}, got {w.device}")
-    return w.data_ptr()
+def _at(c, name, t, dtype, shape):
+    """The address of a contiguous tensor of the call."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.shape == shape and t.is_contiguous() and t.get_device() == c.gpu:
+        return t.data_ptr()
+    _expect(name, t, dtype, shape)
+    raise ValueError(f"{name} must be on {c.device}, got {t.device}")
 
 
 def _inputs(rot, q, k, positions, q_weight, k_weight, eps):
@@ -135,19 +132,23 @@ def _inputs(rot, q, k, positions, q_weight, k_weight, eps):
         raise ValueError(f"k must be a [rows][kv_heads][{rot.head_dim}] tensor")
     KV = k.shape[1]
     rq, rk = _rows(c, "q", q, H, n), _as_long(c, "k", k, KV, n)
-    if eps is not None and not 2.0 ** -100 <= eps <= 2.0 ** 100:
-        raise ValueError(f"eps must be within [2^-100, 2^100], or None for no norm, got {eps}")
     if not isinstance(positions, torch.Tensor) or positions.dim() not in (1, 2):
         raise ValueError("positions must be a [rows] or [axes][rows] tensor")
-    _expect("positions", positions, torch.int32, (n,) if positions.dim() == 1 and rot.axes == 1 else (rot.axes, n))
-    if positions.get_device() != c.gpu:
-        raise ValueError(f"positions must be on {c.device}, got {positions.device}")
-    w = _weight(c, "q_weight", q_weight, eps), _weight(c, "k_weight", k_weight, eps)
-    return c, n, H, KV, (rot._ref, c.code, n, positions.data_ptr(), H, KV, rq, rk, *w, 0.0 if eps is None else float(eps))
+    at = _at(c, "positions", positions, torch.int32, (n,) if rot.axes == 1 and positions.dim() == 1 else (rot.axes, n))
+    if eps is None:
+        if q_weight is not None or k_weight is not None:
+            raise ValueError("a weight needs a norm (eps)")
+        return c, n, H, KV, (rot._ref, c.code, n, at, H, KV, rq, rk, None, None, 0.0)
+    if not 2.0 ** -100 <= eps <= 2.0 ** 100:
+        raise ValueError(f"eps must be within [2^-100, 2^100], or None for no norm, got {eps}")
+    one = (c.head_dim,)
+    return c, n, H, KV, (rot._ref, c.code, n, at, H, KV, rq, rk,
+                         None if q_weight is None else _at(c, "q_weight", q_weight, c.dtype, one),
+                         None if k_weight is None else _at(c, "k_weight", k_weight, c.dtype, one), eps)
 
 
 def _new_rows(q, k):
-    return q.new_empty(q.shape), k.new_empty(k.shape)
+    return torch.empty_like(q, memory_format=torch.contiguous_format), torch.empty_like(k, memory_format=torch.contiguous_format)
 
 
 def _out_rows(c, out, names, q, k, stream):
@@ -174,7 +175,7 @@ def qk_rotate_fwd(rot: Rotary, q, k, positions, q_weight=None, k_weight=None, ep
 
 
 def _new_weight_grads(c, q_weight, k_weight):
-    return [torch.empty(c.head_dim, dtype=torch.float32, device=c.device) for w in (q_weight, k_weight) if w is not None]
+    return [w.new_empty(w.shape, dtype=torch.float32) for w in (q_weight, k_weight) if w is not None]
 
 
 def qk_rotate_bwd(rot: Rotary, q, k, positions, dq_out, dk_out, q_weight=None, k_weight=None,
@@ -187,12 +188,15 @@ def qk_rotate_bwd(rot: Rotary, q, k, positions, dq_out, dk_out, q_weight=None, k
     c, n, H, KV, args = _inputs(rot, q, k, positions, q_weight, k_weight, eps)
     rdq, rdk = _as_long(c, "dq_out", dq_out, H, n), _as_long(c, "dk_out", dk_out, KV, n)
     out, rows = _out_rows(c, out, ("dq", "dk"), q, k, stream)
-    weights, at, nbytes = [], 0, 0
+    dqw = dkw = at = None
+    nbytes = 0
     if q_weight is not None or k_weight is not None:
-        weights = list(_made(stream, c.device, _new_weight_grads, c, q_weight, k_weight))
-        workspace = _workspace(workspace, lib().bdlm_qk_rotate_workspace_bytes(c.head_dim), c.device, stream)
+        new = iter(_made(stream, c.device, _new_weight_grads, c, q_weight, k_weight))
+        dqw, dkw = (next(new) if w is not None else None for w in (q_weight, k_weight))
+        if c.workspace_bytes is None:
+            c.workspace_bytes = lib().bdlm_qk_rotate_workspace_bytes(c.head_dim)
+        workspace = _workspace(workspace, c.workspace_bytes, c.device, stream)
         at, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    dw = [weights.pop(0) if w is not None else None for w in (q_weight, k_weight)]
-    _launch(c, stream, lib().bdlm_qk_rotate_bwd, *args, rdq, rdk, *rows,
-            *(x.data_ptr() if x is not None else None for x in dw), at, nbytes)
-    return (*out, *dw)
+    _launch(c, stream, lib().bdlm_qk_rotate_bwd, *args, rdq, rdk, *rows, None if dqw is None else dqw.data_ptr(),
+            None if dkw is None else dkw.data_ptr(), at, nbytes)
+    return (*out, dqw, dkw)

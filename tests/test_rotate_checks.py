@@ -193,7 +193,7 @@ def test_new_outputs_of_a_given_stream(monkeypatch):
         yield
         at.pop()
 
-    for owner, name in ((torch, "empty"), (torch.Tensor, "new_empty")):
+    for owner, name in ((torch, "empty"), (torch, "empty_like"), (torch.Tensor, "new_empty")):
         plain = getattr(owner, name)
         monkeypatch.setattr(owner, name, lambda *a, plain=plain, **kw: new.append((plain(*a, **kw), at[-1])) or new[-1][0])
     monkeypatch.setattr(torch.Tensor, "record_stream", lambda t, s: kept.append((t, s)))
