@@ -26,7 +26,7 @@ namespace bdlm {
 // Words of a plan in device memory: a header, the requests' first rows, their first
 // tiles (with the total behind), the items, the merge's units.
 constexpr int kChunkHead = 16;
-enum : int { kPlanItems = 0, kPlanJoins = 1, kPlanRows = 2, kPlanRoom = 3 };  // of the header (room: for items)
+enum : int { kPlanItems = 0, kPlanJoins = 1, kPlanRows = 2, kPlanRoom = 3 };  // of the header (room: for items, in front of the units)
 
 struct ChunkItemRec {
   int32_t seq, token0, pos0, len;  // (-1: none) the request's first row, its position, the sequence's tokens
@@ -49,8 +49,7 @@ struct ChunkPlanArgs {
   int32_t* plan;
   int64_t top;  // tokens that a table holds
   int32_t requests, rows, seqs_in_cache, group, kv_heads, M, window, sinks;
-  int32_t tile, f32;             // rows of a request's tiles where there are many; fp32
-  int32_t limit, least, slots;   // keys of a chunk at most, at least; workgroups that run at once
+  int32_t f32, limit, least, slots;   // keys of a chunk at most, at least; workgroups that run at once
   int32_t join_rows, max_items, max_joins;
   int64_t max_part_rows;
 };
@@ -68,6 +67,8 @@ struct ChunkArgs {
   int64_t qs, os, pitch;  // elements between rows; rows of the LSE
   int64_t part_rows;      // partial rows of a KV head
   int32_t pages, page_size, max_pages;
+  uint32_t page_mul;      // for page_of
+  int32_t page_shift;
   int32_t heads, kv_heads, group, M, window, sinks;
   int32_t rows, fill;     // rows behind the last request's become 0 (LSE -inf)
   int32_t max_items, max_joins;
@@ -156,6 +157,13 @@ __device__ inline int64_t part_row(const PrefixArgs& a, const PrefixItem& it, co
 }
 __device__ inline int64_t part_row(const ChunkArgs& a, const ChunkItem& it, const PrefixRow&, int row) {
   return it.kvh * a.part_rows + it.part + row;
+}
+
+// key / page_size.  Chunks: (key page_mul >> 32) >> page_shift, with page_mul = 1 + floor(2^(32 + page_shift) /
+// page_size), 2^page_shift < page_size <= 2^(page_shift + 1), which is that for key < 2^31 (page_size 1: page_mul 0).
+__device__ inline int page_of(const PrefixArgs& a, int key) { return key / a.page_size; }
+__device__ inline int page_of(const ChunkArgs& a, int key) {
+  return a.page_mul ? (int)(__umulhi((uint32_t)key, a.page_mul) >> a.page_shift) : key;
 }
 
 // Key v of the walk.

@@ -182,6 +182,10 @@ bdlm_status bdlm_chunk_attn(const bdlm_cache* c, const bdlm_chunk* p, int64_t la
   a.pages = ca.pages;
   a.page_size = ca.page_size;
   a.max_pages = ca.max_pages;
+  if (ca.page_size > 1) {
+    while (((int64_t)2 << a.page_shift) < ca.page_size) ++a.page_shift;
+    a.page_mul = (uint32_t)(((uint64_t)1 << (32 + a.page_shift)) / (uint64_t)ca.page_size + 1);
+  }
   a.heads = p->heads;
   a.kv_heads = c->kv_heads;
   a.group = p->heads / c->kv_heads;

@@ -24,11 +24,17 @@
 // rows past the chunk or in no page, which come from a row of zeros, take an
 // address per lane.
 //
+// The same kernels run chunks of new tokens (ChunkArgs in chunk.hpp).  Their tiles start
+// at multiples of 16 keys, so with pages of a multiple of 4 tokens (head_dim 64: 8) the rows of a copy
+// share a page too: its base comes from the lane that has its first row's offset (2,048 rows behind
+// 28,000 tokens, pages of 24: 1,131 -> 1,006 us, of 16 985, of 7, an address per lane, 1,153).
+//
 // Measured, 32 query heads: 64 requests of 4,000 keys each, 8 KV heads, 196 us
 // (5.3 TB/s, a copy's rate); 64 of 60 to 1,500 behind 8K, read again, 38 us.  Blocks
 // of 32 rows of 16 requests behind 16K, 4 KV heads, 156 us (0.9 PFLOP/s): operand
 // reads take LDS as long as the products take the matrix cores, and copies a quarter
-// more (without them 138 us; without the exponentials 145).
+// more (without them 138 us; without the exponentials 145).  Chunks: 64 single tokens of requests
+// of 8,000, 8 KV heads, 360 us (5.8 TB/s); 4,096 rows behind 28,000 tokens 1.95 ms (1.03 PFLOP/s).
 #include "chunk.hpp"
 #include "device.hpp"
 
@@ -54,6 +60,9 @@ __device__ __forceinline__ void dma16(const char* base, uint32_t voff, uint32_t 
 }
 // (a base from readlane, a vector instruction writing scalar registers, needs five wait states before a copy reads it)
 __device__ __forceinline__ void base_ready(const char* a, const char* b) { asm volatile("s_nop 4" ::"s"(a), "s"(b)); }
+__device__ __forceinline__ void base_ready(const char* a, const char* b, const char* c, const char* d) {
+  asm volatile("s_nop 4" ::"s"(a), "s"(b), "s"(c), "s"(d));
+}
 __device__ __forceinline__ void lds_done() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void vm_wait() {
@@ -205,7 +214,7 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
       const int64_t g = groups[(key - start) >> 4];
       return g < 0 ? -1 : g + (key & 15) * row_bytes;
     } else {
-      const int kk = walk_key(it, key), e = kk / a.page_size;
+      const int kk = walk_key(it, key), e = page_of(a, kk);
       int at = e - page0;
       if constexpr (kIsChunk<Args>) at = key < it.gap_at ? e - wp.p0 : wp.n0 + (e - wp.p1);
       const int p = pages[at];
@@ -218,18 +227,37 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
 #pragma unroll
   for (int i = 0; i < GI; ++i) {
     const int r = i * RPI + lane / CH;
-    voff[i] = (uint32_t)(r * (int)row_bytes) + (uint32_t)((lane % CH) ^ chunk_swz<D>(r)) * 16u;
+    voff[i] = (uint32_t)((GROUPS ? r : lane / CH) * (int)row_bytes) + (uint32_t)((lane % CH) ^ chunk_swz<D>(r)) * 16u;
   }
-  // Their two groups' offsets, read ahead of the copies (any value where there is no such pair of groups).
+  // Their two groups' offsets, read ahead of the copies (any value where there is no such pair of groups);
+  // chunks, other pages: the offset of this lane's row of the 32.
   struct Pair {
     int64_t g0, g1;
   };
   auto pair_at = [&](int first) __attribute__((always_inline)) -> Pair {
-    if constexpr (!GROUPS) return Pair{-1, -1};
+    if constexpr (!GROUPS) return Pair{kIsChunk<Args> ? key_offset(first + l32) : -1, -1};
     const int e = imin((first - start) >> 4, kPrefixGroups - 2);
     return Pair{groups[e], groups[e + 1]};
   };
+  auto from_lane = [](int64_t x, int from) __attribute__((always_inline)) {
+    return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(x >> 32), from) << 32 |
+                     (uint32_t)__builtin_amdgcn_readlane((int)x, from));
+  };
   auto copy32 = [&](const char* base, int first, const Pair& ahead, uint32_t dst) __attribute__((always_inline)) {
+    if constexpr (kIsChunk<Args> && !GROUPS) {
+      // (tiles start at multiples of 16 keys: a copy's rows lie in one page)
+      if (a.page_size % RPI == 0 && __builtin_amdgcn_ballot_w64(ahead.g0 < 0) == 0) {
+        const char* b[NI];
+#pragma unroll
+        for (int i = 0; i < NI; ++i) b[i] = base + from_lane(ahead.g0, i * RPI);
+        lds_done();
+#pragma unroll
+        for (int i = 0; i < NI; i += 4) base_ready(b[i], b[i + 1], b[i + 2], b[i + 3]);
+#pragma unroll
+        for (int i = 0; i < NI; ++i) dma16(b[i], voff[i % GI], dst + i * 1024);
+        return;
+      }
+    }
     if constexpr (GROUPS) {
       bool whole = first + 32 <= it.k1;
       if constexpr (kIsChunk<Args>) whole = whole && (first >= it.w0 || first + 32 <= a.sinks);
@@ -249,7 +277,8 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
         }
       }
     }
-    const int64_t mine = key_offset(first + l32);
+    int64_t mine = ahead.g0;
+    if constexpr (!kIsChunk<Args> || GROUPS) mine = key_offset(first + l32);
     lds_done();
 #pragma unroll
     for (int i = 0; i < NI; ++i) {

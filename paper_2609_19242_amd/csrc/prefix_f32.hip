@@ -72,7 +72,7 @@ __global__ __launch_bounds__(kWaves * 64) __attribute__((amdgpu_waves_per_eu(2, 
     if constexpr (kIsChunk<Args>) {
       if (key >= a.sinks && key < it.w0) return -1;
     }
-    const int kk = walk_key(it, key), e = kk / a.page_size;
+    const int kk = walk_key(it, key), e = page_of(a, kk);
     int at = e - page0;
     if constexpr (kIsChunk<Args>) at = key < it.gap_at ? e - wp.p0 : wp.n0 + (e - wp.p1);
     const int p = pages[at];
