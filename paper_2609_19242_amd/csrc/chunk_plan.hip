@@ -3,7 +3,11 @@
 //
 // One workgroup: a scan of the requests' rows and tiles, the walks' lengths, the
 // unit, then the items.  Walks longer than the unit are cut into equal chunks; the
-// longer half of the items comes first.  The numbers do not depend on timing.
+// longer half of the items comes first, and each half from behind, since a prompt's later
+// tiles have longer walks (a prompt of 8,000 tokens, 32/8 heads: 547 -> 514 us, 48 decoding
+// requests with 3 pieces of prompts 186 -> 156).  The numbers do not depend on timing.
+// Bound by latency: the chain count, sequence, length, then three passes over the tiles,
+// 9 us for 5 requests, 14 for 200.
 //
 // The unit.  Half of a workgroup's share of all walks to twice as much, in 32 steps:
 // the one with the least cost in keys, which is the longer of (rounds of longer items
@@ -179,10 +183,10 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
     return walk_of(a, q, g - q.tile0);
   };
 
-  // 0: what all walks come to, and the longest; 1 (more tiles than threads): items of the
-  // longer half of the walks; 2: the items, those first.
+  // 0: what all walks come to, and the longest; 1 (more tiles than threads): items, and those
+  // of the longer half of the walks; 2: the items, those first.
   int unit = 0, half = 0;
-  int64_t longer = 0, placed = 0, parts = 0;  // (longer items << 32 | others; cut tiles << 32 | their partial rows)
+  int64_t all_items = 0, placed = 0, parts = 0;  // (longer items << 32 | others; cut tiles << 32 | their partial rows)
   Request q{};
   Walk w{};
 #pragma unroll 1
@@ -212,18 +216,20 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
       int64_t x = is_longer ? (int64_t)n << 32 : n, y = n > 1 ? (int64_t)units << 32 | n * w.nrows : 0, all_x, all_y;
       block_scan(x, y, all_x, all_y, wsum);
       if (pass == 1) {
-        longer += all_x >> 32;
+        all_items += all_x;
         continue;
       }
-      if (T <= kT) longer = all_x >> 32;
+      if (T <= kT) all_items = all_x;
       x += placed;
       y += parts;
       placed += all_x;
       parts += all_y;
-      const int i0 = is_longer ? (int)(x >> 32) : (int)(longer + (x & 0xffffffff)), j = (int)(y >> 32);
+      // (from behind: a prompt's later tiles are longer)
+      const int longer = (int)(all_items >> 32), others = (int)(all_items & 0xffffffff), j = (int)(y >> 32);
+      const int i0 = (is_longer ? longer - (int)(x >> 32) : longer + others - (int)(x & 0xffffffff)) - n;
       const int64_t part = y & 0xffffffff;
       // (never: the host made room)
-      if (i0 + (int64_t)n > a.max_items || (n > 1 && (j + units > a.max_joins || part + (int64_t)n * w.nrows > a.max_part_rows))) continue;
+      if (i0 < 0 || i0 + (int64_t)n > a.max_items || (n > 1 && (j + units > a.max_joins || part + (int64_t)n * w.nrows > a.max_part_rows))) continue;
       ChunkItemRec rec{q.seq, q.token0, q.pos0, q.len, w.row0, w.nrows, 0, 0, w.gap_at, w.gap, w.w0, 0};
       const int flag = w.shared ? kSharedTile : 0;
 #pragma unroll 1
