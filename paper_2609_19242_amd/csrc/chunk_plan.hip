@@ -7,7 +7,7 @@
 // tiles have longer walks (a prompt of 8,000 tokens, 32/8 heads: 547 -> 514 us, 48 decoding
 // requests with 3 pieces of prompts 186 -> 156).  The numbers do not depend on timing.
 // Bound by latency: the chain count, sequence, length, then three passes over the tiles,
-// 9 us for 5 requests, 14 for 200.
+// 7 us for 5 requests, 9 for 200.
 //
 // The unit.  Half of a workgroup's share of all walks to twice as much, in 32 steps:
 // the one with the least cost in keys, which is the longer of (rounds of longer items
@@ -33,30 +33,42 @@ constexpr int kUnits = 32;
 constexpr float kStartKeys = 64.f;  // a workgroup's start-up
 constexpr float kPartRows = 176.f;  // partial rows that take as long as a key of a slot
 
-// Exclusive prefix sums of x and y over the workgroup's threads; totals of all.
-__device__ __forceinline__ void block_scan(int64_t& x, int64_t& y, int64_t& all_x, int64_t& all_y, int64_t (*wsum)[2]) {
-  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  int64_t u = x, v = y;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const int64_t a = __shfl_up(u, s), b = __shfl_up(v, s);
-    if (lane >= s) u += a, v += b;
-  }
-  __syncthreads();  // (the sums of a scan before are read)
-  if (lane == 63) wsum[w][0] = u, wsum[w][1] = v;
+// A value from a lane before this one, 0 where there is none (row_shr by 1 to 8 within
+// 16 lanes; the last lane of a row of 16, of 32, to those behind): no way through LDS.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int before(int x) { return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t before(int64_t x) {
+  return (int64_t)((uint64_t)(uint32_t)before<CTRL, ROWS>((int)(x >> 32)) << 32 | (uint32_t)before<CTRL, ROWS>((int)x));
+}
+// x of this lane and those before it, joined (0 is neutral); lane 63 has the wave's.
+template <class T, class F>
+__device__ __forceinline__ T wave_scan(T x, F&& join) {
+  x = join(x, before<0x111, 0xf>(x));
+  x = join(x, before<0x112, 0xf>(x));
+  x = join(x, before<0x114, 0xf>(x));
+  x = join(x, before<0x118, 0xf>(x));
+  x = join(x, before<0x142, 0xa>(x));
+  return join(x, before<0x143, 0xc>(x));
+}
+template <class T>
+__device__ __forceinline__ T add(T a, T b) { return a + b; }
+// Exclusive prefix sums over the workgroup's threads, and the total.  (Between two with the same wsum lies a barrier.)
+template <class T>
+__device__ __forceinline__ T block_scan(T x, T& all, int64_t* wsum) {
+  const int w = threadIdx.x >> 6;
+  const T up_to = wave_scan(x, add<T>);
+  if ((threadIdx.x & 63) == 63) wsum[w] = up_to;
   __syncthreads();
-  all_x = all_y = 0;
-  u -= x;
-  v -= y;
+  T first = 0;
+  all = 0;
 #pragma unroll
   for (int k = 0; k < kT / 64; ++k) {
-    const int64_t a = wsum[k][0], b = wsum[k][1];
-    if (k < w) u += a, v += b;
-    all_x += a;
-    all_y += b;
+    const T a = (T)wsum[k];
+    if (k < w) first += a;
+    all += a;
   }
-  x = u;
-  y = v;
+  return first + up_to - x;
 }
 
 __device__ __forceinline__ int tile_rows(const ChunkPlanArgs& a, int per) {
@@ -116,7 +128,7 @@ __device__ __forceinline__ Walk walk_of(const ChunkPlanArgs& a, const Request& q
 
 __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
   __shared__ int req[6][kLdsRequests];
-  __shared__ int64_t wsum[kT / 64][2];
+  __shared__ int64_t wsum[2][kT / 64];
   __shared__ int tile_n[kLdsTiles], tile_nrows[kLdsTiles];
   __shared__ unsigned long long total_lds;
   __shared__ int longest_lds;
@@ -130,21 +142,21 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
   if (tid == 0) longest_lds = 0, total_lds = 0;
 
   // the requests' rows and tiles
-  int64_t rows = 0, tiles = 0;
+  int64_t rows = 0;
+  int tiles = 0;
 #pragma unroll 1
   for (int r0 = 0; r0 < a.requests; r0 += kT) {
     const int r = r0 + tid;
     Request q;
     int count = 0;
     if (r < a.requests) load_request(a, r, q, count);
-    int64_t start = count, none = 0, all, all_tiles;
-    block_scan(start, none, all, all_tiles, wsum);
+    int64_t all;
+    const int64_t start = block_scan((int64_t)count, all, wsum[0]);
     place_request(a, rows + start, count, q);
     rows += all;
     const int per = q.rows * a.group, tr = tile_rows(a, per);
-    int64_t at = (per + tr - 1) / tr;
-    block_scan(at, none, all_tiles, all, wsum);
-    q.tile0 = (int)(tiles + at);
+    int all_tiles;
+    q.tile0 = tiles + block_scan(over(per + tr - 1, tr), all_tiles, wsum[1]);
     tiles += all_tiles;
     if (r < a.requests) {
       starts[r] = q.token0;
@@ -159,9 +171,9 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
       }
     }
   }
-  if (tid == 0) tile0[a.requests] = (int)tiles;
+  if (tid == 0) tile0[a.requests] = tiles;
   __syncthreads();
-  const int T = (int)tiles;
+  const int T = tiles;
   const bool in_lds = a.requests <= kLdsRequests;
   // Tile g of all: its request is the last one whose first tile is not behind it.
   auto walk_at = [&](int g, Request& q) __attribute__((always_inline)) -> Walk {
@@ -186,6 +198,8 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
   // 0: what all walks come to, and the longest; 1 (more tiles than threads): items, and those
   // of the longer half of the walks; 2: the items, those first.
   int unit = 0, half = 0;
+  int64_t total = 0;
+  int longest = 0;
   int64_t all_items = 0, placed = 0, parts = 0;  // (longer items << 32 | others; cut tiles << 32 | their partial rows)
   Request q{};
   Walk w{};
@@ -198,8 +212,8 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
       if (g < T && (pass == 0 || T > kT)) w = walk_at(g, q);
       if (pass == 0) {
         if (g < T) {
-          atomicAdd(&total_lds, (unsigned long long)w.n);
-          atomicMax(&longest_lds, w.n);
+          total += w.n;
+          longest = imax(longest, w.n);
           if (T <= kLdsTiles) tile_n[g] = w.n, tile_nrows[g] = w.nrows;
         }
         continue;
@@ -213,15 +227,16 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
       const bool is_longer = imin(size, w.n) > half;
       // units of the merge: a row each where there are many parts
       const int join = n > kShortJoin ? 1 : a.join_rows, units = n > 1 ? (w.nrows + join - 1) / join : 0;
-      int64_t x = is_longer ? (int64_t)n << 32 : n, y = n > 1 ? (int64_t)units << 32 | n * w.nrows : 0, all_x, all_y;
-      block_scan(x, y, all_x, all_y, wsum);
+      int64_t all_x, all_y;
+      if (T > kT) __syncthreads();
+      int64_t x = block_scan(is_longer ? (int64_t)n << 32 : n, all_x, wsum[0]);
       if (pass == 1) {
         all_items += all_x;
         continue;
       }
       if (T <= kT) all_items = all_x;
+      const int64_t y = parts + block_scan(n > 1 ? (int64_t)units << 32 | n * w.nrows : (int64_t)0, all_y, wsum[1]);
       x += placed;
-      y += parts;
       placed += all_x;
       parts += all_y;
       // (from behind: a prompt's later tiles are longer)
@@ -244,23 +259,28 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
         joins[j + u] = ChunkJoin{q.token0, w.row0 + u * join, imin(join, w.nrows - u * join), (int)part + u * join, n, w.nrows, 0, 0};
     }
     if (pass == 0) {
+      const int64_t wave_total = wave_scan(total, add<int64_t>);
+      const int wave_longest = wave_scan(longest, [](int x, int y) { return imax(x, y); });
+      if ((tid & 63) == 63) {
+        atomicAdd(&total_lds, (unsigned long long)wave_total);
+        atomicMax(&longest_lds, wave_longest);
+      }
       __syncthreads();
-      const int64_t all = (int64_t)total_lds * a.kv_heads, least = (all + 2 * a.slots - 1) >> __builtin_ctz(2 * a.slots);
-      const float share = (float)all / (float)a.slots;
+      const int64_t all = (int64_t)total_lds * a.kv_heads, over_two = (all + 2 * a.slots - 1) >> __builtin_ctz(2 * a.slots);
+      const int least = imax(a.least, over_two < kBig ? (int)over_two : kBig), most = a.limit - 64;
+      const float per_slot = 1.f / (float)a.slots, share = (float)all * per_slot;
       auto unit_of = [&](int k) __attribute__((always_inline)) {
-        const float u = 0.5f * share * exp2f_fast((float)k * (2.f / (kUnits - 1)));
-        const int64_t v = u < 1e9f ? (int64_t)u : (int64_t)1 << 30, x = v < least ? least : v;
-        return (int)(x < a.least ? a.least : x > a.limit - 64 ? a.limit - 64 : x);
+        return imin(imax((int)fminf(0.5f * share * exp2f_fast((float)k * (2.f / (kUnits - 1))), 1e9f), least), most);
       };
       if (T > kLdsTiles) {
         unit = unit_of(kUnits / 2);
       } else {  // a unit per lane, tiles dealt to groups of kUnits lanes
         const int k = tid % kUnits, grp = tid / kUnits;
-        const float u = (float)unit_of(k), inv = 1.f / u;
+        const float u = (float)unit_of(k), inv = __builtin_amdgcn_rcpf(u);
         f32x4 x = {0.f, 0.f, 0.f, 0.f};  // longer items, their keys, items, partial rows
 #pragma unroll 2
         for (int g = grp; g < T; g += kT / kUnits) {
-          const float n = (float)tile_n[g], cut = fmaxf(ceilf(n * inv), 1.f);
+          const float n = (float)tile_n[g], cut = fmaxf(ceilf(fmaf(n, inv, -1e-4f)), 1.f);
           const bool is_longer = 2.f * n > u * cut;
           x += f32x4{is_longer ? cut : 0.f, is_longer ? n : 0.f, cut, cut > 1.f ? cut * (float)tile_nrows[g] : 0.f};
         }
@@ -269,9 +289,9 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
         if (tid < kUnits) {
 #pragma unroll
           for (int j = 1; j < kT / kUnits; ++j) x += sums[j][k];
-          const float kvh = (float)a.kv_heads, slots = (float)a.slots;
-          const float rounds = x[0] > 0.f ? ceilf(x[0] * kvh / slots) * x[1] / x[0] : 0.f;
-          float cost = fmaxf(rounds, share) + x[2] * kvh / slots * kStartKeys + x[3] * kvh / kPartRows;
+          const float kvh = (float)a.kv_heads, kvh_slot = kvh * per_slot;
+          const float rounds = x[0] > 0.f ? ceilf(x[0] * kvh_slot) * x[1] * __builtin_amdgcn_rcpf(x[0]) : 0.f;
+          float cost = fmaxf(rounds, share) + x[2] * kvh_slot * kStartKeys + x[3] * kvh * (1.f / kPartRows);
           int best = k;
 #pragma unroll
           for (int m = kUnits / 2; m > 0; m >>= 1) {  // the longest of the best
