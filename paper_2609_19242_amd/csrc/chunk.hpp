@@ -36,6 +36,7 @@ struct ChunkItemRec {
   int32_t part;                    // first row of its partial outputs, -1: it writes the outputs; bit 30: a tile of 128
 };
 constexpr int32_t kSharedTile = 1 << 30;
+constexpr int kChunkGroups = kPrefixTableEntries;  // bf16, pages of whole groups of 16 tokens: groups of a chunk at most
 constexpr int kFillWgs = 32;  // workgroups beside the items', for rows of no request
 // Rows of a cut tile whose parts a workgroup of the merge joins: `nrows` rows from
 // row0 on, their first parts from partial row `part` on, n parts `step` rows apart.
@@ -86,6 +87,8 @@ struct ChunkItem : PrefixItem {
 };
 template <class A> struct ItemOf { typedef PrefixItem type; };
 template <> struct ItemOf<ChunkArgs> { typedef ChunkItem type; };
+template <class A> struct GroupOf { typedef int64_t type; };
+template <> struct GroupOf<ChunkArgs> { typedef int32_t type; };
 template <class A> constexpr bool kIsChunk = false;
 template <> constexpr inline bool kIsChunk<ChunkArgs> = true;
 

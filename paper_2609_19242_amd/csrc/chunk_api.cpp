@@ -49,13 +49,16 @@ bdlm_status check_chunk(const bdlm_cache* c, const bdlm_chunk* p, Room& room) {
   if (p->reserved != 0) return fail(BDLM_ERR_INVALID, "reserved field must be 0");
   if (!std::isfinite(p->scale)) return fail(BDLM_ERR_INVALID, "scale is not finite");
   const bool f32 = c->dtype == BDLM_F32;
+  // (groups of 16 tokens are numbered in 31 bits)
+  if (c->page_size > ((int64_t)1 << 34) / std::max<int64_t>(c->pages, 1))
+    return fail(BDLM_ERR_UNSUPPORTED, "pages %lld x page_size %lld exceeds 2^34", (long long)c->pages, (long long)c->page_size);
   const int64_t group = p->heads / c->kv_heads, all = p->rows * group;  // query rows of a KV head
   const int64_t some = std::min(p->requests, p->rows);                  // requests with rows
   // tiles: of 16 rows; or of 32 in requests of up to 64, else of 128
   const int64_t tiles = f32 ? some + all / kPrefixRowsF32
                             : std::min(some + all / kPrefixWaveRows, 2 * some + all / kPrefixSharedRows);
   // keys whose pages (or groups) a workgroup can hold, in two runs
-  room.limit = (int32_t)std::min<int64_t>(!f32 && c->page_size % 16 == 0 ? (kPrefixGroups - 2) * 16
+  room.limit = (int32_t)std::min<int64_t>(!f32 && c->page_size % 16 == 0 ? (kChunkGroups - 2) * 16
                                                                          : (kPrefixTableEntries - 4) * c->page_size,
                                           (int64_t)1 << 29);
   const int64_t top = c->max_pages * c->page_size;

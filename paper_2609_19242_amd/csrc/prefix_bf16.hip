@@ -27,14 +27,16 @@
 // The same kernels run chunks of new tokens (ChunkArgs in chunk.hpp).  Their tiles start
 // at multiples of 16 keys, so with pages of a multiple of 4 tokens (head_dim 64: 8) the rows of a copy
 // share a page too: its base comes from the lane that has its first row's offset (2,048 rows behind
-// 28,000 tokens, pages of 24: 1,131 -> 1,006 us, of 16 985, of 7, an address per lane, 1,153).
+// 28,000 tokens, pages of 24: 1,131 -> 980 us, of 16 958, of 7, an address per lane, 1,195).  Groups are
+// held by number there, in 4 bytes: a workgroup holds 32,736 keys, so fewer walks are cut (the same rows,
+// pages of 16: 985 us and 19 of merge before).
 //
 // Measured, 32 query heads: 64 requests of 4,000 keys each, 8 KV heads, 196 us
 // (5.3 TB/s, a copy's rate); 64 of 60 to 1,500 behind 8K, read again, 38 us.  Blocks
 // of 32 rows of 16 requests behind 16K, 4 KV heads, 156 us (0.9 PFLOP/s): operand
 // reads take LDS as long as the products take the matrix cores, and copies a quarter
 // more (without them 138 us; without the exponentials 145).  Chunks: 64 single tokens of requests
-// of 8,000, 8 KV heads, 360 us (5.8 TB/s); 4,096 rows behind 28,000 tokens 1.95 ms (1.03 PFLOP/s).
+// of 8,000, 8 KV heads, 360 us (5.8 TB/s); 4,096 rows behind 28,000 tokens 1.90 ms (1.06 PFLOP/s).
 #include "chunk.hpp"
 #include "device.hpp"
 
@@ -148,7 +150,9 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   __shared__ __attribute__((aligned(1024))) unsigned char lds[L::Bytes];
   const uint32_t L0 = lds_addr(lds);
   int* const pages = (int*)(lds + L::Pages);
-  int64_t* const groups = (int64_t*)(lds + L::Pages);
+  // (chunks: the groups' numbers in the cache, half as long, so that a workgroup holds twice as many)
+  using Group = typename GroupOf<Args>::type;
+  Group* const groups = (Group*)(lds + L::Pages);
   float* const red_m = (float*)(lds + L::Ml);  // [wave][32], the sums behind it
   float* const red_l = red_m + kNW * 32;
 
@@ -182,7 +186,8 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
       if constexpr (kIsChunk<Args> && !GROUPS) pe = wp.page(e);
       const int p = table[pe];
       const bool ok = (unsigned)p < (unsigned)a.pages;
-      if constexpr (GROUPS) groups[e] = ok ? ((int64_t)p * a.page_size + (key - pe * a.page_size)) * row_bytes : -1;
+      const int64_t at = (int64_t)p * a.page_size + (key - pe * a.page_size);
+      if constexpr (GROUPS) groups[e] = ok ? (Group)(kIsChunk<Args> ? at >> 4 : at * row_bytes) : -1;
       else pages[e] = ok ? p : -1;
     }
   }
@@ -212,7 +217,7 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
     }
     if constexpr (GROUPS) {
       const int64_t g = groups[(key - start) >> 4];
-      return g < 0 ? -1 : g + (key & 15) * row_bytes;
+      return g < 0 ? -1 : (kIsChunk<Args> ? g * 16 * row_bytes : g) + (key & 15) * row_bytes;
     } else {
       const int kk = walk_key(it, key), e = page_of(a, kk);
       int at = e - page0;
@@ -236,7 +241,7 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
   };
   auto pair_at = [&](int first) __attribute__((always_inline)) -> Pair {
     if constexpr (!GROUPS) return Pair{kIsChunk<Args> ? key_offset(first + l32) : -1, -1};
-    const int e = imin((first - start) >> 4, kPrefixGroups - 2);
+    const int e = imin((first - start) >> 4, (kIsChunk<Args> ? kChunkGroups : kPrefixGroups) - 2);
     return Pair{groups[e], groups[e + 1]};
   };
   auto from_lane = [](int64_t x, int from) __attribute__((always_inline)) {
@@ -266,9 +271,16 @@ __global__ __launch_bounds__(kNW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))
           return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32 |
                            (uint32_t)__builtin_amdgcn_readfirstlane((int)x));
         };
-        const int64_t g0 = uniform(ahead.g0), g1 = uniform(ahead.g1);
+        int64_t g0, g1;
+        if constexpr (kIsChunk<Args>) {
+          g0 = __builtin_amdgcn_readfirstlane((int)ahead.g0);
+          g1 = __builtin_amdgcn_readfirstlane((int)ahead.g1);
+        } else {
+          g0 = uniform(ahead.g0), g1 = uniform(ahead.g1);
+        }
         if ((g0 | g1) >= 0) {
-          const char *b0 = base + g0, *b1 = base + g1;
+          const int64_t bytes = kIsChunk<Args> ? 16 * row_bytes : 1;
+          const char *b0 = base + g0 * bytes, *b1 = base + g1 * bytes;
           lds_done();  // the rows there have been read
           base_ready(b0, b1);
 #pragma unroll

@@ -279,6 +279,15 @@ def test_walks_longer_than_a_chunk_may_be():
     assert items_of(plan)[0] >= 15
 
 
+@pytest.mark.parametrize("rows", [1, 100])
+def test_a_whole_chunk_of_groups(rows):
+    # one sequence named 56 times: walks of 32,600 keys, which a workgroup's table of groups just holds, and longer ones
+    _, plan, *_ = attend([32600], [rows] * 56, 8, 8, 64, BF, 16, seqs=[0] * 56, seed=14)
+    assert items_of(plan)[0] == 56
+    _, plan, *_ = attend([32700], [rows] * 56, 8, 8, 64, BF, 16, seqs=[0] * 56, seed=15)
+    assert items_of(plan)[0] == 112
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 def test_scales_and_layers(dtype):
     attend([100, 50], [10, 1], 4, 2, 64, dtype, seed=13, scale=0.5, layers=3, layer=2)
