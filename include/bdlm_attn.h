@@ -483,7 +483,7 @@ bdlm_status bdlm_prefix_attn(const bdlm_cache* c, int64_t layer, int64_t request
  *   fill : 1: rows behind the last request's become 0 (LSE -inf), 0: they stay as they are
  * Keys and values that no row of a request sees may hold anything (but for those between
  * the windows of blocks longer than a window); the others of its sequence must be finite.  A page number outside the cache reads as rows of zeros, and lens are
- * taken between 0 and what a table holds.  Rounding as in bdlm_prefix_attn; the cuts follow the
+ * taken between 0 and what a table holds; the cache has at most 2^34 tokens' room.  Rounding as in bdlm_prefix_attn; the cuts follow the
  * plan, so bits may differ with the batch.
  * workspace: bdlm_chunk_workspace_bytes() bytes, 256-byte aligned, contents ignored on
  * entry; calls that may overlap in time need one each (they may share a plan).

@@ -50,7 +50,7 @@ bdlm_status check_chunk(const bdlm_cache* c, const bdlm_chunk* p, Room& room) {
   if (!std::isfinite(p->scale)) return fail(BDLM_ERR_INVALID, "scale is not finite");
   const bool f32 = c->dtype == BDLM_F32;
   // (groups of 16 tokens are numbered in 31 bits)
-  if (c->page_size > ((int64_t)1 << 34) / std::max<int64_t>(c->pages, 1))
+  if (c->page_size > ((int64_t)1 << 34) / c->pages)
     return fail(BDLM_ERR_UNSUPPORTED, "pages %lld x page_size %lld exceeds 2^34", (long long)c->pages, (long long)c->page_size);
   const int64_t group = p->heads / c->kv_heads, all = p->rows * group;  // query rows of a KV head
   const int64_t some = std::min(p->requests, p->rows);                  // requests with rows

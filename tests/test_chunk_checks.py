@@ -119,7 +119,8 @@ def test_the_c_abi_refuses_chunks(kw, status):
 
 
 @host_only
-@pytest.mark.parametrize("kw,status", [(dict(k=0), -1), (dict(head_dim=32), -2), (dict(seqs=0), -1), (dict(table=0), -1), (dict(pages=0), -1)])
+@pytest.mark.parametrize("kw,status", [(dict(k=0), -1), (dict(head_dim=32), -2), (dict(seqs=0), -1), (dict(table=0), -1), (dict(pages=0), -1),
+                                       (dict(pages=(1 << 28) + 1, page_size=64), -2)])
 def test_the_c_abi_refuses_caches(kw, status):
     assert make_plan(crec(**kw)) == status and attend(crec(**kw)) == status
     assert bd.lib().bdlm_chunk_plan_bytes(ctypes.byref(crec(**kw)), ctypes.byref(krec())) == 0
