@@ -120,9 +120,9 @@ def chunk_attn_workspace_bytes(plan: ChunkPlan) -> int:
     return plan.workspace_bytes
 
 
-def _new_outputs(q):
-    n, H, _ = q.shape
-    return q.new_empty(q.shape), q.new_empty((H, n), dtype=torch.float32)
+def _new_outputs(plan):
+    return (torch.empty(plan.rows, plan.heads, plan.head_dim, dtype=plan.dtype, device=plan.device),
+            torch.empty(plan.heads, plan.rows, dtype=torch.float32, device=plan.device))
 
 
 def chunk_attn(plan: ChunkPlan, q, layer: int, out: Optional[tuple] = None, workspace: Optional[torch.Tensor] = None,
@@ -137,7 +137,7 @@ def chunk_attn(plan: ChunkPlan, q, layer: int, out: Optional[tuple] = None, work
     rq = _as_long(plan, "q", q, H, n)
     layer = _int("layer", layer)
     if out is None:
-        o, lse = _made(stream, plan.device, _new_outputs, q)
+        o, lse = _made(stream, plan.device, _new_outputs, plan)
         ro = _Rows(o.data_ptr(), H * plan.head_dim)
     else:
         if len(out) != 2:
