@@ -16,10 +16,10 @@
 // row, under the loads of its first pass, and keeps them for all passes over the
 // row's heads; each pass's loads are issued before the pass in front is computed
 // (backward, 16,384 rows of 32/8 heads, d 128: 141 -> 121 us).
-// Measured, bf16: 30,011 rows of 32/8 heads, d 128, 117 us (5.25 TB/s, a copy's rate);
-// 16,384 rows forward 59 us, backward 113 (4.4 TB/s; two waves per SIMD, for the 32
-// sums of the weights' gradients that a lane keeps); 8,190 rows of 16/16 heads, d 64, 20
-// and 32 us; 64 rows 5 and 9 us, the launch and one row's chain of loads.
+// Measured, bf16: 30,011 rows of 32/8 heads, d 128, 115 us (5.3 TB/s, a copy's rate);
+// 16,384 rows forward 57 us, backward 105 (4.8 TB/s; two waves per SIMD, for the 32
+// sums of the weights' gradients that a lane keeps); 8,190 rows of 16/16 heads, d 64, 15
+// and 25 us; 64 rows 5 us, the launch and one row's chain of loads.
 //
 // Rounding.  An angle is position times frequency in 64 bits, in quarter turns,
 // reduced there to half a quarter; sine and cosine of the rest in fp32 by their

@@ -160,6 +160,14 @@ def test_mixed_requests(dtype, D, page):
     attend([1, 40, 333, 17, 64, 500], [1, 1, 70, 17, 5, 1], 4, 2, D, dtype, page, pad=3, seed=page)
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("page", [2, 4, 7, 8, 12, 40])
+def test_pages_that_are_no_whole_groups(D, page):
+    # copies of 4 or 8 rows share a page or do not; walks with a gap; whole tiles and ends of pages inside them
+    attend([900, 333, 40, 1], [130, 1, 33, 1], 4, 2, D, BF, page, pad=2, seed=page)
+    attend([900, 333, 40, 1], [130, 1, 33, 1], 4, 2, D, BF, page, seed=page + 1, window=150, sinks=5)
+
+
 @pytest.mark.parametrize("dtype", [BF, F32])
 @pytest.mark.parametrize("H,KV", [(1, 1), (3, 1), (8, 2), (6, 6), (24, 1)])
 def test_heads(dtype, H, KV):
