@@ -106,6 +106,7 @@ def chunk_plan(cache, seqs, counts, rows: int, heads: int, block_size: int = 1, 
     _launch_plan(plan, stream, lib().bdlm_chunk_plan, c._ref, ref, a, b, plan._at, plan._bytes)
     if out is not None:
         ctypes.memmove(ctypes.byref(plan._record), ref, ctypes.sizeof(rec))
+        plan._workspace_bytes = None
     return plan
 
 

@@ -30,6 +30,32 @@ struct Room {
   size_t plan_bytes, part_bytes, lse_bytes;
 };
 
+// Items, units of the merge and partial rows, with walks of up to `longest` keys.
+struct Bounds {
+  int64_t items, joins, part_rows;
+};
+Bounds bounds(const bdlm_cache* c, const bdlm_chunk* p, int64_t tiles, int64_t longest, int64_t limit) {
+  const bool f32 = c->dtype == BDLM_F32;
+  const int64_t all = p->rows * (p->heads / c->kv_heads);  // query rows of a KV head
+  // chunks beyond the first of each tile: by the share, or by the limit (n_cut of a tile at most); n_least of a tile
+  // where every chunk is as short as it may be
+  const int64_t by_share = 2 * (f32 ? kSlotsF32 : kSlots) / c->kv_heads + 1;
+  const int64_t n_cut = longest / (limit - 64), by_limit = tiles * n_cut;
+  const int64_t n_least = std::max<int64_t>(longest - 1, 0) / std::min(kLeast, limit - 64), by_least = tiles * n_least;
+  const int64_t more = std::min(std::max(by_share, by_limit), by_least);
+  Bounds b{};
+  if (tiles == 0) return b;
+  b.items = tiles + more;
+  // units of the merge, of cut tiles: of join_rows rows, or of one in those of more than kShortJoin chunks
+  b.joins = std::min(tiles, more) * ((kPrefixSharedRows + join_rows(c->head_dim) - 1) / join_rows(c->head_dim)) +
+            std::min(std::min(tiles, more / kShortJoin) * kPrefixSharedRows, all);
+  // rows of cut tiles' chunks: at most a tile's of twice as many chunks, and as many as all rows have in that many chunks
+  const int64_t tile = f32 ? kPrefixRowsF32 : all > 2 * kPrefixWaveRows ? kPrefixSharedRows : kPrefixWaveRows;
+  const int64_t rows = std::max(std::min(2 * by_share * tile, all * (by_share + 1)), std::min(2 * by_limit * tile, all * (n_cut + 1)));
+  b.part_rows = more == 0 ? 0 : std::min(rows, std::min(2 * by_least * tile, all * (n_least + 1)));
+  return b;
+}
+
 bdlm_status check_chunk(const bdlm_cache* c, const bdlm_chunk* p, Room& room) {
   const bdlm_status st = check_cache(c);
   if (st != BDLM_OK) return st;
@@ -61,23 +87,19 @@ bdlm_status check_chunk(const bdlm_cache* c, const bdlm_chunk* p, Room& room) {
   room.limit = (int32_t)std::min<int64_t>(!f32 && c->page_size % 16 == 0 ? (kChunkGroups - 2) * 16
                                                                          : (kPrefixTableEntries - 4) * c->page_size,
                                           (int64_t)1 << 29);
+  // keys of a walk: what a table holds; with a window its own, the sinks, and those between the windows of a tile's rows
   const int64_t top = c->max_pages * c->page_size;
-  // chunks beyond the first of each tile: by the share, or by the limit (n_cut of a tile at most)
-  const int64_t slots = f32 ? kSlotsF32 : kSlots;
-  const int64_t by_share = 2 * slots / c->kv_heads + 1, n_cut = top / (room.limit - 64), by_limit = tiles * n_cut;
-  const int64_t more = std::max(by_share, by_limit);
-  room.items = tiles > 0 ? tiles + more : 0;
-  // units of the merge, of cut tiles: of join_rows rows, or of one in those of more than kShortJoin chunks
-  room.joins = std::min(tiles, more) * ((kPrefixSharedRows + join_rows(c->head_dim) - 1) / join_rows(c->head_dim)) +
-               std::min(std::min(tiles, more / kShortJoin) * kPrefixSharedRows, all);
-  // rows of cut tiles' chunks: at most a tile's of twice as many chunks, and as many as all rows have in that many chunks
-  const int64_t tile = f32 ? kPrefixRowsF32 : all > 2 * kPrefixWaveRows ? kPrefixSharedRows : kPrefixWaveRows;
-  room.part_rows = std::max(std::min(2 * by_share * tile, all * (by_share + 1)), std::min(2 * by_limit * tile, all * (n_cut + 1)));
+  const int64_t seen = p->window > 0 ? p->sinks + p->window + p->block_size + kPrefixSharedRows + 32 : top;
+  const Bounds most = bounds(c, p, tiles, top, room.limit), here = bounds(c, p, tiles, std::min(top, seen), room.limit);
+  room.items = here.items;
+  room.joins = here.joins;
+  room.part_rows = here.part_rows;
   if (room.items * c->kv_heads > kMaxWgs || room.part_rows >= kSharedTile)
     return fail(BDLM_ERR_UNSUPPORTED, "attention over the cache may need %lld workgroups (limit 2^22)",
                 (long long)(room.items * c->kv_heads));
-  room.plan_bytes = (size_t)(kChunkHead + 2 * p->requests + 1) * sizeof(int32_t) + room.items * sizeof(ChunkItemRec) +
-                    room.joins * sizeof(ChunkJoin);
+  // (the same for every window: a plan may be made anew with another one)
+  room.plan_bytes = (size_t)(kChunkHead + 2 * p->requests + 1) * sizeof(int32_t) + most.items * sizeof(ChunkItemRec) +
+                    most.joins * sizeof(ChunkJoin);
   const size_t parts = (size_t)room.part_rows * c->kv_heads;
   room.part_bytes = align256(parts * c->head_dim * sizeof(float));
   room.lse_bytes = align256(parts * (f32 ? sizeof(PartLse<false>) : sizeof(PartLse<true>)));

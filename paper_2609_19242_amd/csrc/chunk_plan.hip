@@ -18,7 +18,9 @@
 //
 // Room.  With unit >= total / (2 slots / KV heads), chunks beyond the first of each tile
 // are at most sum floor((n - 1) / unit) <= 2 slots / KV heads, or, where the chunk limit is
-// what cuts, tiles times what a table holds by the limit: the host makes that much room.
+// what cuts, tiles times what a table holds by the limit, and never more than tiles times a
+// walk's keys by the least unit: the host makes that much room, and launches no merge where
+// no walk can be that long.
 #include "chunk.hpp"
 #include "device.hpp"
 

@@ -54,6 +54,12 @@ def test_plans_are_used_again_for_the_same_sizes(monkeypatch):
     assert p.starts.shape == (2,) and p.requests == 2 and p.rows == 6
     again = bd.chunk_plan(p.cache, i32(1, 2), i32(1, 1), rows=6, heads=4, window=8, out=p)
     assert again is p and p._record.window == 8
+    # room for a plan does not depend on its window, room for the calls does
+    far = cache(max_pages=64)
+    p2 = bd.chunk_plan(far, i32(0, 1), i32(3, 1), rows=6, heads=4, window=8)
+    assert p2.workspace_bytes == 0
+    bd.chunk_plan(far, i32(0, 1), i32(3, 1), rows=6, heads=4, out=p2)
+    assert p2.workspace_bytes > 0 and p2._bytes >= bd.lib().bdlm_chunk_plan_bytes(far._ref, p2._ref)
     for kw in (dict(cache=cache()), dict(seqs=i32(0), counts=i32(1)), dict(rows=7), dict(heads=2)):
         with pytest.raises(ValueError, match="same"):
             bd.chunk_plan(**dict(dict(cache=p.cache, seqs=i32(0, 1), counts=i32(3, 1), rows=6, heads=4, out=p), **kw))
@@ -137,10 +143,14 @@ def test_the_c_abi_refuses_pointers_and_room():
                dict(qs=260), dict(o=0), dict(os=128), dict(os=1 << 31), dict(lse=0), dict(lse=FAKE + 2), dict(pitch=5), dict(pitch=1 << 40),
                dict(fill=2)):
         assert attend(**kw) == -1, kw
-    need = L.bdlm_chunk_workspace_bytes(ctypes.byref(c), ctypes.byref(k))
+    # (walks that no table or window lets grow past 256 keys are never cut)
+    assert L.bdlm_chunk_workspace_bytes(ctypes.byref(c), ctypes.byref(k)) == 0
+    far = crec(max_pages=64)
+    assert L.bdlm_chunk_workspace_bytes(ctypes.byref(far), ctypes.byref(krec(window=60, sinks=4))) == 0
+    need = L.bdlm_chunk_workspace_bytes(ctypes.byref(far), ctypes.byref(k))
     assert need > 0
     for kw in (dict(ws=0), dict(ws=FAKE + 128), dict(wb=need - 1)):
-        assert attend(**kw) == -4, kw
+        assert attend(far, **kw) == -4, kw
     assert attend(k=krec(rows=0), q=0, o=0, lse=0) == 0  # nothing to do, nothing launched
     assert L.bdlm_chunk_plan(None, ctypes.byref(k), FAKE, FAKE, FAKE, 1 << 30, None) == -1
     assert L.bdlm_chunk_plan(ctypes.byref(c), None, FAKE, FAKE, FAKE, 1 << 30, None) == -1
@@ -152,10 +162,10 @@ def test_workspaces_do_not_grow_with_the_tables():
         c.kv_heads, c.head_dim = 8, 128
         return bd.lib().bdlm_chunk_workspace_bytes(ctypes.byref(c), ctypes.byref(k))
 
-    short = room(max_pages=64)
-    assert short == room(max_pages=8192) and short < 256 << 20
+    short, far = room(max_pages=64), room(max_pages=8192)
+    assert short <= far == room(max_pages=4096) and far < 256 << 20
     # (tables of a million tokens: more chunks than that may be needed where every request has so many)
-    assert room(max_pages=65536) >= short
+    assert room(max_pages=65536) >= far
 
 
 def test_new_tensors_of_a_given_stream(monkeypatch):

@@ -435,6 +435,20 @@ def test_one_plan_on_two_streams_and_again():
     assert all(torch.equal(x, y) for x, y in zip(bd.chunk_attn(plan, q[0], 0), bd.chunk_attn(fresh, q[0], 0)))
 
 
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_a_plan_made_anew_with_another_window(dtype):
+    lens, counts = [3000, 700, 90, 1], [3, 100, 90, 1]
+    cache = make_cache(lens, 2, 64, dtype, 16, seed=21)
+    q = torch.randn(sum(counts), 4, 64, generator=torch.Generator().manual_seed(22)).to(dtype).to(DEV)
+    lists = cache, i32([0, 1, 2, 3]), i32(counts)
+    plan = bd.chunk_plan(*lists, rows=len(q), heads=4, window=30, sinks=3)
+    for window, sinks in ((30, 3), (0, 0), (500, 0), (30, 3), (64, 700)):
+        assert bd.chunk_plan(*lists, rows=len(q), heads=4, window=window, sinks=sinks, out=plan) is plan
+        got = bd.chunk_attn(plan, q, 0)
+        want = attend(lens, counts, 4, 2, 64, dtype, cache=cache, q=q, window=window, sinks=sinks)[3:]
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
 def test_many_requests():
     # more requests than the planner's threads, and than its table in LDS
     n, KV, D = 9000, 1, 64
