@@ -146,7 +146,10 @@ def chunk_attn(plan: ChunkPlan, q, layer: int, out: Optional[tuple] = None, work
         o, lse = out
         ro = _as_long(plan, "o", o, H, n)
         _lse(plan, lse, n)
-    workspace = _workspace(workspace, plan.workspace_bytes, plan.device, stream)
+    at, nbytes = None, plan.workspace_bytes
+    if workspace is not None or nbytes > 0:
+        workspace = _workspace(workspace, nbytes, plan.device, stream)
+        at, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     _launch_plan(plan, stream, lib().bdlm_chunk_attn, plan.cache._ref, plan._ref, layer, plan._at, plan._bytes, rq, ro,
-            lse.data_ptr(), n, 1 if out is None else 0, workspace.data_ptr(), workspace.numel() * workspace.element_size())
+                 lse.data_ptr(), n, 1 if out is None else 0, at, nbytes)
     return o, lse

@@ -28,7 +28,7 @@ struct RotateArgs {
   float* dw[2];
   int32_t axes, dim, rows_per, split, wgs;
   double quarters[kMaxPairs];  // quarter turns per position
-  int32_t axis[kMaxPairs];
+  int8_t axis[kMaxPairs];      // (the launch's time grows with its arguments' size)
 };
 
 hipError_t launch_rotate_fwd(const RotateArgs& a, int head_dim, int bf16, int interleaved, hipStream_t s);

@@ -96,7 +96,7 @@ RotateArgs rotate_args(const bdlm_rotary& r, int64_t rows, const int32_t* pos, d
   a.dim = r.dim;
   for (int i = 0; i < r.dim / 2; ++i) {
     a.quarters[i] = r.freq[i] * 0.63661977236758134308;  // 2 / pi
-    a.axis[i] = r.axis[i];
+    a.axis[i] = (int8_t)r.axis[i];
   }
   return a;
 }

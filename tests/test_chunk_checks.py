@@ -187,7 +187,7 @@ def test_new_tensors_of_a_given_stream(monkeypatch):
     monkeypatch.setattr(torch.cuda, "current_stream", lambda device=None: at[-1])
     monkeypatch.setattr(bd, "_torch_stream", lambda s, device: s)
     monkeypatch.setattr(km, "_launch", lambda *a: None)
-    c = cache()
+    c = cache(max_pages=64)  # (walks that may be cut: with a workspace)
     new.clear()
     p = bd.chunk_plan(c, i32(0, 1), i32(3, 1), rows=6, heads=4, stream="side")
     assert len(new) == 1 and new[0][1] == "side" and any(t is p._items and s == "current" for t, s in kept)
