@@ -19,6 +19,9 @@ constexpr int64_t kMaxStride = (int64_t)1 << 30;
 static_assert(BDLM_CHUNK_STARTS == kChunkHead * sizeof(int32_t), "the plan's layout is the header's");
 
 // Workgroups that run at once, of which the planner fills up to two rounds by cutting, and keys of a chunk at least.
+// Where no walk can have more than twice as many, none is cut, and no merge is launched (one request of 400 keys, 32/8
+// heads, d 128, cut in two 11.0 us and 6.4 for the merge, whole 13.7; 8/2 heads fp32 14.5 and 6.4, 20.0; chunks of 512 at least
+// everywhere: one request of 1,000 keys 11.5 -> 14.0 us, 64 rows behind 1,000 15.8 -> 20.4).
 constexpr int64_t kSlots = 2 * kCus, kSlotsF32 = kCus, kLeast = 256;
 static_assert((kSlots & (kSlots - 1)) == 0 && (kSlotsF32 & (kSlotsF32 - 1)) == 0, "the planner shifts by them");
 
@@ -26,9 +29,12 @@ static_assert((kSlots & (kSlots - 1)) == 0 && (kSlotsF32 & (kSlotsF32 - 1)) == 0
 // (chunk_plan.hip says why it is enough).
 struct Room {
   int64_t items, joins, part_rows;
-  int32_t limit;
+  int32_t limit, least;
   size_t plan_bytes, part_bytes, lse_bytes;
 };
+
+// Keys of a chunk at least, with walks of up to `longest` keys.
+int64_t least_keys(int64_t longest, int64_t limit) { return longest <= 2 * kLeast ? 2 * kLeast : std::min(kLeast, limit - 64); }
 
 // Items, units of the merge and partial rows, with walks of up to `longest` keys.
 struct Bounds {
@@ -41,7 +47,7 @@ Bounds bounds(const bdlm_cache* c, const bdlm_chunk* p, int64_t tiles, int64_t l
   // where every chunk is as short as it may be
   const int64_t by_share = 2 * (f32 ? kSlotsF32 : kSlots) / c->kv_heads + 1;
   const int64_t n_cut = longest / (limit - 64), by_limit = tiles * n_cut;
-  const int64_t n_least = std::max<int64_t>(longest - 1, 0) / std::min(kLeast, limit - 64), by_least = tiles * n_least;
+  const int64_t n_least = std::max<int64_t>(longest - 1, 0) / least_keys(longest, limit), by_least = tiles * n_least;
   const int64_t more = std::min(std::max(by_share, by_limit), by_least);
   Bounds b{};
   if (tiles == 0) return b;
@@ -90,7 +96,9 @@ bdlm_status check_chunk(const bdlm_cache* c, const bdlm_chunk* p, Room& room) {
   // keys of a walk: what a table holds; with a window its own, the sinks, and those between the windows of a tile's rows
   const int64_t top = c->max_pages * c->page_size;
   const int64_t seen = p->window > 0 ? p->sinks + p->window + p->block_size + kPrefixSharedRows + 32 : top;
-  const Bounds most = bounds(c, p, tiles, top, room.limit), here = bounds(c, p, tiles, std::min(top, seen), room.limit);
+  const int64_t longest = std::min(top, seen);
+  const Bounds most = bounds(c, p, tiles, top, room.limit), here = bounds(c, p, tiles, longest, room.limit);
+  room.least = (int32_t)least_keys(longest, room.limit);
   room.items = here.items;
   room.joins = here.joins;
   room.part_rows = here.part_rows;
@@ -157,7 +165,7 @@ bdlm_status bdlm_chunk_plan(const bdlm_cache* c, const bdlm_chunk* p, const int3
   a.sinks = p->window > 0 ? p->sinks : 0;  // (without a window every earlier key is visible)
   a.f32 = c->dtype == BDLM_F32;
   a.limit = room.limit;
-  a.least = (int32_t)std::min<int64_t>(kLeast, room.limit - 64);
+  a.least = room.least;
   a.slots = (int32_t)(a.f32 ? kSlotsF32 : kSlots);
   a.join_rows = join_rows(c->head_dim);
   a.max_items = (int32_t)room.items;

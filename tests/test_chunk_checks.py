@@ -143,7 +143,7 @@ def test_the_c_abi_refuses_pointers_and_room():
                dict(qs=260), dict(o=0), dict(os=128), dict(os=1 << 31), dict(lse=0), dict(lse=FAKE + 2), dict(pitch=5), dict(pitch=1 << 40),
                dict(fill=2)):
         assert attend(**kw) == -1, kw
-    # (walks that no table or window lets grow past 256 keys are never cut)
+    # (walks that no table or window lets grow past 512 keys are never cut)
     assert L.bdlm_chunk_workspace_bytes(ctypes.byref(c), ctypes.byref(k)) == 0
     far = crec(max_pages=64)
     assert L.bdlm_chunk_workspace_bytes(ctypes.byref(far), ctypes.byref(krec(window=60, sinks=4))) == 0
