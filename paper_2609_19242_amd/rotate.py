@@ -174,8 +174,8 @@ def qk_rotate_fwd(rot: Rotary, q, k, positions, q_weight=None, k_weight=None, ep
     return out
 
 
-def _new_weight_grads(c, q_weight, k_weight):
-    return [w.new_empty(w.shape, dtype=torch.float32) for w in (q_weight, k_weight) if w is not None]
+def _new_weight_grads(*weights):
+    return [torch.empty_like(w, dtype=torch.float32) for w in weights]
 
 
 def qk_rotate_bwd(rot: Rotary, q, k, positions, dq_out, dk_out, q_weight=None, k_weight=None,
@@ -188,15 +188,17 @@ def qk_rotate_bwd(rot: Rotary, q, k, positions, dq_out, dk_out, q_weight=None, k
     c, n, H, KV, args = _inputs(rot, q, k, positions, q_weight, k_weight, eps)
     rdq, rdk = _as_long(c, "dq_out", dq_out, H, n), _as_long(c, "dk_out", dk_out, KV, n)
     out, rows = _out_rows(c, out, ("dq", "dk"), q, k, stream)
-    dqw = dkw = at = None
+    dqw = dkw = dqw_at = dkw_at = at = None
     nbytes = 0
     if q_weight is not None or k_weight is not None:
-        new = iter(_made(stream, c.device, _new_weight_grads, c, q_weight, k_weight))
-        dqw, dkw = (next(new) if w is not None else None for w in (q_weight, k_weight))
+        new = _made(stream, c.device, _new_weight_grads, *[w for w in (q_weight, k_weight) if w is not None])
+        if q_weight is not None:
+            dqw, dqw_at = new[0], new[0].data_ptr()
+        if k_weight is not None:
+            dkw, dkw_at = new[-1], new[-1].data_ptr()
         if c.workspace_bytes is None:
             c.workspace_bytes = lib().bdlm_qk_rotate_workspace_bytes(c.head_dim)
         workspace = _workspace(workspace, c.workspace_bytes, c.device, stream)
         at, nbytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
-    _launch(c, stream, lib().bdlm_qk_rotate_bwd, *args, rdq, rdk, *rows, None if dqw is None else dqw.data_ptr(),
-            None if dkw is None else dkw.data_ptr(), at, nbytes)
+    _launch(c, stream, lib().bdlm_qk_rotate_bwd, *args, rdq, rdk, *rows, dqw_at, dkw_at, at, nbytes)
     return (*out, dqw, dkw)
