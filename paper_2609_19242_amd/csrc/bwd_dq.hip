@@ -206,7 +206,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
             const int first = v0 + (cw * IPW + i) * (512 / D), v = first + lane / (D / 8);  // of the instruction, the lane
             const int64_t at = (int64_t)(16 * k - (first < sw.gap_at ? sw.gap : 0)) * CS;
             buf_to_lds<16>(make_rsrc(cc.src + at, bytes), dst + (k * PI + i) * 512,
-                           (v >= a.sinks) & (v < sw.w0) ? ~15u : voff[i], 0);
+                           ((v >= a.sinks) & (v < sw.w0)) ? ~15u : voff[i], 0);
           }
           continue;
         }

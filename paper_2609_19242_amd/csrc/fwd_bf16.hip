@@ -178,7 +178,7 @@ __global__ __launch_bounds__(NT * NW * 64)
         for (int i = 0; i < IPW; ++i) {
           const int first = v0 + (cw * IPW + i) * (512 / D), v = first + lane / (D / 8);  // of the instruction, the lane
           const auto r = make_rsrc(first < sw.gap_at ? cc.src - (int64_t)sw.gap * CS : cc.src, bytes);
-          buf_to_lds<16>(r, dst + i * 512, (v >= a.sinks) & (v < sw.w0) ? ~15u : voff[i], 0);
+          buf_to_lds<16>(r, dst + i * 512, ((v >= a.sinks) & (v < sw.w0)) ? ~15u : voff[i], 0);
         }
         return;
       }
