@@ -519,7 +519,7 @@ bdlm_status bdlm_chunk_attn(const bdlm_cache* c, const bdlm_chunk* p, int64_t la
  *   positions     : [axes][rows] int32 in device memory, of any sign
  *   weights       : [head_dim] in `dtype`
  * Rounding: angles are formed in 64 bits and reduced there; in bf16 sums and products are
- * fp32 (|x| must be below 2^60), in fp32 the sums over a row are fp64; outputs are rounded
+ * fp32 (|x|, and backward |g w|, must be below 2^60), in fp32 the sums over a row are fp64; outputs are rounded
  * once.  A NaN or infinity stays in its head's row (and reaches the weights' gradient).
  */
 typedef struct {

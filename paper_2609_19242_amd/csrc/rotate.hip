@@ -25,7 +25,7 @@
 // reduced there to half a quarter; sine and cosine of the rest in fp32 by their
 // Taylor series to x^9 and x^10 (|x| <= pi / 4: the rest of the series is below
 // 2^-28).  bf16: the sum of squares and all products are fp32 (so squares must stay
-// below 2^127: |x| < 2^60), the outputs are rounded once.  fp32: the sums over a row
+// below 2^127: |x|, |g w| < 2^60), the outputs are rounded once.  fp32: the sums over a row
 // are fp64.  dw: fp32 sums of a lane's rows, a wave's and a workgroup's lanes in a
 // fixed order, the workgroups' in fp64; it is returned in fp32.
 #include "device.hpp"
