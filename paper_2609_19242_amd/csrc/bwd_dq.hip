@@ -14,6 +14,15 @@
 // forms D_i = dO_i . O_i itself (the lane already holds half of dO_i) and
 // leaves each row's statistics in the workspace for the dK/dV kernel, which
 // runs after it.
+//
+// Rows of few keys.  D formed from the rounded O misses sum_j P_ij dP_ij by up to 2^-8 |dO||O|, which is
+// much of dS where a row sees few keys and their values share a large part.  Packed calls form it from the products for
+// rows all of whose keys lie in one tile, as they meet it.  With sinks a row's few keys may lie in several tiles of the
+// walk (always where the window has left the sinks behind): a launch in front (SinkDArgs) then forms D of those
+// that see at most 64 keys, with the first two products alone, and the other one reads it.
+// A second walk in the same kernel took 58 registers that d 128 does not have.  (8 texts of 2,048, 32/8 heads, d 128,
+// window 32, 4 sinks: backward 318 -> 433 us, of which reading Q, dO and O once more is 79 at a copy's rate; windows
+// whose rows see more than 64 keys have no such launch: window 128 383 us with and without.)
 #include "qtiles.hpp"
 
 namespace bdlm {
@@ -21,16 +30,17 @@ namespace bdlm {
 namespace {
 
 constexpr float kLog2e = 1.44269504088896340736f;
+constexpr int kBN = 64;  // keys of a tile
 
 template <int D, int NW, int NST, int HM, class Args, int HP = 1>
 __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2))) void bwd_dq_kernel(
     const Args args) {
-  constexpr int BM = NW * 32 / HP, BN = 64, KS = D / 16, DT = D / 32;
+  constexpr int BM = NW * 32 / HP, BN = kBN, KS = D / 16, DT = D / 32;
   // K and V tiles with swizzled rows: K serves both its row reads (S^T) and
   // its transpose reads (K^T), V its row reads (dP^T).
   constexpr uint32_t RB = D * 2, TB = BN * RB;
   constexpr int STAGE = 2 * BN * D;
-  constexpr bool kPacked = kIsPacked<Args>;
+  constexpr bool kPacked = kIsPacked<Args>, FOR_D = kFormsD<Args>;
   // Copies: each tile is BN * D / 8 16-byte slots, TI instructions of 64 lanes;
   // waves 0 .. NW/2 - 1 copy K and the others V, IPW instructions each.
   constexpr int TI = BN * D / 8 / 64, IPW = TI / (NW / 2);
@@ -50,6 +60,15 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const int row0 = it.t * BM;
   const int nvalid = imin(BM, qr.len - row0);
   const int64_t H = a.heads;
+  // With sinks: whether the tile has rows of few keys that do not all lie in the walk's first tile (such a row
+  // has the fewer the later it is), whose D the launch in front forms.
+  [[maybe_unused]] bool tile_d = false;
+  if constexpr (kHasSinks<Args>) {
+    const int first = qr.pos0 + row0, last = first + nvalid - 1;
+    const SinkWalk walk = sink_walk_of(a, first, last);
+    tile_d = may_see_few(args.sinks, args.window, args.M, BN) && walk.n > BN && row_keys(a, walk, last) <= BN;
+    if (FOR_D && !(tile_d && first_chunk(args, it))) return;
+  }
 
   // This wave's 32 query rows of Q and dO as MFMA B fragments, and
   // D = rowsum(dO * O) of the lane's row: a lane holds half of the row's
@@ -98,6 +117,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   const bool row_ok = my_row < qr.len;
   const int pq = qr.pos0 + imin(my_row, qr.len - 1);
   const int pq0 = qr.pos0 + row0, pq1 = qr.pos0 + row0 + nvalid - 1;
+  [[maybe_unused]] const auto sw = sink_walk_of(a, pq0, pq1);
   // Rows past the range and rows that see no key get P = 0.  The row's
   // statistics for the dK/dV kernel, which runs after this one, go to the
   // workspace: (LSE log2(e), D), or (-LSE / scale, -D) for the scheduled
@@ -107,7 +127,10 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   if (row_ok) {
     const float z = qr.lse[((int64_t)it.b * H + h) * qr.bstride + my_row];
     lse2 = (z == -INFINITY) ? INFINITY : z * kLog2e;
-    if (half == 0 && first_chunk(args, it)) {
+    if constexpr (kHasSinks<Args> && !FOR_D) {
+      if (tile_d && row_keys(a, sw, pq) <= BN) dl = -qr.delta[((int64_t)it.b * H + h) * qr.len + my_row];
+    }
+    if (!FOR_D && half == 0 && first_chunk(args, it)) {
       const int64_t si = ((int64_t)it.b * H + h) * qr.len + my_row;
       if (a.stats_form) {
         if constexpr (!kPacked) qr.delta[si] = -dsum;  // (packed calls: behind the walk)
@@ -150,7 +173,6 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   };
   const bool kwave = w < NW / 2;
   const int64_t CS = kwave ? k_stride<D>(a) : v_stride<D>(a);  // of the tensor this wave copies
-  [[maybe_unused]] const auto sw = sink_walk_of(a, pq0, pq1);
   int u0, u1;
   seen_keys(a, pq0, pq1, u0, u1);
   auto copy_seek = [&](CopyCur cc) -> CopyCur {
@@ -237,7 +259,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // and three stages on long walks, 4 waves and two on short ones).
   KCur c0;
   c0.have = find_key_tile(a, 0, qr.stream, pq0, pq1, BN, c0.j, c0.t, c0.t1, c0.f0, c0.f1);
-  cut_walk(args, it, c0.t, c0.t1, c0.have);
+  if constexpr (!FOR_D) cut_walk(args, it, c0.t, c0.t1, c0.have);
   [[maybe_unused]] const int walk0 = c0.t, walk1 = c0.t1;
   CopyCur cp = copy_seek(CopyCur{c0, any_src, 0});
 #pragma unroll
@@ -249,6 +271,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   int cur = 0;
   int lane_lo = 0, lane_w = 0, lane_j = -1;
   [[maybe_unused]] int lane_s = 0, lane_end = 0;  // with sinks: the end of this lane's, and of its keys
+  [[maybe_unused]] float rest_d = 0.f;  // FOR_D
   [[maybe_unused]] bool few_keys = false;  // packed calls: some row of this wave has no more keys than a tile holds
   while (c0.have) {
     copy_tile(lds + (cur == 0 ? NST - 1 : cur - 1) * STAGE, cp);
@@ -257,7 +280,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
       if constexpr (kHasSinks<Args>) {
         lane_walk(a, sw, pq, lane_lo, lane_w, lane_s);
         lane_end = lane_w > 0 ? lane_lo - k_range(a, j).pos0 + lane_w : lane_s;
-        few_keys = __builtin_amdgcn_ballot_w64(lane_end > 0 && lane_end <= BN) != 0;
+        few_keys = !tile_d && __builtin_amdgcn_ballot_w64(lane_end > 0 && lane_end <= BN) != 0;
       } else {
         lane_key_interval(a, j, qr.stream, pq, lane_lo, lane_w);
       }
@@ -322,6 +345,18 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
             if constexpr (kHasSinks<Args>) hidden &= t * BN + 4 * half + u * 32 + (i >> 2) * 8 + (i & 3) >= lane_s;
             if (hidden) sacc[u][i] = -INFINITY;
           }
+      }
+
+      if constexpr (FOR_D) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) rest_d = fmaf(exp2f_fast(fmaf(sacc[u][i], c, -lse2)), dpacc[u][i], rest_d);
+        vm_wait_barrier<IPW * (NST - 2)>();
+        cur = cur == NST - 1 ? 0 : cur + 1;
+        c0 = next_tile(c0);
+        cp = copy_next(cp);
+        continue;
       }
 
       // Packed calls: a row all of whose keys lie in this tile, seen by all rows or
@@ -423,13 +458,19 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2, 2)))
   // the workgroup's LDS is released.
   __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
 
+  if constexpr (FOR_D) {
+    rest_d += partner(rest_d);
+    if (row_ok && half == 0 && row_keys(a, sw, pq) <= BN) qr.delta[((int64_t)it.b * H + h) * qr.len + my_row] = -(dl + rest_d);
+    return;
+  }
   if constexpr (kPacked) {
     // D, from the chunk of the walk that has the row's first key (which may have corrected it)
     const PackedItem& p = args.items[it.item];
     int lo, wid;
     lane_key_interval(a, 0, qr.stream, pq, lo, wid);
     const int first = (lo - k_range(a, 0).pos0) / BN;
-    const bool mine = p.slot < 0 || (!kHasSinks<Args> && wid > 0 ? first >= walk0 && first < walk1 : p.n0 == 0);
+    bool mine = p.slot < 0 || (!kHasSinks<Args> && wid > 0 ? first >= walk0 && first < walk1 : p.n0 == 0);
+    if constexpr (kHasSinks<Args>) mine = mine && !(tile_d && row_keys(a, sw, pq) <= BN);  // (it is there)
     if (row_ok && half == 0 && mine) qr.delta[((int64_t)it.b * H + h) * qr.len + my_row] = -dl;
     if (p.slot >= 0) {  // a chunk's share of dQ
       float* op = (float*)args.partials + q_partial_row<NW, HP>(args, it, w, l32) * D;
@@ -523,19 +564,25 @@ using PackedQ = SinkQArgs;
 using PackedQ = PackedArgs;
 #endif
 
-template <int D>
-void launch_packed(const PackedQ& a, int n, hipStream_t s) {
+template <int D, class Args>
+void launch_packed(const Args& a, int n, hipStream_t s) {
   constexpr int NW = kQRowsShortBf16 / 32;
   const int hp = packed_tile_heads(a.group);
   const dim3 grid(n), threads(NW * 64);
-  if (hp == 4) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedQ, 4>), grid, threads, 0, s, a);
-  else if (hp == 2) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedQ, 2>), grid, threads, 0, s, a);
-  else hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, PackedQ, 1>), grid, threads, 0, s, a);
+  if (hp == 4) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, Args, 4>), grid, threads, 0, s, a);
+  else if (hp == 2) hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, Args, 2>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((bwd_dq_kernel<D, NW, 2, 0, Args, 1>), grid, threads, 0, s, a);
 }
 
 hipError_t launch_bwd_dq_bf16(const PackedQ& a, int head_dim, hipStream_t s) {
   const int n = workgroups_for(a.n_items * (a.heads / packed_tile_heads(a.group)));
   if (n == 0) return hipSuccess;
+#ifdef BDLM_SINK_CALLS
+  if (may_see_few(a.sinks, a.window, a.M, kBN)) {
+    const SinkDArgs d{a};
+    head_dim == 128 ? launch_packed<128>(d, n, s) : launch_packed<64>(d, n, s);
+  }
+#endif
   head_dim == 128 ? launch_packed<128>(a, n, s) : launch_packed<64>(a, n, s);
   return hipGetLastError();
 }

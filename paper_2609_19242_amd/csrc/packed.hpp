@@ -169,6 +169,7 @@ __device__ __forceinline__ int64_t row_elem(const PackedView&, int, int64_t, int
 //    t-th of the sinks.  A tile of 4 keys costs as much as one of 128 (the same texts:
 //    169 us without, 225 with them; 16K tokens of 3 documents, window 1,024: 633, 671).
 struct SinkQArgs : PackedArgs {};
+struct SinkDArgs : SinkQArgs {};  // D of rows of few keys alone (bwd_dq.hip)
 struct SinkQArgsF32 : PackedArgs {};
 struct SinkKArgs : PackedArgs {};
 
@@ -190,6 +191,12 @@ __host__ __device__ inline SinkWalk sink_walk(const MaskRule& rule, int sinks, i
     w.n = end > first ? below + end - first : imin(below, w.n);  // (a block may end behind its window's start)
   }
   return w;
+}
+
+// Whether a row whose window lies apart from the sinks may see no more than n keys: all of the sinks, and of its window
+// what is left of it where its block of M tokens ends behind the sequence.
+__host__ __device__ inline bool may_see_few(int sinks, int window, int M, int n) {
+  return window > 0 && (int64_t)sinks + (window > M - 1 ? window - (M - 1) : 0) <= n;
 }
 
 struct SinkView : PackedView {
@@ -266,10 +273,14 @@ template <class A> constexpr bool kIsPacked = false;
 template <> constexpr inline bool kIsPacked<PackedArgs> = true;
 template <> constexpr inline bool kIsPacked<PackedView> = true;
 template <> constexpr inline bool kIsPacked<SinkQArgs> = true;
+template <> constexpr inline bool kIsPacked<SinkDArgs> = true;
 template <> constexpr inline bool kIsPacked<SinkQArgsF32> = true;
 template <> constexpr inline bool kIsPacked<SinkKArgs> = true;
 template <class A> constexpr bool kHasSinks = false;
 template <> constexpr inline bool kHasSinks<SinkQArgs> = true;
+template <> constexpr inline bool kHasSinks<SinkDArgs> = true;
+template <class A> constexpr bool kFormsD = false;
+template <> constexpr inline bool kFormsD<SinkDArgs> = true;
 
 hipError_t launch_fwd_bf16(const PackedArgs& a, int head_dim, int teams, hipStream_t s);
 hipError_t launch_packed_fwd_sum(const PackedArgs& a, int head_dim, int slots, hipStream_t s);
@@ -283,7 +294,7 @@ hipError_t launch_bwd_dkv_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_sum_f32(const PackedArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_fwd_bf16(const SinkQArgs& a, int head_dim, int teams, hipStream_t s);
 hipError_t launch_fwd_f32(const SinkQArgsF32& a, int head_dim, hipStream_t s);
-hipError_t launch_bwd_dq_bf16(const SinkQArgs& a, int head_dim, hipStream_t s);
+hipError_t launch_bwd_dq_bf16(const SinkQArgs& a, int head_dim, hipStream_t s);  // (two kernels where rows may see few keys)
 hipError_t launch_bwd_dkdv(const SinkKArgs& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dq_f32(const SinkQArgsF32& a, int head_dim, hipStream_t s);
 hipError_t launch_bwd_dkv_f32(const SinkKArgs& a, int head_dim, hipStream_t s);

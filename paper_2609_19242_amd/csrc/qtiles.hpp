@@ -129,6 +129,13 @@ __device__ inline void lane_walk(const SinkView& a, const SinkWalk& w, int pq, i
   wid = imax(h - l, 0);
   sinks = imin(a.sinks, h);
 }
+// The keys that it sees.
+__device__ inline int row_keys(const SinkView& a, const SinkWalk& w, int pq) {
+  int lo, wid, sinks;
+  lane_walk(a, w, pq, lo, wid, sinks);
+  lo -= a.kr[0].pos0;
+  return imax(sinks, 0) + imax(lo + wid - imax(lo, sinks), 0);
+}
 
 // With sinks, fp32: the sinks, and the window's tiles among the other keys.
 __device__ inline void key_tile_span(const SinkViewF32& a, int j, int, int pq0, int pq1, int BN, int& t0, int& t1, int& f0,
