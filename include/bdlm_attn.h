@@ -539,7 +539,9 @@ bdlm_status bdlm_qk_rotate_fwd(const bdlm_rotary* r, int32_t dtype, int64_t rows
 /*
  * Backward from the same inputs and the outputs' gradients dq_out, dk_out: dq and dk
  * (which may be dq_out and dk_out), and the weights' gradients [head_dim] in fp32 (null:
- * not wanted; without a norm they must be), the same bits in every call.  workspace:
+ * not wanted; without a norm they must be), the same bits in every call.  However many rows and heads: at most 64
+ * products are added one after the other in fp32, those sums in fp64, and the additions are off by less than 2^-17 of
+ * the sum of the products' sizes.  workspace:
  * bdlm_qk_rotate_workspace_bytes(), 256-byte aligned, contents ignored on entry, one per call that may
  * overlap in time; not needed where no weight's gradient is wanted.
  */

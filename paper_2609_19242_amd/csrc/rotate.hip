@@ -26,8 +26,9 @@
 // Taylor series to x^9 and x^10 (|x| <= pi / 4: the rest of the series is below
 // 2^-28).  bf16: the sum of squares and all products are fp32 (so squares must stay
 // below 2^127: |x|, |g w| < 2^60), the outputs are rounded once.  fp32: the sums over a row
-// are fp64.  dw: fp32 sums of a lane's rows, a wave's and a workgroup's lanes in a
-// fixed order, the workgroups' in fp64; it is returned in fp32.
+// are fp64.  dw: a lane adds up to 64 products in fp32 and those sums in fp64 (in LDS, for which it
+// has no registers; calls whose chains cannot be longer run without: 8,190 rows of 16/16 heads, d 64, 28.3 us, with the
+// LDS 28.9), a wave's and a workgroup's lanes are added in fp32 in a fixed order, the workgroups' in fp64; it is returned in fp32.
 #include "device.hpp"
 #include "rotate.hpp"
 
@@ -35,7 +36,7 @@ namespace bdlm {
 
 namespace {
 
-constexpr int kWaves = 4;
+constexpr int kWaves = kRotateWaves;
 
 // 8 consecutive elements, as they lie in memory.
 template <class T> struct Raw8;
@@ -227,7 +228,8 @@ __global__ __launch_bounds__(kWaves * 64) void rotate_fwd_kernel(const RotateArg
   }
 }
 
-template <class T, int D, bool IL, bool NORM>
+// LONG: some lane may add up more than kRotateChain products to a weight's gradient.
+template <class T, int D, bool IL, bool NORM, bool LONG>
 __global__ __launch_bounds__(kWaves * 64) void rotate_bwd_kernel(const RotateArgs a) {
   using S = typename SumOf<T>::type;
   constexpr int LPR = D / 16;
@@ -239,6 +241,10 @@ __global__ __launch_bounds__(kWaves * 64) void rotate_bwd_kernel(const RotateArg
   for (int i = 0; i < 2; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dw[i][e] = 0.f;
+  // this lane's longer sums, and whether there are some (of the wave's, as the chains' lengths)
+  [[maybe_unused]] __shared__ double far[LONG ? kWaves : 1][32][64];
+  [[maybe_unused]] int chain[2] = {0, 0};
+  [[maybe_unused]] bool have_far[2] = {false, false};
   for (int64_t n = (int64_t)blockIdx.x * kWaves + w; n < sets * a.split; n += (int64_t)gridDim.x * kWaves) {
     const int64_t set = n / a.split;
     const int part = (int)(n - set * a.split);
@@ -287,6 +293,18 @@ __global__ __launch_bounds__(kWaves * 64) void rotate_bwd_kernel(const RotateArg
             g[e] = r * fmaf(-(x.a[e] * r), m, g[e] * wt.a[e]);
             k[e] = r * fmaf(-(x.b[e] * r), m, k[e] * wt.b[e]);
           }
+          if constexpr (LONG) {
+            if (++chain[i] == kRotateChain) {
+#pragma unroll
+              for (int e = 0; e < 16; ++e) {
+                double& sum = far[w][16 * i + e][lane];
+                sum = (have_far[i] ? sum : 0.0) + (double)dw[i][e];
+                dw[i][e] = 0.f;
+              }
+              chain[i] = 0;
+              have_far[i] = true;
+            }
+          }
         }
         if (mine) {
           T* o = (T*)t.out + me.row * t.outs + head_of(p);
@@ -306,6 +324,7 @@ __global__ __launch_bounds__(kWaves * 64) void rotate_bwd_kernel(const RotateArg
     for (int i = 0; i < 2; ++i)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
+        if (LONG && have_far[i]) dw[i][e] = (float)(far[w][16 * i + e][lane] + (double)dw[i][e]);
 #pragma unroll
         for (int m = LPR; m < 64; m <<= 1) dw[i][e] += __shfl_xor(dw[i][e], m);
         if (lane < LPR) sums[w][i][(e < 8 ? me.ra : me.rb) + (e & 7)] = dw[i][e];
@@ -359,8 +378,10 @@ void launch(const RotateArgs& a, bool bwd, hipStream_t s) {
     return;
   }
   if (a.wgs == 0) {  // (no rows: zeros)
-  } else if (norm) hipLaunchKernelGGL((rotate_bwd_kernel<T, D, IL, true>), grid, threads, 0, s, a);
-  else hipLaunchKernelGGL((rotate_bwd_kernel<T, D, IL, false>), grid, threads, 0, s, a);
+  } else if (norm && a.partials && a.chain > kRotateChain)
+    hipLaunchKernelGGL((rotate_bwd_kernel<T, D, IL, true, true>), grid, threads, 0, s, a);
+  else if (norm) hipLaunchKernelGGL((rotate_bwd_kernel<T, D, IL, true, false>), grid, threads, 0, s, a);
+  else hipLaunchKernelGGL((rotate_bwd_kernel<T, D, IL, false, false>), grid, threads, 0, s, a);
   if (a.partials) hipLaunchKernelGGL((rotate_dw_kernel<D>), dim3(2 * D / 16), dim3(1024), 0, s, a);
 }
 template <class T, int D>

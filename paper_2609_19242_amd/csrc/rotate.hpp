@@ -8,6 +8,8 @@
 namespace bdlm {
 
 constexpr int kMaxPairs = 64, kMaxAxes = 4;
+constexpr int kRotateWaves = 4;   // of a workgroup
+constexpr int kRotateChain = 64;  // products to a weight's gradient that a lane adds up in fp32
 
 struct RotateTensor {
   const void *x, *dy, *w;  // rows; the outputs' gradients; the weight, or null
@@ -27,6 +29,7 @@ struct RotateArgs {
   float* partials;     // backward: [workgroup][2][D] sums of the weights' gradients
   float* dw[2];
   int32_t axes, dim, rows_per, split, wgs;
+  int64_t chain;       // passes over a tensor's heads that a wave makes, at most
   double quarters[kMaxPairs];  // quarter turns per position
   int8_t axis[kMaxPairs];      // (the launch's time grows with its arguments' size)
 };

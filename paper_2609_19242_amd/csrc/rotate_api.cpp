@@ -15,7 +15,7 @@ namespace {
 constexpr int64_t kMaxRows = (int64_t)1 << 28;
 constexpr int64_t kMaxStride = (int64_t)1 << 30;
 constexpr double kMinEps = 0x1p-100;    // (a sum with it must be an fp32 number, and not 0)
-constexpr int64_t kWaves = 4;           // of a workgroup
+constexpr int64_t kWaves = kRotateWaves;
 constexpr int64_t kFullWaves = 2048;    // waves from which on a row's heads stay with one wave
 constexpr double kApart = 1.3;          // what a pass over heads of several rows takes longer
 constexpr int64_t kMaxFwdWgs = 1 << 20;
@@ -85,6 +85,8 @@ void deal(const bdlm_rotary& r, int64_t rows, int32_t heads, int32_t kv_heads, i
   const int64_t sets = (rows + best - 1) / best, all = (int64_t)a.t[0].passes + a.t[1].passes;
   a.split = (int32_t)std::min(std::max<int64_t>((kFullWaves + sets - 1) / sets, 1), all);
   a.wgs = (int32_t)std::min((sets * a.split + kWaves - 1) / kWaves, max_wgs);
+  const int64_t turns = (sets * a.split + a.wgs * kWaves - 1) / (a.wgs * kWaves);
+  a.chain = turns * ((std::max(a.t[0].passes, a.t[1].passes) + a.split - 1) / a.split);
 }
 
 RotateArgs rotate_args(const bdlm_rotary& r, int64_t rows, const int32_t* pos, double eps) {
