@@ -478,6 +478,9 @@ bdlm_status bdlm_prefix_attn(const bdlm_cache* c, int64_t layer, int64_t request
  * layers of a step; it may be captured in a graph.  It holds while the lengths it was
  * made from do; the table is read by the calls.  After BDLM_CHUNK_STARTS bytes it holds the requests'
  * first rows (int32 [requests], at most `rows`), as bdlm_cache_write takes them.
+ * A call takes a plan that was made with its own bdlm_chunk (but for scale) and a cache of its own's sizes (but for
+ * layers and pages).  With another one (a captured call that is replayed after its plan was made anew with another
+ * window, say), or one that no call has made, every row becomes NaN, whatever `fill` is.
  *   q, o : [rows][heads][head_dim] in the cache's dtype, rows `stride` elements apart
  *   lse  : [heads][lse_pitch] fp32, natural log
  *   fill : 1: rows behind the last request's become 0 (LSE -inf), 0: they stay as they are

@@ -82,7 +82,9 @@ def chunk_plan(cache, seqs, counts, rows: int, heads: int, block_size: int = 1, 
     GPU; after :func:`cache_grow`): their query rows lie one after the other in tensors of ``rows`` rows of ``heads``
     heads.  Each row sees the keys up to the end of its block of ``block_size`` tokens (1: up to itself), with
     ``window`` only the last ``window`` of those and its sequence's first ``sinks`` tokens.  ``out``: an earlier plan of
-    the same cache, requests, rows and heads, which is overwritten (in a graph, say)."""
+    the same cache, requests, rows and heads, which is overwritten (in a graph, say).  A captured :func:`chunk_attn`
+    keeps the block size, window and sinks that its plan had then: replayed with another plan in the same place, it
+    makes all rows NaN."""
     c = _cache(cache)
     a = _list(c, "seqs", seqs)
     n = seqs.shape[0]

@@ -26,7 +26,7 @@ namespace bdlm {
 // Words of a plan in device memory: a header, the requests' first rows, their first
 // tiles (with the total behind), the items, the merge's units.
 constexpr int kChunkHead = 16;
-enum : int { kPlanItems = 0, kPlanJoins = 1, kPlanRows = 2, kPlanRoom = 3 };  // of the header (room: for items, in front of the units)
+enum : int { kPlanItems = 0, kPlanJoins = 1, kPlanRows = 2, kPlanRoom = 3, kPlanKey = 4 };  // of the header (room: for items, in front of the units; key: 8 bytes)
 
 struct ChunkItemRec {
   int32_t seq, token0, pos0, len;  // (-1: none) the request's first row, its position, the sequence's tokens
@@ -53,6 +53,7 @@ struct ChunkPlanArgs {
   int32_t f32, limit, least, slots;   // keys of a chunk at most, at least; workgroups that run at once
   int32_t join_rows, max_items, max_joins;
   int64_t max_part_rows;
+  uint64_t key;
 };
 
 struct ChunkArgs {
@@ -74,6 +75,7 @@ struct ChunkArgs {
   int32_t rows, fill;     // rows behind the last request's become 0 (LSE -inf)
   int32_t max_items, max_joins;
   float scale, scale_log2;
+  uint64_t key;  // the plan's must be the same
 };
 
 hipError_t launch_chunk_plan(const ChunkPlanArgs& a, hipStream_t s);
@@ -92,6 +94,12 @@ template <> struct GroupOf<ChunkArgs> { typedef int32_t type; };
 template <class A> constexpr bool kIsChunk = false;
 template <> constexpr inline bool kIsChunk<ChunkArgs> = true;
 
+// Whether the plan is one of this call's sizes: those that its layout, its items' places and its keys come
+// from (a number that the host forms from them lies in both).  Another one's items could lead anywhere.
+__device__ inline bool plan_fits(const ChunkArgs& a) { return *(const uint64_t*)(a.plan + kPlanKey) == a.key; }
+__device__ inline int plan_items(const ChunkArgs& a) { return plan_fits(a) ? imin(a.plan[kPlanItems], a.max_items) : 0; }
+__device__ inline int plan_joins(const ChunkArgs& a) { return plan_fits(a) ? imin(a.plan[kPlanJoins], a.max_joins) : 0; }
+
 template <bool BF16>
 __device__ inline bool attn_item(const PrefixArgs& a, int wg, PrefixItem& it) {
   if constexpr (!BF16) return prefix_item(a, wg, kPrefixRowsF32, kPrefixRowsF32, it);
@@ -102,7 +110,7 @@ __device__ inline bool attn_item(const PrefixArgs& a, int wg, PrefixItem& it) {
 template <bool BF16>
 __device__ inline bool attn_item(const ChunkArgs& a, int wg, ChunkItem& it) {
   const int n = wg / a.kv_heads;
-  if (n >= imin(a.plan[kPlanItems], a.max_items)) return false;
+  if (n >= plan_items(a)) return false;
   const ChunkItemRec& r = a.items[n];
   it.kvh = wg - n * a.kv_heads;
   it.row0 = r.row0;
@@ -195,20 +203,24 @@ __device__ inline WalkPages walk_pages(const ChunkArgs& a, const ChunkItem& it) 
   return w;
 }
 
-// Rows behind the last request's: the workgroups without an item write zeros (LSE -inf).
+// Rows behind the last request's: the workgroups without an item write zeros (LSE -inf).  With a plan that does not fit,
+// all rows become NaN.
 template <class T, int D>
 __device__ inline void fill_rest(const PrefixArgs&, int, int) {}
 template <class T, int D>
 __device__ inline void fill_rest(const ChunkArgs& a, int wg, int wgs) {
-  if (!a.fill) return;
-  const int used = imin(a.plan[kPlanItems], a.max_items) * a.kv_heads, first = a.plan[kPlanRows];
+  const bool fits = plan_fits(a);
+  if (fits && !a.fill) return;
+  const int used = plan_items(a) * a.kv_heads, first = fits ? a.plan[kPlanRows] : 0;
   typedef int quad __attribute__((ext_vector_type(4)));
+  const int x = fits ? 0 : sizeof(T) == 2 ? 0x7fc07fc0 : 0x7fc00000;  // (NaN)
+  const float z = fits ? -INFINITY : __builtin_nanf("");
   constexpr int PR = D * (int)sizeof(T) / 16;  // 16-byte pieces of a head's row
   const int64_t n = (int64_t)(a.rows - first) * a.heads * PR, step = (int64_t)(wgs - used) * blockDim.x;
   for (int64_t i = (int64_t)(wg - used) * blockDim.x + threadIdx.x; i < n; i += step) {
     const int64_t hr = i / PR, row = hr / a.heads + first, h = hr % a.heads;
-    *(quad*)((T*)a.o + row * a.os + h * D + (i % PR) * (16 / (int)sizeof(T))) = quad{0, 0, 0, 0};
-    if (i % PR == 0) a.lse[h * a.pitch + row] = -INFINITY;
+    *(quad*)((T*)a.o + row * a.os + h * D + (i % PR) * (16 / (int)sizeof(T))) = quad{x, x, x, x};
+    if (i % PR == 0) a.lse[h * a.pitch + row] = z;
   }
 }
 

@@ -5,6 +5,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "cache_check.hpp"
 #include "chunk.hpp"
@@ -31,6 +32,7 @@ struct Room {
   int64_t items, joins, part_rows;
   int32_t limit, least;
   size_t plan_bytes, part_bytes, lse_bytes;
+  uint64_t key;  // of the sizes that a plan is made for, not 0
 };
 
 // Keys of a chunk at least, with walks of up to `longest` keys.
@@ -60,6 +62,16 @@ Bounds bounds(const bdlm_cache* c, const bdlm_chunk* p, int64_t tiles, int64_t l
   const int64_t rows = std::max(std::min(2 * by_share * tile, all * (by_share + 1)), std::min(2 * by_limit * tile, all * (n_cut + 1)));
   b.part_rows = more == 0 ? 0 : std::min(rows, std::min(2 * by_least * tile, all * (n_least + 1)));
   return b;
+}
+
+// One number for some (each is mixed in by steps that lose nothing of those before).
+uint64_t key_of(std::initializer_list<int64_t> xs) {
+  uint64_t h = 0;
+  for (const int64_t x : xs) {
+    h = (h ^ (uint64_t)x) * 0x9e3779b97f4a7c15ull;
+    h ^= h >> 29;
+  }
+  return h ? h : 1;
 }
 
 bdlm_status check_chunk(const bdlm_cache* c, const bdlm_chunk* p, Room& room) {
@@ -111,6 +123,8 @@ bdlm_status check_chunk(const bdlm_cache* c, const bdlm_chunk* p, Room& room) {
   const size_t parts = (size_t)room.part_rows * c->kv_heads;
   room.part_bytes = align256(parts * c->head_dim * sizeof(float));
   room.lse_bytes = align256(parts * (f32 ? sizeof(PartLse<false>) : sizeof(PartLse<true>)));
+  room.key = key_of({c->dtype, c->kv_heads, c->head_dim, c->page_size, c->max_pages, c->seqs, p->requests, p->rows, p->heads,
+                     p->block_size, p->window, p->window > 0 ? p->sinks : 0});
   return BDLM_OK;
 }
 
@@ -171,6 +185,7 @@ bdlm_status bdlm_chunk_plan(const bdlm_cache* c, const bdlm_chunk* p, const int3
   a.max_items = (int32_t)room.items;
   a.max_joins = (int32_t)room.joins;
   a.max_part_rows = room.part_rows;
+  a.key = room.key;
   const hipError_t e = timed(kKChunkPlan, stream, [&] { return launch_chunk_plan(a, stream); });
   return e == hipSuccess ? BDLM_OK : hip_fail(e, "chunk plan launch");
 }
@@ -229,6 +244,7 @@ bdlm_status bdlm_chunk_attn(const bdlm_cache* c, const bdlm_chunk* p, int64_t la
   a.fill = fill;
   a.max_items = (int32_t)room.items;
   a.max_joins = (int32_t)room.joins;
+  a.key = room.key;
   a.scale = p->scale > 0.f ? p->scale : 1.0f / std::sqrt((float)c->head_dim);
   a.scale_log2 = a.scale * 1.44269504088896340736f;
   const int bf16 = c->dtype == BDLM_BF16;

@@ -70,7 +70,7 @@ __global__ __launch_bounds__(256) void chunk_merge_kernel(const ChunkArgs a) {
   static_assert(256 / LPR == join_rows(D), "a unit's rows");
   __shared__ ManyParts<D, Z> many;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t units = (int64_t)imin(a.plan[kPlanJoins], a.max_joins) * a.kv_heads;
+  const int64_t units = (int64_t)plan_joins(a) * a.kv_heads;
   const Z* const z = (const Z*)a.part_lse;
   for (int64_t u = blockIdx.x; u < units; u += gridDim.x) {
     const int n = (int)(u / a.kv_heads), kvh = (int)(u - (int64_t)n * a.kv_heads);

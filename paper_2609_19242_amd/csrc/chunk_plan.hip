@@ -314,6 +314,7 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
     a.plan[kPlanJoins] = (int)(parts >> 32);
     a.plan[kPlanRows] = (int)(rows < a.rows ? rows : a.rows);
     a.plan[kPlanRoom] = a.max_items;
+    *(uint64_t*)(a.plan + kPlanKey) = a.key;
   }
 }
 
