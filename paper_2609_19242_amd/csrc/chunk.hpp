@@ -56,6 +56,16 @@ struct ChunkPlanArgs {
   uint64_t key;
 };
 
+// The header of a plan of (longer items << 32 | others) items, (units << 32 | partial rows) and the requests' rows.  Where
+// not all of them were written, for want of room, it is a plan of nothing that fits no call.
+__host__ __device__ inline void put_chunk_head(const ChunkPlanArgs& a, int64_t items, int64_t parts, int64_t rows, bool written) {
+  a.plan[kPlanItems] = written ? (int32_t)((items >> 32) + (items & 0xffffffff)) : 0;
+  a.plan[kPlanJoins] = written ? (int32_t)(parts >> 32) : 0;
+  a.plan[kPlanRows] = (int32_t)(rows < a.rows ? rows : a.rows);
+  a.plan[kPlanRoom] = a.max_items;
+  *(uint64_t*)(a.plan + kPlanKey) = written ? a.key : 0;  // (no call's key is 0)
+}
+
 struct ChunkArgs {
   const char *k, *v;  // this layer's
   const int32_t* table;

@@ -133,7 +133,7 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
   __shared__ int64_t wsum[2][kT / 64];
   __shared__ int tile_n[kLdsTiles], tile_nrows[kLdsTiles];
   __shared__ unsigned long long total_lds;
-  __shared__ int longest_lds;
+  __shared__ int longest_lds, short_lds;  // (short: whether the room does not hold all)
   __shared__ f32x4 sums[kT / kUnits][kUnits];
   __shared__ int best_lds;
   const int tid = threadIdx.x;
@@ -141,7 +141,7 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
   int32_t* const tile0 = starts + a.requests;
   ChunkItemRec* const items = (ChunkItemRec*)(tile0 + a.requests + 1);
   ChunkJoin* const joins = (ChunkJoin*)(items + a.max_items);
-  if (tid == 0) longest_lds = 0, total_lds = 0;
+  if (tid == 0) longest_lds = 0, short_lds = 0, total_lds = 0;
 
   // the requests' rows and tiles
   int64_t rows = 0;
@@ -245,8 +245,11 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
       const int longer = (int)(all_items >> 32), others = (int)(all_items & 0xffffffff), j = (int)(y >> 32);
       const int i0 = (is_longer ? longer - (int)(x >> 32) : longer + others - (int)(x & 0xffffffff)) - n;
       const int64_t part = y & 0xffffffff;
-      // (never: the host made room)
-      if (i0 < 0 || i0 + (int64_t)n > a.max_items || (n > 1 && (j + units > a.max_joins || part + (int64_t)n * w.nrows > a.max_part_rows))) continue;
+      // (never: the host made room; else there is no plan, below)
+      if (i0 < 0 || i0 + (int64_t)n > a.max_items || (n > 1 && (j + units > a.max_joins || part + (int64_t)n * w.nrows > a.max_part_rows))) {
+        short_lds = 1;
+        continue;
+      }
       ChunkItemRec rec{q.seq, q.token0, q.pos0, q.len, w.row0, w.nrows, 0, 0, w.gap_at, w.gap, w.w0, 0};
       const int flag = w.shared ? kSharedTile : 0;
 #pragma unroll 1
@@ -309,13 +312,9 @@ __global__ __launch_bounds__(kT) void chunk_plan_kernel(const ChunkPlanArgs a) {
       half = imin(longest_lds, unit) / 2;
     }
   }
-  if (tid == 0) {
-    a.plan[kPlanItems] = (int)((placed >> 32) + (placed & 0xffffffff));
-    a.plan[kPlanJoins] = (int)(parts >> 32);
-    a.plan[kPlanRows] = (int)(rows < a.rows ? rows : a.rows);
-    a.plan[kPlanRoom] = a.max_items;
-    *(uint64_t*)(a.plan + kPlanKey) = a.key;
-  }
+  // (a barrier for LDS alone: one that waits for the items' stores too takes 0.5 us)
+  asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+  if (tid == 0) put_chunk_head(a, placed, parts, rows, short_lds == 0);
 }
 
 }  // namespace
