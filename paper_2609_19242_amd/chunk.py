@@ -14,7 +14,7 @@ from typing import Optional
 
 import torch
 
-from . import _launch, _made, _stream, _torch_stream, lib
+from . import _launch, _made, _raw_stream, _stream, _torch_stream, lib
 from .cache import _cache, _Cache, _list
 from .packed import _as_long, _int, _lse, _Rows, _workspace
 
@@ -50,7 +50,9 @@ class ChunkPlan:
         self.requests, self.rows, self.heads = record.requests, record.rows, record.heads
         self.dtype, self.device, self.gpu, self.head_dim = cache.dtype, cache.device, cache.gpu, cache.head_dim
         # (the items come from the memory of the stream that makes them)
-        self._tensors, self._streams = (items,), {_stream(stream)} if self.gpu >= 0 else set()
+        self._tensors, self._streams = (items,), set()
+        if self.gpu >= 0:  # (its own GPU's, which may not be the current one)
+            self._streams.add(_raw_stream(self.gpu) if stream is None else _stream(stream))
 
     @property
     def workspace_bytes(self):
