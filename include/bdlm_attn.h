@@ -301,7 +301,9 @@ int64_t bdlm_visible_pairs(const bdlm_problem* p, int32_t n_q, const bdlm_range*
  * Rounding.  bf16: scores, softmax statistics, D and all sums are fp32; P (and,
  * backward, dS) is rounded to bf16 for its second product, off by at most 2^-8 of
  * itself, as in bdlm_attn_fwd and bdlm_attn_bwd without hilo, which packed calls do
- * not have; outputs are rounded once.  fp32: fp64 between the inputs and the outputs,
+ * not have; outputs are rounded once.  Backward takes D = dO . O from the rounded O, off by up to
+ * 2^-8 |dO||O|, but for rows of few keys, where it comes from the products: without sinks, rows all of
+ * whose keys lie in one of the sequence's runs of 64, with sinks, rows that see at most 64.  fp32: fp64 between the inputs and the outputs,
  * but for the LSE that backward reads and D between its kernels, which are fp32.  The
  * same plan and inputs give the same bits.  In another batch a sequence's walks may
  * be cut elsewhere, so that its sums run in another order.

@@ -17,9 +17,10 @@
 // row's heads; each pass's loads are issued before the pass in front is computed
 // (backward, 16,384 rows of 32/8 heads, d 128: 141 -> 121 us).
 // Measured, bf16: 30,011 rows of 32/8 heads, d 128, 115 us (5.3 TB/s, a copy's rate);
-// 16,384 rows forward 57 us, backward 105 (4.8 TB/s; two waves per SIMD, for the 32
-// sums of the weights' gradients that a lane keeps); 8,190 rows of 16/16 heads, d 64, 15
-// and 25 us; 64 rows 5 us, the launch and one row's chain of loads.
+// 16,384 rows forward 60 us, backward 113 (4.5 TB/s; two waves per SIMD, for the 32
+// sums of the weights' gradients that a lane keeps); 8,190 rows of 16/16 heads, d 64, 14
+// and 24 us; 64 rows 5 us, the launch and one row's chain of loads.  fp32: 16,384 rows
+// forward 130 us, backward with the weights' sums 196 (5.2 TB/s).
 //
 // Rounding.  An angle is position times frequency in 64 bits, in quarter turns,
 // reduced there to half a quarter; sine and cosine of the rest in fp32 by their
@@ -27,8 +28,8 @@
 // 2^-28).  bf16: the sum of squares and all products are fp32 (so squares must stay
 // below 2^127: |x|, |g w| < 2^60), the outputs are rounded once.  fp32: the sums over a row
 // are fp64.  dw: a lane adds up to 64 products in fp32 and those sums in fp64 (in LDS, for which it
-// has no registers; calls whose chains cannot be longer run without: 8,190 rows of 16/16 heads, d 64, 28.3 us, with the
-// LDS 28.9), a wave's and a workgroup's lanes are added in fp32 in a fixed order, the workgroups' in fp64; it is returned in fp32.
+// has no registers; calls whose chains cannot be longer run without: 8,190 rows of 16/16 heads, d 64, with the weights'
+// sums 28.3 us, with that LDS 28.9), a wave's and a workgroup's lanes are added in fp32 in a fixed order, the workgroups' in fp64; it is returned in fp32.
 #include "device.hpp"
 #include "rotate.hpp"
 

@@ -61,14 +61,17 @@ bdlm_status check_weight(const void* w, const char* what, double eps) {
   return BDLM_OK;
 }
 
-// Rows of a wave, and waves that share a row's heads.  Where one row's heads fill a
-// wave, one row at a time: its loads then are of one run of memory (30,011 rows of 32/8
-// heads, d 128, with 8 rows a wave 141 us, with one 117; 16,384 66 and 59).  Few heads, or a row whose
-// passes would be few beside its angles, take several (8,190 rows of 16/16 heads, d 64:
-// 16 rows a wave 19 us, one 22, backward 32 and 43; 2,000 of 12/2, d 128: 9.3 and 11.5).
-// More waves than 2,048 for the same rows cost more in angles than they hide (4,000 rows
-// of 32/8 heads, d 64, backward: 2,048 33 us, 4,096 35, 8,192 39).  Backward: up to 512 workgroups, two per
-// CU, go through the rows (1,024: 16,384 rows 119 us, 8,190 39, 512: 114, 33).
+// Rows of a wave, and waves that share a row's heads.  Times are of calls in a row on the same inputs, backward with the
+// weights' sums.  Where one row's heads fill a wave, one row at a time: its loads then are of one run of memory (30,011 rows
+// of 32/8 heads, d 128, with 8 rows a wave 140 us, with one 112; 16,384 77 and 63).  Few heads, or a row whose
+// passes would be few beside its angles, take several (8,190 rows of 16/16 heads, d 64: 16 rows a wave 14.5 us, one
+// 15.4, backward 28.0 and 29.7; 2,000 of 12/2, d 128: 6.5 and 7.4, 15.8 and 16.9).  More waves than 2,048 for the same rows
+// cost more in angles than they hide (4,000 rows of 32/8 heads, d 64: 2,048 10.6 us, 4,096 11.4, 8,192 13.2, backward 24.2, 24.3,
+// 27.8).  Backward: up to 512 workgroups, two per CU, go through the rows (4,000 rows of 32/8 heads, d 64, in 1,024
+// 28.9 us, in 512 24.2; 30,011, d 128, 185 and 181).
+// fp32, with the same numbers: 16,384 rows of 8/2 heads, d 64, 16 rows a wave 16 us, one 27, backward 30 and 47; 16,384 of
+// 32/8, d 128, 149 and 130, 219 and 196; 2,000 of 12/2, d 128, 9.1 and 9.3; 4,000 of 32/8, d 128, 2,048 waves 26.9 us, 4,096
+// 27.9.  Rows of 16/16 heads, d 64, would rather be taken one at a time there (8,190: 24 us, as dealt 30, backward 42 and 47).
 void deal(const bdlm_rotary& r, int64_t rows, int32_t heads, int32_t kv_heads, int64_t max_wgs, RotateArgs& a) {
   const int side = 64 / (r.head_dim / 16);  // heads of a wave
   auto passes = [&](int64_t h, int per) { return (h + side / per - 1) / (side / per); };
